@@ -250,12 +250,74 @@ isam_status_t isam_conv1d(int64_t batch, int64_t L, int64_t Ki, int64_t D, int64
                           const void* A, const void* B, int accumulate, int c_type, void* C,
                           void* stream);
 
+/*
+ * Linear GRU: a GRU whose gates do not see the state, so that a whole sequence
+ * is a scan (no step waits for a matrix product).  With gate blocks stacked z, n
+ * in gx, as one product of the inputs with [2*hidden][input] weights gives them:
+ *   z_t = sigmoid(gz_t + b_z)
+ *   n_t = tanh(gn_t + b_n)  (candidate ISAM_TANH)  or  gn_t + b_n  (ISAM_LINEAR)
+ *   h_t = z_t * h_{t-1} + (1 - z_t) * n_t,  h_{-1} = h0
+ * Where reset is given and nonzero at (t, b), the step starts from a zero state
+ * (a packed sequence's first step); nothing from before it, infinities and NaN
+ * included, reaches a later state, nor any gradient an earlier step.
+ *
+ *   gx      row (t, b) of 2*hidden values at gx + t*gx_stride_t + b*gx_stride_b
+ *           (type; strides in elements, >= 0), so [T][batch] and [batch][T]
+ *           orders and slices of wider rows are both read in place
+ *   bias    [2*hidden] fp32 (b_z, b_n), or NULL
+ *   h0      [batch][hidden] fp32, or NULL for zeros
+ *   reset   byte (t, b) at reset + t*reset_stride_t + b*reset_stride_b, or NULL
+ *   h_seq   row (t, b) of hidden values (type) at its own strides, or NULL; rows
+ *           must not overlap each other
+ *   h_T     [batch][hidden] fp32, or NULL
+ *   states  [ceil(T / 256)][batch][hidden] fp32, or NULL: the state before steps
+ *           0, 256, 512, ...: what the backward pass needs of the forward pass
+ * At least one of h_seq, h_T and states.  T == 0: h_T = h0 (or zeros); batch or
+ * hidden == 0: no-op.  The state is fp32 throughout; h_seq is rounded once.
+ * Results repeat bit for bit.  Tensors may pass 2^31 bytes here.
+ * Workspace: isam_linear_gru_workspace_size bytes (0 unless sequences and
+ * channels are too few to fill the device and time is cut into segments).
+ */
+typedef enum { ISAM_LINEAR = 0, ISAM_TANH = 1 } isam_candidate_t;
+
+isam_status_t isam_linear_gru(int64_t T, int64_t batch, int64_t hidden, int type, int candidate, const void* gx,
+                              int64_t gx_stride_t, int64_t gx_stride_b, const float* bias, const float* h0,
+                              const uint8_t* reset, int64_t reset_stride_t, int64_t reset_stride_b, void* h_seq,
+                              int64_t h_stride_t, int64_t h_stride_b, float* h_T, float* states, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+size_t isam_linear_gru_workspace_size(int64_t T, int64_t batch, int64_t hidden, int type);
+
+/*
+ * Gradient of isam_linear_gru.  With d_t the gradient of h_t (dh_seq, and what
+ * later steps pass back), h_{t-1} taken as 0 at a reset:
+ *   d_t   = dh_seq_t + z_{t+1} * d_{t+1}  (no second term before a reset; + dh_T at the last step)
+ *   dgz_t = d_t * (h_{t-1} - n_t) * z_t * (1 - z_t)
+ *   dgn_t = d_t * (1 - z_t) * (1 - n_t^2)  (tanh)  or  d_t * (1 - z_t)  (linear)
+ *   dh0   = z_0 * d_0,  dbias = sums of dgx over t and b
+ * gx, bias, reset and candidate as in the forward call, states as it left them
+ * (its first row stands for h0; NULL only for T == 0).
+ *   dh_seq  row (t, b) of hidden values (type), or NULL for zeros
+ *   dh_T    [batch][hidden] fp32, or NULL for zeros
+ *   dgx     row (t, b) of 2*hidden values (type); rows must not overlap
+ *   dh0     [batch][hidden] fp32, or NULL        dbias  [2*hidden] fp32, or NULL
+ * Sums are fp32, in a fixed order.  batch == 0: dbias = 0.
+ */
+isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int64_t hidden, int type, int candidate, const void* gx,
+                                       int64_t gx_stride_t, int64_t gx_stride_b, const float* bias, const uint8_t* reset,
+                                       int64_t reset_stride_t, int64_t reset_stride_b, const float* states,
+                                       const void* dh_seq, int64_t dh_stride_t, int64_t dh_stride_b, const float* dh_T,
+                                       void* dgx, int64_t dgx_stride_t, int64_t dgx_stride_b, float* dh0, float* dbias,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
+size_t isam_linear_gru_backward_workspace_size(int64_t T, int64_t batch, int64_t hidden, int type);
+
 /* Static text for a status code. */
 const char* isam_status_string(int status);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */
 const char* isam_last_error(void);
 /* Library version, major*10000 + minor*100 + patch. */
-int isam_version(void);  /* 101: adds isam_conv1d */
+int isam_version(void);  /* 101: adds isam_conv1d; 102: the operators of a recurrent block */
 
 #ifdef __cplusplus
 }

@@ -1,5 +1,5 @@
 """MI355X (gfx950) hot path of ISA Mapper (arXiv 1810.09958): GEMM, separable depthwise
-convolution and GRU forward, as hand-written HIP kernels behind the C ABI in
+convolution and GRU forward, and the operators of a gated recurrent block with their gradients, as hand-written HIP kernels behind the C ABI in
 ``include/isam.h``.
 
 This module is argument marshalling only: it checks torch tensors (device, dtype,
@@ -18,7 +18,8 @@ from ._lib import (ISAM_BF16, ISAM_F32, IsamError, lib, lib_path)
 
 __all__ = ["gemm", "conv1d", "dwsep_conv", "gru_forward", "gru_forward_noalloc", "gemm_workspace_size",
            "dwsep_conv_workspace_size", "gru_forward_workspace_size", "IsamError",
-           "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
+           "linear_gru", "linear_gru_backward", "linear_gru_states_shape", "linear_gru_workspace_size",
+           "linear_gru_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
 
 _DT = {torch.float32: ISAM_F32, torch.bfloat16: ISAM_BF16}
 
@@ -223,3 +224,140 @@ def gru_forward_noalloc(x: torch.Tensor, W: torch.Tensor, U: torch.Tensor, h_seq
                                         _ptr(bias_hn), _ptr(h_seq), _ptr(h_T), _stream())
     _call(rc, "isam_gru_forward_noalloc")
     return h_seq, h_T
+
+
+# ---------------------------------------------------------------------------------------
+# Linear GRU
+# ---------------------------------------------------------------------------------------
+_CANDIDATES = {"linear": 0, "tanh": 1}
+
+
+def _code(table, name, what):
+    try:
+        return table[name]
+    except (KeyError, TypeError):
+        raise ValueError(f"{what} must be one of {', '.join(sorted(table))}") from None
+
+
+def _want(t, name, shape, dtype=torch.float32, device=None):
+    """Checks a contiguous tensor argument (None passes)."""
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor")
+
+
+def _rows(t, name, shape, dtype):
+    """Strides of the rows of a [T][batch][width] tensor with unit inner stride (None: zeros)."""
+    if t is None:
+        return 0, 0
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}")
+    if t.dim() == 3 and t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} needs unit inner stride")
+    return t.stride(0), t.stride(1)
+
+
+def _same_device(dev, **ts):
+    for name, t in ts.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} must be on {dev}")
+
+
+def _room(workspace, nbytes, dev):
+    return torch.empty(max(nbytes, 1), device=dev, dtype=torch.uint8) if workspace is None else workspace
+
+
+def _bytes(t):
+    return t.numel() * t.element_size()
+
+
+def linear_gru_workspace_size(T, batch, hidden, dtype) -> int:
+    return lib().isam_linear_gru_workspace_size(T, batch, hidden, dtype)
+
+
+def linear_gru_backward_workspace_size(T, batch, hidden, dtype) -> int:
+    return lib().isam_linear_gru_backward_workspace_size(T, batch, hidden, dtype)
+
+
+def linear_gru_states_shape(T, batch, hidden):
+    """Shape of the ``states`` tensor: the state before steps 0, 256, 512, ..."""
+    return (T + 255) // 256, batch, hidden
+
+
+def _linear_gru_args(gx, bias, reset):
+    if gx.dim() != 3 or gx.shape[2] % 2:
+        raise ValueError("gx must be [T][batch][2 * hidden]")
+    T, B, H2 = gx.shape
+    _want(bias, "bias", (H2,))
+    gs = _rows(gx, "gx", (T, B, H2), gx.dtype)
+    if reset is not None and reset.dtype not in (torch.bool, torch.uint8):
+        raise TypeError("reset must be bool or uint8")
+    rs = (0, 0) if reset is None else _rows(reset, "reset", (T, B), reset.dtype)
+    return T, B, H2 // 2, _dt(gx), gs, rs
+
+
+def linear_gru(gx: torch.Tensor, *, bias=None, h0=None, reset=None, candidate="tanh", return_sequence=True, h_seq=None,
+               h_T=None, states=None, workspace: torch.Tensor | None = None):
+    """Linear GRU (gates that do not see the state): h_t = z_t h_{t-1} + (1 - z_t) n_t with z =
+    sigmoid(gz + b_z) and n = tanh(gn + b_n), or gn + b_n for candidate="linear".
+    gx [T][batch][2H] (blocks z, n; float32 or bfloat16; any strides of the first two
+    dimensions, so batch-first tensors go in transposed), bias [2H] and h0 [batch][H] float32,
+    reset [T][batch] bool (the step starts from a zero state).  states
+    (``linear_gru_states_shape``, float32) receives what ``linear_gru_backward`` needs.
+    Returns (h_seq in gx's dtype, h_T in float32)."""
+    _check_dev(gx, bias, h0, reset, h_seq, h_T, states, workspace)
+    T, B, H, dt, gs, rs = _linear_gru_args(gx, bias, reset)
+    cand = _code(_CANDIDATES, candidate, "candidate")
+    dev = gx.device
+    _same_device(dev, bias=bias, h0=h0, reset=reset, h_seq=h_seq, h_T=h_T, states=states, workspace=workspace)
+    _want(h0, "h0", (B, H))
+    _want(states, "states", linear_gru_states_shape(T, B, H))
+    if h_seq is None and return_sequence:
+        h_seq = torch.empty((T, B, H), device=dev, dtype=gx.dtype)
+    if h_T is None:
+        h_T = torch.empty((B, H), device=dev, dtype=torch.float32)
+    _want(h_T, "h_T", (B, H))
+    hs = _rows(h_seq, "h_seq", (T, B, H), gx.dtype)
+    if workspace is None:
+        workspace = _room(None, linear_gru_workspace_size(T, B, H, dt), dev)
+    rc = lib().isam_linear_gru(T, B, H, dt, cand, _ptr(gx), *gs, _ptr(bias), _ptr(h0), _ptr(reset), *rs, _ptr(h_seq), *hs,
+                               _ptr(h_T), _ptr(states), _ptr(workspace), _bytes(workspace), _stream())
+    _call(rc, "isam_linear_gru")
+    return h_seq, h_T
+
+
+def linear_gru_backward(gx: torch.Tensor, dh_seq: torch.Tensor | None, *, states, bias=None, reset=None, candidate="tanh",
+                        dh_T=None, dgx=None, dh0=None, dbias=None, workspace: torch.Tensor | None = None):
+    """Gradient of ``linear_gru``: gx, bias, reset, candidate and states as in (and from) the forward
+    call, dh_seq [T][batch][H] in gx's dtype or None, dh_T [batch][H] float32 or None.  Returns
+    (dgx in gx's dtype, dh0, dbias in float32; dbias is None without a bias unless given)."""
+    _check_dev(gx, dh_seq, states, bias, reset, dh_T, dgx, dh0, dbias, workspace)
+    T, B, H, dt, gs, rs = _linear_gru_args(gx, bias, reset)
+    cand = _code(_CANDIDATES, candidate, "candidate")
+    dev = gx.device
+    _same_device(dev, dh_seq=dh_seq, states=states, bias=bias, reset=reset, dh_T=dh_T, dgx=dgx, dh0=dh0, dbias=dbias,
+                 workspace=workspace)
+    _want(states, "states", linear_gru_states_shape(T, B, H))
+    _want(dh_T, "dh_T", (B, H))
+    ds = _rows(dh_seq, "dh_seq", (T, B, H), gx.dtype)
+    if dgx is None:
+        dgx = torch.empty((T, B, 2 * H), device=dev, dtype=gx.dtype)
+    if dh0 is None:
+        dh0 = torch.empty((B, H), device=dev, dtype=torch.float32)
+    if dbias is None and bias is not None:
+        dbias = torch.empty((2 * H,), device=dev, dtype=torch.float32)
+    _want(dh0, "dh0", (B, H))
+    _want(dbias, "dbias", (2 * H,))
+    dgs = _rows(dgx, "dgx", (T, B, 2 * H), gx.dtype)
+    if workspace is None:
+        workspace = _room(None, linear_gru_backward_workspace_size(T, B, H, dt), dev)
+    rc = lib().isam_linear_gru_backward(T, B, H, dt, cand, _ptr(gx), *gs, _ptr(bias), _ptr(reset), *rs, _ptr(states),
+                                        _ptr(dh_seq), *ds, _ptr(dh_T), _ptr(dgx), *dgs, _ptr(dh0), _ptr(dbias),
+                                        _ptr(workspace), _bytes(workspace), _stream())
+    _call(rc, "isam_linear_gru_backward")
+    return dgx, dh0, dbias

@@ -18,6 +18,11 @@ SIGNATURES = {
     "isam_gru_forward_workspace_size": (sz, [i64, i64, i64, i64, ci]),
     "isam_gru_forward_noalloc": (ci, [i64, i64, i64, i64, ci, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
     "isam_conv1d": (ci, [i64, i64, i64, i64, i64, ci, vp, vp, ci, ci, vp, vp]),
+    "isam_linear_gru": (ci, [i64, i64, i64, ci, ci, vp, i64, i64, vp, vp, vp, i64, i64, vp, i64, i64, vp, vp, vp, sz, vp]),
+    "isam_linear_gru_workspace_size": (sz, [i64, i64, i64, ci]),
+    "isam_linear_gru_backward": (ci, [i64, i64, i64, ci, ci, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64,
+                                      i64, vp, vp, vp, sz, vp]),
+    "isam_linear_gru_backward_workspace_size": (sz, [i64, i64, i64, ci]),
     "isam_status_string": (ctypes.c_char_p, [ci]),
     "isam_last_error": (ctypes.c_char_p, []),
     "isam_version": (ci, []),

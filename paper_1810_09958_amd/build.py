@@ -15,7 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libisam.so")
-SOURCES = ["api.cpp", "launch_cache.cpp", "gemm.hip", "gemm_bf16.hip", "gemm_f32.hip", "gemm_dma.hip", "gemm_dma_sk.hip", "gemm_ring.hip", "gemm_f32x.hip", "gemm_small.hip", "gemm_stream.hip", "pack.hip", "skinny.hip", "dwconv.hip", "dwsep_fused.hip", "dwsep_fused_f32.hip", "gru.hip"]
+SOURCES = ["api.cpp", "api_block.cpp", "launch_cache.cpp", "gemm.hip", "gemm_bf16.hip", "gemm_f32.hip", "gemm_dma.hip", "gemm_dma_sk.hip", "gemm_ring.hip", "gemm_f32x.hip", "gemm_small.hip", "gemm_stream.hip", "pack.hip", "skinny.hip", "dwconv.hip", "dwsep_fused.hip", "dwsep_fused_f32.hip", "gru.hip", "linear_gru.hip", "colsum.hip"]
+HOST_SOURCES = ["api.cpp", "api_block.cpp"]  # argument checks and dispatch, no kernels
 ARCH = "gfx950"
 
 
@@ -70,19 +71,21 @@ SAN_LIB = os.path.join(BUILD, "libisam_san.so")
 
 
 def build_sanitized() -> str:
-    """A copy of the library whose host code (argument validation, planning and dispatch in
-    api.cpp) is built with g++ under AddressSanitizer and UndefinedBehaviorSanitizer, linked
+    """A copy of the library whose host code (argument validation, planning and dispatch, the
+    C-ABI sources) is built with g++ under AddressSanitizer and UndefinedBehaviorSanitizer, linked
     with the device objects of the regular build.  For the CPU test tier: load it with gcc's
     libasan and libubsan preloaded and ISAM_LIB pointing at it."""
     if not all(os.path.exists(os.path.join(BUILD, src + ".o")) for src in SOURCES):
         build()
-    obj = os.path.join(BUILD, "api.cpp.san.o")
     rocm = os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
     san = ["-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer"]
-    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fPIC", "-D__HIP_PLATFORM_AMD__",
-                    "-I", os.path.join(rocm, "include"), "-I", os.path.join(HERE, "..", "include"), *san,
-                    "-c", os.path.join(CSRC, "api.cpp"), "-o", obj], check=True)
-    objs = [obj] + [os.path.join(BUILD, src + ".o") for src in SOURCES if src != "api.cpp"]
+    objs = []
+    for src in HOST_SOURCES:
+        objs.append(os.path.join(BUILD, src + ".san.o"))
+        subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fPIC", "-D__HIP_PLATFORM_AMD__",
+                        "-I", os.path.join(rocm, "include"), "-I", os.path.join(HERE, "..", "include"), *san,
+                        "-c", os.path.join(CSRC, src), "-o", objs[-1]], check=True)
+    objs += [os.path.join(BUILD, src + ".o") for src in SOURCES if src not in HOST_SOURCES]
     tmp = SAN_LIB + ".tmp"
     subprocess.run(["g++", "-shared", "-o", tmp, *objs, "-L", os.path.join(rocm, "lib"),
                     "-Wl,-rpath," + os.path.join(rocm, "lib"), "-lamdhip64", *san], check=True)

@@ -19,14 +19,19 @@
 #include <mutex>
 #include <string>
 
-#include "../../include/isam.h"
-#include "kernels.hpp"
+#include "api.hpp"
 
 using namespace isam;
 
-namespace {
+namespace isam {
+namespace api {
 
+namespace {
 thread_local std::string g_last_error;
+}
+
+void clear_error() { g_last_error.clear(); }
+const char* last_error() { return g_last_error.c_str(); }
 
 isam_status_t fail(isam_status_t st, const char* fmt, ...) {
     char buf[512];
@@ -50,11 +55,6 @@ bool log_enabled() {
     const char* v = getenv("ISAM_LOG");
     return v && v[0] && v[0] != '0';
 }
-
-bool valid_dtype(int t) { return t == ISAM_F32 || t == ISAM_BF16; }
-size_t dsize(int t) { return t == ISAM_BF16 ? 2 : 4; }
-
-constexpr int64_t kMaxExtent = (int64_t(1) << 31) - 1;
 
 bool overlaps(const void* a, size_t an, const void* b, size_t bn) {
     if (!a || !b || an == 0 || bn == 0) return false;
@@ -91,6 +91,13 @@ int device_cus() {
     return cache[dev];
 }
 
+}  // namespace api
+}  // namespace isam
+
+using namespace isam::api;
+
+namespace {
+
 // Largest LDS allocation of one workgroup on the current device, cached;
 // 160 KiB (gfx950) when no device is visible.
 int device_lds_max() {
@@ -123,8 +130,6 @@ int device_lds_max() {
 // ---------------------------------------------------------------------------
 // GEMM plan
 // ---------------------------------------------------------------------------
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, int ab_type, int cus, bool allow_skinny = true) {
     GemmPlan p{};
     p.vec = 1;
@@ -911,8 +916,6 @@ isam_status_t run_gemm(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K
     return ISAM_OK;
 }
 
-size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
-
 // Workspace of a product's preferred plan, as far as the sizes tell (split_copies:
 // as run_gemm's).
 size_t gemm_query(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int ab_type, bool split_copies = true) {
@@ -965,6 +968,23 @@ size_t gemm_query(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int
 
 }  // namespace
 
+namespace isam {
+namespace api {
+
+isam_status_t product(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int ab_type, const void* A, int64_t lda,
+                      const void* B, int64_t ldb, int c_type, void* C, int64_t ldc, void* workspace, size_t workspace_bytes,
+                      hipStream_t stream, const char* who) {
+    return run_gemm(trans_a, trans_b, M, N, K, ab_type, A, lda, B, ldb, 0, c_type, C, ldc, nullptr, workspace,
+                    workspace_bytes, stream, who);
+}
+
+size_t product_workspace(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int ab_type) {
+    return gemm_query(trans_a, trans_b, M, N, K, ab_type);
+}
+
+}  // namespace api
+}  // namespace isam
+
 // ---------------------------------------------------------------------------
 // Exported entry points
 // ---------------------------------------------------------------------------
@@ -974,7 +994,7 @@ isam_status_t isam_gemm(int trans_a, int trans_b, int64_t M, int64_t N, int64_t 
                         const void* A, int64_t lda, const void* B, int64_t ldb, int accumulate,
                         int c_type, void* C, int64_t ldc, void* workspace, size_t workspace_bytes,
                         void* stream) {
-    g_last_error.clear();
+    clear_error();
     isam_status_t st = validate_gemm(trans_a, trans_b, M, N, K, ab_type, A, lda, B, ldb, accumulate,
                                      c_type, C, ldc, "isam_gemm");
     if (st != ISAM_OK || M == 0 || N == 0) return st;
@@ -1063,7 +1083,7 @@ isam_status_t isam_dwsep_conv(int64_t batch, int64_t H, int64_t W, int64_t C_in,
                               int in_type, const void* x, const void* dw_filter, const void* pw_weight,
                               int out_type, void* y, void* workspace, size_t workspace_bytes,
                               void* stream) {
-    g_last_error.clear();
+    clear_error();
     const char* who = "isam_dwsep_conv";
     if (batch < 0 || H <= 0 || W <= 0 || C_in <= 0 || depth_mult <= 0 || kh <= 0 || kw <= 0 ||
         stride <= 0 || pad < 0 || C_out <= 0)
@@ -1359,7 +1379,7 @@ extern "C" isam_status_t isam_gru_forward(int64_t T, int64_t batch, int64_t inpu
                                           const void* U, const float* bias, const float* bias_hn,
                                           float* h_seq, float* h_T, void* workspace,
                                           size_t workspace_bytes, void* stream) {
-    g_last_error.clear();
+    clear_error();
     return gru_forward_impl(T, batch, input_size, hidden_size, w_type, x, h0, W, U, bias, bias_hn, h_seq, h_T,
                             workspace, workspace_bytes, stream, "isam_gru_forward", false);
 }
@@ -1368,7 +1388,7 @@ extern "C" isam_status_t isam_gru_forward_noalloc(int64_t T, int64_t batch, int6
                                                   int64_t hidden_size, int w_type, const void* x, const float* h0,
                                                   const void* W, const void* U, const float* bias,
                                                   const float* bias_hn, float* h_seq, float* h_T, void* stream) {
-    g_last_error.clear();
+    clear_error();
     return gru_forward_impl(T, batch, input_size, hidden_size, w_type, x, h0, W, U, bias, bias_hn, h_seq, h_T,
                             nullptr, 0, stream, "isam_gru_forward_noalloc", true);
 }
@@ -1376,7 +1396,7 @@ extern "C" isam_status_t isam_gru_forward_noalloc(int64_t T, int64_t batch, int6
 extern "C" isam_status_t isam_conv1d(int64_t batch, int64_t L, int64_t Ki, int64_t D, int64_t Ko, int ab_type,
                                      const void* A, const void* B, int accumulate, int c_type, void* C,
                                      void* stream) {
-    g_last_error.clear();
+    clear_error();
     const char* who = "isam_conv1d";
     if (batch < 0 || L < 0 || Ki <= 0 || D <= 0 || Ko < 0)
         return fail(ISAM_ERR_INVALID_ARG, "%s: batch, L, Ko >= 0 and Ki, D > 0 required", who);
@@ -1413,8 +1433,8 @@ const char* isam_status_string(int status) {
     }
 }
 
-const char* isam_last_error(void) { return g_last_error.c_str(); }
+const char* isam_last_error(void) { return last_error(); }
 
-int isam_version(void) { return 101; }
+int isam_version(void) { return 102; }
 
 }  // extern "C"

@@ -1,0 +1,224 @@
+// C-ABI layer of the operators of a gated recurrent block: argument validation
+// (pure host code, no HIP call) and dispatch.
+#include "api.hpp"
+
+using namespace isam;
+using namespace isam::api;
+
+namespace {
+
+// Workspaces start at the first multiple of 256 bytes of what the caller gives.
+size_t room(size_t bytes) { return bytes ? bytes + 255 : 0; }
+char* room_start(void* ws) { return reinterpret_cast<char*>(((uintptr_t)ws + 255) & ~(uintptr_t)255); }
+
+// One tensor of a call: its address range, and whether the call writes it.
+struct Tensor {
+    const char* name;
+    const void* p;
+    size_t bytes;
+    bool out;
+};
+
+// Outputs (and the workspace) must not overlap any other tensor of the call.
+template <size_t N>
+isam_status_t disjoint(const Tensor (&t)[N], const char* who) {
+    for (size_t i = 0; i < N; ++i) {
+        for (size_t j = i + 1; j < N; ++j) {
+            if ((t[i].out || t[j].out) && overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes))
+                return fail(ISAM_ERR_INVALID_ARG, "%s: %s overlaps %s", who, t[i].name, t[j].name);
+        }
+    }
+    return ISAM_OK;
+}
+
+// Address range of rows (i, j), i < n, j < m, of `width` elements; false if it
+// passes 2^46 bytes (no such tensor exists, and offsets stay within 64 bits).
+bool extent(int64_t n, int64_t stride_n, int64_t m, int64_t stride_m, int64_t width, size_t es, size_t* bytes) {
+    *bytes = 0;
+    if (n == 0 || m == 0 || width == 0) return true;
+    const __int128 e = ((__int128)(n - 1) * stride_n + (__int128)(m - 1) * stride_m + width) * (__int128)es;
+    if (e > ((__int128)1 << 46)) return false;
+    *bytes = (size_t)e;
+    return true;
+}
+
+// Whether no two rows (i, j) of `width` elements share an element.
+bool rows_apart(int64_t n, int64_t stride_n, int64_t m, int64_t stride_m, int64_t width) {
+    const bool inner_m = m <= 1 || stride_m >= width, inner_n = n <= 1 || stride_n >= width;
+    return (inner_m && (n <= 1 || (__int128)stride_n >= (__int128)(m - 1) * (m > 1 ? stride_m : 0) + width)) ||
+           (inner_n && (m <= 1 || (__int128)stride_m >= (__int128)(n - 1) * (n > 1 ? stride_n : 0) + width));
+}
+
+// ---------------------------------------------------------------------------
+// Linear GRU
+// ---------------------------------------------------------------------------
+// Sizes whose products stay far below 2^63 (states, partial sums and grids).
+bool lingru_sizes(int64_t T, int64_t batch, int64_t H) {
+    return T < ((int64_t)1 << 40) && batch < ((int64_t)1 << 31) && H < ((int64_t)1 << 31) &&
+           (__int128)T * batch * H < ((__int128)1 << 46);
+}
+
+// Bytes of the segments' compositions and of the bias gradient's partial sums.
+size_t lingru_agg_bytes(int64_t segs, int64_t batch, int64_t H) {
+    return segs > 1 ? align256((size_t)(2 * segs * batch * H) * sizeof(float)) : 0;
+}
+size_t lingru_bias_bytes(int64_t segs, int64_t batch, int64_t H) { return (size_t)(segs * batch * 2 * H) * sizeof(float); }
+
+isam_status_t lingru_check(int64_t T, int64_t batch, int64_t H, int type, int candidate, const char* who) {
+    if (T < 0 || batch < 0 || H < 0)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: negative size T=%lld batch=%lld hidden=%lld", who, (long long)T,
+                    (long long)batch, (long long)H);
+    if (!valid_dtype(type)) return fail(ISAM_ERR_INVALID_ARG, "%s: dtype must be ISAM_F32 (0) or ISAM_BF16 (1)", who);
+    if (candidate != ISAM_LINEAR && candidate != ISAM_TANH)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: candidate must be ISAM_LINEAR (0) or ISAM_TANH (1)", who);
+    if (!lingru_sizes(T, batch, H)) return fail(ISAM_ERR_UNSUPPORTED, "%s: sizes too large", who);
+    return ISAM_OK;
+}
+
+}  // namespace
+
+extern "C" isam_status_t isam_linear_gru(int64_t T, int64_t batch, int64_t hidden, int type, int candidate, const void* gx,
+                                         int64_t gx_stride_t, int64_t gx_stride_b, const float* bias, const float* h0,
+                                         const uint8_t* reset, int64_t reset_stride_t, int64_t reset_stride_b, void* h_seq,
+                                         int64_t h_stride_t, int64_t h_stride_b, float* h_T, float* states,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_linear_gru";
+    isam_status_t st = lingru_check(T, batch, hidden, type, candidate, who);
+    if (st != ISAM_OK || batch == 0 || hidden == 0) return st;
+    if (!h_seq && !h_T && !states) return fail(ISAM_ERR_INVALID_ARG, "%s: no output", who);
+    if (T > 0 && !gx) return fail(ISAM_ERR_INVALID_ARG, "%s: gx is NULL", who);
+    if (gx_stride_t < 0 || gx_stride_b < 0 || (h_seq && (h_stride_t < 0 || h_stride_b < 0)) ||
+        (reset && (reset_stride_t < 0 || reset_stride_b < 0)))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: negative stride", who);
+    if (h_seq && T > 0 && !rows_apart(T, h_stride_t, batch, h_stride_b, hidden))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: rows of h_seq overlap", who);
+    const size_t es = dsize(type), state = (size_t)(batch * hidden) * sizeof(float);
+    LinGruArgs a{};
+    lingru_segments(T, batch, hidden, type, device_cus(), &a.segs, &a.tiles_per_seg);
+    const size_t need = lingru_agg_bytes(a.segs, batch, hidden);
+    if (need && (!workspace || workspace_bytes < room(need)))
+        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
+                    room(need));
+    size_t gx_b, h_b, r_b;
+    if (!extent(T, gx_stride_t, batch, gx_stride_b, 2 * hidden, es, &gx_b) ||
+        !extent(h_seq ? T : 0, h_stride_t, batch, h_stride_b, hidden, es, &h_b) ||
+        !extent(reset ? T : 0, reset_stride_t, batch, reset_stride_b, 1, 1, &r_b))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: a tensor spans more than 2^46 bytes", who);
+    const Tensor all[] = {{"gx", gx, gx_b, false},
+                          {"bias", bias, (size_t)(2 * hidden) * 4, false},
+                          {"h0", h0, state, false},
+                          {"reset", reset, r_b, false},
+                          {"h_seq", h_seq, h_b, true},
+                          {"h_T", h_T, state, true},
+                          {"states", states, (size_t)cdiv(T, kLinGruChunk) * state, true},
+                          {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    a.T = T;
+    a.batch = batch;
+    a.H = hidden;
+    a.type = type;
+    a.candidate = candidate;
+    a.gx = gx;
+    a.gx_t = gx_stride_t;
+    a.gx_b = gx_stride_b;
+    a.bias = bias;
+    a.h0 = h0;
+    a.reset = reset;
+    a.rs_t = reset_stride_t;
+    a.rs_b = reset_stride_b;
+    a.h_seq = h_seq;
+    a.h_t = h_stride_t;
+    a.h_b = h_stride_b;
+    a.h_T = h_T;
+    a.states = states;
+    a.agg = need ? reinterpret_cast<float*>(room_start(workspace)) : nullptr;
+    const hipError_t e = launch_lingru_forward(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_linear_gru_workspace_size(int64_t T, int64_t batch, int64_t hidden, int type) {
+    if (T <= 0 || batch <= 0 || hidden <= 0 || !valid_dtype(type) || !lingru_sizes(T, batch, hidden)) return 0;
+    int64_t segs, per;
+    lingru_segments(T, batch, hidden, type, device_cus(), &segs, &per);
+    return room(lingru_agg_bytes(segs, batch, hidden));
+}
+
+extern "C" isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int64_t hidden, int type, int candidate,
+                                                  const void* gx, int64_t gx_stride_t, int64_t gx_stride_b,
+                                                  const float* bias, const uint8_t* reset, int64_t reset_stride_t,
+                                                  int64_t reset_stride_b, const float* states, const void* dh_seq,
+                                                  int64_t dh_stride_t, int64_t dh_stride_b, const float* dh_T, void* dgx,
+                                                  int64_t dgx_stride_t, int64_t dgx_stride_b, float* dh0, float* dbias,
+                                                  void* workspace, size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_linear_gru_backward";
+    isam_status_t st = lingru_check(T, batch, hidden, type, candidate, who);
+    if (st != ISAM_OK || hidden == 0) return st;
+    if (T > 0 && batch > 0 && (!gx || !states || !dgx))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: gx, states or dgx is NULL", who);
+    if (gx_stride_t < 0 || gx_stride_b < 0 || dgx_stride_t < 0 || dgx_stride_b < 0 ||
+        (dh_seq && (dh_stride_t < 0 || dh_stride_b < 0)) || (reset && (reset_stride_t < 0 || reset_stride_b < 0)))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: negative stride", who);
+    if (T > 0 && batch > 0 && !rows_apart(T, dgx_stride_t, batch, dgx_stride_b, 2 * hidden))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: rows of dgx overlap", who);
+    const size_t es = dsize(type), state = (size_t)(batch * hidden) * sizeof(float);
+    LinGruArgs a{};
+    lingru_segments(T, batch, hidden, type, device_cus(), &a.segs, &a.tiles_per_seg);
+    const size_t agg = lingru_agg_bytes(a.segs, batch, hidden);
+    const size_t need = agg + (dbias ? lingru_bias_bytes(a.segs, batch, hidden) : 0);
+    if (need && (!workspace || workspace_bytes < room(need)))
+        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
+                    room(need));
+    size_t gx_b, dg_b, dh_b, r_b;
+    if (!extent(T, gx_stride_t, batch, gx_stride_b, 2 * hidden, es, &gx_b) ||
+        !extent(T, dgx_stride_t, batch, dgx_stride_b, 2 * hidden, es, &dg_b) ||
+        !extent(dh_seq ? T : 0, dh_stride_t, batch, dh_stride_b, hidden, es, &dh_b) ||
+        !extent(reset ? T : 0, reset_stride_t, batch, reset_stride_b, 1, 1, &r_b))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: a tensor spans more than 2^46 bytes", who);
+    const Tensor all[] = {{"gx", gx, gx_b, false},
+                          {"bias", bias, (size_t)(2 * hidden) * 4, false},
+                          {"reset", reset, r_b, false},
+                          {"states", states, (size_t)cdiv(T, kLinGruChunk) * state, false},
+                          {"dh_seq", dh_seq, dh_b, false},
+                          {"dh_T", dh_T, state, false},
+                          {"dgx", dgx, dg_b, true},
+                          {"dh0", dh0, state, true},
+                          {"dbias", dbias, (size_t)(2 * hidden) * 4, true},
+                          {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    a.T = T;
+    a.batch = batch;
+    a.H = hidden;
+    a.type = type;
+    a.candidate = candidate;
+    a.gx = gx;
+    a.gx_t = gx_stride_t;
+    a.gx_b = gx_stride_b;
+    a.bias = bias;
+    a.reset = reset;
+    a.rs_t = reset_stride_t;
+    a.rs_b = reset_stride_b;
+    a.states = const_cast<float*>(states);
+    a.dh_seq = dh_seq;
+    a.dh_t = dh_stride_t;
+    a.dh_b = dh_stride_b;
+    a.dh_T = dh_T;
+    a.dgx = dgx;
+    a.dg_t = dgx_stride_t;
+    a.dg_b = dgx_stride_b;
+    a.dh0 = dh0;
+    a.dbias = dbias;
+    char* ws = room_start(workspace);
+    a.agg = agg ? reinterpret_cast<float*>(ws) : nullptr;
+    a.bias_part = dbias ? reinterpret_cast<float*>(ws + agg) : nullptr;
+    const hipError_t e = launch_lingru_backward(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_linear_gru_backward_workspace_size(int64_t T, int64_t batch, int64_t hidden, int type) {
+    if (T < 0 || batch <= 0 || hidden <= 0 || !valid_dtype(type) || !lingru_sizes(T, batch, hidden)) return 0;
+    int64_t segs, per;
+    lingru_segments(T, batch, hidden, type, device_cus(), &segs, &per);
+    return room(lingru_agg_bytes(segs, batch, hidden) + lingru_bias_bytes(segs, batch, hidden));
+}

@@ -233,4 +233,41 @@ hipError_t gru_scratch(void** ptr);
 // T == 0: h_T = h0 (or zeros when h0 is null).
 hipError_t launch_gru_copy_state(const float* h0, float* h_T, int64_t n, hipStream_t s);
 
+
+// Linear GRU (linear_gru.hip).  Strides in elements; rows are [2H] (gx, dgx) or [H].
+constexpr int64_t kLinGruChunk = 256;  // steps between two rows of `states`
+struct LinGruArgs {
+    int64_t T, batch, H;
+    int type;                // of gx, h_seq, dh_seq and dgx
+    int candidate;           // 1: tanh, 0: linear
+    const void* gx;
+    int64_t gx_t, gx_b;
+    const float* bias;       // [2H] or null
+    const float* h0;         // [batch][H] or null
+    const uint8_t* reset;    // nonzero: the step starts from a zero state; or null
+    int64_t rs_t, rs_b;
+    void* h_seq;             // or null
+    int64_t h_t, h_b;
+    float* h_T;              // [batch][H] or null
+    float* states;           // [ceil(T / 256)][batch][H]: state before steps 0, 256, ...; or null (forward)
+    // backward
+    const void* dh_seq;      // or null
+    int64_t dh_t, dh_b;
+    const float* dh_T;       // [batch][H] or null
+    void* dgx;
+    int64_t dg_t, dg_b;
+    float* dh0;              // [batch][H] or null
+    float* dbias;            // [2H] or null
+    // segments of time (lingru_segments) and workspace
+    int64_t segs, tiles_per_seg;
+    float* agg;              // [2][segs][batch][H] (segs > 1)
+    float* bias_part;        // [segs][batch][2H] (dbias)
+};
+void lingru_segments(int64_t T, int64_t batch, int64_t H, int type, int cus, int64_t* segs, int64_t* tiles_per_seg);
+hipError_t launch_lingru_forward(const LinGruArgs& a, hipStream_t s);
+hipError_t launch_lingru_backward(const LinGruArgs& a, hipStream_t s);
+
+// out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros).
+hipError_t launch_colsum(const float* part, int64_t rows, int64_t cols, int64_t groups, int out_type, void* out, hipStream_t s);
+
 }  // namespace isam
