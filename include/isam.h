@@ -312,6 +312,43 @@ isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int64_t hidden,
 
 size_t isam_linear_gru_backward_workspace_size(int64_t T, int64_t batch, int64_t hidden, int type);
 
+/*
+ * Gated residual norm: the norm after a block, its gate and scale, the residual
+ * sum and the norm before the next block, over rows of D values:
+ *   u = x / sqrt(mean(x^2) + eps) * w_post      (u = x if w_post is NULL)
+ *   r_out = r + scale * gate * u
+ *   y = r_out / sqrt(mean(r_out^2) + eps) * w_pre
+ *   x, r, r_out, y  [rows][D] (type) at leading dimensions ld* >= D.  r_out may be r
+ *           itself (same address and ldr).  y is formed from r_out before it is rounded.
+ *   gate    [gates][D] (type), row i using gate row i / (rows / gates): 1 (one
+ *           gate for all), a divisor of rows (one for each sequence) or rows;
+ *           NULL for ones (gates is then not looked at)
+ *   w_post, w_pre  [D] fp32 (w_post may be NULL)
+ * x NULL: y = norm of r alone, as before a first block (r_out, gate and w_post
+ * must be NULL).  D up to 16384.  Statistics and sums are fp32.  rows or D == 0: no-op.
+ */
+isam_status_t isam_norm_residual(int64_t rows, int64_t D, int64_t gates, int type, const void* x, int64_t ldx, const void* r,
+                                 int64_t ldr, const void* gate, const float* w_post, const float* w_pre, float scale,
+                                 float eps, void* r_out, int64_t ldro, void* y, int64_t ldy, void* stream);
+
+/*
+ * Gradient of isam_norm_residual from dy and dr_out, the gradients of y and r_out
+ * (dr_out NULL for zeros); r_out as the forward pass left it, the rest as it was
+ * given.  dr may be dr_out itself (same address and leading dimension).
+ *   dx, dr  [rows][D] (type), dgate [gates][D] (type), dw_post, dw_pre [D] fp32
+ * dgate, dw_post and dw_pre may be NULL; dgate needs a gate, dw_post w_post.  x NULL: dx,
+ * dgate and dw_post must be NULL.  rows == 0: dgate, dw_post and dw_pre are 0.
+ * Sums over rows are fp32, in a fixed order.
+ */
+isam_status_t isam_norm_residual_backward(int64_t rows, int64_t D, int64_t gates, int type, const void* x, int64_t ldx,
+                                          const void* r_out, int64_t ldro, const void* gate, const float* w_post,
+                                          const float* w_pre, float scale, float eps, const void* dy, int64_t lddy,
+                                          const void* dr_out, int64_t lddro, void* dx, int64_t lddx, void* dr, int64_t lddr,
+                                          void* dgate, float* dw_post, float* dw_pre, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64_t D, int64_t gates, int type);
+
 /* Static text for a status code. */
 const char* isam_status_string(int status);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */

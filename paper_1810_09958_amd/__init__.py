@@ -19,7 +19,8 @@ from ._lib import (ISAM_BF16, ISAM_F32, IsamError, lib, lib_path)
 __all__ = ["gemm", "conv1d", "dwsep_conv", "gru_forward", "gru_forward_noalloc", "gemm_workspace_size",
            "dwsep_conv_workspace_size", "gru_forward_workspace_size", "IsamError",
            "linear_gru", "linear_gru_backward", "linear_gru_states_shape", "linear_gru_workspace_size",
-           "linear_gru_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
+           "linear_gru_backward_workspace_size", "norm_residual", "norm_residual_backward",
+           "norm_residual_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
 
 _DT = {torch.float32: ISAM_F32, torch.bfloat16: ISAM_BF16}
 
@@ -361,3 +362,95 @@ def linear_gru_backward(gx: torch.Tensor, dh_seq: torch.Tensor | None, *, states
                                         _ptr(workspace), _bytes(workspace), _stream())
     _call(rc, "isam_linear_gru_backward")
     return dgx, dh0, dbias
+
+
+# ---------------------------------------------------------------------------------------
+# Gated residual norm
+# ---------------------------------------------------------------------------------------
+def _matrix(t, name, shape, dtype):
+    """Leading dimension of a [rows][D] tensor with unit inner stride (None: 0)."""
+    if t is None:
+        return 0
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} needs unit inner stride")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _norm_args(r, gate, w_post, w_pre):
+    if r.dim() != 2:
+        raise ValueError("rows must be [rows][D]")
+    R, D = r.shape
+    if gate is not None and (gate.dim() != 2 or gate.shape[1] != D or (R and (gate.shape[0] == 0 or R % gate.shape[0]))):
+        raise ValueError("gate must be [gates][D] with gates a divisor of rows")
+    G = 1 if gate is None else gate.shape[0]
+    _want(gate, "gate", (G, D), r.dtype)
+    _want(w_post, "w_post", (D,))
+    _want(w_pre, "w_pre", (D,))
+    return R, D, G
+
+
+def norm_residual_backward_workspace_size(rows, D, gates, dtype) -> int:
+    return lib().isam_norm_residual_backward_workspace_size(rows, D, gates, dtype)
+
+
+def norm_residual(x: torch.Tensor | None, r: torch.Tensor, *, w_pre, w_post=None, gate=None, scale=1.0, eps=1e-6, r_out=None,
+                  y=None):
+    """Gated residual norm over rows: r_out = r + scale * gate * u with u = x / rms(x) * w_post (u = x
+    without w_post), y = r_out / rms(r_out) * w_pre, rms(v) = sqrt(mean(v^2) + eps).
+    x, r [rows][D] (float32 or bfloat16; row strides may exceed D), gate [gates][D] in their
+    dtype with gates a divisor of rows, w_post and w_pre [D] float32.  r_out may be r.
+    x None: y = norm of r alone.  Returns (r_out, y); r_out is r without x."""
+    _check_dev(x, r, w_pre, w_post, gate, r_out, y)
+    R, D, G = _norm_args(r, gate, w_post, w_pre)
+    dt, dev = _dt(r), r.device
+    _same_device(dev, x=x, w_pre=w_pre, w_post=w_post, gate=gate, r_out=r_out, y=y)
+    if r_out is None and x is not None:
+        r_out = torch.empty((R, D), device=dev, dtype=r.dtype)
+    if y is None:
+        y = torch.empty((R, D), device=dev, dtype=r.dtype)
+    shape, ty = (R, D), r.dtype
+    ldx, ldr = _matrix(x, "x", shape, ty), _matrix(r, "r", shape, ty)
+    ldro, ldy = _matrix(r_out, "r_out", shape, ty), _matrix(y, "y", shape, ty)
+    rc = lib().isam_norm_residual(R, D, G, dt, _ptr(x), ldx, _ptr(r), ldr, _ptr(gate), _ptr(w_post), _ptr(w_pre), scale, eps,
+                                  _ptr(r_out), ldro, _ptr(y), ldy, _stream())
+    _call(rc, "isam_norm_residual")
+    return (r if x is None else r_out), y
+
+
+def norm_residual_backward(x: torch.Tensor | None, r_out: torch.Tensor, dy: torch.Tensor, *, w_pre, w_post=None, gate=None,
+                           scale=1.0, eps=1e-6, dr_out=None, dx=None, dr=None, dgate=None, dw_post=None, dw_pre=None,
+                           workspace: torch.Tensor | None = None):
+    """Gradient of ``norm_residual``: x, gate, w_post, w_pre, scale and eps as in the forward call, r_out
+    as it left it, dy and dr_out (None for zeros) the gradients of y and r_out.  dr may be dr_out.
+    Returns (dx, dr, dgate, dw_post, dw_pre), None where the forward call had no such input."""
+    _check_dev(x, r_out, dy, w_pre, w_post, gate, dr_out, dx, dr, dgate, dw_post, dw_pre, workspace)
+    R, D, G = _norm_args(r_out, gate, w_post, w_pre)
+    dt, dev, shape, ty = _dt(r_out), r_out.device, (R, D), r_out.dtype
+    _same_device(dev, x=x, dy=dy, w_pre=w_pre, w_post=w_post, gate=gate, dr_out=dr_out, dx=dx, dr=dr, dgate=dgate,
+                 dw_post=dw_post, dw_pre=dw_pre, workspace=workspace)
+    if dx is None and x is not None:
+        dx = torch.empty(shape, device=dev, dtype=ty)
+    if dr is None:
+        dr = torch.empty(shape, device=dev, dtype=ty)
+    if dgate is None and gate is not None:
+        dgate = torch.empty((G, D), device=dev, dtype=ty)
+    if dw_post is None and w_post is not None:
+        dw_post = torch.empty((D,), device=dev, dtype=torch.float32)
+    if dw_pre is None:
+        dw_pre = torch.empty((D,), device=dev, dtype=torch.float32)
+    _want(dgate, "dgate", (G, D), ty)
+    _want(dw_post, "dw_post", (D,))
+    _want(dw_pre, "dw_pre", (D,))
+    if workspace is None:
+        workspace = _room(None, norm_residual_backward_workspace_size(R, D, G, dt), dev)
+    rc = lib().isam_norm_residual_backward(
+        R, D, G, dt, _ptr(x), _matrix(x, "x", shape, ty), _ptr(r_out), _matrix(r_out, "r_out", shape, ty), _ptr(gate),
+        _ptr(w_post), _ptr(w_pre), scale, eps, _ptr(dy), _matrix(dy, "dy", shape, ty), _ptr(dr_out),
+        _matrix(dr_out, "dr_out", shape, ty), _ptr(dx), _matrix(dx, "dx", shape, ty), _ptr(dr), _matrix(dr, "dr", shape, ty),
+        _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(workspace), _bytes(workspace), _stream())
+    _call(rc, "isam_norm_residual_backward")
+    return dx, dr, dgate, dw_post, dw_pre

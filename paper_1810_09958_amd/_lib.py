@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ISAM_F32, ISAM_BF16 = 0, 1
 
 # name -> (restype, argtypes), mirroring include/isam.h
-i64, vp, sz, ci = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+i64, vp, sz, ci, cf = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
 SIGNATURES = {
     "isam_gemm": (ci, [ci, ci, i64, i64, i64, ci, vp, i64, vp, i64, ci, ci, vp, i64, vp, sz, vp]),
     "isam_gemm_workspace_size": (sz, [ci, ci, i64, i64, i64, ci, ci]),
@@ -23,6 +23,10 @@ SIGNATURES = {
     "isam_linear_gru_backward": (ci, [i64, i64, i64, ci, ci, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64,
                                       i64, vp, vp, vp, sz, vp]),
     "isam_linear_gru_backward_workspace_size": (sz, [i64, i64, i64, ci]),
+    "isam_norm_residual": (ci, [i64, i64, i64, ci, vp, i64, vp, i64, vp, vp, vp, cf, cf, vp, i64, vp, i64, vp]),
+    "isam_norm_residual_backward": (ci, [i64, i64, i64, ci, vp, i64, vp, i64, vp, vp, vp, cf, cf, vp, i64, vp, i64, vp, i64,
+                                         vp, i64, vp, vp, vp, vp, sz, vp]),
+    "isam_norm_residual_backward_workspace_size": (sz, [i64, i64, i64, ci]),
     "isam_status_string": (ctypes.c_char_p, [ci]),
     "isam_last_error": (ctypes.c_char_p, []),
     "isam_version": (ci, []),

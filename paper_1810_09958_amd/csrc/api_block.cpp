@@ -222,3 +222,174 @@ extern "C" size_t isam_linear_gru_backward_workspace_size(int64_t T, int64_t bat
     lingru_segments(T, batch, hidden, type, device_cus(), &segs, &per);
     return room(lingru_agg_bytes(segs, batch, hidden) + lingru_bias_bytes(segs, batch, hidden));
 }
+
+// ---------------------------------------------------------------------------
+// Gated residual norm
+// ---------------------------------------------------------------------------
+namespace {
+
+bool norm_sizes(int64_t rows, int64_t D) { return D <= kNormMaxD && rows < ((int64_t)1 << 40); }
+
+isam_status_t norm_check(int64_t rows, int64_t D, int64_t* gates, int type, const void* gate, float scale, float eps,
+                         const char* who) {
+    if (rows < 0 || D < 0) return fail(ISAM_ERR_INVALID_ARG, "%s: negative size rows=%lld D=%lld", who, (long long)rows, (long long)D);
+    if (!valid_dtype(type)) return fail(ISAM_ERR_INVALID_ARG, "%s: dtype must be ISAM_F32 (0) or ISAM_BF16 (1)", who);
+    if (!(eps >= 0.0f)) return fail(ISAM_ERR_INVALID_ARG, "%s: eps must not be negative", who);
+    if (scale != scale) return fail(ISAM_ERR_INVALID_ARG, "%s: scale is NaN", who);
+    if (!gate) *gates = 1;
+    if (*gates < 0 || (rows > 0 && (*gates == 0 || rows % *gates)))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: gates=%lld must divide rows=%lld", who, (long long)*gates, (long long)rows);
+    if (!norm_sizes(rows, D))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: D=%lld above %lld, or too many rows", who, (long long)D, (long long)kNormMaxD);
+    return ISAM_OK;
+}
+
+// Address range of a matrix operand (0 bytes for NULL); false if a row is longer than
+// its leading dimension or the range passes 2^46 bytes.
+bool matrix(const void* p, int64_t rows, int64_t D, int64_t ld, size_t es, size_t* bytes) {
+    *bytes = 0;
+    if (!p) return true;
+    return ld >= D && extent(rows, ld, 1, 0, D, es, bytes);
+}
+
+}  // namespace
+
+extern "C" isam_status_t isam_norm_residual(int64_t rows, int64_t D, int64_t gates, int type, const void* x, int64_t ldx,
+                                            const void* r, int64_t ldr, const void* gate, const float* w_post,
+                                            const float* w_pre, float scale, float eps, void* r_out, int64_t ldro, void* y,
+                                            int64_t ldy, void* stream) {
+    clear_error();
+    const char* who = "isam_norm_residual";
+    isam_status_t st = norm_check(rows, D, &gates, type, gate, scale, eps, who);
+    if (st != ISAM_OK || rows == 0 || D == 0) return st;
+    if (!r || !w_pre || !y) return fail(ISAM_ERR_INVALID_ARG, "%s: r, w_pre or y is NULL", who);
+    if (x ? !r_out : (r_out || gate || w_post))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: x needs r_out; r_out, gate and w_post need x", who);
+    const size_t es = dsize(type);
+    size_t x_b, r_b, ro_b, y_b, g_b;
+    if (!matrix(x, rows, D, ldx, es, &x_b) || !matrix(r, rows, D, ldr, es, &r_b) || !matrix(r_out, rows, D, ldro, es, &ro_b) ||
+        !matrix(y, rows, D, ldy, es, &y_b) || !matrix(gate, gates, D, D, es, &g_b))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: a leading dimension is below D, or a tensor spans more than 2^46 bytes", who);
+    const bool in_place = r_out == r && ldro == ldr;  // each row is read whole before it is written
+    const Tensor all[] = {{"x", x, x_b, false},
+                          {"r", r, r_b, false},
+                          {"gate", gate, g_b, false},
+                          {"w_post", w_post, (size_t)D * 4, false},
+                          {"w_pre", w_pre, (size_t)D * 4, false},
+                          {"r_out", in_place ? nullptr : r_out, ro_b, true},
+                          {"y", y, y_b, true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    if (in_place) {
+        const Tensor out[] = {{"r_out", r_out, ro_b, true}, {"x", x, x_b, false}, {"gate", gate, g_b, false},
+                              {"w_post", w_post, (size_t)D * 4, false}, {"w_pre", w_pre, (size_t)D * 4, false}, {"y", y, y_b, true}};
+        if ((st = disjoint(out, who)) != ISAM_OK) return st;
+    }
+    NormArgs a{};
+    a.rows = rows;
+    a.D = D;
+    a.type = type;
+    a.gates = gates;
+    a.rows_per_gate = rows / gates;
+    a.x = x;
+    a.r = r;
+    a.gate = gate;
+    a.ld_x = ldx;
+    a.ld_r = ldr;
+    a.w_post = w_post;
+    a.w_pre = w_pre;
+    a.scale = scale;
+    a.eps = eps;
+    a.r_out = r_out;
+    a.y = y;
+    a.ld_ro = ldro;
+    a.ld_y = ldy;
+    const hipError_t e = launch_norm_forward(a, device_cus(), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" isam_status_t isam_norm_residual_backward(int64_t rows, int64_t D, int64_t gates, int type, const void* x,
+                                                     int64_t ldx, const void* r_out, int64_t ldro, const void* gate,
+                                                     const float* w_post, const float* w_pre, float scale, float eps,
+                                                     const void* dy, int64_t lddy, const void* dr_out, int64_t lddro,
+                                                     void* dx, int64_t lddx, void* dr, int64_t lddr, void* dgate,
+                                                     float* dw_post, float* dw_pre, void* workspace,
+                                                     size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_norm_residual_backward";
+    const bool rows0 = rows == 0;
+    const int64_t gate_rows = gates;
+    isam_status_t st = norm_check(rows, D, &gates, type, gate, scale, eps, who);
+    if (st != ISAM_OK || D == 0) return st;
+    if (!rows0 && (!r_out || !w_pre || !dy || !dr)) return fail(ISAM_ERR_INVALID_ARG, "%s: r_out, w_pre, dy or dr is NULL", who);
+    if (!rows0 && (x ? !dx : (dx || gate || w_post)))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: x needs dx; dx, gate and w_post need x", who);
+    if (!rows0 && ((dgate && !gate) || (dw_post && !w_post)))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: dgate needs gate, dw_post w_post", who);
+    if (rows0) gates = gate_rows;  // dgate is cleared whatever stands for the gate
+    const size_t es = dsize(type);
+    if (rows0 && dgate && (gates < 0 || gates > ((int64_t)1 << 40) / D))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: gates=%lld", who, (long long)gates);
+    NormArgs a{};
+    int64_t grid = 0;
+    if (!rows0) norm_bwd_grid(rows, D, gates, type, device_cus(), &grid, &a.parts);
+    const size_t need = (size_t)(3 * grid * D) * sizeof(float);
+    if (need && (!workspace || workspace_bytes < room(need)))
+        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
+                    room(need));
+    size_t x_b, r_b, dy_b, dro_b, dx_b, dr_b, g_b, dg_b;
+    if (!matrix(x, rows, D, ldx, es, &x_b) || !matrix(r_out, rows, D, ldro, es, &r_b) || !matrix(dy, rows, D, lddy, es, &dy_b) ||
+        !matrix(dr_out, rows, D, lddro, es, &dro_b) || !matrix(dx, rows, D, lddx, es, &dx_b) ||
+        !matrix(dr, rows, D, lddr, es, &dr_b) || !matrix(gate, gates, D, D, es, &g_b) || !matrix(dgate, gates, D, D, es, &dg_b))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: a leading dimension is below D, or a tensor spans more than 2^46 bytes", who);
+    const size_t w_b = (size_t)D * 4;
+    const bool in_place = dr && dr == dr_out && lddr == lddro;
+    const Tensor all[] = {{"x", x, x_b, false},           {"r_out", r_out, r_b, false},
+                          {"gate", gate, g_b, false},     {"w_post", w_post, w_b, false},
+                          {"w_pre", w_pre, w_b, false},   {"dy", dy, dy_b, false},
+                          {"dr_out", in_place ? nullptr : dr_out, dro_b, false},
+                          {"dx", dx, dx_b, true},         {"dr", dr, dr_b, true},
+                          {"dgate", dgate, dg_b, true},   {"dw_post", dw_post, w_b, true},
+                          {"dw_pre", dw_pre, w_b, true},  {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    a.rows = rows;
+    a.D = D;
+    a.type = type;
+    a.gates = gates;
+    a.rows_per_gate = rows0 ? 1 : rows / gates;
+    a.x = x;
+    a.r = r_out;
+    a.gate = gate;
+    a.ld_x = ldx;
+    a.ld_r = ldro;
+    a.w_post = w_post;
+    a.w_pre = w_pre;
+    a.scale = scale;
+    a.eps = eps;
+    a.dy = dy;
+    a.dr_out = dr_out;
+    a.dx = dx;
+    a.dr = dr;
+    a.ld_dy = lddy;
+    a.ld_dro = lddro;
+    a.ld_dx = lddx;
+    a.ld_dr = lddr;
+    a.dgate = dgate;
+    a.dw_post = dw_post;
+    a.dw_pre = dw_pre;
+    a.partial = reinterpret_cast<float*>(room_start(workspace));
+    const hipError_t e = launch_norm_backward(a, grid, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64_t D, int64_t gates, int type) {
+    if (rows <= 0 || D <= 0 || !valid_dtype(type) || !norm_sizes(rows, D)) return 0;
+    // without a gate the call has one gate row
+    int64_t grid, most = 0;
+    int parts;
+    for (const int64_t g : {gates, (int64_t)1}) {
+        if (g <= 0 || rows % g) continue;
+        norm_bwd_grid(rows, D, g, type, device_cus(), &grid, &parts);
+        if (grid > most) most = grid;
+    }
+    return room((size_t)(3 * most * D) * sizeof(float));
+}

@@ -267,6 +267,39 @@ void lingru_segments(int64_t T, int64_t batch, int64_t H, int type, int cus, int
 hipError_t launch_lingru_forward(const LinGruArgs& a, hipStream_t s);
 hipError_t launch_lingru_backward(const LinGruArgs& a, hipStream_t s);
 
+// Gated residual norm (norm_residual.hip): rows of D values at their own leading
+// dimensions, gate and dgate dense [gates][D], rows / gates rows to a gate row.
+constexpr int64_t kNormMaxD = 16384;
+struct NormArgs {
+    int64_t rows, D;
+    int type;                       // of every matrix
+    int64_t gates, rows_per_gate;   // 1 and all rows without a gate
+    const void* x;                  // or null: r_out = r
+    const void* r;                  // backward: r_out of the forward pass
+    const void* gate;               // or null
+    int64_t ld_x, ld_r;
+    const float* w_post;            // or null: no norm after the block
+    const float* w_pre;
+    float scale, eps;
+    void* r_out;
+    void* y;
+    int64_t ld_ro, ld_y;
+    // backward
+    const void* dy;
+    const void* dr_out;             // or null
+    void* dx;
+    void* dr;
+    int64_t ld_dy, ld_dro, ld_dx, ld_dr;
+    void* dgate;                    // or null
+    float* dw_post;                 // or null
+    float* dw_pre;                  // or null
+    int parts;                      // workgroups of a gate row; 0: row groups own whole gate rows
+    float* partial;                 // [3][grid][D]: sums for w_pre, w_post and the gate
+};
+void norm_bwd_grid(int64_t rows, int64_t D, int64_t gates, int type, int cus, int64_t* grid, int* parts);
+hipError_t launch_norm_forward(const NormArgs& a, int cus, hipStream_t s);
+hipError_t launch_norm_backward(const NormArgs& a, int64_t grid, hipStream_t s);
+
 // out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros).
 hipError_t launch_colsum(const float* part, int64_t rows, int64_t cols, int64_t groups, int out_type, void* out, hipStream_t s);
 

@@ -70,3 +70,45 @@ def test_linear_gru_workspace(L):
         assert L.isam_linear_gru_workspace_size(*bad) == 0
         if bad[0]:
             assert L.isam_linear_gru_backward_workspace_size(*bad) == 0
+
+
+def norm(L, R=6, D=8, G=1, dt=F32, x=at(0), ldx=8, r=at(1), ldr=8, gate=at(2), wa=at(3), wb=at(4), scale=1.0, eps=1e-6, ro=at(5),
+         ldro=8, y=at(6), ldy=8):
+    return L.isam_norm_residual(R, D, G, dt, x, ldx, r, ldr, gate, wa, wb, scale, eps, ro, ldro, y, ldy, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(R=-1), INVALID), (dict(D=-1), INVALID), (dict(dt=2), INVALID), (dict(G=4), INVALID), (dict(G=0), INVALID),
+    (dict(G=-1), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(r=None), INVALID), (dict(wb=None), INVALID), (dict(y=None), INVALID), (dict(ro=None), INVALID),
+    (dict(x=None), INVALID), (dict(x=None, ro=None, gate=None), INVALID), (dict(ldx=7), INVALID), (dict(ldy=7), INVALID),
+    (dict(y=at(0)), INVALID), (dict(y=at(1)), INVALID), (dict(ro=at(0)), INVALID), (dict(ro=at(1), ldro=9), INVALID),
+    (dict(ro=at(1), y=at(1)), INVALID), (dict(D=16385, ldx=20000, ldr=20000, ldro=20000, ldy=20000), UNSUPPORTED),
+])
+def test_norm_residual_refusals(L, kw, code):
+    assert norm(L, **kw) == code
+    assert L.isam_last_error() != b""
+
+
+def norm_bwd(L, R=6, D=8, G=1, dt=F32, x=at(0), r=at(1), gate=at(2), wa=at(3), wb=at(4), dy=at(5), dro=at(6), lddro=8, dx=at(7),
+             dr=at(8), dg=at(9), da=at(10), db=at(11), ws=at(12), wsb=1 << 20):
+    return L.isam_norm_residual_backward(R, D, G, dt, x, 8, r, 8, gate, wa, wb, 1.0, 1e-6, dy, 8, dro, lddro, dx, 8, dr, 8, dg, da,
+                                         db, ws, wsb, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(R=-1), INVALID), (dict(G=5), INVALID), (dict(dy=None), INVALID), (dict(dr=None), INVALID), (dict(dx=None), INVALID),
+    (dict(x=None), INVALID), (dict(gate=None), INVALID), (dict(wa=None), INVALID), (dict(dx=at(0)), INVALID),
+    (dict(dr=at(6), lddro=9), INVALID), (dict(dg=at(2)), INVALID), (dict(da=at(11)), INVALID), (dict(ws=at(7)), INVALID),
+    (dict(ws=None), WORKSPACE), (dict(wsb=100), WORKSPACE),
+])
+def test_norm_residual_backward_refusals(L, kw, code):
+    assert norm_bwd(L, **kw) == code
+    assert L.isam_last_error() != b""
+
+
+def test_norm_residual_no_op_and_workspace(L):
+    assert norm(L, R=0) == OK and norm(L, D=0) == OK
+    assert L.isam_norm_residual_backward_workspace_size(100, 64, 1, BF16) >= 3 * 64 * 4
+    for bad in ((0, 64, 1, F32), (4, 0, 1, F32), (4, 16385, 1, F32), (4, 64, 1, 7)):
+        assert L.isam_norm_residual_backward_workspace_size(*bad) == 0
