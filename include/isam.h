@@ -349,6 +349,49 @@ isam_status_t isam_norm_residual_backward(int64_t rows, int64_t D, int64_t gates
 
 size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64_t D, int64_t gates, int type);
 
+/*
+ * Gated feed-forward block: both projections, the activation and the product,
+ *   out[m][f] = act(sum_k x[m][k] W[f][k] + bias[f]) * (sum_k x[m][k] W[F+f][k] + bias[F+f])
+ * with the gate rows of W before the up rows.
+ *   x    [M][K] (type) at leading dimension ldx >= K
+ *   W    [2*F][K] (type) at ldw >= K          bias  [2*F] fp32, or NULL
+ *   out  [M][F] (type) at ldo >= F
+ *   act  sigmoid(g), g * sigmoid(g) (silu) or g * (1 + erf(g / sqrt 2)) / 2 (gelu)
+ * Sums are fp32; out is rounded once.  K > 0; M or F == 0: no-op.
+ * bf16 beyond 16 rows runs as one kernel on 16-byte aligned rows (x and W on 16 bytes,
+ * K, ldx and ldw multiples of 8); other rows are copied into the workspace first.
+ * fp32 beyond 16 rows forms the two projections by the matrix product of isam_gemm
+ * in the workspace.  Up to 16 rows no workspace is used.
+ * Workspace: isam_gated_ffn_workspace_size bytes; aligned = 0 also makes room for the copies
+ * (K off 8 says so by itself), which a call with unaligned pointers or leading
+ * dimensions needs.  Each matrix, and M x 2F values of `type`, below 2^31 bytes.
+ */
+typedef enum { ISAM_ACT_SIGMOID = 0, ISAM_ACT_SILU = 1, ISAM_ACT_GELU = 2 } isam_activation_t;
+
+isam_status_t isam_gated_ffn(int64_t M, int64_t K, int64_t F, int type, int act, const void* x, int64_t ldx, const void* W,
+                             int64_t ldw, const float* bias, void* out, int64_t ldo, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+size_t isam_gated_ffn_workspace_size(int64_t M, int64_t K, int64_t F, int type, int aligned);
+
+/*
+ * Gradient of isam_gated_ffn from dout, the gradient of out.  With g and u the two
+ * projections (formed again; nothing is kept from the forward call):
+ *   dg = dout * u * act'(g),  du = dout * act(g)
+ *   dx = dg . W[0:F] + du . W[F:2F],  dW = [dg du]^T . x,  dbias = column sums of [dg du]
+ *   dx [M][K] (type) at lddx >= K, dW [2*F][K] (type) at lddw >= K, dbias [2*F] fp32;
+ *   each may be NULL, not all
+ * bf16: dg and du are rounded to bf16 as the operands of the products (dbias is summed
+ * from the unrounded values).  Everything else is fp32.  Sums are in a fixed order.
+ * M == 0: dW and dbias are 0.
+ */
+isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F, int type, int act, const void* x, int64_t ldx,
+                                      const void* W, int64_t ldw, const float* bias, const void* dout, int64_t lddo, void* dx,
+                                      int64_t lddx, void* dW, int64_t lddw, float* dbias, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+size_t isam_gated_ffn_backward_workspace_size(int64_t M, int64_t K, int64_t F, int type, int aligned);
+
 /* Static text for a status code. */
 const char* isam_status_string(int status);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */

@@ -20,7 +20,8 @@ __all__ = ["gemm", "conv1d", "dwsep_conv", "gru_forward", "gru_forward_noalloc",
            "dwsep_conv_workspace_size", "gru_forward_workspace_size", "IsamError",
            "linear_gru", "linear_gru_backward", "linear_gru_states_shape", "linear_gru_workspace_size",
            "linear_gru_backward_workspace_size", "norm_residual", "norm_residual_backward",
-           "norm_residual_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
+           "norm_residual_backward_workspace_size", "gated_ffn", "gated_ffn_backward", "gated_ffn_workspace_size",
+           "gated_ffn_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
 
 _DT = {torch.float32: ISAM_F32, torch.bfloat16: ISAM_BF16}
 
@@ -454,3 +455,77 @@ def norm_residual_backward(x: torch.Tensor | None, r_out: torch.Tensor, dy: torc
         _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(workspace), _bytes(workspace), _stream())
     _call(rc, "isam_norm_residual_backward")
     return dx, dr, dgate, dw_post, dw_pre
+
+
+# ---------------------------------------------------------------------------------------
+# Gated feed-forward block
+# ---------------------------------------------------------------------------------------
+_ACTIVATIONS = {"sigmoid": 0, "silu": 1, "gelu": 2}
+
+
+def gated_ffn_workspace_size(M, K, F, dtype, aligned=True) -> int:
+    return lib().isam_gated_ffn_workspace_size(M, K, F, dtype, int(aligned))
+
+
+def gated_ffn_backward_workspace_size(M, K, F, dtype, aligned=True) -> int:
+    return lib().isam_gated_ffn_backward_workspace_size(M, K, F, dtype, int(aligned))
+
+
+def _gated_args(x, W, bias):
+    if x.dim() != 2 or W.dim() != 2 or W.shape[0] % 2 or W.shape[1] != x.shape[1]:
+        raise ValueError("x must be [M][K] and W [2 * F][K]")
+    M, K = x.shape
+    F = W.shape[0] // 2
+    _want(bias, "bias", (2 * F,))
+    return M, K, F, _dt(x), _matrix(x, "x", (M, K), x.dtype), _matrix(W, "W", (2 * F, K), x.dtype)
+
+
+def _aligned(t, ld):
+    return t.data_ptr() % 16 == 0 and ld % 8 == 0
+
+
+def gated_ffn(x: torch.Tensor, W: torch.Tensor, *, bias=None, activation="silu", out=None,
+              workspace: torch.Tensor | None = None):
+    """Gated feed-forward block: act(x Wg^T + bg) * (x Wu^T + bu), both projections, the activation
+    ("sigmoid", "silu" or "gelu") and the product together.  x [M][K], W [2F][K] (gate rows, then up
+    rows; float32 or bfloat16; row strides may exceed K), bias [2F] float32.  Returns out [M][F] in
+    x's dtype."""
+    _check_dev(x, W, bias, out, workspace)
+    M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
+    act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
+    _same_device(dev, W=W, bias=bias, out=out, workspace=workspace)
+    if out is None:
+        out = torch.empty((M, F), device=dev, dtype=x.dtype)
+    ldo = _matrix(out, "out", (M, F), x.dtype)
+    if workspace is None:
+        workspace = _room(None, gated_ffn_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
+    rc = lib().isam_gated_ffn(M, K, F, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(out), ldo, _ptr(workspace),
+                              _bytes(workspace), _stream())
+    _call(rc, "isam_gated_ffn")
+    return out
+
+
+def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, bias=None, activation="silu", dx=None, dW=None,
+                       dbias=None, workspace: torch.Tensor | None = None):
+    """Gradient of ``gated_ffn`` from dout [M][F]: the projections are formed again, nothing is kept
+    from the forward call.  Returns (dx [M][K], dW [2F][K] in x's dtype, dbias [2F] float32 or
+    None without a bias)."""
+    _check_dev(x, W, dout, bias, dx, dW, dbias, workspace)
+    M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
+    act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
+    _same_device(dev, W=W, dout=dout, bias=bias, dx=dx, dW=dW, dbias=dbias, workspace=workspace)
+    if dx is None:
+        dx = torch.empty((M, K), device=dev, dtype=x.dtype)
+    if dW is None:
+        dW = torch.empty((2 * F, K), device=dev, dtype=x.dtype)
+    if dbias is None and bias is not None:
+        dbias = torch.empty((2 * F,), device=dev, dtype=torch.float32)
+    _want(dbias, "dbias", (2 * F,))
+    lddo, lddx = _matrix(dout, "dout", (M, F), x.dtype), _matrix(dx, "dx", (M, K), x.dtype)
+    lddw = _matrix(dW, "dW", (2 * F, K), x.dtype)
+    if workspace is None:
+        workspace = _room(None, gated_ffn_backward_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
+    rc = lib().isam_gated_ffn_backward(M, K, F, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(dout), lddo, _ptr(dx), lddx,
+                                       _ptr(dW), lddw, _ptr(dbias), _ptr(workspace), _bytes(workspace), _stream())
+    _call(rc, "isam_gated_ffn_backward")
+    return dx, dW, dbias

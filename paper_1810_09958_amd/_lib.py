@@ -27,6 +27,10 @@ SIGNATURES = {
     "isam_norm_residual_backward": (ci, [i64, i64, i64, ci, vp, i64, vp, i64, vp, vp, vp, cf, cf, vp, i64, vp, i64, vp, i64,
                                          vp, i64, vp, vp, vp, vp, sz, vp]),
     "isam_norm_residual_backward_workspace_size": (sz, [i64, i64, i64, ci]),
+    "isam_gated_ffn": (ci, [i64, i64, i64, ci, ci, vp, i64, vp, i64, vp, vp, i64, vp, sz, vp]),
+    "isam_gated_ffn_workspace_size": (sz, [i64, i64, i64, ci, ci]),
+    "isam_gated_ffn_backward": (ci, [i64, i64, i64, ci, ci, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]),
+    "isam_gated_ffn_backward_workspace_size": (sz, [i64, i64, i64, ci, ci]),
     "isam_status_string": (ctypes.c_char_p, [ci]),
     "isam_last_error": (ctypes.c_char_p, []),
     "isam_version": (ci, []),

@@ -1,5 +1,7 @@
 // C-ABI layer of the operators of a gated recurrent block: argument validation
 // (pure host code, no HIP call) and dispatch.
+#include <algorithm>
+
 #include "api.hpp"
 
 using namespace isam;
@@ -392,4 +394,240 @@ extern "C" size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64
         if (grid > most) most = grid;
     }
     return room((size_t)(3 * most * D) * sizeof(float));
+}
+
+// ---------------------------------------------------------------------------
+// Gated feed-forward block
+// ---------------------------------------------------------------------------
+namespace {
+
+// Parts of the workspace, in order: copies of x and W with aligned rows, the
+// projections (fp32) or their gradients, the bias gradient's partial sums, and
+// what the matrix products use.
+struct GatedPlan {
+    int64_t Kp;                       // row length of the copies
+    bool copy_x, copy_w;
+    int tile;
+    size_t x_b, w_b, pair_b, bias_b, gemm_b;
+    size_t total() const { return x_b + w_b + pair_b + bias_b + gemm_b; }
+};
+
+bool rows_aligned(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+GatedPlan gated_plan(int64_t M, int64_t K, int64_t F, int type, bool x_ok, bool w_ok, bool backward) {
+    GatedPlan p{};
+    const size_t es = dsize(type);
+    if (M == 0 || (!backward && M <= kGatedTokens)) return p;
+    if (type == ISAM_BF16) {
+        p.copy_x = !x_ok || K % 8;
+        p.copy_w = !w_ok || K % 8;
+        // whole 64-deep tiles where that adds at most an eighth (no range checks in the kernel)
+        p.Kp = (cdiv(K, 64) * 64 - K) * 8 <= K ? cdiv(K, 64) * 64 : cdiv(K, 8) * 8;
+        if (!(p.copy_x && p.copy_w)) p.Kp = cdiv(K, 8) * 8;
+        if (p.copy_x) p.x_b = align256((size_t)(M * p.Kp) * es);
+        if (p.copy_w) p.w_b = align256((size_t)(2 * F * p.Kp) * es);
+        p.tile = gated_tile(M, F, device_cus());
+    }
+    if (backward || type == ISAM_F32) p.pair_b = align256((size_t)(M * 2 * F) * es);
+    if (backward) p.bias_b = align256((size_t)((type == ISAM_BF16 ? gated_bias_rows(p.tile, M) : cdiv(M, kGatedRows)) * 2 * F) * sizeof(float));
+    if (type == ISAM_F32) p.gemm_b = product_workspace(0, 1, M, 2 * F, K, type);
+    if (backward) {
+        p.gemm_b = std::max(p.gemm_b, product_workspace(0, 0, M, K, 2 * F, type));
+        p.gemm_b = std::max(p.gemm_b, product_workspace(1, 0, 2 * F, K, M, type));
+    }
+    p.gemm_b = align256(p.gemm_b);
+    return p;
+}
+
+isam_status_t gated_check(int64_t M, int64_t K, int64_t F, int type, int act, const char* who) {
+    if (M < 0 || K <= 0 || F < 0)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: bad size M=%lld K=%lld F=%lld", who, (long long)M, (long long)K, (long long)F);
+    if (!valid_dtype(type)) return fail(ISAM_ERR_INVALID_ARG, "%s: dtype must be ISAM_F32 (0) or ISAM_BF16 (1)", who);
+    if (act < ISAM_ACT_SIGMOID || act > ISAM_ACT_GELU)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: activation must be 0 (sigmoid), 1 (silu) or 2 (gelu)", who);
+    return ISAM_OK;
+}
+
+// A matrix operand whose extent must stay below 2^31 bytes; a null one has none.
+isam_status_t gated_matrix(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, size_t es, size_t* bytes,
+                           const char* who) {
+    *bytes = 0;
+    if (!p || rows == 0 || cols == 0) return ISAM_OK;
+    if (ld < cols) return fail(ISAM_ERR_INVALID_ARG, "%s: leading dimension %lld of %s below %lld", who, (long long)ld, name, (long long)cols);
+    if (!extent(rows, ld, 1, 0, cols, es, bytes) || *bytes > (size_t)kMaxExtent)
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: %s spans more than 2^31 bytes", who, name);
+    return ISAM_OK;
+}
+
+// Sizes for which every buffer the plan adds stays below 2^31 bytes as well.
+bool gated_sizes(int64_t M, int64_t K, int64_t F, int type) {
+    const __int128 es = (__int128)dsize(type), most = kMaxExtent;
+    const __int128 Kp = (__int128)K + 64;
+    return (__int128)M * 2 * F * es <= most && (__int128)M * Kp * es <= most && (__int128)2 * F * Kp * es <= most &&
+           (type == ISAM_BF16 || M <= 65535 * kGatedRows);
+}
+
+// Copies of x and W with aligned rows, where the plan has them; x, W and their
+// leading dimensions become those of the copies.
+hipError_t gated_copies(const GatedPlan& p, char* ws, GatedArgs& a, hipStream_t s) {
+    if (!p.copy_x && !p.copy_w) return hipSuccess;
+    PackRows cx{}, cw{};
+    if (p.copy_x) cx = PackRows{static_cast<const uint16_t*>(a.x), a.M, a.K, a.ld_x, reinterpret_cast<uint16_t*>(ws), p.Kp};
+    if (p.copy_w)
+        cw = PackRows{static_cast<const uint16_t*>(a.W), 2 * a.F, a.K, a.ld_w, reinterpret_cast<uint16_t*>(ws + p.x_b), p.Kp};
+    const hipError_t e = launch_pack_rows(cx, cw, device_cus(), s);
+    if (e != hipSuccess) return e;
+    // (one operand copied: rows of K rounded up to 8 there, K itself a multiple of 8)
+    if (p.copy_x) {
+        a.x = cx.dst;
+        a.ld_x = p.Kp;
+    }
+    if (p.copy_w) {
+        a.W = cw.dst;
+        a.ld_w = p.Kp;
+    }
+    a.K = p.Kp;
+    return hipSuccess;
+}
+
+}  // namespace
+
+extern "C" isam_status_t isam_gated_ffn(int64_t M, int64_t K, int64_t F, int type, int act, const void* x, int64_t ldx,
+                                        const void* W, int64_t ldw, const float* bias, void* out, int64_t ldo, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_gated_ffn";
+    isam_status_t st = gated_check(M, K, F, type, act, who);
+    if (st != ISAM_OK || M == 0 || F == 0) return st;
+    if (!x || !W || !out) return fail(ISAM_ERR_INVALID_ARG, "%s: x, W or out is NULL", who);
+    const size_t es = dsize(type);
+    size_t x_b, w_b, o_b;
+    if ((st = gated_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
+        (st = gated_matrix("W", W, 2 * F, K, ldw, es, &w_b, who)) != ISAM_OK ||
+        (st = gated_matrix("out", out, M, F, ldo, es, &o_b, who)) != ISAM_OK)
+        return st;
+    if (!gated_sizes(M, K, F, type)) return fail(ISAM_ERR_UNSUPPORTED, "%s: M x 2F, M x K or 2F x K passes 2^31 bytes", who);
+    const GatedPlan p = gated_plan(M, K, F, type, rows_aligned(x, ldx), rows_aligned(W, ldw), false);
+    const size_t need = p.total();
+    if (need && (!workspace || workspace_bytes < room(need)))
+        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
+                    room(need));
+    const Tensor all[] = {{"x", x, x_b, false},
+                          {"W", W, w_b, false},
+                          {"bias", bias, (size_t)(2 * F) * 4, false},
+                          {"out", out, o_b, true},
+                          {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* ws = room_start(workspace);
+    GatedArgs a{};
+    a.M = M;
+    a.K = K;
+    a.F = F;
+    a.act = act;
+    a.x = x;
+    a.W = W;
+    a.bias = bias;
+    a.ld_x = ldx;
+    a.ld_w = ldw;
+    a.out = out;
+    a.ld_out = ldo;
+    hipError_t e;
+    if (M <= kGatedTokens) {
+        e = launch_gated_tokens(a, type, s);
+    } else if (type == ISAM_BF16) {
+        e = gated_copies(p, ws, a, s);
+        if (e == hipSuccess) e = launch_gated_tiles(a, p.tile, false, s);
+    } else {
+        a.gu = reinterpret_cast<float*>(ws);
+        st = product(0, 1, M, 2 * F, K, type, x, ldx, W, ldw, ISAM_F32, a.gu, 2 * F, ws + p.pair_b, p.gemm_b, s, who);
+        if (st != ISAM_OK) return st;
+        e = launch_gated_pairs(a, false, s);
+    }
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_gated_ffn_workspace_size(int64_t M, int64_t K, int64_t F, int type, int aligned) {
+    if (M <= 0 || K <= 0 || F <= 0 || !valid_dtype(type) || !gated_sizes(M, K, F, type)) return 0;
+    return room(gated_plan(M, K, F, type, aligned != 0, aligned != 0, false).total());
+}
+
+extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F, int type, int act, const void* x, int64_t ldx,
+                                                 const void* W, int64_t ldw, const float* bias, const void* dout, int64_t lddo,
+                                                 void* dx, int64_t lddx, void* dW, int64_t lddw, float* dbias, void* workspace,
+                                                 size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_gated_ffn_backward";
+    isam_status_t st = gated_check(M, K, F, type, act, who);
+    if (st != ISAM_OK) return st;
+    if (F == 0 && M > 0 && dx) return fail(ISAM_ERR_INVALID_ARG, "%s: F is 0", who);
+    if (F == 0) return ISAM_OK;
+    if (!dx && !dW && !dbias) return fail(ISAM_ERR_INVALID_ARG, "%s: no output", who);
+    if (M > 0 && (!x || !W || !dout)) return fail(ISAM_ERR_INVALID_ARG, "%s: x, W or dout is NULL", who);
+    const size_t es = dsize(type);
+    size_t x_b, w_b, do_b, dx_b, dw_b;
+    if ((st = gated_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
+        (st = gated_matrix("W", W, 2 * F, K, ldw, es, &w_b, who)) != ISAM_OK ||
+        (st = gated_matrix("dout", dout, M, F, lddo, es, &do_b, who)) != ISAM_OK ||
+        (st = gated_matrix("dx", dx, M, K, lddx, es, &dx_b, who)) != ISAM_OK ||
+        (st = gated_matrix("dW", dW, 2 * F, K, lddw, es, &dw_b, who)) != ISAM_OK)
+        return st;
+    if (!gated_sizes(M, K, F, type)) return fail(ISAM_ERR_UNSUPPORTED, "%s: M x 2F, M x K or 2F x K passes 2^31 bytes", who);
+    const GatedPlan p = gated_plan(M, K, F, type, rows_aligned(x, ldx), rows_aligned(W, ldw), true);
+    const size_t need = p.total();
+    if (need && (!workspace || workspace_bytes < room(need)))
+        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
+                    room(need));
+    const size_t b_b = (size_t)(2 * F) * 4;
+    const Tensor all[] = {{"x", x, x_b, false},       {"W", W, w_b, false},   {"bias", bias, b_b, false},
+                          {"dout", dout, do_b, false}, {"dx", dx, dx_b, true}, {"dW", dW, dw_b, true},
+                          {"dbias", dbias, b_b, true}, {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* ws = room_start(workspace);
+    char* const pairs = ws + p.x_b + p.w_b;
+    float* const bias_part = reinterpret_cast<float*>(pairs + p.pair_b);
+    char* const gemm_ws = pairs + p.pair_b + p.bias_b;
+    hipError_t e = hipSuccess;
+    if (M > 0) {
+        GatedArgs a{};
+        a.M = M;
+        a.K = K;
+        a.F = F;
+        a.act = act;
+        a.x = x;
+        a.W = W;
+        a.bias = bias;
+        a.ld_x = ldx;
+        a.ld_w = ldw;
+        a.out = pairs;
+        a.ld_out = 2 * F;
+        a.dout = dout;
+        a.ld_dout = lddo;
+        a.bias_part = dbias ? bias_part : nullptr;
+        if (type == ISAM_BF16) {
+            e = gated_copies(p, ws, a, s);
+            if (e == hipSuccess) e = launch_gated_tiles(a, p.tile, true, s);
+        } else {
+            a.gu = reinterpret_cast<float*>(pairs);
+            st = product(0, 1, M, 2 * F, K, type, x, ldx, W, ldw, ISAM_F32, a.gu, 2 * F, gemm_ws, p.gemm_b, s, who);
+            if (st != ISAM_OK) return st;
+            e = launch_gated_pairs(a, true, s);
+        }
+        if (e != hipSuccess) return hip_fail(e, who);
+        if (dx && (st = product(0, 0, M, K, 2 * F, type, pairs, 2 * F, W, ldw, type, dx, lddx, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
+            return st;
+    }
+    if (dW && (st = product(1, 0, 2 * F, K, M, type, pairs, 2 * F, x, M ? ldx : K, type, dW, lddw, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
+        return st;
+    if (dbias) {
+        const int64_t rows = M == 0 ? 0 : type == ISAM_BF16 ? gated_bias_rows(p.tile, M) : cdiv(M, kGatedRows);
+        e = launch_colsum(bias_part, rows, 2 * F, 1, kF32, dbias, s);
+    }
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_gated_ffn_backward_workspace_size(int64_t M, int64_t K, int64_t F, int type, int aligned) {
+    if (M <= 0 || K <= 0 || F <= 0 || !valid_dtype(type) || !gated_sizes(M, K, F, type)) return 0;
+    return room(gated_plan(M, K, F, type, aligned != 0, aligned != 0, true).total());
 }

@@ -1,0 +1,163 @@
+// Launch of the gated feed-forward kernels, the kernel for a few tokens and the
+// element-wise step of the fp32 path.
+#include "gated_ffn.hpp"
+
+namespace isam {
+
+namespace {
+
+typedef void (*GatedFn)(GatedArgs, TileMapArgs);
+
+TileMapArgs tile_map(int64_t tiles_m, int64_t tiles_n) {
+    TileMapArgs t{};
+    t.tiles_m = (int)tiles_m;
+    t.tiles_n = (int)tiles_n;
+    t.group_m = 8;
+    t.xcd_remap = 1;
+    return t;
+}
+
+// A few tokens (M <= 16): the weights are streamed once, straight into the
+// matrix instructions' operand registers, 16 rows of Wg and the same 16 of Wu
+// per workgroup; its eight waves take every eighth K step and their sums meet
+// in LDS.  x (the other operand: a column per token) comes from the caches.
+// Bound by the stream of W.
+template <int ES>
+__global__ __launch_bounds__(512) void gated_token_kernel(GatedArgs a) {
+    using IO = Row16<ES>;
+    constexpr int E = IO::E, KS = 4 * E, U = 4;  // values of K of a lane, of a step; steps in flight
+    __shared__ float sums[8][2][4][64];
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int64_t f0 = (int64_t)blockIdx.x * 16, f = f0 + li;
+    const int nk = (int)((a.K + KS - 1) / KS);
+    f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int s0 = wid; s0 < nk; s0 += 8 * U) {
+        uint4 wg[U], wu[U], x[U];
+        static_for<U>([&](auto u) {
+            const int64_t k = (int64_t)(s0 + 8 * u) * KS + g * E;
+            const int valid = (int)max((int64_t)0, min((int64_t)E, a.K - k));
+            wg[u] = IO::load(a.W, f * a.ld_w + k, f < a.F ? valid : 0);
+            wu[u] = IO::load(a.W, (a.F + f) * a.ld_w + k, f < a.F ? valid : 0);
+            x[u] = IO::load(a.x, li * a.ld_x + k, li < a.M ? valid : 0);
+        });
+        static_for<U>([&](auto u) {
+            if constexpr (ES == 2) {
+                mfma16_bf16(acc[0], wg[u], x[u]);
+                mfma16_bf16(acc[1], wu[u], x[u]);
+            } else {
+                mfma16_f32x4(acc[0], wg[u], x[u]);
+                mfma16_f32x4(acc[1], wu[u], x[u]);
+            }
+        });
+    }
+    static_for<2>([&](auto j) { static_for<4>([&](auto v) { sums[wid][j][v][lane] = acc[j][decltype(v)::value]; }); });
+    __syncthreads();
+    // thread (v, lane) of the first four waves: f = f0 + 4 g + v, token li
+    if (wid >= 4) return;
+    const int v = wid;
+    float G = 0.0f, Uv = 0.0f;
+    for (int w = 0; w < 8; ++w) {
+        G += sums[w][0][v][lane];
+        Uv += sums[w][1][v][lane];
+    }
+    const int64_t fo = f0 + 4 * g + v;
+    if (fo >= a.F || li >= a.M) return;
+    if (a.bias) {
+        G += a.bias[fo];
+        Uv += a.bias[a.F + fo];
+    }
+    float slope;
+    const float s = a.act == 0 ? gate_act<0>(G, slope) : a.act == 1 ? gate_act<1>(G, slope) : gate_act<2>(G, slope);
+    IO::put(a.out, (int64_t)li * a.ld_out + fo, s * Uv);
+}
+
+// fp32: p, or (BWD) dG and dU in place, from G and U in memory ([M][2F] at
+// a.gu).  A workgroup takes 64 columns of f and kGatedRows rows, four at a time,
+// and leaves one partial row of the bias gradient.
+template <bool BWD>
+__global__ __launch_bounds__(256) void gated_pairs_kernel(GatedArgs a) {
+    __shared__ float sums[2][4][64];
+    const int cl = threadIdx.x & 63, rl = threadIdx.x >> 6;
+    const int64_t f = (int64_t)blockIdx.x * 64 + cl, m0 = (int64_t)blockIdx.y * kGatedRows, m1 = min(a.M, m0 + kGatedRows);
+    float sg = 0.0f, su = 0.0f;
+    if (f < a.F) {
+        const float bg = a.bias ? a.bias[f] : 0.0f, bu = a.bias ? a.bias[a.F + f] : 0.0f;
+#pragma unroll 2
+        for (int64_t m = m0 + rl; m < m1; m += 4) {
+            float* const gu = a.gu + m * 2 * a.F + f;
+            const float G = gu[0] + bg, U = gu[a.F] + bu;
+            float slope;
+            const float s = a.act == 0 ? gate_act<0>(G, slope) : a.act == 1 ? gate_act<1>(G, slope) : gate_act<2>(G, slope);
+            if constexpr (BWD) {
+                const float dp = static_cast<const float*>(a.dout)[m * a.ld_dout + f], dg = dp * U * slope, du = dp * s;
+                gu[0] = dg;
+                gu[a.F] = du;
+                sg += dg;
+                su += du;
+            } else {
+                static_cast<float*>(a.out)[m * a.ld_out + f] = s * U;
+            }
+        }
+    }
+    if constexpr (BWD) {
+        sums[0][rl][cl] = sg;
+        sums[1][rl][cl] = su;
+        __syncthreads();
+        if (!a.bias_part || rl != 0 || f >= a.F) return;
+        float* const out = a.bias_part + (int64_t)blockIdx.y * 2 * a.F + f;
+        out[0] = (sums[0][0][cl] + sums[0][1][cl]) + (sums[0][2][cl] + sums[0][3][cl]);
+        out[a.F] = (sums[1][0][cl] + sums[1][1][cl]) + (sums[1][2][cl] + sums[1][3][cl]);
+    }
+}
+
+template <bool BWD>
+GatedFn tile_fn(int tile, bool k_full) {
+    switch (tile) {
+        case kGated256: return k_full ? gated_dma_kernel<256, 256, 2, 4, true, BWD> : gated_dma_kernel<256, 256, 2, 4, false, BWD>;
+        case kGated128: return k_full ? gated_dma_kernel<128, 128, 2, 2, true, BWD> : gated_dma_kernel<128, 128, 2, 2, false, BWD>;
+        default: return gated_ring_kernel<BWD>;
+    }
+}
+
+}  // namespace
+
+// bf16 tiles: 256 rows x 128 values of f while they give every compute unit one,
+// then 128 x 64, then 64 x 32.
+int gated_tile(int64_t M, int64_t F, int cus) {
+    auto tiles = [&](int64_t bm, int64_t hb) { return ((M + bm - 1) / bm) * ((F + hb - 1) / hb); };
+    if (tiles(256, 128) >= cus) return kGated256;
+    if (tiles(128, 64) >= cus) return kGated128;
+    return kGated64;
+}
+
+int64_t gated_bias_rows(int tile, int64_t M) {
+    const int64_t bm = tile == kGated256 ? 256 : tile == kGated128 ? 128 : 64;
+    return (M + bm - 1) / bm * 2;  // two wave rows a tile
+}
+
+hipError_t launch_gated_tiles(const GatedArgs& a, int tile, bool backward, hipStream_t s) {
+    const int64_t bm = tile == kGated256 ? 256 : tile == kGated128 ? 128 : 64, hb = bm / 2;
+    const int64_t tm = (a.M + bm - 1) / bm, tn = (a.F + hb - 1) / hb;
+    if (tm * tn > INT32_MAX || a.K <= 0) return hipErrorInvalidValue;
+    const bool k_full = a.K % 64 == 0;
+    const GatedFn fn = backward ? tile_fn<true>(tile, k_full) : tile_fn<false>(tile, k_full);
+    hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(tile == kGated256 ? 512 : 256), 0, s, a, tile_map(tm, tn));
+    return hipGetLastError();
+}
+
+hipError_t launch_gated_tokens(const GatedArgs& a, int type, hipStream_t s) {
+    if (a.M > kGatedTokens || (a.F + 15) / 16 > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((type == kBF16 ? gated_token_kernel<2> : gated_token_kernel<4>), dim3((unsigned)((a.F + 15) / 16)), dim3(512), 0,
+                       s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_gated_pairs(const GatedArgs& a, bool backward, hipStream_t s) {
+    const int64_t gx = (a.F + 63) / 64, gy = (a.M + kGatedRows - 1) / kGatedRows;
+    if (gx > INT32_MAX || gy > 65535) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((backward ? gated_pairs_kernel<true> : gated_pairs_kernel<false>), dim3((unsigned)gx, (unsigned)gy), dim3(256), 0, s,
+                       a);
+    return hipGetLastError();
+}
+
+}  // namespace isam

@@ -300,6 +300,32 @@ void norm_bwd_grid(int64_t rows, int64_t D, int64_t gates, int type, int cus, in
 hipError_t launch_norm_forward(const NormArgs& a, int cus, hipStream_t s);
 hipError_t launch_norm_backward(const NormArgs& a, int64_t grid, hipStream_t s);
 
+// Gated feed-forward block (gated_ffn.hpp): bf16 tiles over 16-byte aligned rows,
+// a kernel for up to kGatedTokens rows of x (either type, any alignment), and the
+// element-wise step behind fp32 products.
+constexpr int64_t kGatedTokens = 16;
+constexpr int64_t kGatedRows = 64;   // rows of a workgroup of the element-wise step
+enum GatedTile : int { kGated256 = 0, kGated128 = 1, kGated64 = 2 };
+struct GatedArgs {
+    int64_t M, K, F;
+    int act;                  // 0 sigmoid, 1 silu, 2 gelu
+    const void* x;            // [M][K]
+    const void* W;            // [2F][K]: gate rows, then up rows
+    const float* bias;        // [2F] or null
+    int64_t ld_x, ld_w;
+    void* out;                // p [M][F]; backward: [dG dU], [M][2F]
+    int64_t ld_out;
+    const void* dout;         // backward: dp [M][F]
+    int64_t ld_dout;
+    float* bias_part;         // backward: partial sums [rows][2F], or null
+    float* gu;                // element-wise step: G and U, [M][2F]
+};
+int gated_tile(int64_t M, int64_t F, int cus);
+int64_t gated_bias_rows(int tile, int64_t M);
+hipError_t launch_gated_tiles(const GatedArgs& a, int tile, bool backward, hipStream_t s);
+hipError_t launch_gated_tokens(const GatedArgs& a, int type, hipStream_t s);
+hipError_t launch_gated_pairs(const GatedArgs& a, bool backward, hipStream_t s);
+
 // out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros).
 hipError_t launch_colsum(const float* part, int64_t rows, int64_t cols, int64_t groups, int out_type, void* out, hipStream_t s);
 

@@ -112,3 +112,47 @@ def test_norm_residual_no_op_and_workspace(L):
     assert L.isam_norm_residual_backward_workspace_size(100, 64, 1, BF16) >= 3 * 64 * 4
     for bad in ((0, 64, 1, F32), (4, 0, 1, F32), (4, 16385, 1, F32), (4, 64, 1, 7)):
         assert L.isam_norm_residual_backward_workspace_size(*bad) == 0
+
+
+def gffn(L, M=40, K=16, F=8, dt=BF16, act=1, x=at(0), ldx=16, W=at(1), ldw=16, bias=at(2), out=at(3), ldo=8, ws=None, wsb=0):
+    return L.isam_gated_ffn(M, K, F, dt, act, x, ldx, W, ldw, bias, out, ldo, ws, wsb, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(M=-1), INVALID), (dict(K=0), INVALID), (dict(F=-1), INVALID), (dict(dt=3), INVALID), (dict(act=3), INVALID),
+    (dict(act=-1), INVALID), (dict(x=None), INVALID), (dict(W=None), INVALID), (dict(out=None), INVALID), (dict(ldx=15), INVALID),
+    (dict(ldw=15), INVALID), (dict(ldo=7), INVALID), (dict(out=at(0)), INVALID), (dict(out=at(2)), INVALID),
+    (dict(dt=F32), WORKSPACE), (dict(ldx=17), WORKSPACE), (dict(K=15), WORKSPACE), (dict(ldx=17, ws=at(5), wsb=64), WORKSPACE),
+    (dict(ldx=17, ws=at(3), wsb=1 << 20), INVALID),
+    (dict(M=1 << 20, ldx=1 << 11), UNSUPPORTED), (dict(M=1 << 20, F=1 << 12, ldo=1 << 12), UNSUPPORTED),
+    (dict(F=1 << 20, ldw=1 << 12), UNSUPPORTED),
+])
+def test_gated_ffn_refusals(L, kw, code):
+    assert gffn(L, **kw) == code
+    assert L.isam_last_error() != b""
+
+
+def gffn_bwd(L, M=40, K=16, F=8, dt=BF16, act=1, x=at(0), ldx=16, W=at(1), bias=at(2), do=at(3), lddo=8, dx=at(4), dW=at(5), db=at(6),
+             ws=at(7), wsb=1 << 24):
+    return L.isam_gated_ffn_backward(M, K, F, dt, act, x, ldx, W, 16, bias, do, lddo, dx, 16, dW, 16, db, ws, wsb, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(M=-1), INVALID), (dict(act=5), INVALID), (dict(do=None), INVALID), (dict(dx=None, dW=None, db=None), INVALID),
+    (dict(lddo=7), INVALID), (dict(dx=at(0)), INVALID), (dict(dW=at(1)), INVALID), (dict(db=at(2)), INVALID),
+    (dict(ws=at(5)), INVALID), (dict(ws=None), WORKSPACE), (dict(wsb=10), WORKSPACE), (dict(F=0), INVALID),
+])
+def test_gated_ffn_backward_refusals(L, kw, code):
+    assert gffn_bwd(L, **kw) == code
+    assert L.isam_last_error() != b""
+
+
+def test_gated_ffn_workspace(L):
+    assert gffn(L, M=0) == OK and gffn(L, F=0) == OK
+    q = L.isam_gated_ffn_workspace_size
+    assert q(4096, 1024, 4096, BF16, 1) == 0 and q(16, 33, 17, F32, 0) == 0
+    assert q(4096, 1024, 4096, BF16, 0) == 2 * 1024 * (4096 + 8192) + 255          # both copied
+    assert q(100, 33, 64, BF16, 1) == 2 * (100 * 40 + 128 * 40) + 255 + (-(2 * 100 * 40)) % 256
+    assert q(100, 32, 64, F32, 1) >= 100 * 128 * 4
+    for bad in ((0, 8, 8, F32, 1), (8, 0, 8, F32, 1), (8, 8, 0, BF16, 1), (8, 8, 8, 5, 1)):
+        assert q(*bad) == 0 and L.isam_gated_ffn_backward_workspace_size(*bad) == 0
