@@ -270,13 +270,14 @@ isam_status_t isam_conv1d(int64_t batch, int64_t L, int64_t Ki, int64_t D, int64
  *   h_seq   row (t, b) of hidden values (type) at its own strides, or NULL; rows
  *           must not overlap each other
  *   h_T     [batch][hidden] fp32, or NULL
- *   states  [ceil(T / 256)][batch][hidden] fp32, or NULL: the state before steps
- *           0, 256, 512, ...: what the backward pass needs of the forward pass
+ *   states  [ceil(T / 128)][batch][hidden] fp32, or NULL: the state before steps
+ *           0, 128, 256, ...: what the backward pass needs of the forward pass
  * At least one of h_seq, h_T and states.  T == 0: h_T = h0 (or zeros); batch or
  * hidden == 0: no-op.  The state is fp32 throughout; h_seq is rounded once.
- * Results repeat bit for bit.  Tensors may pass 2^31 bytes here.
- * Workspace: isam_linear_gru_workspace_size bytes (0 unless sequences and
- * channels are too few to fill the device and time is cut into segments).
+ * Results repeat bit for bit.  Tensors may pass 2^31 bytes here, as long as 32
+ * steps of each stay below.
+ * Workspace: isam_linear_gru_workspace_size bytes (0 up to 256 steps; beyond, the
+ * tiles of time hand the state on through it).
  */
 typedef enum { ISAM_LINEAR = 0, ISAM_TANH = 1 } isam_candidate_t;
 

@@ -287,8 +287,8 @@ def linear_gru_backward_workspace_size(T, batch, hidden, dtype) -> int:
 
 
 def linear_gru_states_shape(T, batch, hidden):
-    """Shape of the ``states`` tensor: the state before steps 0, 256, 512, ..."""
-    return (T + 255) // 256, batch, hidden
+    """Shape of the ``states`` tensor: the state before steps 0, 128, 256, ..."""
+    return (T + 127) // 128, batch, hidden
 
 
 def _linear_gru_args(gx, bias, reset):

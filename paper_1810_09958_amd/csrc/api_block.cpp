@@ -60,11 +60,10 @@ bool lingru_sizes(int64_t T, int64_t batch, int64_t H) {
            (__int128)T * batch * H < ((__int128)1 << 46);
 }
 
-// Bytes of the segments' compositions and of the bias gradient's partial sums.
-size_t lingru_agg_bytes(int64_t segs, int64_t batch, int64_t H) {
-    return segs > 1 ? align256((size_t)(2 * segs * batch * H) * sizeof(float)) : 0;
+// Bytes of the bias gradient's partial sums, one row per tile of time and sequence.
+size_t lingru_bias_bytes(int64_t T, int64_t batch, int64_t H) {
+    return (size_t)(lingru_tiles(T, true) * batch * 2 * H) * sizeof(float);
 }
-size_t lingru_bias_bytes(int64_t segs, int64_t batch, int64_t H) { return (size_t)(segs * batch * 2 * H) * sizeof(float); }
 
 isam_status_t lingru_check(int64_t T, int64_t batch, int64_t H, int type, int candidate, const char* who) {
     if (T < 0 || batch < 0 || H < 0)
@@ -97,8 +96,7 @@ extern "C" isam_status_t isam_linear_gru(int64_t T, int64_t batch, int64_t hidde
         return fail(ISAM_ERR_INVALID_ARG, "%s: rows of h_seq overlap", who);
     const size_t es = dsize(type), state = (size_t)(batch * hidden) * sizeof(float);
     LinGruArgs a{};
-    lingru_segments(T, batch, hidden, type, device_cus(), &a.segs, &a.tiles_per_seg);
-    const size_t need = lingru_agg_bytes(a.segs, batch, hidden);
+    const size_t need = lingru_chain_bytes(T, batch, hidden, false);
     if (need && (!workspace || workspace_bytes < room(need)))
         return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
                     room(need));
@@ -107,6 +105,9 @@ extern "C" isam_status_t isam_linear_gru(int64_t T, int64_t batch, int64_t hidde
         !extent(h_seq ? T : 0, h_stride_t, batch, h_stride_b, hidden, es, &h_b) ||
         !extent(reset ? T : 0, reset_stride_t, batch, reset_stride_b, 1, 1, &r_b))
         return fail(ISAM_ERR_UNSUPPORTED, "%s: a tensor spans more than 2^46 bytes", who);
+    if (!lingru_strides(gx_stride_t, 2 * hidden, es) || (h_seq && !lingru_strides(h_stride_t, hidden, es)) ||
+        (reset && !lingru_strides(reset_stride_t, 1, 1)))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: 32 steps of a tensor span more than 2^31 bytes", who);
     const Tensor all[] = {{"gx", gx, gx_b, false},
                           {"bias", bias, (size_t)(2 * hidden) * 4, false},
                           {"h0", h0, state, false},
@@ -134,16 +135,14 @@ extern "C" isam_status_t isam_linear_gru(int64_t T, int64_t batch, int64_t hidde
     a.h_b = h_stride_b;
     a.h_T = h_T;
     a.states = states;
-    a.agg = need ? reinterpret_cast<float*>(room_start(workspace)) : nullptr;
+    a.chain = need ? reinterpret_cast<uint64_t*>(room_start(workspace)) : nullptr;
     const hipError_t e = launch_lingru_forward(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
 }
 
 extern "C" size_t isam_linear_gru_workspace_size(int64_t T, int64_t batch, int64_t hidden, int type) {
     if (T <= 0 || batch <= 0 || hidden <= 0 || !valid_dtype(type) || !lingru_sizes(T, batch, hidden)) return 0;
-    int64_t segs, per;
-    lingru_segments(T, batch, hidden, type, device_cus(), &segs, &per);
-    return room(lingru_agg_bytes(segs, batch, hidden));
+    return room(lingru_chain_bytes(T, batch, hidden, false));
 }
 
 extern "C" isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int64_t hidden, int type, int candidate,
@@ -166,9 +165,8 @@ extern "C" isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int6
         return fail(ISAM_ERR_INVALID_ARG, "%s: rows of dgx overlap", who);
     const size_t es = dsize(type), state = (size_t)(batch * hidden) * sizeof(float);
     LinGruArgs a{};
-    lingru_segments(T, batch, hidden, type, device_cus(), &a.segs, &a.tiles_per_seg);
-    const size_t agg = lingru_agg_bytes(a.segs, batch, hidden);
-    const size_t need = agg + (dbias ? lingru_bias_bytes(a.segs, batch, hidden) : 0);
+    const size_t chain = align256(lingru_chain_bytes(T, batch, hidden, true));
+    const size_t need = chain + (dbias ? lingru_bias_bytes(T, batch, hidden) : 0);
     if (need && (!workspace || workspace_bytes < room(need)))
         return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
                     room(need));
@@ -178,6 +176,9 @@ extern "C" isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int6
         !extent(dh_seq ? T : 0, dh_stride_t, batch, dh_stride_b, hidden, es, &dh_b) ||
         !extent(reset ? T : 0, reset_stride_t, batch, reset_stride_b, 1, 1, &r_b))
         return fail(ISAM_ERR_UNSUPPORTED, "%s: a tensor spans more than 2^46 bytes", who);
+    if (!lingru_strides(gx_stride_t, 2 * hidden, es) || !lingru_strides(dgx_stride_t, 2 * hidden, es) ||
+        (dh_seq && !lingru_strides(dh_stride_t, hidden, es)) || (reset && !lingru_strides(reset_stride_t, 1, 1)))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: 32 steps of a tensor span more than 2^31 bytes", who);
     const Tensor all[] = {{"gx", gx, gx_b, false},
                           {"bias", bias, (size_t)(2 * hidden) * 4, false},
                           {"reset", reset, r_b, false},
@@ -212,17 +213,15 @@ extern "C" isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int6
     a.dh0 = dh0;
     a.dbias = dbias;
     char* ws = room_start(workspace);
-    a.agg = agg ? reinterpret_cast<float*>(ws) : nullptr;
-    a.bias_part = dbias ? reinterpret_cast<float*>(ws + agg) : nullptr;
+    a.chain = chain ? reinterpret_cast<uint64_t*>(ws) : nullptr;
+    a.bias_part = dbias ? reinterpret_cast<float*>(ws + chain) : nullptr;
     const hipError_t e = launch_lingru_backward(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
 }
 
 extern "C" size_t isam_linear_gru_backward_workspace_size(int64_t T, int64_t batch, int64_t hidden, int type) {
     if (T < 0 || batch <= 0 || hidden <= 0 || !valid_dtype(type) || !lingru_sizes(T, batch, hidden)) return 0;
-    int64_t segs, per;
-    lingru_segments(T, batch, hidden, type, device_cus(), &segs, &per);
-    return room(lingru_agg_bytes(segs, batch, hidden) + lingru_bias_bytes(segs, batch, hidden));
+    return room(align256(lingru_chain_bytes(T, batch, hidden, true)) + lingru_bias_bytes(T, batch, hidden));
 }
 
 // ---------------------------------------------------------------------------

@@ -235,7 +235,9 @@ hipError_t launch_gru_copy_state(const float* h0, float* h_T, int64_t n, hipStre
 
 
 // Linear GRU (linear_gru.hip).  Strides in elements; rows are [2H] (gx, dgx) or [H].
-constexpr int64_t kLinGruChunk = 256;  // steps between two rows of `states`
+constexpr int64_t kLinGruChunk = 128;  // steps between two rows of `states`
+constexpr int kLinGruFwdSteps = 8, kLinGruBwdSteps = 8;  // steps of a group: tiles of 32 times as many
+constexpr uint64_t kLinGruTimeoutTicks = 200000000ull;   // bound of a wait for an earlier tile (2 s at 100 MHz)
 struct LinGruArgs {
     int64_t T, batch, H;
     int type;                // of gx, h_seq, dh_seq and dgx
@@ -249,7 +251,7 @@ struct LinGruArgs {
     void* h_seq;             // or null
     int64_t h_t, h_b;
     float* h_T;              // [batch][H] or null
-    float* states;           // [ceil(T / 256)][batch][H]: state before steps 0, 256, ...; or null (forward)
+    float* states;           // [ceil(T / 128)][batch][H]: state before steps 0, 128, ...; or null (forward)
     // backward
     const void* dh_seq;      // or null
     int64_t dh_t, dh_b;
@@ -258,12 +260,13 @@ struct LinGruArgs {
     int64_t dg_t, dg_b;
     float* dh0;              // [batch][H] or null
     float* dbias;            // [2H] or null
-    // segments of time (lingru_segments) and workspace
-    int64_t segs, tiles_per_seg;
-    float* agg;              // [2][segs][batch][H] (segs > 1)
-    float* bias_part;        // [segs][batch][2H] (dbias)
+    uint64_t* chain;         // lingru_chain_bytes: counter, then the tiles' words; or null (a single tile)
+    float* bias_part;        // [tiles][batch][2H] (dbias)
 };
-void lingru_segments(int64_t T, int64_t batch, int64_t H, int type, int cus, int64_t* segs, int64_t* tiles_per_seg);
+// Tiles of one column of channels, and the bytes of their chain.
+int64_t lingru_tiles(int64_t T, bool backward);
+bool lingru_strides(int64_t stride_t, int64_t width, int64_t es);
+size_t lingru_chain_bytes(int64_t T, int64_t batch, int64_t H, bool backward);
 hipError_t launch_lingru_forward(const LinGruArgs& a, hipStream_t s);
 hipError_t launch_lingru_backward(const LinGruArgs& a, hipStream_t s);
 

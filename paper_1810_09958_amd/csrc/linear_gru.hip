@@ -8,26 +8,33 @@
 //
 // Both are first-order recurrences of each channel: a run of steps maps the
 // state v before it to A v + B, and two runs compose to (A1 A2, A2 B1 + B2).
-// Per value the forward pass reads two gates and writes one state (6 bytes in
-// bf16 against some 20 fp32 operations, four of them transcendental), so memory
-// bounds it and the schedule is built to touch each value once:
-//   * a workgroup owns one sequence's block of 128 bytes of channels (8 lanes x
-//     16 bytes) and walks time in tiles of 256 steps: 64 groups of 8 lanes with
-//     4 steps each.  A group composes its steps, the 8 groups of a wave are
-//     scanned by lane exchanges, the 8 waves through LDS (one barrier), and the
-//     state at the tile's end stays in registers for the next tile, whose gates
-//     were requested before this tile's arithmetic;
-//   * where sequences and channels alone leave compute units idle, time is cut
-//     into segments: a first kernel composes each segment to its (A, B), and a
-//     segment's workgroup starts from the state those of the segments before it
-//     give.  Everything is combined in one order, so results repeat bit for bit;
+// Per value the forward pass reads two gates and writes one state, the backward
+// pass reads three and writes two.  The bytes bound them, with the vector units
+// close behind (four transcendentals and some 20 plain instructions a value forward,
+// twice that backward), so each value is loaded, and its gates are formed, once:
+//   * a workgroup takes a tile of time x 64 channels of one sequence into
+//     registers: 16 lanes x 4 channels make a row, a wave four groups of rows, each
+//     group R consecutive steps.  A group composes its steps, the groups of a wave
+//     are scanned by lane exchanges, the waves through LDS;
+//   * tiles of one column of channels are chained in memory: a tile publishes its
+//     composition (A, B) as soon as it has it, and takes the state before it from the
+//     nearest earlier tile that has published one, through the compositions of
+//     those between.  Workgroups draw their tiles from a counter in time order, so
+//     those a tile waits for are always held by running workgroups: the chain needs
+//     no co-residency.  A tile's published state is its composition applied to the state
+//     before it wherever that came from, so results repeat bit for bit.  Each
+//     published number is one 8-byte word with a mark beside it, written and read
+//     with device scope, so no ordering between words is needed; the words and the
+//     counter are cleared by a kernel before (a captured launch replays);
 //   * the backward pass keeps no sequence of states: the forward pass leaves the
-//     state before every 256 steps, and each tile forms its states again in
+//     state before every 128 steps, and each tile forms its states again in
 //     registers while it scans e from its end (5 values moved per element, 6 with
 //     stored states, which would have to be fp32 to give fp32 gradients).
 // A reset must cut off whatever stands before it, NaN included, which 0 * NaN
 // does not: its a is -0, and a sign bit in A (kept through products) makes a
 // composition drop the left side.
+#include <type_traits>
+
 #include "kernels.hpp"
 #include "rowio.hpp"
 
@@ -35,7 +42,7 @@ namespace isam {
 
 namespace {
 
-constexpr int kSteps = 4;  // steps per group and tile
+constexpr int kCols = 64;  // channels of a tile
 
 __device__ __forceinline__ bool drops(float a) { return (int)__float_as_uint(a) < 0; }
 
@@ -53,131 +60,330 @@ __device__ __forceinline__ float apply(float a, float b, float v) {
     return r;
 }
 
-// What one workgroup works on: a block of channels of one sequence.
-template <int ES>
-struct Column {
-    static constexpr int E = Row16<ES>::E;
-    int64_t b, c;  // sequence, this lane's first channel
-    int valid;     // channels of this lane that exist
-    __device__ __forceinline__ Column(const LinGruArgs& a, int lane) {
-        const int64_t blocks = (a.H + 8 * E - 1) / (8 * E);
-        b = (int64_t)blockIdx.x / blocks;
-        c = ((int64_t)blockIdx.x - b * blocks) * (8 * E) + (lane & 7) * E;
-        valid = (int)max((int64_t)0, min((int64_t)E, a.H - c));
+// The four channels of a lane.  VEC (hidden a multiple of 4, rows on 4 bytes): one
+// piece of four, moved as one; otherwise channels 16 apart, moved one by one.  A
+// block's lanes past the last channel repeat it (same loads, same values, same
+// stores), so nothing below depends on how many of them exist, and no load or
+// store stands in a branch of lanes (the compiler has copied registers inside such
+// a branch, for its lanes only, in a kernel that uses nearly all of them).
+template <bool VEC>
+__device__ __forceinline__ int64_t channel(int64_t H, int64_t c0, int l, int e) {
+    if constexpr (VEC) return min(c0 + 4 * l, H - 4) + e;
+    return min(c0 + 16 * e + l, H - 1);
+}
+
+// Rows of one tensor as a wave sees them: row r of the lane's group of R steps at
+// base + (group * R + r) * step + the lane's channels.  Rows outside are addressed
+// past the buffer's end: loads give zeros, stores are dropped.
+template <int ES, bool VEC, int R>
+struct Rows {
+    static constexpr int W = ES == 2 ? 2 : 4;  // 32-bit words of four values
+    __amdgpu_buffer_rsrc_t rs;
+    uint32_t off[VEC ? 1 : 4], step;
+    // p: first row of the wave (null: no rows); stride in elements.
+    __device__ __forceinline__ Rows(const void* p, int64_t at, int64_t stride, int64_t H, int64_t c0, int lane) {
+        rs = make_rsrc(p ? static_cast<const char*>(p) + at * ES : nullptr, p ? 0x7fffffffu : 0u);
+        step = (uint32_t)(stride * ES);
+        static_for<VEC ? 1 : 4>([&](auto e) {
+            off[e] = (uint32_t)(lane >> 4) * R * step + (uint32_t)channel<VEC>(H, c0, lane & 15, e) * ES;
+        });
     }
+    // `extra`: bytes added to every address (the second block of a row).
+    __device__ __forceinline__ void load(uint32_t (&w)[W], int r, bool in, uint32_t extra) const {
+        const int so = (int)(r * step + extra);
+        if constexpr (VEC && ES == 4) {
+            const i32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(in ? off[0] : kOob), so, 0);
+            static_for<4>([&](auto e) { w[e] = (uint32_t)v[decltype(e)::value]; });
+        } else if constexpr (VEC) {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(in ? off[0] : kOob), so, 0);
+            w[0] = (uint32_t)v[0];
+            w[1] = (uint32_t)v[1];
+        } else if constexpr (ES == 4) {
+            static_for<4>([&](auto e) { w[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, (int)(in ? off[e] : kOob), so, 0); });
+        } else {
+            uint32_t h[4];
+            static_for<4>([&](auto e) { h[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(in ? off[e] : kOob), so, 0) & 0xffffu; });
+            w[0] = h[0] | h[1] << 16;
+            w[1] = h[2] | h[3] << 16;
+        }
+    }
+    // bf16: rounded to nearest even.
+    __device__ __forceinline__ void store(const float (&f)[4], int r, bool in, uint32_t extra) const {
+        const int so = (int)(r * step + extra);
+        if constexpr (ES == 4) {
+            if constexpr (VEC) {
+                // The offset in the address register: after a 16-byte store whose offset sits in
+                // a scalar register the compiler lets the next instruction overwrite the data,
+                // and lanes have then stored the new value.
+                const i32x4_t v = __builtin_bit_cast(i32x4_t, f32x4_t{f[0], f[1], f[2], f[3]});
+                __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)(in ? off[0] + (uint32_t)so : kOob), 0, 0);
+            } else {
+                static_for<4>([&](auto e) { __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(f[e]), rs, (int)(in ? off[e] : kOob), so, 0); });
+            }
+        } else {
+            const uint32_t w[2] = {pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3])};
+            if constexpr (VEC) {
+                __builtin_amdgcn_raw_buffer_store_b64((i32x2_t){(int)w[0], (int)w[1]}, rs, (int)(in ? off[0] : kOob), so, 0);
+            } else {
+                static_for<4>([&](auto e) {
+                    __builtin_amdgcn_raw_buffer_store_b16((short)(w[e / 2] >> (16 * (e & 1))), rs, (int)(in ? off[e] : kOob), so, 0);
+                });
+            }
+        }
+    }
+    __device__ __forceinline__ static void unpack(const uint32_t (&w)[W], float (&f)[4]) {
+        static_for<4>([&](auto e) {
+            if constexpr (ES == 4) f[e] = __uint_as_float(w[e]);
+            else if constexpr (e & 1) f[e] = bf16hi(w[e / 2]);
+            else f[e] = bf16lo(w[e / 2]);
+        });
+    }
+    // Every value with which sigmoid gives 1 whatever the (finite) bias.
+    static constexpr uint32_t kKeep = ES == 2 ? 0x7f807f80u : 0x7f800000u;
 };
 
-// Inclusive scan over the wave's 8 groups in time order (UP) or against it.
-template <int E, bool RESET, bool UP>
-__device__ __forceinline__ void wave_scan(float (&A)[E], float (&B)[E], int lane) {
-    static_for<3>([&](auto dc) {
-        constexpr int d = 8 << decltype(dc)::value;
+// fp32 values of the lane's channels (zeros without a tensor).
+template <bool VEC>
+__device__ __forceinline__ void load_channels(const float* p, int64_t at, int64_t H, int64_t c0, int lane, float (&f)[4]) {
+    static_for<4>([&](auto e) { f[e] = p ? p[at + channel<VEC>(H, c0, lane & 15, e)] : 0.0f; });
+}
+// The same stored, by the lanes with `on`.
+template <bool VEC>
+__device__ __forceinline__ void store_channels(float* p, int64_t at, int64_t H, int64_t c0, int lane, bool on, const float (&f)[4]) {
+    const Rows<4, VEC, 0> rows(p, at, 0, H, c0, lane);
+    rows.store(f, 0, on, 0);
+}
+
+constexpr float kLog2e = 1.44269504f;
+
+// z = sigmoid(v) and 1 - z from w = -v log2(e), each to fp32 accuracy also where it is
+// small (1 - z formed from z would lose the digits that decide how long a state
+// lives).  The bound on w keeps 2^w z finite; a NaN passes.
+__device__ __forceinline__ void gate_pair(float w, float& z, float& omz) {
+    const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(w, 126.0f));
+    z = __builtin_amdgcn_rcpf(1.0f + e);
+    omz = e * z;
+}
+// tanh(v), absolute error of a few 2^-24.
+template <int ES>
+__device__ __forceinline__ float gate_tanh(float v) {
+    if constexpr (ES == 4) return tanh_f32(v);
+    return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * (2.0f * kLog2e))), 1.0f);
+}
+
+// Inclusive scan over the wave's four groups in time order (UP) or against it.
+template <bool RESET, bool UP>
+__device__ __forceinline__ void wave_scan(float (&A)[4], float (&B)[4], int lane) {
+    static_for<2>([&](auto dc) {
+        constexpr int d = 16 << decltype(dc)::value;
         const bool has = UP ? lane >= d : lane + d < 64;
-        static_for<E>([&](auto e) {
+        static_for<4>([&](auto e) {
             const float pa = UP ? __shfl_up(A[e], d) : __shfl_down(A[e], d);
             const float pb = UP ? __shfl_up(B[e], d) : __shfl_down(B[e], d);
-            if (has) {
-                B[e] = apply<RESET>(A[e], B[e], pb);
-                A[e] = compose_a<RESET>(A[e], pa);
-            }
+            B[e] = has ? apply<RESET>(A[e], B[e], pb) : B[e];
+            A[e] = has ? compose_a<RESET>(A[e], pa) : A[e];
         });
     });
 }
 
-// The state that reaches `seg` (from the end if BACK): `v` taken through the
-// composed segments before it.
-template <int E, bool RESET, bool BACK>
-__device__ __forceinline__ void segment_in(const LinGruArgs& a, int64_t seg, int64_t b, int64_t c, int valid, float (&v)[E]) {
-    const int64_t n = a.batch * a.H, at = b * a.H + c;
-    const float* A = a.agg;
-    const float* B = a.agg + a.segs * n;
-    const int64_t count = BACK ? a.segs - 1 - seg : seg;
-#pragma unroll 4
-    for (int64_t i = 0; i < count; ++i) {
-        const int64_t s = BACK ? a.segs - 1 - i : i;
-        float sa[E], sb[E];
-        load_f32<E>(A, s * n + at, valid, sa);
-        load_f32<E>(B, s * n + at, valid, sb);
-        static_for<E>([&](auto e) { v[e] = apply<RESET>(sa[e], sb[e], v[e]); });
+// The chain of tiles.  Tile `id` has three words for each of its channels: state
+// after it, A and B; the upper half of a word that has been written is 1.
+__device__ __forceinline__ uint64_t* chain_word(const LinGruArgs& a, int64_t id, int field, int ch) {
+    return a.chain + 8 + (id * 3 + field) * kCols + ch;
+}
+__device__ __forceinline__ void chain_put(uint64_t* w, float v) {
+    __hip_atomic_store(w, (1ull << 32) | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t chain_get(const uint64_t* w) {
+    return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// State that reaches the tile `id`, `before` tiles into its column (lane: channel;
+// whole wave).  `first`: the state before the column's first tile.  NaN if a word
+// should not arrive within 2 s (it is written by a running workgroup).
+template <bool RESET>
+__device__ __forceinline__ float chain_in(const LinGruArgs& a, int64_t id, int64_t before, int64_t cols, int lane, float first) {
+    constexpr int W = 4;  // tiles looked at together
+    const uint64_t t0 = wall_clock64();
+    for (;;) {
+        uint64_t s[W], ca[W], cb[W];
+        static_for<W>([&](auto i) {
+            const int64_t p = id - (i + 1) * cols;
+            s[i] = i == before ? (1ull << 32) | __float_as_uint(first) : 0;
+            ca[i] = cb[i] = 0;
+            if (i < before) {
+                s[i] = chain_get(chain_word(a, p, 0, lane));
+                ca[i] = chain_get(chain_word(a, p, 1, lane));
+                cb[i] = chain_get(chain_word(a, p, 2, lane));
+            }
+        });
+        int at = -1;
+        bool open = true;
+        static_for<W>([&](auto i) {
+            if (open && __all((int)(s[i] >> 32))) {
+                at = i;
+                open = false;
+            }
+            open = open && __all((int)(ca[i] >> 32) & (int)(cb[i] >> 32));
+        });
+        if (at >= 0) {
+            float v = 0.0f;
+            static_for<W>([&](auto i) {
+                if (i == at) v = __uint_as_float((uint32_t)s[i]);
+            });
+            static_for<W - 1>([&](auto j) {
+                constexpr int i = W - 2 - decltype(j)::value;
+                if (i < at) v = apply<RESET>(__uint_as_float((uint32_t)ca[i]), __uint_as_float((uint32_t)cb[i]), v);
+            });
+            return v;
+        }
+        if (wall_clock64() - t0 > kLinGruTimeoutTicks) return __builtin_nanf("");
+        __builtin_amdgcn_s_sleep(1);
     }
 }
 
-// Forward pass.  NW waves: tiles of NW * 32 steps.
-template <int ES, int NW, bool RESET>
-__global__ __launch_bounds__(NW * 64) void lingru_fwd_kernel(LinGruArgs a) {
-    constexpr int E = Row16<ES>::E, R = kSteps, TS = NW * 8 * R;
-    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = wid * 8 + (lane >> 3);
-    const Column<ES> k(a, lane);
-    __shared__ float totals[2][NW][2][8][E];
+// Which tile a workgroup has: number, place in its column (from the end if
+// backward), sequence and first channel.
+struct Tile {
+    int64_t id, k, cols, b, c0;
+    template <bool CHAIN>
+    __device__ __forceinline__ static Tile take(const LinGruArgs& a, unsigned* shared) {
+        Tile t;
+        const int64_t blocks = (a.H + kCols - 1) / kCols;
+        t.cols = a.batch * blocks;
+        if constexpr (CHAIN) {
+            if (threadIdx.x == 0)
+                *shared = __hip_atomic_fetch_add(reinterpret_cast<unsigned*>(a.chain), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            t.id = __builtin_amdgcn_readfirstlane(*shared);
+            t.k = t.id / t.cols;
+        } else {
+            t.id = blockIdx.x;
+            t.k = 0;
+        }
+        const int64_t col = t.id - t.k * t.cols;
+        t.b = col / blocks;
+        t.c0 = (col - t.b * blocks) * kCols;
+        return t;
+    }
+};
 
-    float bz[E], bn[E], h[E];
-    load_f32<E>(a.bias, k.c, k.valid, bz);
-    load_f32<E>(a.bias, a.H + k.c, k.valid, bn);
-    load_f32<E>(a.h0, k.b * a.H + k.c, k.valid, h);
-    const int64_t tiles = (a.T + TS - 1) / TS;
-    const int64_t tile0 = (int64_t)blockIdx.y * a.tiles_per_seg, tile1 = min(tiles, tile0 + a.tiles_per_seg);
-    segment_in<E, RESET, false>(a, blockIdx.y, k.b, k.c, k.valid, h);
-
-    const char* gx = static_cast<const char*>(a.gx) + k.b * a.gx_b * ES;
-    char* hs = static_cast<char*>(a.h_seq) + k.b * a.h_b * ES;
-    uint4 pz[R], pn[R];
-    uint8_t pr[R];
-    auto fetch = [&](int64_t tile) {
+// What the kernels hold of a wave's steps: reset marks, a bit for each.
+template <int R, bool RESET>
+__device__ __forceinline__ uint32_t reset_bits(const LinGruArgs& a, int64_t b, int64_t tw, int lane, int left) {
+    uint32_t bits = 0;
+    if constexpr (RESET) {
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.reset + b * a.rs_b + tw * a.rs_t, 0x7fffffffu);
         static_for<R>([&](auto r) {
-            const int64_t t = tile * TS + g * R + r;
-            const int valid = tile < tile1 && t < a.T ? k.valid : 0;
-            pz[r] = Row16<ES>::load(gx, t * a.gx_t + k.c, valid);
-            pn[r] = Row16<ES>::load(gx, t * a.gx_t + a.H + k.c, valid);
-            if constexpr (RESET) pr[r] = valid ? a.reset[t * a.rs_t + k.b * a.rs_b] : 0;
-        });
-    };
-    fetch(tile0);
-    for (int64_t tile = tile0; tile < tile1; ++tile) {
-        if (a.states && g == 0) store_f32<E>(a.states, (tile * a.batch + k.b) * a.H + k.c, k.valid, h);
-        const int64_t t0 = tile * TS + g * R;
-        float ca[R][E], cb[R][E], A[E], B[E];
-        static_for<R>([&](auto r) {
-            float gz[E], gn[E];
-            Row16<ES>::unpack(pz[r], gz);
-            Row16<ES>::unpack(pn[r], gn);
-            const bool in = t0 + r < a.T;
-            static_for<E>([&](auto e) {
-                float z, omz;
-                sigmoid_pair(gz[e] + bz[e], z, omz);
-                const float v = gn[e] + bn[e], n = a.candidate ? tanh_f32(v) : v;
-                ca[r][e] = in ? z : 1.0f;
-                cb[r][e] = in ? omz * n : 0.0f;
-                if constexpr (RESET) ca[r][e] = in && pr[r] ? -0.0f : ca[r][e];
-                A[e] = r == 0 ? ca[r][e] : compose_a<RESET>(A[e], ca[r][e]);
-                B[e] = r == 0 ? cb[r][e] : apply<RESET>(ca[r][e], cb[r][e], B[e]);
-            });
-        });
-        fetch(tile + 1);
-        wave_scan<E, RESET, true>(A, B, lane);
-        float (&tot)[NW][2][8][E] = totals[tile & 1];
-        if ((lane >> 3) == 7) static_for<E>([&](auto e) {
-            tot[wid][0][lane & 7][e] = A[e];
-            tot[wid][1][lane & 7][e] = B[e];
-        });
-        __syncthreads();  // (the next tile writes the other half)
-        float v[E];
-        static_for<E>([&](auto e) { v[e] = h[e]; });
-        static_for<NW>([&](auto w) {
-            static_for<E>([&](auto e) {
-                h[e] = apply<RESET>(tot[w][0][lane & 7][e], tot[w][1][lane & 7][e], h[e]);
-                if (w < wid) v[e] = h[e];
-            });
-        });
-        static_for<E>([&](auto e) {
-            const float pa = __shfl_up(A[e], 8), pb = __shfl_up(B[e], 8);
-            if (lane >= 8) v[e] = apply<RESET>(pa, pb, v[e]);
-        });
-        static_for<R>([&](auto r) {
-            static_for<E>([&](auto e) { v[e] = apply<RESET>(ca[r][e], cb[r][e], v[e]); });
-            if (a.h_seq) Row16<ES>::store(hs, (t0 + r) * a.h_t + k.c, Row16<ES>::pack(v), t0 + r < a.T ? k.valid : 0);
+            const int i = (lane >> 4) * R + r;
+            const uint32_t v = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(i < left ? (uint32_t)i * (uint32_t)a.rs_t : kOob), 0, 0);
+            bits |= ((v & 0xffu) ? 1u : 0u) << r;
         });
     }
-    if (a.h_T && tile1 == tiles && g == 0) store_f32<E>(a.h_T, k.b * a.H + k.c, k.valid, h);
+    return bits;
+}
+
+// A wave's totals: the lanes of its last group (or first) to the tile's row, the
+// others to a row that nobody reads.
+__device__ __forceinline__ void put4(float* row, float* spare, int lane, bool on, const float (&f)[4]) {
+    *reinterpret_cast<float4*>((on ? row : spare) + (lane & 15) * 4) = make_float4(f[0], f[1], f[2], f[3]);
+}
+__device__ __forceinline__ void get4(const float* row, int lane, float (&f)[4]) {
+    const float4 v = *reinterpret_cast<const float4*>(row + (lane & 15) * 4);
+    f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+}
+
+// Forward pass: NW waves of 4 groups of R steps.
+template <int ES, bool VEC, int NW, int R, bool RESET, bool CHAIN>
+__global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(LinGruArgs a) {
+    using S = Rows<ES, VEC, R>;
+    constexpr int TS = NW * 4 * R;
+    __shared__ __attribute__((aligned(16))) float tot[NW][2][kCols];
+    __shared__ __attribute__((aligned(16))) float start[NW][kCols];
+    __shared__ __attribute__((aligned(16))) float spare[kCols];
+    __shared__ unsigned ticket;
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
+    const Tile tile = Tile::take<CHAIN>(a, &ticket);
+    const int64_t b = tile.b, c0 = tile.c0, tw = tile.k * TS + wid * 4 * R;
+    const int left = (int)max((int64_t)0, min((int64_t)(4 * R), a.T - tw));  // steps of this wave that exist
+    const bool last = (tile.k + 1) * TS >= a.T;
+
+    const S gx(a.gx, b * a.gx_b + tw * a.gx_t, a.gx_t, a.H, c0, lane);
+    uint32_t pz[R][S::W], pn[R][S::W];
+    static_for<R>([&](auto r) {
+        gx.load(pz[r], r, q * R + r < left, 0);
+        gx.load(pn[r], r, q * R + r < left, (uint32_t)a.H * ES);
+    });
+    const uint32_t reset = reset_bits<R, RESET>(a, b, tw, lane, left);
+    float bz[4], bn[4];
+    load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
+    load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
+    static_for<4>([&](auto e) { bz[e] *= -kLog2e; });
+
+    float ca[R][4], cb[R][4], A[4], B[4];
+    static_for<R>([&](auto r) {
+        float gz[4], n[4];
+        static_for<S::W>([&](auto w) { pz[r][w] = q * R + r < left ? pz[r][w] : S::kKeep; });
+        S::unpack(pz[r], gz);
+        S::unpack(pn[r], n);
+        static_for<4>([&](auto e) { n[e] += bn[e]; });
+        if (a.candidate) static_for<4>([&](auto e) { n[e] = gate_tanh<ES>(n[e]); });
+        static_for<4>([&](auto e) {
+            float z, omz;
+            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z, omz);
+            ca[r][e] = RESET && (reset >> r & 1) ? -0.0f : z;
+            cb[r][e] = omz * n[e];
+            A[e] = r == 0 ? ca[r][e] : compose_a<RESET>(A[e], ca[r][e]);
+            B[e] = r == 0 ? cb[r][e] : apply<RESET>(ca[r][e], cb[r][e], B[e]);
+        });
+    });
+    wave_scan<RESET, true>(A, B, lane);
+    put4(tot[wid][0], spare, lane, q == 3, A);
+    put4(tot[wid][1], spare, lane, q == 3, B);
+    __syncthreads();
+    if (wid == 0) {
+        // lane: one of the tile's channels, in the lanes' order
+        const int64_t ch = channel<VEC>(a.H, c0, lane >> 2, lane & 3);
+        float wa[NW], wb[NW];
+        static_for<NW>([&](auto w) {
+            wa[w] = tot[w][0][lane];
+            wb[w] = tot[w][1][lane];
+        });
+        const float first = a.h0 ? a.h0[b * a.H + ch] : 0.0f;
+        float h = first;
+        if constexpr (CHAIN) {
+            float ta = wa[0], tb = wb[0];
+            static_for<NW - 1>([&](auto w) {
+                tb = apply<RESET>(wa[w + 1], wb[w + 1], tb);
+                ta = compose_a<RESET>(ta, wa[w + 1]);
+            });
+            if (!last) {
+                chain_put(chain_word(a, tile.id, 1, lane), ta);
+                chain_put(chain_word(a, tile.id, 2, lane), tb);
+            }
+            h = chain_in<RESET>(a, tile.id, tile.k, tile.cols, lane, first);
+            if (!last) chain_put(chain_word(a, tile.id, 0, lane), apply<RESET>(ta, tb, h));
+        }
+        static_for<NW>([&](auto w) {
+            start[w][lane] = h;
+            h = apply<RESET>(wa[w], wb[w], h);
+        });
+    }
+    __syncthreads();
+    float v[4];
+    get4(start[wid], lane, v);
+    static_for<4>([&](auto e) {
+        const float pa = __shfl_up(A[e], 16), pb = __shfl_up(B[e], 16);
+        v[e] = q > 0 ? apply<RESET>(pa, pb, v[e]) : v[e];
+    });
+    if (a.states && wid * 4 * R % kLinGruChunk == 0 && left > 0)
+        store_channels<VEC>(a.states, (tw / kLinGruChunk * a.batch + b) * a.H, a.H, c0, lane, q == 0, v);
+    const S hs(a.h_seq, b * a.h_b + tw * a.h_t, a.h_t, a.H, c0, lane);
+    static_for<R>([&](auto r) {
+        static_for<4>([&](auto e) { v[e] = apply<RESET>(ca[r][e], cb[r][e], v[e]); });
+        hs.store(v, r, q * R + r < left, 0);
+    });
+    // (steps past the end leave the state as it is)
+    if (a.h_T && last && wid == NW - 1) store_channels<VEC>(a.h_T, b * a.H, a.H, c0, lane, q == 3, v);
 }
 
 // A few steps, one thread per channel: decoding (no tile to fill).
@@ -203,8 +409,8 @@ __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
     static_for<kFewSteps>([&](auto t) {
         if (t < T) {
             float z, omz;
-            sigmoid_pair(gz[t] + bz, z, omz);
-            const float v = gn[t] + bn, n = a.candidate ? tanh_f32(v) : v;
+            gate_pair(__builtin_fmaf(gz[t], -kLog2e, bz * -kLog2e), z, omz);
+            const float v = gn[t] + bn, n = a.candidate ? gate_tanh<ES>(v) : v;
             h = drop[t] ? omz * n : __builtin_fmaf(z, h, omz * n);
             if (a.h_seq) Row16<ES>::put(a.h_seq, b * a.h_b + t * a.h_t + c, h);
         }
@@ -212,298 +418,239 @@ __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
     if (a.h_T) a.h_T[i] = h;
 }
 
-// (A, B) of each segment, forward or (BACK) of e: the 64 groups of a workgroup
-// take equal runs of the segment's steps, then compose.
-template <int ES, bool RESET, bool BACK>
-__global__ __launch_bounds__(512) void lingru_segment_kernel(LinGruArgs a) {
-    constexpr int E = Row16<ES>::E, U = 4;
-    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = wid * 8 + (lane >> 3);
-    const Column<ES> k(a, lane);
-    __shared__ float totals[8][2][8][E];
-    float bz[E], bn[E], A[E], B[E];
-    load_f32<E>(a.bias, k.c, k.valid, bz);
-    load_f32<E>(a.bias, a.H + k.c, k.valid, bn);
-    static_for<E>([&](auto e) { A[e] = 1.0f; B[e] = 0.0f; });
-    const int64_t steps = a.tiles_per_seg * 256, t0 = (int64_t)blockIdx.y * steps, t1 = min(a.T, t0 + steps);
-    const int run = (int)(steps / 64);  // a multiple of U
-    const char* gx = static_cast<const char*>(a.gx) + k.b * a.gx_b * ES;
-    const char* dh = static_cast<const char*>(a.dh_seq) + k.b * a.dh_b * ES;
-    for (int i0 = 0; i0 < run; i0 += U) {
-        uint4 pz[U], po[U];
-        uint8_t pr[U];
-        static_for<U>([&](auto u) {
-            const int i = BACK ? run - 1 - (i0 + u) : i0 + u;
-            const int64_t t = t0 + (int64_t)g * run + i;
-            const int valid = t < t1 ? k.valid : 0;
-            pz[u] = Row16<ES>::load(gx, t * a.gx_t + k.c, valid);
-            if constexpr (BACK) po[u] = Row16<ES>::load(dh, t * a.dh_t + k.c, a.dh_seq ? valid : 0);
-            else po[u] = Row16<ES>::load(gx, t * a.gx_t + a.H + k.c, valid);
-            if constexpr (RESET) pr[u] = valid ? a.reset[t * a.rs_t + k.b * a.rs_b] : 0;
-        });
-        static_for<U>([&](auto u) {
-            const int i = BACK ? run - 1 - (i0 + u) : i0 + u;
-            const bool in = t0 + (int64_t)g * run + i < t1;
-            float gz[E], o[E];
-            Row16<ES>::unpack(pz[u], gz);
-            Row16<ES>::unpack(po[u], o);
-            static_for<E>([&](auto e) {
-                float z, omz, b;
-                sigmoid_pair(gz[e] + bz[e], z, omz);
-                if constexpr (BACK) {
-                    b = z * o[e];
-                } else {
-                    const float v = o[e] + bn[e];
-                    b = omz * (a.candidate ? tanh_f32(v) : v);
-                }
-                float s = in ? z : 1.0f;
-                if constexpr (RESET) {
-                    s = in && pr[u] ? -0.0f : s;
-                    if (BACK && in && pr[u]) b = 0.0f;
-                }
-                b = in ? b : 0.0f;
-                B[e] = apply<RESET>(s, b, B[e]);
-                A[e] = compose_a<RESET>(A[e], s);
-            });
-        });
-    }
-    wave_scan<E, RESET, !BACK>(A, B, lane);
-    if ((lane >> 3) == (BACK ? 0 : 7)) static_for<E>([&](auto e) {
-        totals[wid][0][lane & 7][e] = A[e];
-        totals[wid][1][lane & 7][e] = B[e];
+// Backward pass; tiles count from the end of time.  The tile's states are formed
+// again from the one before it.
+template <int ES, bool VEC, int NW, int R, bool RESET, bool CHAIN>
+__global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd_kernel(LinGruArgs a) {
+    using S = Rows<ES, VEC, R>;
+    constexpr int TS = NW * 4 * R;
+    static_assert(!CHAIN || TS % kLinGruChunk == 0, "a tile starts at a kept state");
+    __shared__ __attribute__((aligned(16))) float tot[NW][3][kCols];
+    __shared__ __attribute__((aligned(16))) float start[NW][2][kCols];
+    __shared__ __attribute__((aligned(16))) float spare[kCols];
+    __shared__ unsigned ticket;
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
+    const Tile tile = Tile::take<CHAIN>(a, &ticket);
+    const int64_t tiles = (a.T + TS - 1) / TS, kt = tiles - 1 - tile.k;
+    const int64_t b = tile.b, c0 = tile.c0, tw = kt * TS + wid * 4 * R;
+    const int left = (int)max((int64_t)0, min((int64_t)(4 * R), a.T - tw));
+
+    const S gx(a.gx, b * a.gx_b + tw * a.gx_t, a.gx_t, a.H, c0, lane);
+    const S dh(a.dh_seq, b * a.dh_b + tw * a.dh_t, a.dh_t, a.H, c0, lane);
+    uint32_t pz[R][S::W], pn[R][S::W], pd[R][S::W];
+    static_for<R>([&](auto r) {
+        gx.load(pz[r], r, q * R + r < left, 0);
+        gx.load(pn[r], r, q * R + r < left, (uint32_t)a.H * ES);
+        dh.load(pd[r], r, q * R + r < left, 0);
     });
-    __syncthreads();
-    if (g != 0) return;
-    static_for<8>([&](auto i) {
-        constexpr int w = BACK ? 7 - decltype(i)::value : decltype(i)::value;
-        static_for<E>([&](auto e) {
-            const float wa = totals[w][0][lane & 7][e], wb = totals[w][1][lane & 7][e];
-            B[e] = i == 0 ? wb : apply<RESET>(wa, wb, B[e]);
-            A[e] = i == 0 ? wa : compose_a<RESET>(A[e], wa);
+    const uint32_t reset = reset_bits<R, RESET>(a, b, tw, lane, left);
+    float bz[4], bn[4];
+    load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
+    load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
+    static_for<4>([&](auto e) { bz[e] *= -kLog2e; });
+
+    // z, 1 - z and n of each step; (A, B) composes the state, (Z, C) e
+    float z[R][4], omz[R][4], n[R][4], A[4], B[4], Z[4], C[4];
+    static_for<R>([&](auto r) {
+        float gz[4];
+        static_for<S::W>([&](auto w) { pz[r][w] = q * R + r < left ? pz[r][w] : S::kKeep; });
+        S::unpack(pz[r], gz);
+        S::unpack(pn[r], n[r]);
+        static_for<4>([&](auto e) { n[r][e] += bn[e]; });
+        if (a.candidate) static_for<4>([&](auto e) { n[r][e] = gate_tanh<ES>(n[r][e]); });
+        static_for<4>([&](auto e) {
+            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z[r][e], omz[r][e]);
+            const float s = RESET && (reset >> r & 1) ? -0.0f : z[r][e], w = omz[r][e] * n[r][e];
+            A[e] = r == 0 ? s : compose_a<RESET>(A[e], s);
+            B[e] = r == 0 ? w : apply<RESET>(s, w, B[e]);
         });
     });
-    const int64_t n = a.batch * a.H, at = (int64_t)blockIdx.y * n + k.b * a.H + k.c;
-    store_f32<E>(a.agg, at, k.valid, A);
-    store_f32<E>(a.agg + a.segs * n, at, k.valid, B);
-}
-
-// Backward pass.  The tile's states are formed again from the one before it.
-template <int ES, int NW, bool RESET>
-__global__ __launch_bounds__(NW * 64) void lingru_bwd_kernel(LinGruArgs a) {
-    constexpr int E = Row16<ES>::E, R = kSteps, TS = NW * 8 * R;
-    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = wid * 8 + (lane >> 3);
-    const Column<ES> k(a, lane);
-    __shared__ float totals[2][NW][3][8][E];
-
-    float bz[E], bn[E], er[E], sz[E], sn[E];
-    load_f32<E>(a.bias, k.c, k.valid, bz);
-    load_f32<E>(a.bias, a.H + k.c, k.valid, bn);
-    load_f32<E>(a.dh_T, k.b * a.H + k.c, k.valid, er);
-    static_for<E>([&](auto e) { sz[e] = 0.0f; sn[e] = 0.0f; });
-    const int64_t tiles = (a.T + TS - 1) / TS;
-    const int64_t tile0 = (int64_t)blockIdx.y * a.tiles_per_seg, tile1 = min(tiles, tile0 + a.tiles_per_seg);
-    segment_in<E, RESET, true>(a, blockIdx.y, k.b, k.c, k.valid, er);
-
-    const char* gx = static_cast<const char*>(a.gx) + k.b * a.gx_b * ES;
-    const char* dh = static_cast<const char*>(a.dh_seq) + k.b * a.dh_b * ES;
-    char* dg = static_cast<char*>(a.dgx) + k.b * a.dg_b * ES;
-    uint4 pz[R], pn[R], pd[R];
-    uint8_t pr[R];
-    float ps[E];
-    auto fetch = [&](int64_t tile) {
-        const int vt = tile >= tile0 ? k.valid : 0;
-        static_for<R>([&](auto r) {
-            const int64_t t = tile * TS + g * R + r;
-            const int valid = t < a.T ? vt : 0;
-            pz[r] = Row16<ES>::load(gx, t * a.gx_t + k.c, valid);
-            pn[r] = Row16<ES>::load(gx, t * a.gx_t + a.H + k.c, valid);
-            pd[r] = Row16<ES>::load(dh, t * a.dh_t + k.c, a.dh_seq ? valid : 0);
-            if constexpr (RESET) pr[r] = valid ? a.reset[t * a.rs_t + k.b * a.rs_b] : 0;
-        });
-        load_f32<E>(a.states, (tile * a.batch + k.b) * a.H + k.c, vt, ps);
-    };
-    fetch(tile1 - 1);
-    for (int64_t tile = tile1 - 1; tile >= tile0; --tile) {
-        const int64_t t0 = tile * TS + g * R;
-        float z[R][E], omz[R][E], n[R][E], d[R][E], A[E], B[E], Z[E], C[E], hs[E];
-        bool drop[R];
-        static_for<R>([&](auto r) {
-            float gz[E], gn[E];
-            Row16<ES>::unpack(pz[r], gz);
-            Row16<ES>::unpack(pn[r], gn);
-            Row16<ES>::unpack(pd[r], d[r]);
-            const bool in = t0 + r < a.T;
-            drop[r] = RESET && in && pr[r];
-            static_for<E>([&](auto e) {
-                sigmoid_pair(gz[e] + bz[e], z[r][e], omz[r][e]);
-                const float v = gn[e] + bn[e];
-                n[r][e] = a.candidate ? tanh_f32(v) : v;
-                if (!in) { z[r][e] = 1.0f; omz[r][e] = 0.0f; n[r][e] = 0.0f; }
-                const float s = RESET && drop[r] ? -0.0f : z[r][e], b = omz[r][e] * n[r][e];
-                A[e] = r == 0 ? s : compose_a<RESET>(A[e], s);
-                B[e] = r == 0 ? b : apply<RESET>(s, b, B[e]);
-            });
-        });
-        static_for<E>([&](auto e) {
-            hs[e] = ps[e];
+    static_for<R>([&](auto i) {
+        constexpr int r = R - 1 - decltype(i)::value;
+        float d[4];
+        S::unpack(pd[r], d);
+        static_for<4>([&](auto e) {
+            const float w = z[r][e] * (i == 0 ? d[e] : d[e] + C[e]);
+            C[e] = RESET && (reset >> r & 1) ? 0.0f : w;
             Z[e] = A[e];
-            C[e] = 0.0f;
-            static_for<R>([&](auto i) {
-                constexpr int r = R - 1 - decltype(i)::value;
-                C[e] = RESET && drop[r] ? 0.0f : z[r][e] * (d[r][e] + C[e]);
-            });
-        });
-        fetch(tile - 1);
-        wave_scan<E, RESET, true>(A, B, lane);
-        wave_scan<E, RESET, false>(Z, C, lane);
-        float (&tot)[NW][3][8][E] = totals[tile & 1];
-        if ((lane >> 3) == 7) static_for<E>([&](auto e) {
-            tot[wid][0][lane & 7][e] = A[e];
-            tot[wid][1][lane & 7][e] = B[e];
-        });
-        if ((lane >> 3) == 0) static_for<E>([&](auto e) { tot[wid][2][lane & 7][e] = C[e]; });
-        __syncthreads();
-        float en[E];
-        static_for<E>([&](auto e) { en[e] = er[e]; });
-        static_for<NW>([&](auto i) {
-            constexpr int w = decltype(i)::value, wr = NW - 1 - w;
-            static_for<E>([&](auto e) {
-                if (w < wid) hs[e] = apply<RESET>(tot[w][0][lane & 7][e], tot[w][1][lane & 7][e], hs[e]);
-                er[e] = apply<RESET>(tot[wr][0][lane & 7][e], tot[wr][2][lane & 7][e], er[e]);
-                if (wr > wid) en[e] = er[e];
-            });
-        });
-        // state before this group's steps, e after them
-        float hb[R][E];
-        static_for<E>([&](auto e) {
-            const float pa = __shfl_up(A[e], 8), pb = __shfl_up(B[e], 8);
-            if (lane >= 8) hs[e] = apply<RESET>(pa, pb, hs[e]);
-            const float qa = __shfl_down(Z[e], 8), qc = __shfl_down(C[e], 8);
-            if (lane < 56) en[e] = apply<RESET>(qa, qc, en[e]);
-            static_for<R>([&](auto r) {
-                hb[r][e] = RESET && drop[r] ? 0.0f : hs[e];
-                hs[e] = RESET && drop[r] ? omz[r][e] * n[r][e] : __builtin_fmaf(z[r][e], hs[e], omz[r][e] * n[r][e]);
-            });
-        });
-        static_for<R>([&](auto i) {
-            constexpr int r = R - 1 - decltype(i)::value;
-            const bool in = t0 + r < a.T;
-            float oz[E], on[E];
-            static_for<E>([&](auto e) {
-                const float dt = d[r][e] + en[e], q = dt * omz[r][e];
-                oz[e] = q * z[r][e] * (hb[r][e] - n[r][e]);
-                on[e] = a.candidate ? q * (1.0f - n[r][e] * n[r][e]) : q;
-                en[e] = RESET && drop[r] ? 0.0f : z[r][e] * dt;
-                if (in) {
-                    sz[e] += oz[e];
-                    sn[e] += on[e];
-                }
-            });
-            Row16<ES>::store(dg, (t0 + r) * a.dg_t + k.c, Row16<ES>::pack(oz), in ? k.valid : 0);
-            Row16<ES>::store(dg, (t0 + r) * a.dg_t + a.H + k.c, Row16<ES>::pack(on), in ? k.valid : 0);
-        });
-        // (step by step, closer than the composition of the tile)
-        if (a.dh0 && tile == 0 && g == 0) store_f32<E>(a.dh0, k.b * a.H + k.c, k.valid, en);
-    }
-    if (a.dh0 && tiles == 0 && g == 0) store_f32<E>(a.dh0, k.b * a.H + k.c, k.valid, er);
-    if (!a.dbias) return;
-    // this workgroup's sums over time: lanes of a wave, then waves
-    static_for<3>([&](auto dc) {
-        constexpr int d = 8 << decltype(dc)::value;
-        static_for<E>([&](auto e) {
-            sz[e] += __shfl_down(sz[e], d);
-            sn[e] += __shfl_down(sn[e], d);
         });
     });
+    wave_scan<RESET, true>(A, B, lane);
+    wave_scan<RESET, false>(Z, C, lane);
+    put4(tot[wid][0], spare, lane, q == 3, A);
+    put4(tot[wid][1], spare, lane, q == 3, B);
+    put4(tot[wid][2], spare, lane, q == 0, C);
     __syncthreads();
-    if ((lane >> 3) == 0) static_for<E>([&](auto e) {
-        totals[0][wid][0][lane & 7][e] = sz[e];
-        totals[0][wid][1][lane & 7][e] = sn[e];
-    });
-    __syncthreads();
-    if (g != 0) return;
-    static_for<NW - 1>([&](auto i) {
-        static_for<E>([&](auto e) {
-            sz[e] += totals[0][i + 1][0][lane & 7][e];
-            sn[e] += totals[0][i + 1][1][lane & 7][e];
+    if (wid == 0) {
+        const int64_t ch = channel<VEC>(a.H, c0, lane >> 2, lane & 3);
+        float wa[NW], wc[NW];
+        float h = a.states[(kt * TS / kLinGruChunk * a.batch + b) * a.H + ch];
+        static_for<NW>([&](auto w) {
+            wa[w] = tot[w][0][lane];
+            wc[w] = tot[w][2][lane];
+            start[w][0][lane] = h;
+            h = apply<RESET>(wa[w], tot[w][1][lane], h);
         });
-    });
-    const int64_t row = ((int64_t)blockIdx.y * a.batch + k.b) * 2 * a.H + k.c;
-    store_f32<E>(a.bias_part, row, k.valid, sz);
-    store_f32<E>(a.bias_part, row + a.H, k.valid, sn);
-}
-
-template <int ES>
-int64_t columns(const LinGruArgs& a) {
-    const int64_t cb = 8 * Row16<ES>::E;
-    return a.batch * ((a.H + cb - 1) / cb);
-}
-
-template <int ES>
-hipError_t forward(const LinGruArgs& a, hipStream_t s) {
-    const int64_t cols = columns<ES>(a), n = a.batch * a.H;
-    if (cols > INT32_MAX || (n + 63) / 64 > INT32_MAX) return hipErrorInvalidValue;
-    if (a.T <= kFewSteps) {
-        hipLaunchKernelGGL(lingru_few_kernel<ES>, dim3((unsigned)((n + 63) / 64)), dim3(64), 0, s, a);
-        return hipGetLastError();
-    }
-    const dim3 grid((unsigned)cols, (unsigned)a.segs);
-    if (a.segs > 1) {
-        hipLaunchKernelGGL((a.reset ? lingru_segment_kernel<ES, true, false> : lingru_segment_kernel<ES, false, false>), grid,
-                           dim3(512), 0, s, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (a.T <= 64)
-        hipLaunchKernelGGL((a.reset ? lingru_fwd_kernel<ES, 2, true> : lingru_fwd_kernel<ES, 2, false>), grid, dim3(128), 0, s, a);
-    else
-        hipLaunchKernelGGL((a.reset ? lingru_fwd_kernel<ES, 8, true> : lingru_fwd_kernel<ES, 8, false>), grid, dim3(512), 0, s, a);
-    return hipGetLastError();
-}
-
-template <int ES>
-hipError_t backward(const LinGruArgs& a, hipStream_t s) {
-    const int64_t cols = columns<ES>(a);
-    if (cols > INT32_MAX) return hipErrorInvalidValue;
-    if (cols > 0) {
-        const dim3 grid((unsigned)cols, (unsigned)a.segs);
-        if (a.segs > 1) {
-            hipLaunchKernelGGL((a.reset ? lingru_segment_kernel<ES, true, true> : lingru_segment_kernel<ES, false, true>), grid,
-                               dim3(512), 0, s, a);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
+        const float first = a.dh_T ? a.dh_T[b * a.H + ch] : 0.0f;
+        float g = first;
+        if constexpr (CHAIN) {
+            float ta = wa[NW - 1], tc = wc[NW - 1];
+            static_for<NW - 1>([&](auto i) {
+                constexpr int w = NW - 2 - decltype(i)::value;
+                tc = apply<RESET>(wa[w], wc[w], tc);
+                ta = compose_a<RESET>(ta, wa[w]);
+            });
+            if (kt > 0) {
+                chain_put(chain_word(a, tile.id, 1, lane), ta);
+                chain_put(chain_word(a, tile.id, 2, lane), tc);
+            }
+            g = chain_in<RESET>(a, tile.id, tile.k, tile.cols, lane, first);
+            if (kt > 0) chain_put(chain_word(a, tile.id, 0, lane), apply<RESET>(ta, tc, g));
         }
-        if (a.T <= 64)
-            hipLaunchKernelGGL((a.reset ? lingru_bwd_kernel<ES, 2, true> : lingru_bwd_kernel<ES, 2, false>), grid, dim3(128), 0, s, a);
-        else
-            hipLaunchKernelGGL((a.reset ? lingru_bwd_kernel<ES, 8, true> : lingru_bwd_kernel<ES, 8, false>), grid, dim3(512), 0, s, a);
+        static_for<NW>([&](auto i) {
+            constexpr int w = NW - 1 - decltype(i)::value;
+            start[w][1][lane] = g;
+            g = apply<RESET>(wa[w], wc[w], g);
+        });
+    }
+    __syncthreads();
+    float hs[4], en[4], hb[R][4], sz[4], sn[4];
+    get4(start[wid][0], lane, hs);
+    get4(start[wid][1], lane, en);
+    static_for<4>([&](auto e) {
+        const float pa = __shfl_up(A[e], 16), pb = __shfl_up(B[e], 16);
+        hs[e] = q > 0 ? apply<RESET>(pa, pb, hs[e]) : hs[e];
+        const float qa = __shfl_down(Z[e], 16), qc = __shfl_down(C[e], 16);
+        en[e] = q < 3 ? apply<RESET>(qa, qc, en[e]) : en[e];
+        sz[e] = sn[e] = 0.0f;
+        static_for<R>([&](auto r) {
+            hb[r][e] = RESET && (reset >> r & 1) ? 0.0f : hs[e];
+            hs[e] = __builtin_fmaf(z[r][e], hb[r][e], omz[r][e] * n[r][e]);
+        });
+    });
+    const S dg(a.dgx, b * a.dg_b + tw * a.dg_t, a.dg_t, a.H, c0, lane);
+    static_for<R>([&](auto i) {
+        constexpr int r = R - 1 - decltype(i)::value;
+        float d[4], oz[4], on[4];
+        S::unpack(pd[r], d);
+        static_for<4>([&](auto e) {
+            const float dt = d[e] + en[e], w = dt * omz[r][e];  // (0 past the end)
+            oz[e] = w * z[r][e] * (hb[r][e] - n[r][e]);
+            on[e] = a.candidate ? w * __builtin_fmaf(-n[r][e], n[r][e], 1.0f) : w;
+            const float back = z[r][e] * dt;
+            en[e] = RESET && (reset >> r & 1) ? 0.0f : back;
+            sz[e] += oz[e];
+            sn[e] += on[e];
+        });
+        dg.store(oz, r, q * R + r < left, 0);
+        dg.store(on, r, q * R + r < left, (uint32_t)a.H * ES);
+    });
+    if (a.dh0 && kt == 0 && wid == 0) store_channels<VEC>(a.dh0, b * a.H, a.H, c0, lane, q == 0, en);
+    if (!a.dbias) return;
+    // this tile's sums over time: groups of a wave, then waves
+    static_for<4>([&](auto e) {
+        static_for<2>([&](auto dc) {
+            sz[e] += __shfl_xor(sz[e], 16 << decltype(dc)::value);
+            sn[e] += __shfl_xor(sn[e], 16 << decltype(dc)::value);
+        });
+    });
+    put4(tot[wid][0], spare, lane, q == 0, sz);  // (tot was last read before the second barrier)
+    put4(tot[wid][1], spare, lane, q == 0, sn);
+    __syncthreads();
+    if (wid >= 2) return;
+    float s = 0.0f;
+    static_for<NW>([&](auto w) { s += tot[w][wid][lane]; });
+    a.bias_part[(kt * a.batch + b) * 2 * a.H + wid * a.H + channel<VEC>(a.H, c0, lane >> 2, lane & 3)] = s;
+}
+
+__global__ __launch_bounds__(256) void lingru_clear_kernel(uint4* p, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = make_uint4(0, 0, 0, 0);
+}
+// dst = src, or zeros.
+__global__ __launch_bounds__(256) void lingru_copy_kernel(const float* src, float* dst, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) dst[i] = src ? src[i] : 0.0f;
+}
+
+typedef void (*LinGruFn)(LinGruArgs);
+
+template <int ES, bool VEC, bool BWD, bool RESET>
+LinGruFn tile_fn(bool few, bool chain) {
+    constexpr int R = BWD ? kLinGruBwdSteps : kLinGruFwdSteps;
+    if constexpr (BWD) {
+        if (few) return lingru_bwd_kernel<ES, VEC, 2, 8, RESET, false>;
+        return chain ? lingru_bwd_kernel<ES, VEC, 8, R, RESET, true> : lingru_bwd_kernel<ES, VEC, 8, R, RESET, false>;
+    } else {
+        if (few) return lingru_fwd_kernel<ES, VEC, 2, 8, RESET, false>;
+        return chain ? lingru_fwd_kernel<ES, VEC, 8, R, RESET, true> : lingru_fwd_kernel<ES, VEC, 8, R, RESET, false>;
+    }
+}
+
+// Whether every row of p starts on 4 bytes and holds whole pieces of four (fp32
+// rows: whole pieces).
+bool pieces(const void* p, int64_t st, int64_t sb, const LinGruArgs& a) {
+    return !p || (a.H % 4 == 0 && (a.type == kF32 || ((uintptr_t)p % 4 == 0 && st % 2 == 0 && sb % 2 == 0)));
+}
+
+template <int ES, bool BWD>
+hipError_t launch_tiles(const LinGruArgs& a, hipStream_t s) {
+    const int64_t cols = a.batch * ((a.H + kCols - 1) / kCols);
+    const bool few = a.T <= 64;
+    const int64_t tiles = lingru_tiles(a.T, BWD), total = cols * tiles;
+    if (total > INT32_MAX) return hipErrorInvalidValue;
+    const bool chain = tiles > 1;
+    if (chain) {
+        const int64_t n = (int64_t)(lingru_chain_bytes(a.T, a.batch, a.H, BWD) / 16), blocks = (n + 255) / 256;
+        hipLaunchKernelGGL(lingru_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s,
+                           reinterpret_cast<uint4*>(a.chain), n);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    return a.dbias ? launch_colsum(a.bias_part, a.segs * a.batch, 2 * a.H, 1, kF32, a.dbias, s) : hipSuccess;
+    const bool vec = pieces(a.gx, a.gx_t, a.gx_b, a) && (BWD ? pieces(a.dh_seq, a.dh_t, a.dh_b, a) && pieces(a.dgx, a.dg_t, a.dg_b, a)
+                                                             : pieces(a.h_seq, a.h_t, a.h_b, a));
+    const LinGruFn fn = vec ? (a.reset ? tile_fn<ES, true, BWD, true>(few, chain) : tile_fn<ES, true, BWD, false>(few, chain))
+                            : (a.reset ? tile_fn<ES, false, BWD, true>(few, chain) : tile_fn<ES, false, BWD, false>(few, chain));
+    hipLaunchKernelGGL(fn, dim3((unsigned)total), dim3(few ? 128 : 512), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-// Segments of time: none while sequences and channel blocks give every compute
-// unit a workgroup, otherwise enough for two per unit, of two tiles or more.
-void lingru_segments(int64_t T, int64_t batch, int64_t H, int type, int cus, int64_t* segs, int64_t* tiles_per_seg) {
-    const int64_t cb = type == kBF16 ? 64 : 32, cols = batch * ((H + cb - 1) / cb), tiles = (T + kLinGruChunk - 1) / kLinGruChunk;
-    int64_t s = 1;
-    if (cols > 0 && cols < cus && tiles >= 4) s = (2 * (int64_t)cus) / cols;
-    if (s > tiles / 2) s = tiles / 2;
-    if (s < 1) s = 1;
-    int64_t per = (tiles + s - 1) / s;
-    if (per < 1) per = 1;
-    *tiles_per_seg = per;
-    *segs = tiles > 0 ? (tiles + per - 1) / per : 1;
+// Whether a wave's rows lie within 31 bits of its first.
+bool lingru_strides(int64_t stride_t, int64_t width, int64_t es) {
+    return (__int128)stride_t * es * 32 + (__int128)width * es < ((__int128)1 << 31);
+}
+
+int64_t lingru_tiles(int64_t T, bool backward) {
+    const int64_t ts = 32 * (backward ? kLinGruBwdSteps : kLinGruFwdSteps);
+    return T <= 64 ? (T > 0 ? 1 : 0) : (T + ts - 1) / ts;
+}
+
+// The counter's line and three words for each tile and channel; nothing for single tiles.
+size_t lingru_chain_bytes(int64_t T, int64_t batch, int64_t H, bool backward) {
+    const int64_t tiles = lingru_tiles(T, backward), cols = batch * ((H + kCols - 1) / kCols);
+    return tiles > 1 ? 64 + (size_t)(tiles * cols) * 3 * kCols * 8 : 0;
 }
 
 hipError_t launch_lingru_forward(const LinGruArgs& a, hipStream_t s) {
-    return a.type == kBF16 ? forward<2>(a, s) : forward<4>(a, s);
+    const int64_t n = a.batch * a.H;
+    if (a.T > kFewSteps) return a.type == kBF16 ? launch_tiles<2, false>(a, s) : launch_tiles<4, false>(a, s);
+    if ((n + 63) / 64 > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((a.type == kBF16 ? lingru_few_kernel<2> : lingru_few_kernel<4>), dim3((unsigned)((n + 63) / 64)), dim3(64), 0, s, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_lingru_backward(const LinGruArgs& a, hipStream_t s) {
-    return a.type == kBF16 ? backward<2>(a, s) : backward<4>(a, s);
+    const int64_t n = a.batch * a.H, tiles = lingru_tiles(a.T, true);
+    hipError_t e = hipSuccess;
+    if (n > 0 && tiles > 0) {
+        e = a.type == kBF16 ? launch_tiles<2, true>(a, s) : launch_tiles<4, true>(a, s);
+    } else if (n > 0 && a.dh0) {
+        const int64_t blocks = (n + 255) / 256;
+        hipLaunchKernelGGL(lingru_copy_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, a.dh_T, a.dh0, n);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || !a.dbias) return e;
+    return launch_colsum(a.bias_part, tiles * a.batch, 2 * a.H, 1, kF32, a.dbias, s);
 }
 
 }  // namespace isam
