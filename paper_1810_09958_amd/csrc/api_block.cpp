@@ -331,27 +331,6 @@ extern "C" isam_status_t isam_norm_residual_backward(int64_t rows, int64_t D, in
     if (rows0 && dgate && (gates < 0 || gates > ((int64_t)1 << 40) / D))
         return fail(ISAM_ERR_INVALID_ARG, "%s: gates=%lld", who, (long long)gates);
     NormArgs a{};
-    int64_t grid = 0;
-    if (!rows0) norm_bwd_grid(rows, D, gates, type, device_cus(), &grid, &a.parts);
-    const size_t need = (size_t)(3 * grid * D) * sizeof(float);
-    if (need && (!workspace || workspace_bytes < room(need)))
-        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
-                    room(need));
-    size_t x_b, r_b, dy_b, dro_b, dx_b, dr_b, g_b, dg_b;
-    if (!matrix(x, rows, D, ldx, es, &x_b) || !matrix(r_out, rows, D, ldro, es, &r_b) || !matrix(dy, rows, D, lddy, es, &dy_b) ||
-        !matrix(dr_out, rows, D, lddro, es, &dro_b) || !matrix(dx, rows, D, lddx, es, &dx_b) ||
-        !matrix(dr, rows, D, lddr, es, &dr_b) || !matrix(gate, gates, D, D, es, &g_b) || !matrix(dgate, gates, D, D, es, &dg_b))
-        return fail(ISAM_ERR_INVALID_ARG, "%s: a leading dimension is below D, or a tensor spans more than 2^46 bytes", who);
-    const size_t w_b = (size_t)D * 4;
-    const bool in_place = dr && dr == dr_out && lddr == lddro;
-    const Tensor all[] = {{"x", x, x_b, false},           {"r_out", r_out, r_b, false},
-                          {"gate", gate, g_b, false},     {"w_post", w_post, w_b, false},
-                          {"w_pre", w_pre, w_b, false},   {"dy", dy, dy_b, false},
-                          {"dr_out", in_place ? nullptr : dr_out, dro_b, false},
-                          {"dx", dx, dx_b, true},         {"dr", dr, dr_b, true},
-                          {"dgate", dgate, dg_b, true},   {"dw_post", dw_post, w_b, true},
-                          {"dw_pre", dw_pre, w_b, true},  {"workspace", workspace, room(need), true}};
-    if ((st = disjoint(all, who)) != ISAM_OK) return st;
     a.rows = rows;
     a.D = D;
     a.type = type;
@@ -377,6 +356,27 @@ extern "C" isam_status_t isam_norm_residual_backward(int64_t rows, int64_t D, in
     a.dgate = dgate;
     a.dw_post = dw_post;
     a.dw_pre = dw_pre;
+    int64_t grid = 0;
+    if (!rows0) norm_bwd_grid(a, device_cus(), &grid, &a.parts);
+    const size_t need = (size_t)(3 * grid * D) * sizeof(float);
+    if (need && (!workspace || workspace_bytes < room(need)))
+        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
+                    room(need));
+    size_t x_b, r_b, dy_b, dro_b, dx_b, dr_b, g_b, dg_b;
+    if (!matrix(x, rows, D, ldx, es, &x_b) || !matrix(r_out, rows, D, ldro, es, &r_b) || !matrix(dy, rows, D, lddy, es, &dy_b) ||
+        !matrix(dr_out, rows, D, lddro, es, &dro_b) || !matrix(dx, rows, D, lddx, es, &dx_b) ||
+        !matrix(dr, rows, D, lddr, es, &dr_b) || !matrix(gate, gates, D, D, es, &g_b) || !matrix(dgate, gates, D, D, es, &dg_b))
+        return fail(ISAM_ERR_INVALID_ARG, "%s: a leading dimension is below D, or a tensor spans more than 2^46 bytes", who);
+    const size_t w_b = (size_t)D * 4;
+    const bool in_place = dr && dr == dr_out && lddr == lddro;
+    const Tensor all[] = {{"x", x, x_b, false},           {"r_out", r_out, r_b, false},
+                          {"gate", gate, g_b, false},     {"w_post", w_post, w_b, false},
+                          {"w_pre", w_pre, w_b, false},   {"dy", dy, dy_b, false},
+                          {"dr_out", in_place ? nullptr : dr_out, dro_b, false},
+                          {"dx", dx, dx_b, true},         {"dr", dr, dr_b, true},
+                          {"dgate", dgate, dg_b, true},   {"dw_post", dw_post, w_b, true},
+                          {"dw_pre", dw_pre, w_b, true},  {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
     a.partial = reinterpret_cast<float*>(room_start(workspace));
     const hipError_t e = launch_norm_backward(a, grid, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
@@ -385,12 +385,15 @@ extern "C" isam_status_t isam_norm_residual_backward(int64_t rows, int64_t D, in
 extern "C" size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64_t D, int64_t gates, int type) {
     if (rows <= 0 || D <= 0 || !valid_dtype(type) || !norm_sizes(rows, D)) return 0;
     // without a gate the call has one gate row
-    int64_t grid, most = 0;
-    int parts;
+    int64_t most = 0;
     for (const int64_t g : {gates, (int64_t)1}) {
         if (g <= 0 || rows % g) continue;
-        norm_bwd_grid(rows, D, g, type, device_cus(), &grid, &parts);
-        if (grid > most) most = grid;
+        NormArgs a{};
+        a.rows = rows;
+        a.D = D;
+        a.type = type;
+        a.gates = g;
+        most = std::max(most, norm_bwd_most(a, device_cus()));
     }
     return room((size_t)(3 * most * D) * sizeof(float));
 }
@@ -621,7 +624,8 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
         return st;
     if (dbias) {
         const int64_t rows = M == 0 ? 0 : type == ISAM_BF16 ? gated_bias_rows(p.tile, M) : cdiv(M, kGatedRows);
-        e = launch_colsum(bias_part, rows, 2 * F, 1, kF32, dbias, s);
+        const ColSum sum{bias_part, dbias, rows, 2 * F, 1, kF32};
+        e = launch_colsum(&sum, 1, s);
     }
     return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
 }

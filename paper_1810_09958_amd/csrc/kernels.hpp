@@ -299,7 +299,11 @@ struct NormArgs {
     int parts;                      // workgroups of a gate row; 0: row groups own whole gate rows
     float* partial;                 // [3][grid][D]: sums for w_pre, w_post and the gate
 };
-void norm_bwd_grid(int64_t rows, int64_t D, int64_t gates, int type, int cus, int64_t* grid, int* parts);
+// Grid and a.parts of the backward pass; the pointers and leading dimensions count by their
+// alignment (none given: aligned).
+void norm_bwd_grid(const NormArgs& a, int cus, int64_t* grid, int* parts);
+// Most workgroups it takes at any alignment.
+int64_t norm_bwd_most(const NormArgs& a, int cus);
 hipError_t launch_norm_forward(const NormArgs& a, int cus, hipStream_t s);
 hipError_t launch_norm_backward(const NormArgs& a, int64_t grid, hipStream_t s);
 
@@ -329,7 +333,14 @@ hipError_t launch_gated_tiles(const GatedArgs& a, int tile, bool backward, hipSt
 hipError_t launch_gated_tokens(const GatedArgs& a, int type, hipStream_t s);
 hipError_t launch_gated_pairs(const GatedArgs& a, bool backward, hipStream_t s);
 
-// out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros).
-hipError_t launch_colsum(const float* part, int64_t rows, int64_t cols, int64_t groups, int out_type, void* out, hipStream_t s);
+// out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros), up to three such
+// sums in one launch.
+struct ColSum {
+    const float* part;
+    void* out;
+    int64_t rows, cols, groups;
+    int type;  // of out
+};
+hipError_t launch_colsum(const ColSum* sums, int count, hipStream_t s);
 
 }  // namespace isam

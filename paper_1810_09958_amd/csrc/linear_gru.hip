@@ -650,7 +650,8 @@ hipError_t launch_lingru_backward(const LinGruArgs& a, hipStream_t s) {
         e = hipGetLastError();
     }
     if (e != hipSuccess || !a.dbias) return e;
-    return launch_colsum(a.bias_part, tiles * a.batch, 2 * a.H, 1, kF32, a.dbias, s);
+    const ColSum sum{a.bias_part, a.dbias, tiles * a.batch, 2 * a.H, 1, kF32};
+    return launch_colsum(&sum, 1, s);
 }
 
 }  // namespace isam

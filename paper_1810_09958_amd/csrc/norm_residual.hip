@@ -31,7 +31,7 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*lds)[N], int slot
     });
     if constexpr (TPR > 64) {
         const int wid = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) static_for<N>([&](auto n) { lds[wid][n] = v[n]; });
+        static_for<N>([&](auto n) { lds[wid][n] = v[n]; });  // (every lane the same value: no branch of lanes)
         __syncthreads();
         static_for<N>([&](auto n) { v[n] = 0.0f; });
         static_for<TPR / 64>([&](auto w) {
@@ -40,67 +40,73 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*lds)[N], int slot
     }
 }
 
-template <int ES, int TPR, int V, int BLOCK>
+// Thread j of its row, row group ng of the workgroup, the group's first wave; the
+// groups are whole waves, so ng is uniform over a wave.
+template <int TPR, int BLOCK>
 struct RowPart {
-    static constexpr int E = Row16<ES>::E, NR = BLOCK / TPR, WAVES = BLOCK / 64;
-    int j, ng, slot0;  // thread in its row, row group in the workgroup, the group's first wave
-    __device__ __forceinline__ RowPart() : j(threadIdx.x % TPR), ng(threadIdx.x / TPR), slot0(threadIdx.x / TPR * (TPR / 64)) {}
-    __device__ __forceinline__ int64_t at(int i) const { return ((int64_t)i * TPR + j) * E; }
-    __device__ __forceinline__ int valid(const NormArgs& a, int i) const {
-        return (int)max((int64_t)0, min((int64_t)E, a.D - at(i)));
+    static constexpr int NR = BLOCK / TPR, WAVES = BLOCK / 64;
+    int j, ng, slot0;
+    __device__ __forceinline__ RowPart() {
+        const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        j = threadIdx.x % TPR;
+        ng = wid / (TPR / 64);
+        slot0 = ng * (TPR / 64);
     }
 };
 
-template <int ES, int TPR, int V, int BLOCK>
+template <int ES, bool VEC, int TPR, int V, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a) {
-    using P = RowPart<ES, TPR, V, BLOCK>;
-    using IO = Row16<ES>;
-    constexpr int E = P::E;
+    using P = RowPart<TPR, BLOCK>;
+    constexpr int E = 16 / ES;
+    using B = RowBuf<ES, VEC, TPR, E>;
     const P part;
+    const int j = part.j;
     __shared__ float lds[2][P::WAVES][1];
     float wa[V][E], wb[V][E];
+    using W = RowBuf<4, VEC, TPR, 4>;
+    const __amdgpu_buffer_rsrc_t ra = W::row(a.w_post, 0, a.D, true), rb = W::row(a.w_pre, 0, a.D, true);
     static_for<V>([&](auto i) {
-        load_f32<E>(a.w_post, part.at(i), part.valid(a, i), wa[i]);
-        load_f32<E>(a.w_pre, part.at(i), part.valid(a, i), wb[i]);
+        B::load32(ra, i, j, wa[i]);
+        B::load32(rb, i, j, wb[i]);
     });
     const float inv = 1.0f / (float)a.D;
     const int64_t step = (int64_t)gridDim.x * P::NR;
     for (int64_t base = (int64_t)blockIdx.x * P::NR; base < a.rows; base += step) {
         const int64_t row = base + part.ng;
         const bool live = row < a.rows;
-        uint4 px[V], pr[V], pg[V];
+        const __amdgpu_buffer_rsrc_t rx = B::row(a.x, row * a.ld_x, a.D, live), rr = B::row(a.r, row * a.ld_r, a.D, live),
+                                     rg = B::row(a.gate, row / a.rows_per_gate * a.D, a.D, live);
+        typename B::Piece px[V], pr[V], pg[V];
         static_for<V>([&](auto i) {
-            const int valid = live ? part.valid(a, i) : 0;
-            pr[i] = IO::load(a.r, row * a.ld_r + part.at(i), valid);
-            px[i] = IO::load(a.x, row * a.ld_x + part.at(i), a.x ? valid : 0);
-            pg[i] = IO::load(a.gate, row / a.rows_per_gate * a.D + part.at(i), a.gate ? valid : 0);
+            pr[i] = B::load(rr, i, j);
+            px[i] = B::load(rx, i, j);
+            pg[i] = B::load(rg, i, j);
         });
         float r[V][E];
+        static_for<V>([&](auto i) { B::unpack(pr[i], r[i]); });
         if (a.x) {
             float q = 1.0f;
             if (a.w_post) {
                 float sum[1] = {0.0f};
                 static_for<V>([&](auto i) {
                     float x[E];
-                    IO::unpack(px[i], x);
+                    B::unpack(px[i], x);
                     static_for<E>([&](auto e) { sum[0] += x[e] * x[e]; });
                 });
                 row_sum<TPR, 1>(sum, lds[0], part.slot0);
                 q = 1.0f / sqrtf(sum[0] * inv + a.eps);
             }
+            const __amdgpu_buffer_rsrc_t ro = B::row(a.r_out, row * a.ld_ro, a.D, live);
             static_for<V>([&](auto i) {
                 float x[E], g[E];
-                IO::unpack(px[i], x);
-                IO::unpack(pg[i], g);
-                IO::unpack(pr[i], r[i]);
+                B::unpack(px[i], x);
+                B::unpack(pg[i], g);
                 static_for<E>([&](auto e) {
                     const float u = a.w_post ? x[e] * q * wa[i][e] : x[e];
                     r[i][e] += (a.gate ? a.scale * g[e] : a.scale) * u;
                 });
-                IO::store(a.r_out, row * a.ld_ro + part.at(i), IO::pack(r[i]), live ? part.valid(a, i) : 0);
+                B::store(ro, i, j, r[i]);
             });
-        } else {
-            static_for<V>([&](auto i) { IO::unpack(pr[i], r[i]); });
         }
         float sum[1] = {0.0f};
         static_for<V>([&](auto i) {
@@ -108,9 +114,10 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a) {
         });
         row_sum<TPR, 1>(sum, lds[1], part.slot0);
         const float p = 1.0f / sqrtf(sum[0] * inv + a.eps);
+        const __amdgpu_buffer_rsrc_t ry = B::row(a.y, row * a.ld_y, a.D, live);
         static_for<V>([&](auto i) {
             static_for<E>([&](auto e) { r[i][e] *= p * wb[i][e]; });
-            IO::store(a.y, row * a.ld_y + part.at(i), IO::pack(r[i]), live ? part.valid(a, i) : 0);
+            B::store(ry, i, j, r[i]);
         });
         // The first sum of the next row writes lds[0], last read before this
         // row's second barrier; the second one lds[1], read before the next
@@ -119,30 +126,44 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a) {
     }
 }
 
-// Rows of the backward pass.  With at least as many gate rows as row groups
-// (a.parts == 0) each row group takes whole gate rows and writes their
-// gradient itself; otherwise a.parts workgroups share a gate row and leave
-// partial sums.
-template <int ES, int TPR, int V, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormArgs a) {
-    using P = RowPart<ES, TPR, V, BLOCK>;
-    using IO = Row16<ES>;
-    constexpr int E = P::E, NR = P::NR;
+// Rows of the backward pass.  With few rows to a gate row (a.parts == 0) each row
+// group takes whole gate rows and writes their gradient itself; otherwise a.parts
+// workgroups share a gate row (one: writes the gradient; more: leave partial sums).
+// HOLD: the weights stay in registers and the next row is requested before this
+// row's arithmetic; the longest rows have no registers for that.
+template <int ES, bool VEC, int TPR, int E, int V, int BLOCK, int MINW, bool HOLD>
+__global__ __launch_bounds__(BLOCK, MINW) void norm_bwd_kernel(NormArgs a) {
+    using P = RowPart<TPR, BLOCK>;
+    constexpr int NR = P::NR, VH = HOLD ? V : 1;
+    using B = RowBuf<ES, VEC, TPR, E>;
+    using B4 = RowBuf<4, VEC, TPR, 4>;
     const P part;
+    const int j = part.j;
     __shared__ float lds[2][P::WAVES][3];
     extern __shared__ float fold[];  // [TPR * V * E]
-    float wa[V][E], wb[V][E], sa[V][E], sb[V][E], sg[V][E];
+    float ha[VH][E], hb[VH][E], sa[V][E], sb[V][E], sg[V][E];
+    const __amdgpu_buffer_rsrc_t ra = B4::row(a.w_post, 0, a.D, true), rb = B4::row(a.w_pre, 0, a.D, true);
     static_for<V>([&](auto i) {
-        load_f32<E>(a.w_post, part.at(i), part.valid(a, i), wa[i]);
-        load_f32<E>(a.w_pre, part.at(i), part.valid(a, i), wb[i]);
+        if constexpr (HOLD) {
+            B::load32(ra, i, j, ha[i]);
+            B::load32(rb, i, j, hb[i]);
+        }
         static_for<E>([&](auto e) { sa[i][e] = 0.0f; sb[i][e] = 0.0f; sg[i][e] = 0.0f; });
     });
+    // Weights of piece i.
+    auto post = [&](auto i, float (&w)[E]) {
+        if constexpr (HOLD) static_for<E>([&](auto e) { w[e] = ha[i][e]; });
+        else B::load32(ra, i, j, w);
+    };
+    auto pre = [&](auto i, float (&w)[E]) {
+        if constexpr (HOLD) static_for<E>([&](auto e) { w[e] = hb[i][e]; });
+        else B::load32(rb, i, j, w);
+    };
     const float inv = 1.0f / (float)a.D;
     const int64_t rpg = a.rows_per_gate, groups = a.gates;
     const int64_t workers = (int64_t)gridDim.x * NR, me = (int64_t)blockIdx.x * NR + part.ng;
-    // The row of iteration i and whether it exists.
-    int64_t iters, grp, k = 0;
-    int64_t share = 0;
+    // Row k of gate row grp, `iters` of them in turn.
+    int64_t iters, grp, k = 0, share = 0;
     if (a.parts == 0) {
         iters = (groups + workers - 1) / workers * rpg;
         grp = me;
@@ -152,23 +173,25 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormArgs a) {
         k = ((int64_t)blockIdx.x - grp * a.parts) * NR + part.ng;
         iters = (rpg + share - 1) / share;
     }
-    uint4 px[V], pr[V], pg[V], py[V], pd[V];
-    auto fetch = [&](int64_t row, bool live) {
+    typename B::Piece px[V], pr[V], pg[V], py[V], pd[V];
+    auto fetch = [&](int64_t row, int64_t gate, bool live) {
+        const __amdgpu_buffer_rsrc_t rx = B::row(a.x, row * a.ld_x, a.D, live), rr = B::row(a.r, row * a.ld_r, a.D, live),
+                                     ry = B::row(a.dy, row * a.ld_dy, a.D, live),
+                                     rd = B::row(a.dr_out, row * a.ld_dro, a.D, live), rg = B::row(a.gate, gate * a.D, a.D, live);
         static_for<V>([&](auto i) {
-            const int valid = live ? part.valid(a, i) : 0;
-            const int64_t at = part.at(i);
-            px[i] = IO::load(a.x, row * a.ld_x + at, a.x ? valid : 0);
-            pr[i] = IO::load(a.r, row * a.ld_r + at, valid);
-            py[i] = IO::load(a.dy, row * a.ld_dy + at, valid);
-            pd[i] = IO::load(a.dr_out, row * a.ld_dro + at, a.dr_out ? valid : 0);
-            pg[i] = IO::load(a.gate, row / rpg * a.D + at, a.gate ? valid : 0);
+            px[i] = B::load(rx, i, j);
+            pr[i] = B::load(rr, i, j);
+            py[i] = B::load(ry, i, j);
+            pd[i] = B::load(rd, i, j);
+            pg[i] = B::load(rg, i, j);
         });
     };
     auto is_live = [&] { return grp < groups && k < rpg; };
-    fetch(grp * rpg + k, is_live());
+    if constexpr (HOLD) fetch(grp * rpg + k, grp, is_live());
     for (int64_t it = 0; it < iters; ++it) {
         const int64_t row = grp * rpg + k, cur = grp;
         const bool live = is_live();
+        if constexpr (!HOLD) fetch(row, cur, live);
         bool last = false;
         if (a.parts == 0) {
             if (++k == rpg) {
@@ -179,135 +202,181 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormArgs a) {
         } else {
             k += share;
         }
-        float x[V][E], r[V][E], dr[V][E], g[V][E], sum[3] = {0.0f, 0.0f, 0.0f};
+        // (a row that does not exist is all zeros, and so is what it adds)
+        float x[V][E], r[V][E], dr[V][E], dy[V][E], sum[3] = {0.0f, 0.0f, 0.0f};
+        typename B::Piece gr[V];
         static_for<V>([&](auto i) {
-            float dy[E];
-            IO::unpack(px[i], x[i]);
-            IO::unpack(pr[i], r[i]);
-            IO::unpack(py[i], dy);
-            IO::unpack(pd[i], dr[i]);
-            IO::unpack(pg[i], g[i]);
+            float w[E];
+            pre(i, w);
+            B::unpack(px[i], x[i]);
+            B::unpack(pr[i], r[i]);
+            B::unpack(py[i], dy[i]);
+            B::unpack(pd[i], dr[i]);
+            gr[i] = pg[i];
             static_for<E>([&](auto e) {
-                g[i][e] = a.gate ? a.scale * g[i][e] : a.scale;
                 sum[0] += x[i][e] * x[i][e];
                 sum[1] += r[i][e] * r[i][e];
-                sum[2] += dy[e] * wb[i][e] * r[i][e];
+                sum[2] += dy[i][e] * w[e] * r[i][e];
             });
         });
+        if constexpr (HOLD) fetch(grp * rpg + k, grp, it + 1 < iters && is_live());
         row_sum<TPR, 3>(sum, lds[0], part.slot0);
-        const float q = a.w_post ? 1.0f / sqrtf(sum[0] * inv + a.eps) : 1.0f;
-        const float p = 1.0f / sqrtf(sum[1] * inv + a.eps), c = sum[2] * inv * p * p * p;
-        float dot[3] = {0.0f, 0.0f, 0.0f};
+        const float q = a.w_post && live ? 1.0f / sqrtf(sum[0] * inv + a.eps) : 1.0f;
+        const float p = live ? 1.0f / sqrtf(sum[1] * inv + a.eps) : 0.0f, c = sum[2] * inv * p * p * p;
+        const __amdgpu_buffer_rsrc_t wr = B::row(a.dr, row * a.ld_dr, a.D, live);
         static_for<V>([&](auto i) {
-            float dy[E];
-            IO::unpack(py[i], dy);
+            float w[E];
+            pre(i, w);
             static_for<E>([&](auto e) {
-                dr[i][e] += p * dy[e] * wb[i][e] - c * r[i][e];
-                if (live) sb[i][e] += dy[e] * p * r[i][e];
+                dr[i][e] += p * dy[i][e] * w[e] - c * r[i][e];
+                sb[i][e] += dy[i][e] * p * r[i][e];
             });
-            IO::store(a.dr, row * a.ld_dr + part.at(i), IO::pack(dr[i]), live ? part.valid(a, i) : 0);
+            B::store(wr, i, j, dr[i]);
         });
-        // the next row's values arrive under the rest of this one's arithmetic
-        fetch(grp * rpg + k, it + 1 < iters && is_live());
         if (a.x) {
+            float dot[1] = {0.0f};
             static_for<V>([&](auto i) {
+                float w[E], g[E];
+                post(i, w);
+                B::unpack(gr[i], g);
                 static_for<E>([&](auto e) {
-                    const float u = a.w_post ? x[i][e] * q * wa[i][e] : x[i][e], du = g[i][e] * dr[i][e];
-                    if (live) {
-                        sg[i][e] += a.scale * u * dr[i][e];
-                        sa[i][e] += du * x[i][e] * q;
-                    }
-                    dr[i][e] = a.w_post ? du * wa[i][e] : du;
+                    const float u = a.w_post ? x[i][e] * q * w[e] : x[i][e];
+                    const float du = (a.gate ? a.scale * g[e] : a.scale) * dr[i][e];
+                    sg[i][e] += a.scale * u * dr[i][e];
+                    sa[i][e] += du * x[i][e] * q;
+                    dr[i][e] = a.w_post ? du * w[e] : du;
                     dot[0] += dr[i][e] * x[i][e];
                 });
             });
             float m = 0.0f;
             if (a.w_post) {
-                float d1[1] = {dot[0]};
-                row_sum<TPR, 1>(d1, reinterpret_cast<float(*)[1]>(&lds[1][0][0]), part.slot0);
-                m = d1[0] * inv * q * q * q;
+                row_sum<TPR, 1>(dot, reinterpret_cast<float(*)[1]>(&lds[1][0][0]), part.slot0);
+                m = dot[0] * inv * q * q * q;
             }
+            const __amdgpu_buffer_rsrc_t wx = B::row(a.dx, row * a.ld_dx, a.D, live);
             static_for<V>([&](auto i) {
                 if (a.w_post) static_for<E>([&](auto e) { dr[i][e] = q * dr[i][e] - m * x[i][e]; });
-                IO::store(a.dx, row * a.ld_dx + part.at(i), IO::pack(dr[i]), live ? part.valid(a, i) : 0);
-                if (last) {
-                    if (a.dgate) IO::store(a.dgate, cur * a.D + part.at(i), IO::pack(sg[i]), live ? part.valid(a, i) : 0);
-                    static_for<E>([&](auto e) { sg[i][e] = 0.0f; });
-                }
+                B::store(wx, i, j, dr[i]);
             });
+            if (last) {
+                const __amdgpu_buffer_rsrc_t wg = B::row(a.dgate, cur * a.D, a.D, live);
+                static_for<V>([&](auto i) {
+                    B::store(wg, i, j, sg[i]);
+                    static_for<E>([&](auto e) { sg[i][e] = 0.0f; });
+                });
+            }
         }
         // as in the forward pass
         if (TPR > 64 && !(a.x && a.w_post)) __syncthreads();
     }
-    // The workgroup's sums: row groups one after the other through LDS.
-    auto total = [&](float (&s)[V][E], float* out) {
+    // The workgroup's sums: row groups one after the other through LDS, to the first.
+    auto total = [&](float (&s)[V][E]) {
         static_for<NR - 1>([&](auto n) {
             __syncthreads();
             if (part.ng == n + 1) static_for<V>([&](auto i) {
-                static_for<E>([&](auto e) { fold[(i * E + e) * TPR + part.j] = s[i][e]; });
+                static_for<E>([&](auto e) { fold[(i * E + e) * TPR + j] = s[i][e]; });
             });
             __syncthreads();
             if (part.ng == 0) static_for<V>([&](auto i) {
-                static_for<E>([&](auto e) { s[i][e] += fold[(i * E + e) * TPR + part.j]; });
+                static_for<E>([&](auto e) { s[i][e] += fold[(i * E + e) * TPR + j]; });
             });
         });
-        if (part.ng == 0) static_for<V>([&](auto i) {
-            store_f32<E>(out, (int64_t)blockIdx.x * a.D + part.at(i), part.valid(a, i), s[i]);
-        });
+    };
+    auto leave = [&](float (&s)[V][E], float* out) {
+        total(s);
+        const __amdgpu_buffer_rsrc_t w = B4::row(out, (int64_t)blockIdx.x * a.D, a.D, part.ng == 0);
+        static_for<V>([&](auto i) { B::store32(w, i, j, s[i]); });
     };
     const int64_t n = (int64_t)gridDim.x * a.D;
-    if (a.dw_pre) total(sb, a.partial);
-    if (a.dw_post) total(sa, a.partial + n);
-    if (a.dgate && a.parts) total(sg, a.partial + 2 * n);
+    if (a.dw_pre) leave(sb, a.partial);
+    if (a.dw_post) leave(sa, a.partial + n);
+    if (a.dgate && a.parts > 1) leave(sg, a.partial + 2 * n);
+    if (a.dgate && a.parts == 1) {
+        total(sg);
+        const __amdgpu_buffer_rsrc_t w = B::row(a.dgate, (int64_t)blockIdx.x * a.D, a.D, part.ng == 0);
+        static_for<V>([&](auto i) { B::store(w, i, j, sg[i]); });
+    }
 }
 
 typedef void (*NormFn)(NormArgs);
 struct Config {
     NormFn fn;
     int tpr, block, values;  // threads of a row, of a workgroup; values of a thread
+    int per_cu;              // workgroups of a compute unit
 };
 
 // Forward: a wave holds a row of up to 2048 (bf16) values; longer rows take a
 // workgroup.
-template <int ES>
+template <int ES, bool VEC>
 Config fwd_config(int64_t D) {
     constexpr int E = 16 / ES;
     const int64_t pieces = (D + E - 1) / E;
-    if (pieces <= 64) return {norm_fwd_kernel<ES, 64, 1, 256>, 64, 256, E};
-    if (pieces <= 128) return {norm_fwd_kernel<ES, 64, 2, 256>, 64, 256, 2 * E};
-    if (pieces <= 256) return {norm_fwd_kernel<ES, 64, 4, 256>, 64, 256, 4 * E};
-    if (pieces <= 512) return {norm_fwd_kernel<ES, 256, 2, 256>, 256, 256, 2 * E};
-    if (pieces <= 1024) return {norm_fwd_kernel<ES, 256, 4, 256>, 256, 256, 4 * E};
-    if (pieces <= 2048) return {norm_fwd_kernel<ES, 1024, 2, 1024>, 1024, 1024, 2 * E};
-    return {norm_fwd_kernel<ES, 1024, 4, 1024>, 1024, 1024, 4 * E};
+    if (pieces <= 64) return {norm_fwd_kernel<ES, VEC, 64, 1, 256>, 64, 256, E, 8};
+    if (pieces <= 128) return {norm_fwd_kernel<ES, VEC, 64, 2, 256>, 64, 256, 2 * E, 8};
+    if (pieces <= 256) return {norm_fwd_kernel<ES, VEC, 64, 4, 256>, 64, 256, 4 * E, 8};
+    if (pieces <= 512) return {norm_fwd_kernel<ES, VEC, 256, 2, 256>, 256, 256, 2 * E, 8};
+    if (pieces <= 1024) return {norm_fwd_kernel<ES, VEC, 256, 4, 256>, 256, 256, 4 * E, 8};
+    if (pieces <= 2048) return {norm_fwd_kernel<ES, VEC, 1024, 2, 1024>, 1024, 1024, 2 * E, 2};
+    return {norm_fwd_kernel<ES, VEC, 1024, 4, 1024>, 1024, 1024, 4 * E, 2};
 }
 
-// Backward: eight values per thread (the sums and weights take six registers a
-// value), sixteen for the longest rows.
-template <int ES>
+// Backward: the sums, weights and values of a row take some 14 registers a value.
+// bf16 rows in whole pieces of eight: sixteen values to a thread, so that a wave holds
+// a row of 1024 and the sums over longer rows meet fewer waves; two waves to a
+// SIMD.  fp32, and rows moved value by value: four values and four waves.  The
+// longest rows: no registers for the weights and the next row.
+template <int ES, bool VEC>
 Config bwd_config(int64_t D) {
-    constexpr int V = ES == 2 ? 1 : 2;
-    if (D <= 512) return {norm_bwd_kernel<ES, 64, V, 512>, 64, 512, 8};
-    if (D <= 1024) return {norm_bwd_kernel<ES, 128, V, 512>, 128, 512, 8};
-    if (D <= 2048) return {norm_bwd_kernel<ES, 256, V, 512>, 256, 512, 8};
-    if (D <= 4096) return {norm_bwd_kernel<ES, 512, V, 512>, 512, 512, 8};
-    if (D <= 8192) return {norm_bwd_kernel<ES, 1024, V, 1024>, 1024, 1024, 8};
-    return {norm_bwd_kernel<ES, 1024, 2 * V, 1024>, 1024, 1024, 16};
+    if constexpr (ES == 2 && VEC) {
+        if (D <= 512) return {norm_bwd_kernel<ES, VEC, 64, 8, 1, 256, 4, true>, 64, 256, 8, 4};
+        if (D <= 1024) return {norm_bwd_kernel<ES, VEC, 64, 8, 2, 256, 2, true>, 64, 256, 16, 2};
+        if (D <= 2048) return {norm_bwd_kernel<ES, VEC, 128, 8, 2, 256, 2, true>, 128, 256, 16, 2};
+        if (D <= 4096) return {norm_bwd_kernel<ES, VEC, 256, 8, 2, 256, 2, true>, 256, 256, 16, 2};
+        if (D <= 8192) return {norm_bwd_kernel<ES, VEC, 512, 8, 2, 512, 2, true>, 512, 512, 16, 1};
+        return {norm_bwd_kernel<ES, VEC, 1024, 8, 2, 1024, 4, false>, 1024, 1024, 16, 1};
+    } else {
+        if (D <= 256) return {norm_bwd_kernel<ES, VEC, 64, 4, 1, 256, 4, true>, 64, 256, 4, 4};
+        if (D <= 512) return {norm_bwd_kernel<ES, VEC, 128, 4, 1, 256, 4, true>, 128, 256, 4, 4};
+        if (D <= 1024) return {norm_bwd_kernel<ES, VEC, 256, 4, 1, 256, 4, true>, 256, 256, 4, 4};
+        if (D <= 2048) return {norm_bwd_kernel<ES, VEC, 512, 4, 1, 512, 4, true>, 512, 512, 4, 2};
+        if (D <= 4096) return {norm_bwd_kernel<ES, VEC, 1024, 4, 1, 1024, 4, true>, 1024, 1024, 4, 1};
+        if (D <= 8192) return {norm_bwd_kernel<ES, VEC, 1024, 4, 2, 1024, 4, false>, 1024, 1024, 8, 1};
+        return {norm_bwd_kernel<ES, VEC, 1024, 4, 4, 1024, 4, false>, 1024, 1024, 16, 1};
+    }
+}
+
+// Whole pieces in every row, on 4 bytes.
+bool pieces(const NormArgs& a) {
+    const int64_t E = a.type == kF32 ? 4 : 8, es = a.type == kF32 ? 4 : 2;
+    auto ok = [&](const void* p, int64_t ld) { return !p || (ld * es % 4 == 0 && (uintptr_t)p % 4 == 0); };
+    return a.D % E == 0 && ok(a.x, a.ld_x) && ok(a.r, a.ld_r) && ok(a.gate, a.D) && ok(a.r_out, a.ld_ro) && ok(a.y, a.ld_y) &&
+           ok(a.dy, a.ld_dy) && ok(a.dr_out, a.ld_dro) && ok(a.dx, a.ld_dx) && ok(a.dr, a.ld_dr) && ok(a.dgate, a.D);
+}
+
+Config config(const NormArgs& a, bool backward) {
+    if (a.type == kBF16) {
+        if (pieces(a)) return backward ? bwd_config<2, true>(a.D) : fwd_config<2, true>(a.D);
+        return backward ? bwd_config<2, false>(a.D) : fwd_config<2, false>(a.D);
+    }
+    if (pieces(a)) return backward ? bwd_config<4, true>(a.D) : fwd_config<4, true>(a.D);
+    return backward ? bwd_config<4, false>(a.D) : fwd_config<4, false>(a.D);
 }
 
 }  // namespace
 
-// Workgroups of the backward pass: two per compute unit of 512 threads (one of
-// 1024) as far as the rows go.
-void norm_bwd_grid(int64_t rows, int64_t D, int64_t gates, int type, int cus, int64_t* grid, int* parts) {
-    const Config c = type == kBF16 ? bwd_config<2>(D) : bwd_config<4>(D);
-    const int64_t nr = c.block / c.tpr, most = (c.block == 1024 ? 1 : 2) * (int64_t)cus;
-    if (gates >= most * nr) {
+// Workgroups of the backward pass: those the device holds at once, as far as the
+// rows go.  Gate rows of fewer than eight rows are owned by row
+// groups (a workgroup to each would leave more partial sums than it reads).
+void norm_bwd_grid(const NormArgs& a, int cus, int64_t* grid, int* parts) {
+    const Config c = config(a, true);
+    const int64_t nr = c.block / c.tpr, most = (int64_t)c.per_cu * cus, gates = a.gates, rpg = a.rows / gates;
+    if (rpg < 8 && gates > 1) {
+        const int64_t need = (gates + nr - 1) / nr;
         *parts = 0;
-        *grid = most;
+        *grid = need < most ? need : most;
         return;
     }
-    const int64_t rpg = rows / gates, fill = (rpg + nr - 1) / nr;
+    const int64_t fill = (rpg + nr - 1) / nr;
     int64_t p = most / gates;
     if (p > fill) p = fill;
     if (p < 1) p = 1;
@@ -315,15 +384,25 @@ void norm_bwd_grid(int64_t rows, int64_t D, int64_t gates, int type, int cus, in
     *grid = p * gates;
 }
 
+int64_t norm_bwd_most(const NormArgs& a, int cus) {
+    NormArgs b = a;
+    int64_t grid, most;
+    int parts;
+    norm_bwd_grid(b, cus, &most, &parts);
+    b.r = reinterpret_cast<const void*>(2);  // (an address off 4 bytes)
+    norm_bwd_grid(b, cus, &grid, &parts);
+    return grid > most ? grid : most;
+}
+
 hipError_t launch_norm_forward(const NormArgs& a, int cus, hipStream_t s) {
-    const Config c = a.type == kBF16 ? fwd_config<2>(a.D) : fwd_config<4>(a.D);
-    const int64_t nr = c.block / c.tpr, need = (a.rows + nr - 1) / nr, most = (int64_t)cus * (c.block == 1024 ? 2 : 8);
+    const Config c = config(a, false);
+    const int64_t nr = c.block / c.tpr, need = (a.rows + nr - 1) / nr, most = (int64_t)cus * c.per_cu;
     hipLaunchKernelGGL(c.fn, dim3((unsigned)(need < most ? need : most)), dim3(c.block), 0, s, a);
     return hipGetLastError();
 }
 
 hipError_t launch_norm_backward(const NormArgs& a, int64_t grid, hipStream_t s) {
-    const Config c = a.type == kBF16 ? bwd_config<2>(a.D) : bwd_config<4>(a.D);
+    const Config c = config(a, true);
     hipError_t e = hipSuccess;
     if (grid > 0) {
         const size_t lds = (size_t)c.tpr * c.values * sizeof(float);
@@ -331,12 +410,17 @@ hipError_t launch_norm_backward(const NormArgs& a, int64_t grid, hipStream_t s) 
         hipLaunchKernelGGL(c.fn, dim3((unsigned)grid), dim3(c.block), lds, s, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
+    if (a.rows == 0 && a.dgate) {
+        ColSum z[1] = {{a.partial, a.dgate, 0, a.gates * a.D, 1, a.type}};
+        if ((e = launch_colsum(z, 1, s)) != hipSuccess) return e;
+    }
     const int64_t n = grid * a.D;
-    if (a.dw_pre && (e = launch_colsum(a.partial, grid, a.D, 1, kF32, a.dw_pre, s)) != hipSuccess) return e;
-    if (a.dw_post && (e = launch_colsum(a.partial + n, grid, a.D, 1, kF32, a.dw_post, s)) != hipSuccess) return e;
-    if (a.dgate && a.rows == 0) return launch_colsum(a.partial, 0, a.gates * a.D, 1, a.type, a.dgate, s);
-    if (a.dgate && a.parts) e = launch_colsum(a.partial + 2 * n, a.parts, a.D, a.gates, a.type, a.dgate, s);
-    return e;
+    ColSum sums[3];
+    int count = 0;
+    if (a.dw_pre) sums[count++] = ColSum{a.partial, a.dw_pre, grid, a.D, 1, kF32};
+    if (a.dw_post) sums[count++] = ColSum{a.partial + n, a.dw_post, grid, a.D, 1, kF32};
+    if (a.dgate && a.parts > 1) sums[count++] = ColSum{a.partial + 2 * n, a.dgate, a.parts, a.D, a.gates, a.type};
+    return launch_colsum(sums, count, s);
 }
 
 }  // namespace isam
