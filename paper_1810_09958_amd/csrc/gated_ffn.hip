@@ -141,7 +141,10 @@ hipError_t launch_gated_tiles(const GatedArgs& a, int tile, bool backward, hipSt
     if (tm * tn > INT32_MAX || a.K <= 0) return hipErrorInvalidValue;
     const bool k_full = a.K % 64 == 0;
     const GatedFn fn = backward ? tile_fn<true>(tile, k_full) : tile_fn<false>(tile, k_full);
-    hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(tile == kGated256 ? 512 : 256), 0, s, a, tile_map(tm, tn));
+    GatedArgs p = a;
+    auto on4 = [](const void* q, int64_t ld) { return (uintptr_t)q % 4 == 0 && ld % 2 == 0; };
+    p.whole = a.F % 8 == 0 && on4(a.out, a.ld_out) && (!backward || on4(a.dout, a.ld_dout));
+    hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(tile == kGated256 ? 512 : 256), 0, s, p, tile_map(tm, tn));
     return hipGetLastError();
 }
 

@@ -60,36 +60,64 @@ struct GatedCopier : DmaCopier<BM, BN, true, NW> {
     }
 };
 
+// Eight bf16 values from `off` bytes of a matrix, of which `valid` exist.  WHOLE: all
+// or none, on 4 bytes.  What does not exist loads as zeros and is not stored; no load
+// or store stands in a branch of lanes (beside nearly all registers in use, the
+// compiler has copied a register inside such a branch, for its lanes only).
+template <bool WHOLE>
+__device__ __forceinline__ uint4 gated_load8(__amdgpu_buffer_rsrc_t rs, uint32_t off, int valid) {
+    if constexpr (WHOLE) return buf_load16(rs, valid > 0 ? off : kOob);
+    uint32_t h[8];
+    static_for<8>([&](auto e) { h[e] = buf_load2(rs, e < valid ? off + 2 * e : kOob) & 0xffffu; });
+    return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+}
+template <bool WHOLE>
+__device__ __forceinline__ void gated_store8(__amdgpu_buffer_rsrc_t rs, uint32_t off, int valid, uint4 v) {
+    if constexpr (WHOLE) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4_t, v), rs, (int)(valid > 0 ? off : kOob), 0, 0);
+    } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        static_for<8>([&](auto e) {
+            __builtin_amdgcn_raw_buffer_store_b16((short)(w[e / 2] >> (16 * (e & 1))), rs, (int)(e < valid ? off + 2 * e : kOob), 0, 0);
+        });
+    }
+}
+__device__ __forceinline__ uint32_t gated_bytes(int64_t rows, int64_t cols, int64_t ld) { return (uint32_t)(((rows - 1) * ld + cols) * 2); }
+
 // Epilogue of a tile of BM rows and HB = BN / 2 values of f.  `smem` is idle.
-template <int ACT, bool BWD, int BM, int HB, int WM, int WTM, int MI, int NT>
+template <int ACT, bool BWD, bool WHOLE, int BM, int HB, int WM, int WTM, int MI, int NT>
 __device__ __forceinline__ void gated_epilogue(const GatedArgs& a, f32x16_t (&acc)[MI][2], char* smem, int64_t m0, int64_t f0,
                                                int tm, int wm, int wn, bool active, int tid, int lane) {
-    using IO = Row16<2>;
+    // Both indexes go through an empty asm, so that what is computed from them is not
+    // held in registers across the main loop or shared by the instances.
+    asm volatile("" : "+v"(lane), "+v"(tid));
     constexpr int LD = HB * 2 + 16, TILE = BM * LD, PIECES = HB / 8, RPI = NT / PIECES;
     static_assert(NT % PIECES == 0 && BM % RPI == 0, "whole rows per pass");
-    const int piece = tid % PIECES, row0 = tid / PIECES;
+    const int piece = tid % PIECES, row0 = tid / PIECES, rows = (int)min((int64_t)BM, a.M - m0);
     const int valid = (int)max((int64_t)0, min((int64_t)8, a.F - (f0 + piece * 8)));
     if constexpr (BWD) {
         // dp takes the place that dG will have
-        for (int r = row0; r < BM; r += 4 * RPI) {
-            uint4 v[4];
-            static_for<4>([&](auto i) {
-                const int64_t m = m0 + r + i * RPI;
-                v[i] = IO::load(a.dout, m * a.ld_dout + f0 + piece * 8, r + i * RPI < BM && m < a.M ? valid : 0);
+        const __amdgpu_buffer_rsrc_t rp = make_rsrc(a.dout, gated_bytes(a.M, a.F, a.ld_dout));
+        const uint32_t at = (uint32_t)((m0 * a.ld_dout + f0 + piece * 8) * 2), step = (uint32_t)(a.ld_dout * 2);
+        constexpr int U = WHOLE && BM / RPI >= 4 ? 4 : 1;
+#pragma unroll 1
+        for (int r = row0; r < BM; r += U * RPI) {
+            uint4 v[U];
+            static_for<U>([&](auto i) {
+                const int rr = r + i * RPI;
+                v[i] = gated_load8<WHOLE>(rp, at + (uint32_t)rr * step, rr < rows ? valid : 0);
             });
-            static_for<4>([&](auto i) {
-                if (r + i * RPI < BM) *reinterpret_cast<uint4*>(smem + (r + i * RPI) * LD + piece * 16) = v[i];
-            });
+            static_for<U>([&](auto i) { *reinterpret_cast<uint4*>(smem + (r + i * RPI) * LD + piece * 16) = v[i]; });
         }
         __syncthreads();
     }
     if (active) {
         const int64_t f = f0 + wn * 32 + (lane & 31);
-        float bg = 0.0f, bu = 0.0f, sg = 0.0f, su = 0.0f;
-        if (a.bias && f < a.F) {
-            bg = a.bias[f];
-            bu = a.bias[a.F + f];
-        }
+        const bool in = f < a.F;
+        const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.bias, a.bias ? (uint32_t)(a.F * 8) : 0u);
+        const float bg = __uint_as_float(buf_load4(rb, in ? (uint32_t)(f * 4) : kOob));
+        const float bu = __uint_as_float(buf_load4(rb, in ? (uint32_t)((a.F + f) * 4) : kOob));
+        float sg = 0.0f, su = 0.0f;
         static_for<MI>([&](auto i) {
             static_for<16>([&](auto v) {
                 const int r = wm * WTM + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
@@ -102,12 +130,16 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& a, f32x16_t (&ac
                     const uint32_t w = pack_bf16_rne(dg, du);
                     at[0] = (uint16_t)w;
                     at[TILE / 2] = (uint16_t)(w >> 16);
-                    if (m0 + r < a.M) {
-                        sg += dg;
-                        su += du;
-                    }
+                    sg += r < rows ? dg : 0.0f;
+                    su += r < rows ? du : 0.0f;
                 } else {
                     *at = (uint16_t)pack_bf16_rne(s * u, 0.0f);
+                }
+                // Four values at a time: the compiler would hold all of dG and dU in registers
+                // and sum them where the sums are used.
+                if constexpr (BWD && (v & 3) == 3) {
+                    asm volatile("" : "+v"(sg), "+v"(su));
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             });
         });
@@ -115,30 +147,36 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& a, f32x16_t (&ac
             // the two lane halves hold the other rows of the same f; one partial row per wave row
             sg += __shfl_xor(sg, 32);
             su += __shfl_xor(su, 32);
-            if (lane < 32 && f < a.F) {
-                float* const out = a.bias_part + ((int64_t)tm * WM + wm) * 2 * a.F + f;
-                out[0] = sg;
-                out[a.F] = su;
-            }
+            const __amdgpu_buffer_rsrc_t ro = make_rsrc(a.bias_part + ((int64_t)tm * WM + wm) * 2 * a.F, (uint32_t)(a.F * 8));
+            const bool on = in && lane < 32;
+            __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(sg), ro, (int)(on ? (uint32_t)(f * 4) : kOob), 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(su), ro, (int)(on ? (uint32_t)((a.F + f) * 4) : kOob), 0, 0);
         }
     }
     __syncthreads();
+    const int64_t cols = BWD ? 2 * a.F : a.F;
+    const __amdgpu_buffer_rsrc_t ro = make_rsrc(a.out, gated_bytes(a.M, cols, a.ld_out));
+    const uint32_t at = (uint32_t)((m0 * a.ld_out + f0 + piece * 8) * 2), step = (uint32_t)(a.ld_out * 2), half = (uint32_t)(a.F * 2);
 #pragma unroll 2
     for (int r = row0; r < BM; r += RPI) {
-        const int64_t m = m0 + r;
         const char* const src = smem + r * LD + piece * 16;
-        const int n = m < a.M ? valid : 0;
-        IO::store(a.out, m * a.ld_out + f0 + piece * 8, *reinterpret_cast<const uint4*>(src), n);
-        if constexpr (BWD) IO::store(a.out, m * a.ld_out + a.F + f0 + piece * 8, *reinterpret_cast<const uint4*>(src + TILE), n);
+        const int n = r < rows ? valid : 0;
+        gated_store8<WHOLE>(ro, at + (uint32_t)r * step, n, *reinterpret_cast<const uint4*>(src));
+        if constexpr (BWD) gated_store8<WHOLE>(ro, at + (uint32_t)r * step + half, n, *reinterpret_cast<const uint4*>(src + TILE));
     }
 }
 
 template <bool BWD, int BM, int HB, int WM, int WTM, int MI, int NT>
 __device__ __forceinline__ void gated_finish(const GatedArgs& a, f32x16_t (&acc)[MI][2], char* smem, int64_t m0, int64_t f0, int tm,
                                              int wm, int wn, bool active, int tid, int lane) {
-    if (a.act == 0) gated_epilogue<0, BWD, BM, HB, WM, WTM, MI, NT>(a, acc, smem, m0, f0, tm, wm, wn, active, tid, lane);
-    else if (a.act == 1) gated_epilogue<1, BWD, BM, HB, WM, WTM, MI, NT>(a, acc, smem, m0, f0, tm, wm, wn, active, tid, lane);
-    else gated_epilogue<2, BWD, BM, HB, WM, WTM, MI, NT>(a, acc, smem, m0, f0, tm, wm, wn, active, tid, lane);
+    auto act = [&](auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        if (a.act == 0) gated_epilogue<0, BWD, W, BM, HB, WM, WTM, MI, NT>(a, acc, smem, m0, f0, tm, wm, wn, active, tid, lane);
+        else if (a.act == 1) gated_epilogue<1, BWD, W, BM, HB, WM, WTM, MI, NT>(a, acc, smem, m0, f0, tm, wm, wn, active, tid, lane);
+        else gated_epilogue<2, BWD, W, BM, HB, WM, WTM, MI, NT>(a, acc, smem, m0, f0, tm, wm, wn, active, tid, lane);
+    };
+    if (a.whole) act(std::true_type{});
+    else act(std::false_type{});
 }
 
 __device__ __forceinline__ GemmArgs gated_gemm(const GatedArgs& a) {

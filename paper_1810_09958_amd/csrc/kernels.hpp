@@ -325,6 +325,7 @@ struct GatedArgs {
     const void* dout;         // backward: dp [M][F]
     int64_t ld_dout;
     float* bias_part;         // backward: partial sums [rows][2F], or null
+    int whole;                // rows of out and dout on 4 bytes, F a multiple of 8 (set by the launch)
     float* gu;                // element-wise step: G and U, [M][2F]
 };
 int gated_tile(int64_t M, int64_t F, int cus);

@@ -22,17 +22,18 @@
 //     those between.  Workgroups draw their tiles from a counter in time order, so
 //     those a tile waits for are always held by running workgroups: the chain needs
 //     no co-residency.  A tile's published state is its composition applied to the state
-//     before it wherever that came from, so results repeat bit for bit.  Each
-//     published number is one 8-byte word with a mark beside it, written and read
-//     with device scope, so no ordering between words is needed; the words and the
-//     counter are cleared by a kernel before (a captured launch replays);
+//     before it wherever that came from, so results repeat bit for bit.  A word of
+//     the chain is valid once it differs from the pattern a kernel before fills it
+//     with (a captured launch replays), and is written and read with device scope, so
+//     no ordering between words is needed;
 //   * the backward pass keeps no sequence of states: the forward pass leaves the
 //     state before every 128 steps, and each tile forms its states again in
 //     registers while it scans e from its end (5 values moved per element, 6 with
 //     stored states, which would have to be fp32 to give fp32 gradients).
 // A reset must cut off whatever stands before it, NaN included, which 0 * NaN
-// does not: its a is -0, and a sign bit in A (kept through products) makes a
-// composition drop the left side.
+// does not.  Within a group's steps the state before it is replaced by 0; in a
+// composition its A is -0, and a sign bit in A (kept through products) makes it drop
+// the left side.
 #include <type_traits>
 
 #include "kernels.hpp"
@@ -42,7 +43,8 @@ namespace isam {
 
 namespace {
 
-constexpr int kCols = 64;  // channels of a tile
+constexpr int kCols = 64;        // channels of a tile
+constexpr int kChainWindow = 4;  // tiles that one look back along the chain sees
 
 __device__ __forceinline__ bool drops(float a) { return (int)__float_as_uint(a) < 0; }
 
@@ -58,6 +60,17 @@ __device__ __forceinline__ float apply(float a, float b, float v) {
     const float r = __builtin_fmaf(a, v, b);
     if constexpr (RESET) return drops(a) ? b : r;
     return r;
+}
+
+// (A, B) of a group's steps so far, then one more: z (positive, so a sign of A stays).
+__device__ __forceinline__ void step(bool drop, bool first, float z, float b, float& A, float& B) {
+    if (first) {
+        A = drop ? -0.0f : z;
+        B = b;
+    } else {
+        A = drop ? -0.0f : A * z;
+        B = __builtin_fmaf(z, drop ? 0.0f : B, b);
+    }
 }
 
 // The four channels of a lane.  VEC (hidden a multiple of 4, rows on 4 bytes): one
@@ -164,12 +177,17 @@ __device__ __forceinline__ void gate_pair(float w, float& z, float& omz) {
     z = __builtin_amdgcn_rcpf(1.0f + e);
     omz = e * z;
 }
-// tanh(v), absolute error of a few 2^-24.
+// tanh(v) from w = 2 v log2(e), absolute error of a few 2^-24.
 template <int ES>
-__device__ __forceinline__ float gate_tanh(float v) {
-    if constexpr (ES == 4) return tanh_f32(v);
-    return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * (2.0f * kLog2e))), 1.0f);
+__device__ __forceinline__ float gate_tanh(float w) {
+    if constexpr (ES == 4) {
+        const float t = __builtin_amdgcn_exp2f(-__builtin_fabsf(w));
+        return __builtin_copysignf((1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), w);
+    }
+    return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w)), 1.0f);
 }
+// Factor of the candidate's argument.
+__device__ __forceinline__ float candidate_scale(const LinGruArgs& a) { return a.candidate ? 2.0f * kLog2e : 1.0f; }
 
 // Inclusive scan over the wave's four groups in time order (UP) or against it.
 template <bool RESET, bool UP>
@@ -186,53 +204,57 @@ __device__ __forceinline__ void wave_scan(float (&A)[4], float (&B)[4], int lane
     });
 }
 
-// The chain of tiles.  Tile `id` has three words for each of its channels: state
-// after it, A and B; the upper half of a word that has been written is 1.
-__device__ __forceinline__ uint64_t* chain_word(const LinGruArgs& a, int64_t id, int field, int ch) {
-    return a.chain + 8 + (id * 3 + field) * kCols + ch;
+// The chain of tiles: a counter, then for each tile 64 pairs (A, B) of 8 bytes and 64
+// states after it, every bit set until they are published.  A published NaN is the
+// canonical one, so no published word is all ones.
+__device__ __forceinline__ uint64_t* chain_pair(const LinGruArgs& a, int64_t id, int ch) {
+    return a.chain + 8 + id * (kCols + kCols / 2) + ch;
 }
-__device__ __forceinline__ void chain_put(uint64_t* w, float v) {
-    __hip_atomic_store(w, (1ull << 32) | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ uint32_t* chain_state(const LinGruArgs& a, int64_t id, int ch) {
+    return reinterpret_cast<uint32_t*>(a.chain + 8 + id * (kCols + kCols / 2) + kCols) + ch;
 }
-__device__ __forceinline__ uint64_t chain_get(const uint64_t* w) {
-    return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ uint32_t chain_bits(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
+__device__ __forceinline__ void chain_put(const LinGruArgs& a, int64_t id, int ch, float ta, float tb) {
+    __hip_atomic_store(chain_pair(a, id, ch), (uint64_t)chain_bits(ta) | (uint64_t)chain_bits(tb) << 32, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void chain_put(const LinGruArgs& a, int64_t id, int ch, float v) {
+    __hip_atomic_store(chain_state(a, id, ch), chain_bits(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 // State that reaches the tile `id`, `before` tiles into its column (lane: channel;
 // whole wave).  `first`: the state before the column's first tile.  NaN if a word
 // should not arrive within 2 s (it is written by a running workgroup).
 template <bool RESET>
 __device__ __forceinline__ float chain_in(const LinGruArgs& a, int64_t id, int64_t before, int64_t cols, int lane, float first) {
-    constexpr int W = 4;  // tiles looked at together
+    constexpr int W = kChainWindow;  // tiles looked at together
     const uint64_t t0 = wall_clock64();
     for (;;) {
-        uint64_t s[W], ca[W], cb[W];
+        uint64_t ab[W];
+        uint32_t st[W];
         static_for<W>([&](auto i) {
             const int64_t p = id - (i + 1) * cols;
-            s[i] = i == before ? (1ull << 32) | __float_as_uint(first) : 0;
-            ca[i] = cb[i] = 0;
+            st[i] = i == before ? chain_bits(first) : ~0u;
+            ab[i] = ~0ull;
             if (i < before) {
-                s[i] = chain_get(chain_word(a, p, 0, lane));
-                ca[i] = chain_get(chain_word(a, p, 1, lane));
-                cb[i] = chain_get(chain_word(a, p, 2, lane));
+                st[i] = __hip_atomic_load(chain_state(a, p, lane), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                ab[i] = __hip_atomic_load(chain_pair(a, p, lane), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
         });
         int at = -1;
         bool open = true;
         static_for<W>([&](auto i) {
-            if (open && __all((int)(s[i] >> 32))) {
+            if (open && __all(st[i] != ~0u)) {
                 at = i;
                 open = false;
             }
-            open = open && __all((int)(ca[i] >> 32) & (int)(cb[i] >> 32));
+            open = open && __all(ab[i] != ~0ull);
         });
         if (at >= 0) {
             float v = 0.0f;
-            static_for<W>([&](auto i) {
-                if (i == at) v = __uint_as_float((uint32_t)s[i]);
-            });
-            static_for<W - 1>([&](auto j) {
-                constexpr int i = W - 2 - decltype(j)::value;
-                if (i < at) v = apply<RESET>(__uint_as_float((uint32_t)ca[i]), __uint_as_float((uint32_t)cb[i]), v);
+            static_for<W>([&](auto j) {
+                constexpr int i = W - 1 - decltype(j)::value;
+                if (i == at) v = __uint_as_float(st[i]);
+                if (i < at) v = apply<RESET>(__uint_as_float((uint32_t)ab[i]), __uint_as_float((uint32_t)(ab[i] >> 32)), v);
             });
             return v;
         }
@@ -317,23 +339,26 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(Li
     float bz[4], bn[4];
     load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
     load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
-    static_for<4>([&](auto e) { bz[e] *= -kLog2e; });
+    const float scale = candidate_scale(a);
+    static_for<4>([&](auto e) {
+        bz[e] *= -kLog2e;
+        bn[e] *= scale;
+    });
 
     float ca[R][4], cb[R][4], A[4], B[4];
     static_for<R>([&](auto r) {
+        const bool drop = RESET && (reset >> r & 1);
         float gz[4], n[4];
         static_for<S::W>([&](auto w) { pz[r][w] = q * R + r < left ? pz[r][w] : S::kKeep; });
         S::unpack(pz[r], gz);
         S::unpack(pn[r], n);
-        static_for<4>([&](auto e) { n[e] += bn[e]; });
+        static_for<4>([&](auto e) { n[e] = __builtin_fmaf(n[e], scale, bn[e]); });
         if (a.candidate) static_for<4>([&](auto e) { n[e] = gate_tanh<ES>(n[e]); });
         static_for<4>([&](auto e) {
-            float z, omz;
-            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z, omz);
-            ca[r][e] = RESET && (reset >> r & 1) ? -0.0f : z;
+            float omz;
+            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), ca[r][e], omz);
             cb[r][e] = omz * n[e];
-            A[e] = r == 0 ? ca[r][e] : compose_a<RESET>(A[e], ca[r][e]);
-            B[e] = r == 0 ? cb[r][e] : apply<RESET>(ca[r][e], cb[r][e], B[e]);
+            step(drop, r == 0, ca[r][e], cb[r][e], A[e], B[e]);
         });
     });
     wave_scan<RESET, true>(A, B, lane);
@@ -356,12 +381,9 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(Li
                 tb = apply<RESET>(wa[w + 1], wb[w + 1], tb);
                 ta = compose_a<RESET>(ta, wa[w + 1]);
             });
-            if (!last) {
-                chain_put(chain_word(a, tile.id, 1, lane), ta);
-                chain_put(chain_word(a, tile.id, 2, lane), tb);
-            }
+            if (!last) chain_put(a, tile.id, lane, ta, tb);
             h = chain_in<RESET>(a, tile.id, tile.k, tile.cols, lane, first);
-            if (!last) chain_put(chain_word(a, tile.id, 0, lane), apply<RESET>(ta, tb, h));
+            if (!last) chain_put(a, tile.id, lane, apply<RESET>(ta, tb, h));
         }
         static_for<NW>([&](auto w) {
             start[w][lane] = h;
@@ -379,7 +401,8 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(Li
         store_channels<VEC>(a.states, (tw / kLinGruChunk * a.batch + b) * a.H, a.H, c0, lane, q == 0, v);
     const S hs(a.h_seq, b * a.h_b + tw * a.h_t, a.h_t, a.H, c0, lane);
     static_for<R>([&](auto r) {
-        static_for<4>([&](auto e) { v[e] = apply<RESET>(ca[r][e], cb[r][e], v[e]); });
+        const bool drop = RESET && (reset >> r & 1);
+        static_for<4>([&](auto e) { v[e] = __builtin_fmaf(ca[r][e], drop ? 0.0f : v[e], cb[r][e]); });
         hs.store(v, r, q * R + r < left, 0);
     });
     // (steps past the end leave the state as it is)
@@ -406,11 +429,12 @@ __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
         }
     });
     if (a.states && T > 0) a.states[i] = h;
+    const float scale = candidate_scale(a);
     static_for<kFewSteps>([&](auto t) {
         if (t < T) {
             float z, omz;
             gate_pair(__builtin_fmaf(gz[t], -kLog2e, bz * -kLog2e), z, omz);
-            const float v = gn[t] + bn, n = a.candidate ? gate_tanh<ES>(v) : v;
+            const float v = __builtin_fmaf(gn[t], scale, bn * scale), n = a.candidate ? gate_tanh<ES>(v) : v;
             h = drop[t] ? omz * n : __builtin_fmaf(z, h, omz * n);
             if (a.h_seq) Row16<ES>::put(a.h_seq, b * a.h_b + t * a.h_t + c, h);
         }
@@ -447,22 +471,25 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
     float bz[4], bn[4];
     load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
     load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
-    static_for<4>([&](auto e) { bz[e] *= -kLog2e; });
+    const float scale = candidate_scale(a);
+    static_for<4>([&](auto e) {
+        bz[e] *= -kLog2e;
+        bn[e] *= scale;
+    });
 
     // z, 1 - z and n of each step; (A, B) composes the state, (Z, C) e
     float z[R][4], omz[R][4], n[R][4], A[4], B[4], Z[4], C[4];
     static_for<R>([&](auto r) {
+        const bool drop = RESET && (reset >> r & 1);
         float gz[4];
         static_for<S::W>([&](auto w) { pz[r][w] = q * R + r < left ? pz[r][w] : S::kKeep; });
         S::unpack(pz[r], gz);
         S::unpack(pn[r], n[r]);
-        static_for<4>([&](auto e) { n[r][e] += bn[e]; });
+        static_for<4>([&](auto e) { n[r][e] = __builtin_fmaf(n[r][e], scale, bn[e]); });
         if (a.candidate) static_for<4>([&](auto e) { n[r][e] = gate_tanh<ES>(n[r][e]); });
         static_for<4>([&](auto e) {
             gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z[r][e], omz[r][e]);
-            const float s = RESET && (reset >> r & 1) ? -0.0f : z[r][e], w = omz[r][e] * n[r][e];
-            A[e] = r == 0 ? s : compose_a<RESET>(A[e], s);
-            B[e] = r == 0 ? w : apply<RESET>(s, w, B[e]);
+            step(drop, r == 0, z[r][e], omz[r][e] * n[r][e], A[e], B[e]);
         });
     });
     static_for<R>([&](auto i) {
@@ -500,12 +527,9 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
                 tc = apply<RESET>(wa[w], wc[w], tc);
                 ta = compose_a<RESET>(ta, wa[w]);
             });
-            if (kt > 0) {
-                chain_put(chain_word(a, tile.id, 1, lane), ta);
-                chain_put(chain_word(a, tile.id, 2, lane), tc);
-            }
+            if (kt > 0) chain_put(a, tile.id, lane, ta, tc);
             g = chain_in<RESET>(a, tile.id, tile.k, tile.cols, lane, first);
-            if (kt > 0) chain_put(chain_word(a, tile.id, 0, lane), apply<RESET>(ta, tc, g));
+            if (kt > 0) chain_put(a, tile.id, lane, apply<RESET>(ta, tc, g));
         }
         static_for<NW>([&](auto i) {
             constexpr int w = NW - 1 - decltype(i)::value;
@@ -563,8 +587,12 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
     a.bias_part[(kt * a.batch + b) * 2 * a.H + wid * a.H + channel<VEC>(a.H, c0, lane >> 2, lane & 3)] = s;
 }
 
+// The chain before a launch: the counter's line of 64 bytes zero, every other bit set.
 __global__ __launch_bounds__(256) void lingru_clear_kernel(uint4* p, int64_t n) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = make_uint4(0, 0, 0, 0);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const uint32_t v = i < 4 ? 0u : ~0u;
+        p[i] = make_uint4(v, v, v, v);
+    }
 }
 // dst = src, or zeros.
 __global__ __launch_bounds__(256) void lingru_copy_kernel(const float* src, float* dst, int64_t n) {
@@ -625,10 +653,10 @@ int64_t lingru_tiles(int64_t T, bool backward) {
     return T <= 64 ? (T > 0 ? 1 : 0) : (T + ts - 1) / ts;
 }
 
-// The counter's line and three words for each tile and channel; nothing for single tiles.
+// The counter's line and 12 bytes for each tile and channel; nothing for single tiles.
 size_t lingru_chain_bytes(int64_t T, int64_t batch, int64_t H, bool backward) {
     const int64_t tiles = lingru_tiles(T, backward), cols = batch * ((H + kCols - 1) / kCols);
-    return tiles > 1 ? 64 + (size_t)(tiles * cols) * 3 * kCols * 8 : 0;
+    return tiles > 1 ? 64 + (size_t)(tiles * cols) * kCols * 12 : 0;
 }
 
 hipError_t launch_lingru_forward(const LinGruArgs& a, hipStream_t s) {
