@@ -241,13 +241,13 @@ def _code(table, name, what):
         raise ValueError(f"{what} must be one of {', '.join(sorted(table))}") from None
 
 
-def _want(t, name, shape, dtype=torch.float32, device=None):
+def _want(t, name, shape, dtype=torch.float32):
     """Checks a contiguous tensor argument (None passes)."""
     if t is None:
         return
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(shape)} tensor")
 
 
@@ -255,23 +255,28 @@ def _rows(t, name, shape, dtype):
     """Strides of the rows of a [T][batch][width] tensor with unit inner stride (None: zeros)."""
     if t is None:
         return 0, 0
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}")
-    if t.dim() == 3 and t.shape[2] > 1 and t.stride(2) != 1:
+    st = t.stride()
+    if len(st) == 3 and st[2] != 1 and shape[2] > 1:
         raise ValueError(f"{name} needs unit inner stride")
-    return t.stride(0), t.stride(1)
+    return st[0], st[1]
 
 
-def _same_device(dev, **ts):
-    for name, t in ts.items():
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name} must be on {dev}")
+def _on(first, *ts):
+    """Checks that every tensor given is on the first one's GPU."""
+    at = first.get_device()
+    if at < 0:
+        raise ValueError("tensors must be on the GPU")
+    for t in ts:
+        if t is not None and t.get_device() != at:
+            raise ValueError("tensors must be on one GPU")
 
 
-def _room(workspace, nbytes, dev):
-    return torch.empty(max(nbytes, 1), device=dev, dtype=torch.uint8) if workspace is None else workspace
+def _room(nbytes, dev):
+    return torch.empty(max(nbytes, 1), device=dev, dtype=torch.uint8)
 
 
 def _bytes(t):
@@ -312,11 +317,10 @@ def linear_gru(gx: torch.Tensor, *, bias=None, h0=None, reset=None, candidate="t
     reset [T][batch] bool (the step starts from a zero state).  states
     (``linear_gru_states_shape``, float32) receives what ``linear_gru_backward`` needs.
     Returns (h_seq in gx's dtype, h_T in float32)."""
-    _check_dev(gx, bias, h0, reset, h_seq, h_T, states, workspace)
+    _on(gx, bias, h0, reset, h_seq, h_T, states, workspace)
     T, B, H, dt, gs, rs = _linear_gru_args(gx, bias, reset)
     cand = _code(_CANDIDATES, candidate, "candidate")
     dev = gx.device
-    _same_device(dev, bias=bias, h0=h0, reset=reset, h_seq=h_seq, h_T=h_T, states=states, workspace=workspace)
     _want(h0, "h0", (B, H))
     _want(states, "states", linear_gru_states_shape(T, B, H))
     if h_seq is None and return_sequence:
@@ -326,7 +330,7 @@ def linear_gru(gx: torch.Tensor, *, bias=None, h0=None, reset=None, candidate="t
     _want(h_T, "h_T", (B, H))
     hs = _rows(h_seq, "h_seq", (T, B, H), gx.dtype)
     if workspace is None:
-        workspace = _room(None, linear_gru_workspace_size(T, B, H, dt), dev)
+        workspace = _room(linear_gru_workspace_size(T, B, H, dt), dev)
     rc = lib().isam_linear_gru(T, B, H, dt, cand, _ptr(gx), *gs, _ptr(bias), _ptr(h0), _ptr(reset), *rs, _ptr(h_seq), *hs,
                                _ptr(h_T), _ptr(states), _ptr(workspace), _bytes(workspace), _stream())
     _call(rc, "isam_linear_gru")
@@ -338,12 +342,10 @@ def linear_gru_backward(gx: torch.Tensor, dh_seq: torch.Tensor | None, *, states
     """Gradient of ``linear_gru``: gx, bias, reset, candidate and states as in (and from) the forward
     call, dh_seq [T][batch][H] in gx's dtype or None, dh_T [batch][H] float32 or None.  Returns
     (dgx in gx's dtype, dh0, dbias in float32; dbias is None without a bias unless given)."""
-    _check_dev(gx, dh_seq, states, bias, reset, dh_T, dgx, dh0, dbias, workspace)
+    _on(gx, dh_seq, states, bias, reset, dh_T, dgx, dh0, dbias, workspace)
     T, B, H, dt, gs, rs = _linear_gru_args(gx, bias, reset)
     cand = _code(_CANDIDATES, candidate, "candidate")
     dev = gx.device
-    _same_device(dev, dh_seq=dh_seq, states=states, bias=bias, reset=reset, dh_T=dh_T, dgx=dgx, dh0=dh0, dbias=dbias,
-                 workspace=workspace)
     _want(states, "states", linear_gru_states_shape(T, B, H))
     _want(dh_T, "dh_T", (B, H))
     ds = _rows(dh_seq, "dh_seq", (T, B, H), gx.dtype)
@@ -357,7 +359,7 @@ def linear_gru_backward(gx: torch.Tensor, dh_seq: torch.Tensor | None, *, states
     _want(dbias, "dbias", (2 * H,))
     dgs = _rows(dgx, "dgx", (T, B, 2 * H), gx.dtype)
     if workspace is None:
-        workspace = _room(None, linear_gru_backward_workspace_size(T, B, H, dt), dev)
+        workspace = _room(linear_gru_backward_workspace_size(T, B, H, dt), dev)
     rc = lib().isam_linear_gru_backward(T, B, H, dt, cand, _ptr(gx), *gs, _ptr(bias), _ptr(reset), *rs, _ptr(states),
                                         _ptr(dh_seq), *ds, _ptr(dh_T), _ptr(dgx), *dgs, _ptr(dh0), _ptr(dbias),
                                         _ptr(workspace), _bytes(workspace), _stream())
@@ -372,13 +374,14 @@ def _matrix(t, name, shape, dtype):
     """Leading dimension of a [rows][D] tensor with unit inner stride (None: 0)."""
     if t is None:
         return 0
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    ld, inner = t.stride()
+    if inner != 1 and shape[1] > 1:
         raise ValueError(f"{name} needs unit inner stride")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return ld if shape[0] > 1 else shape[1]
 
 
 def _norm_args(r, gate, w_post, w_pre):
@@ -405,10 +408,9 @@ def norm_residual(x: torch.Tensor | None, r: torch.Tensor, *, w_pre, w_post=None
     x, r [rows][D] (float32 or bfloat16; row strides may exceed D), gate [gates][D] in their
     dtype with gates a divisor of rows, w_post and w_pre [D] float32.  r_out may be r.
     x None: y = norm of r alone.  Returns (r_out, y); r_out is r without x."""
-    _check_dev(x, r, w_pre, w_post, gate, r_out, y)
+    _on(r, x, w_pre, w_post, gate, r_out, y)
     R, D, G = _norm_args(r, gate, w_post, w_pre)
     dt, dev = _dt(r), r.device
-    _same_device(dev, x=x, w_pre=w_pre, w_post=w_post, gate=gate, r_out=r_out, y=y)
     if r_out is None and x is not None:
         r_out = torch.empty((R, D), device=dev, dtype=r.dtype)
     if y is None:
@@ -428,11 +430,9 @@ def norm_residual_backward(x: torch.Tensor | None, r_out: torch.Tensor, dy: torc
     """Gradient of ``norm_residual``: x, gate, w_post, w_pre, scale and eps as in the forward call, r_out
     as it left it, dy and dr_out (None for zeros) the gradients of y and r_out.  dr may be dr_out.
     Returns (dx, dr, dgate, dw_post, dw_pre), None where the forward call had no such input."""
-    _check_dev(x, r_out, dy, w_pre, w_post, gate, dr_out, dx, dr, dgate, dw_post, dw_pre, workspace)
+    _on(r_out, x, dy, w_pre, w_post, gate, dr_out, dx, dr, dgate, dw_post, dw_pre, workspace)
     R, D, G = _norm_args(r_out, gate, w_post, w_pre)
     dt, dev, shape, ty = _dt(r_out), r_out.device, (R, D), r_out.dtype
-    _same_device(dev, x=x, dy=dy, w_pre=w_pre, w_post=w_post, gate=gate, dr_out=dr_out, dx=dx, dr=dr, dgate=dgate,
-                 dw_post=dw_post, dw_pre=dw_pre, workspace=workspace)
     if dx is None and x is not None:
         dx = torch.empty(shape, device=dev, dtype=ty)
     if dr is None:
@@ -447,7 +447,7 @@ def norm_residual_backward(x: torch.Tensor | None, r_out: torch.Tensor, dy: torc
     _want(dw_post, "dw_post", (D,))
     _want(dw_pre, "dw_pre", (D,))
     if workspace is None:
-        workspace = _room(None, norm_residual_backward_workspace_size(R, D, G, dt), dev)
+        workspace = _room(norm_residual_backward_workspace_size(R, D, G, dt), dev)
     rc = lib().isam_norm_residual_backward(
         R, D, G, dt, _ptr(x), _matrix(x, "x", shape, ty), _ptr(r_out), _matrix(r_out, "r_out", shape, ty), _ptr(gate),
         _ptr(w_post), _ptr(w_pre), scale, eps, _ptr(dy), _matrix(dy, "dy", shape, ty), _ptr(dr_out),
@@ -490,15 +490,14 @@ def gated_ffn(x: torch.Tensor, W: torch.Tensor, *, bias=None, activation="silu",
     ("sigmoid", "silu" or "gelu") and the product together.  x [M][K], W [2F][K] (gate rows, then up
     rows; float32 or bfloat16; row strides may exceed K), bias [2F] float32.  Returns out [M][F] in
     x's dtype."""
-    _check_dev(x, W, bias, out, workspace)
+    _on(x, W, bias, out, workspace)
     M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
     act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
-    _same_device(dev, W=W, bias=bias, out=out, workspace=workspace)
     if out is None:
         out = torch.empty((M, F), device=dev, dtype=x.dtype)
     ldo = _matrix(out, "out", (M, F), x.dtype)
     if workspace is None:
-        workspace = _room(None, gated_ffn_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
+        workspace = _room(gated_ffn_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
     rc = lib().isam_gated_ffn(M, K, F, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(out), ldo, _ptr(workspace),
                               _bytes(workspace), _stream())
     _call(rc, "isam_gated_ffn")
@@ -510,10 +509,9 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
     """Gradient of ``gated_ffn`` from dout [M][F]: the projections are formed again, nothing is kept
     from the forward call.  Returns (dx [M][K], dW [2F][K] in x's dtype, dbias [2F] float32 or
     None without a bias)."""
-    _check_dev(x, W, dout, bias, dx, dW, dbias, workspace)
+    _on(x, W, dout, bias, dx, dW, dbias, workspace)
     M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
     act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
-    _same_device(dev, W=W, dout=dout, bias=bias, dx=dx, dW=dW, dbias=dbias, workspace=workspace)
     if dx is None:
         dx = torch.empty((M, K), device=dev, dtype=x.dtype)
     if dW is None:
@@ -524,7 +522,7 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
     lddo, lddx = _matrix(dout, "dout", (M, F), x.dtype), _matrix(dx, "dx", (M, K), x.dtype)
     lddw = _matrix(dW, "dW", (2 * F, K), x.dtype)
     if workspace is None:
-        workspace = _room(None, gated_ffn_backward_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
+        workspace = _room(gated_ffn_backward_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
     rc = lib().isam_gated_ffn_backward(M, K, F, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(dout), lddo, _ptr(dx), lddx,
                                        _ptr(dW), lddw, _ptr(dbias), _ptr(workspace), _bytes(workspace), _stream())
     _call(rc, "isam_gated_ffn_backward")

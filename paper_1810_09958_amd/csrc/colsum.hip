@@ -24,7 +24,7 @@ __global__ __launch_bounds__(1024) void colsum_kernel(ColSums all) {
         float s = 0.0f;
         if (col < c.cols) {
             const float* const p = c.part + z * c.rows * c.cols + col;
-#pragma unroll 8
+#pragma unroll 16
             for (int64_t r = g; r < c.rows; r += 32) s += p[r * c.cols];
         }
         sums[g][cl] = s;

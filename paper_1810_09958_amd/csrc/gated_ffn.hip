@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void gated_pairs_kernel(GatedArgs a) {
     float sg = 0.0f, su = 0.0f;
     if (f < a.F) {
         const float bg = a.bias ? a.bias[f] : 0.0f, bu = a.bias ? a.bias[a.F + f] : 0.0f;
-#pragma unroll 2
+#pragma unroll 4
         for (int64_t m = m0 + rl; m < m1; m += 4) {
             float* const gu = a.gu + m * 2 * a.F + f;
             const float G = gu[0] + bg, U = gu[a.F] + bu;

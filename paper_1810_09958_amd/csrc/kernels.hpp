@@ -311,7 +311,7 @@ hipError_t launch_norm_backward(const NormArgs& a, int64_t grid, hipStream_t s);
 // a kernel for up to kGatedTokens rows of x (either type, any alignment), and the
 // element-wise step behind fp32 products.
 constexpr int64_t kGatedTokens = 16;
-constexpr int64_t kGatedRows = 64;   // rows of a workgroup of the element-wise step
+constexpr int64_t kGatedRows = 16;   // rows of a workgroup of the element-wise step
 enum GatedTile : int { kGated256 = 0, kGated128 = 1, kGated64 = 2 };
 struct GatedArgs {
     int64_t M, K, F;
