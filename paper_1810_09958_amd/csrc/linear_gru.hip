@@ -62,13 +62,14 @@ __device__ __forceinline__ float apply(float a, float b, float v) {
     return r;
 }
 
-// (A, B) of a group's steps so far, then one more: z (positive, so a sign of A stays).
+// (A, B) of a group's steps so far, then one more.  A's sign stays (also where z is NaN).
+template <bool RESET>
 __device__ __forceinline__ void step(bool drop, bool first, float z, float b, float& A, float& B) {
     if (first) {
         A = drop ? -0.0f : z;
         B = b;
     } else {
-        A = drop ? -0.0f : A * z;
+        A = drop ? -0.0f : RESET ? __builtin_copysignf(A * z, A) : A * z;
         B = __builtin_fmaf(z, drop ? 0.0f : B, b);
     }
 }
@@ -151,8 +152,6 @@ struct Rows {
             else f[e] = bf16lo(w[e / 2]);
         });
     }
-    // Every value with which sigmoid gives 1 whatever the (finite) bias.
-    static constexpr uint32_t kKeep = ES == 2 ? 0x7f807f80u : 0x7f800000u;
 };
 
 // fp32 values of the lane's channels (zeros without a tensor).
@@ -214,9 +213,11 @@ __device__ __forceinline__ uint32_t* chain_state(const LinGruArgs& a, int64_t id
     return reinterpret_cast<uint32_t*>(a.chain + 8 + id * (kCols + kCols / 2) + kCols) + ch;
 }
 __device__ __forceinline__ uint32_t chain_bits(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
+template <bool RESET>
 __device__ __forceinline__ void chain_put(const LinGruArgs& a, int64_t id, int ch, float ta, float tb) {
-    __hip_atomic_store(chain_pair(a, id, ch), (uint64_t)chain_bits(ta) | (uint64_t)chain_bits(tb) << 32, __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
+    // (an A that drops keeps its sign, also where it is NaN)
+    const uint32_t wa = RESET && drops(ta) ? 0x80000000u : chain_bits(ta);
+    __hip_atomic_store(chain_pair(a, id, ch), (uint64_t)wa | (uint64_t)chain_bits(tb) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void chain_put(const LinGruArgs& a, int64_t id, int ch, float v) {
     __hip_atomic_store(chain_state(a, id, ch), chain_bits(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -345,20 +346,21 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(Li
         bn[e] *= scale;
     });
 
+    // (a step that does not exist leaves the state as it is, whatever the bias)
     float ca[R][4], cb[R][4], A[4], B[4];
     static_for<R>([&](auto r) {
-        const bool drop = RESET && (reset >> r & 1);
+        const bool drop = RESET && (reset >> r & 1), in = q * R + r < left;
         float gz[4], n[4];
-        static_for<S::W>([&](auto w) { pz[r][w] = q * R + r < left ? pz[r][w] : S::kKeep; });
         S::unpack(pz[r], gz);
         S::unpack(pn[r], n);
         static_for<4>([&](auto e) { n[e] = __builtin_fmaf(n[e], scale, bn[e]); });
         if (a.candidate) static_for<4>([&](auto e) { n[e] = gate_tanh<ES>(n[e]); });
         static_for<4>([&](auto e) {
-            float omz;
-            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), ca[r][e], omz);
-            cb[r][e] = omz * n[e];
-            step(drop, r == 0, ca[r][e], cb[r][e], A[e], B[e]);
+            float z, omz;
+            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z, omz);
+            ca[r][e] = in ? z : 1.0f;
+            cb[r][e] = in ? omz * n[e] : 0.0f;
+            step<RESET>(drop, r == 0, ca[r][e], cb[r][e], A[e], B[e]);
         });
     });
     wave_scan<RESET, true>(A, B, lane);
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(Li
                 tb = apply<RESET>(wa[w + 1], wb[w + 1], tb);
                 ta = compose_a<RESET>(ta, wa[w + 1]);
             });
-            if (!last) chain_put(a, tile.id, lane, ta, tb);
+            if (!last) chain_put<RESET>(a, tile.id, lane, ta, tb);
             h = chain_in<RESET>(a, tile.id, tile.k, tile.cols, lane, first);
             if (!last) chain_put(a, tile.id, lane, apply<RESET>(ta, tb, h));
         }
@@ -480,16 +482,18 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
     // z, 1 - z and n of each step; (A, B) composes the state, (Z, C) e
     float z[R][4], omz[R][4], n[R][4], A[4], B[4], Z[4], C[4];
     static_for<R>([&](auto r) {
-        const bool drop = RESET && (reset >> r & 1);
+        const bool drop = RESET && (reset >> r & 1), in = q * R + r < left;
         float gz[4];
-        static_for<S::W>([&](auto w) { pz[r][w] = q * R + r < left ? pz[r][w] : S::kKeep; });
         S::unpack(pz[r], gz);
         S::unpack(pn[r], n[r]);
         static_for<4>([&](auto e) { n[r][e] = __builtin_fmaf(n[r][e], scale, bn[e]); });
         if (a.candidate) static_for<4>([&](auto e) { n[r][e] = gate_tanh<ES>(n[r][e]); });
         static_for<4>([&](auto e) {
             gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z[r][e], omz[r][e]);
-            step(drop, r == 0, z[r][e], omz[r][e] * n[r][e], A[e], B[e]);
+            z[r][e] = in ? z[r][e] : 1.0f;
+            omz[r][e] = in ? omz[r][e] : 0.0f;
+            n[r][e] = in ? n[r][e] : 0.0f;
+            step<RESET>(drop, r == 0, z[r][e], omz[r][e] * n[r][e], A[e], B[e]);
         });
     });
     static_for<R>([&](auto i) {
@@ -527,7 +531,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
                 tc = apply<RESET>(wa[w], wc[w], tc);
                 ta = compose_a<RESET>(ta, wa[w]);
             });
-            if (kt > 0) chain_put(a, tile.id, lane, ta, tc);
+            if (kt > 0) chain_put<RESET>(a, tile.id, lane, ta, tc);
             g = chain_in<RESET>(a, tile.id, tile.k, tile.cols, lane, first);
             if (kt > 0) chain_put(a, tile.id, lane, apply<RESET>(ta, tc, g));
         }

@@ -213,6 +213,39 @@ def test_reset_cuts_off_bad_values(T, dtype, bad):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [7, 60, 700, 4000])
+def test_reset_cuts_off_bad_gates(T, dtype):
+    # spans of NaN gates between resets, one in every 100 steps: what follows them, and the
+    # gradients of what stands before them, do not see them
+    H, B = 40, 2
+    x = inputs(T, B, H, dtype, seed=T)
+    at = torch.arange(T)
+    bad = (at % 100 >= 3) & (at % 100 < 6)
+    r = (at % 100 == 3) | (at % 100 == 6)
+    x["reset"] = r[:, None].expand(T, B).contiguous().cuda()
+    ref = reference(x, "tanh", H)
+    x["gx"][bad] = float("nan")
+    out = run(x, "tanh")
+    good = ~bad
+    for k in ("h_seq", "dgx"):
+        check(out[k][good], (ref[k][0][good], ref[k][1][good]), k)
+        assert torch.isnan(out[k][bad].float()).all()
+    check(out["dh0"], ref["dh0"], "dh0")
+    if not bad[-1]:
+        check(out["h_T"], ref["h_T"], "h_T")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [40, 700])
+def test_infinite_bias(T, dtype):
+    # a gate bias of either infinity is a gate shut or open; the steps past a tile's end do not see it
+    H, B = 16, 2
+    x = inputs(T, B, H, dtype, seed=T)
+    x["bias"][1], x["bias"][2] = float("-inf"), float("inf")
+    compare(x, "tanh")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_saturated_gates(dtype):
     # gates of the type's lowest and highest values and infinities: z is exactly 0 or 1
     T, B, H = 300, 2, 16
