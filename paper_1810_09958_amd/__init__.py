@@ -1,6 +1,6 @@
 """MI355X (gfx950) hot path of ISA Mapper (arXiv 1810.09958): GEMM, separable depthwise
-convolution and GRU forward, and the operators of a gated recurrent block with their gradients, as hand-written HIP kernels behind the C ABI in
-``include/isam.h``.
+convolution and GRU forward, and the operators of a gated recurrent language-model block with
+their gradients, as hand-written HIP kernels behind the C ABI in ``include/isam.h``.
 
 This module is argument marshalling only: it checks torch tensors (device, dtype,
 contiguity), sizes and allocates the workspace, and calls the C ABI on torch's current
