@@ -236,7 +236,8 @@ hipError_t launch_gru_copy_state(const float* h0, float* h_T, int64_t n, hipStre
 
 // Linear GRU (linear_gru.hip).  Strides in elements; rows are [2H] (gx, dgx) or [H].
 constexpr int64_t kLinGruChunk = 128;  // steps between two rows of `states`
-constexpr int kLinGruFwdSteps = 8, kLinGruBwdSteps = 8;  // steps of a group: tiles of 32 times as many
+constexpr int kLinGruSteps = 8;                              // steps of a group, four groups to a wave
+constexpr int kLinGruFwdWaves = 8, kLinGruBwdWaves = 4;      // waves of a tile
 constexpr uint64_t kLinGruTimeoutTicks = 200000000ull;   // bound of a wait for an earlier tile (2 s at 100 MHz)
 struct LinGruArgs {
     int64_t T, batch, H;

@@ -44,7 +44,7 @@ namespace isam {
 namespace {
 
 constexpr int kCols = 64;        // channels of a tile
-constexpr int kChainWindow = 4;  // tiles that one look back along the chain sees
+constexpr int kChainWindow = 2;  // tiles that one look back along the chain sees
 
 __device__ __forceinline__ bool drops(float a) { return (int)__float_as_uint(a) < 0; }
 
@@ -290,20 +290,21 @@ struct Tile {
     }
 };
 
-// What the kernels hold of a wave's steps: reset marks, a bit for each.
+// Reset marks of a wave's 4 R steps: one byte a lane, then a bit for each of the group's steps.
 template <int R, bool RESET>
-__device__ __forceinline__ uint32_t reset_bits(const LinGruArgs& a, int64_t b, int64_t tw, int lane, int left) {
-    uint32_t bits = 0;
-    if constexpr (RESET) {
-        const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.reset + b * a.rs_b + tw * a.rs_t, 0x7fffffffu);
-        static_for<R>([&](auto r) {
-            const int i = (lane >> 4) * R + r;
-            const uint32_t v = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(i < left ? (uint32_t)i * (uint32_t)a.rs_t : kOob), 0, 0);
-            bits |= ((v & 0xffu) ? 1u : 0u) << r;
-        });
+struct Resets {
+    static_assert(4 * R <= 32, "a lane for each step, a word of marks");
+    uint32_t v = 0;
+    __device__ __forceinline__ Resets(const LinGruArgs& a, int64_t b, int64_t tw, int lane, int left) {
+        if constexpr (RESET) {
+            const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.reset + b * a.rs_b + tw * a.rs_t, 0x7fffffffu);
+            v = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(lane < left ? (uint32_t)lane * (uint32_t)a.rs_t : kOob), 0, 0);
+        }
     }
-    return bits;
-}
+    __device__ __forceinline__ uint32_t bits(int q) const {
+        return RESET ? (uint32_t)__ballot((v & 0xffu) != 0) >> (q * R) : 0u;
+    }
+};
 
 // A wave's totals: the lanes of its last group (or first) to the tile's row, the
 // others to a row that nobody reads.
@@ -317,7 +318,7 @@ __device__ __forceinline__ void get4(const float* row, int lane, float (&f)[4]) 
 
 // Forward pass: NW waves of 4 groups of R steps.
 template <int ES, bool VEC, int NW, int R, bool RESET, bool CHAIN>
-__global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(LinGruArgs a) {
+__global__ __launch_bounds__(NW * 64, 4) void lingru_fwd_kernel(LinGruArgs a) {
     using S = Rows<ES, VEC, R>;
     constexpr int TS = NW * 4 * R;
     __shared__ __attribute__((aligned(16))) float tot[NW][2][kCols];
@@ -330,13 +331,14 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void lingru_fwd_kernel(Li
     const int left = (int)max((int64_t)0, min((int64_t)(4 * R), a.T - tw));  // steps of this wave that exist
     const bool last = (tile.k + 1) * TS >= a.T;
 
+    const Resets<R, RESET> marks(a, b, tw, lane, left);
     const S gx(a.gx, b * a.gx_b + tw * a.gx_t, a.gx_t, a.H, c0, lane);
     uint32_t pz[R][S::W], pn[R][S::W];
     static_for<R>([&](auto r) {
         gx.load(pz[r], r, q * R + r < left, 0);
         gx.load(pn[r], r, q * R + r < left, (uint32_t)a.H * ES);
     });
-    const uint32_t reset = reset_bits<R, RESET>(a, b, tw, lane, left);
+    const uint32_t reset = marks.bits(q);
     float bz[4], bn[4];
     load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
     load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
@@ -447,7 +449,7 @@ __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
 // Backward pass; tiles count from the end of time.  The tile's states are formed
 // again from the one before it.
 template <int ES, bool VEC, int NW, int R, bool RESET, bool CHAIN>
-__global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd_kernel(LinGruArgs a) {
+__global__ __launch_bounds__(NW * 64, ES == 2 && VEC ? 3 : 2) void lingru_bwd_kernel(LinGruArgs a) {
     using S = Rows<ES, VEC, R>;
     constexpr int TS = NW * 4 * R;
     static_assert(!CHAIN || TS % kLinGruChunk == 0, "a tile starts at a kept state");
@@ -461,6 +463,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
     const int64_t b = tile.b, c0 = tile.c0, tw = kt * TS + wid * 4 * R;
     const int left = (int)max((int64_t)0, min((int64_t)(4 * R), a.T - tw));
 
+    const Resets<R, RESET> marks(a, b, tw, lane, left);
     const S gx(a.gx, b * a.gx_b + tw * a.gx_t, a.gx_t, a.H, c0, lane);
     const S dh(a.dh_seq, b * a.dh_b + tw * a.dh_t, a.dh_t, a.H, c0, lane);
     uint32_t pz[R][S::W], pn[R][S::W], pd[R][S::W];
@@ -469,7 +472,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
         gx.load(pn[r], r, q * R + r < left, (uint32_t)a.H * ES);
         dh.load(pd[r], r, q * R + r < left, 0);
     });
-    const uint32_t reset = reset_bits<R, RESET>(a, b, tw, lane, left);
+    const uint32_t reset = marks.bits(q);
     float bz[4], bn[4];
     load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
     load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
@@ -542,7 +545,20 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
         });
     }
     __syncthreads();
-    float hs[4], en[4], hb[R][4], sz[4], sn[4];
+    // The states again; of each step then remain z and the factors of d in dgz and dgn, which
+    // take the places of 1 - z and n.  The empty asm keeps the compiler from holding what it
+    // formed of them before the scans (another 60 registers).
+    static_for<R>([&](auto r) {
+        static_for<4>([&](auto e) {
+            float& v = omz[r][e];
+            asm volatile("" : "+v"(v));
+        });
+        static_for<S::W>([&](auto w) {
+            uint32_t& v = pd[r][w];
+            asm volatile("" : "+v"(v));
+        });
+    });
+    float hs[4], en[4], sz[4], sn[4];
     get4(start[wid][0], lane, hs);
     get4(start[wid][1], lane, en);
     static_for<4>([&](auto e) {
@@ -552,8 +568,10 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
         en[e] = q < 3 ? apply<RESET>(qa, qc, en[e]) : en[e];
         sz[e] = sn[e] = 0.0f;
         static_for<R>([&](auto r) {
-            hb[r][e] = RESET && (reset >> r & 1) ? 0.0f : hs[e];
-            hs[e] = __builtin_fmaf(z[r][e], hb[r][e], omz[r][e] * n[r][e]);
+            const float hb = RESET && (reset >> r & 1) ? 0.0f : hs[e], w = omz[r][e], c = n[r][e];
+            hs[e] = __builtin_fmaf(z[r][e], hb, w * c);
+            omz[r][e] = w * z[r][e] * (hb - c);
+            n[r][e] = a.candidate ? w * __builtin_fmaf(-c, c, 1.0f) : w;
         });
     });
     const S dg(a.dgx, b * a.dg_b + tw * a.dg_t, a.dg_t, a.H, c0, lane);
@@ -562,9 +580,9 @@ __global__ __launch_bounds__(NW * 64, NW == 8 && R <= 4 ? 4 : 1) void lingru_bwd
         float d[4], oz[4], on[4];
         S::unpack(pd[r], d);
         static_for<4>([&](auto e) {
-            const float dt = d[e] + en[e], w = dt * omz[r][e];  // (0 past the end)
-            oz[e] = w * z[r][e] * (hb[r][e] - n[r][e]);
-            on[e] = a.candidate ? w * __builtin_fmaf(-n[r][e], n[r][e], 1.0f) : w;
+            const float dt = d[e] + en[e];
+            oz[e] = dt * omz[r][e];  // (0 past the end)
+            on[e] = dt * n[r][e];
             const float back = z[r][e] * dt;
             en[e] = RESET && (reset >> r & 1) ? 0.0f : back;
             sz[e] += oz[e];
@@ -607,13 +625,13 @@ typedef void (*LinGruFn)(LinGruArgs);
 
 template <int ES, bool VEC, bool BWD, bool RESET>
 LinGruFn tile_fn(bool few, bool chain) {
-    constexpr int R = BWD ? kLinGruBwdSteps : kLinGruFwdSteps;
+    constexpr int R = kLinGruSteps, NW = BWD ? kLinGruBwdWaves : kLinGruFwdWaves;
     if constexpr (BWD) {
-        if (few) return lingru_bwd_kernel<ES, VEC, 2, 8, RESET, false>;
-        return chain ? lingru_bwd_kernel<ES, VEC, 8, R, RESET, true> : lingru_bwd_kernel<ES, VEC, 8, R, RESET, false>;
+        if (few) return lingru_bwd_kernel<ES, VEC, 2, R, RESET, false>;
+        return chain ? lingru_bwd_kernel<ES, VEC, NW, R, RESET, true> : lingru_bwd_kernel<ES, VEC, NW, R, RESET, false>;
     } else {
-        if (few) return lingru_fwd_kernel<ES, VEC, 2, 8, RESET, false>;
-        return chain ? lingru_fwd_kernel<ES, VEC, 8, R, RESET, true> : lingru_fwd_kernel<ES, VEC, 8, R, RESET, false>;
+        if (few) return lingru_fwd_kernel<ES, VEC, 2, R, RESET, false>;
+        return chain ? lingru_fwd_kernel<ES, VEC, NW, R, RESET, true> : lingru_fwd_kernel<ES, VEC, NW, R, RESET, false>;
     }
 }
 
@@ -641,7 +659,7 @@ hipError_t launch_tiles(const LinGruArgs& a, hipStream_t s) {
                                                              : pieces(a.h_seq, a.h_t, a.h_b, a));
     const LinGruFn fn = vec ? (a.reset ? tile_fn<ES, true, BWD, true>(few, chain) : tile_fn<ES, true, BWD, false>(few, chain))
                             : (a.reset ? tile_fn<ES, false, BWD, true>(few, chain) : tile_fn<ES, false, BWD, false>(few, chain));
-    hipLaunchKernelGGL(fn, dim3((unsigned)total), dim3(few ? 128 : 512), 0, s, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)total), dim3(few ? 128 : 64 * (BWD ? kLinGruBwdWaves : kLinGruFwdWaves)), 0, s, a);
     return hipGetLastError();
 }
 
@@ -653,7 +671,7 @@ bool lingru_strides(int64_t stride_t, int64_t width, int64_t es) {
 }
 
 int64_t lingru_tiles(int64_t T, bool backward) {
-    const int64_t ts = 32 * (backward ? kLinGruBwdSteps : kLinGruFwdSteps);
+    const int64_t ts = 4 * kLinGruSteps * (backward ? kLinGruBwdWaves : kLinGruFwdWaves);
     return T <= 64 ? (T > 0 ? 1 : 0) : (T + ts - 1) / ts;
 }
 
