@@ -409,7 +409,9 @@ namespace {
 struct GatedPlan {
     int64_t Kp;                       // row length of the copies
     bool copy_x, copy_w;
+    bool direct;                      // fp32 projections formed in the block's own kernel
     int tile;
+    int64_t bias_rows;                // partial sums of the bias gradient
     size_t x_b, w_b, pair_b, bias_b, gemm_b;
     size_t total() const { return x_b + w_b + pair_b + bias_b + gemm_b; }
 };
@@ -430,9 +432,11 @@ GatedPlan gated_plan(int64_t M, int64_t K, int64_t F, int type, bool x_ok, bool 
         if (p.copy_w) p.w_b = align256((size_t)(2 * F * p.Kp) * es);
         p.tile = gated_tile(M, F, device_cus());
     }
-    if (backward || type == ISAM_F32) p.pair_b = align256((size_t)(M * 2 * F) * es);
-    if (backward) p.bias_b = align256((size_t)((type == ISAM_BF16 ? gated_bias_rows(p.tile, M) : cdiv(M, kGatedRows)) * 2 * F) * sizeof(float));
-    if (type == ISAM_F32) p.gemm_b = product_workspace(0, 1, M, 2 * F, K, type);
+    p.direct = type == ISAM_F32 && gated_f32_direct(M, K, F, device_cus());
+    if (backward || (type == ISAM_F32 && !p.direct)) p.pair_b = align256((size_t)(M * 2 * F) * es);
+    p.bias_rows = type == ISAM_BF16 ? gated_bias_rows(p.tile, M) : p.direct ? cdiv(M, kGatedF32Tile) * 2 : cdiv(M, kGatedRows);
+    if (backward) p.bias_b = align256((size_t)(p.bias_rows * 2 * F) * sizeof(float));
+    if (type == ISAM_F32 && !p.direct) p.gemm_b = product_workspace(0, 1, M, 2 * F, K, type);
     if (backward) {
         p.gemm_b = std::max(p.gemm_b, product_workspace(0, 0, M, K, 2 * F, type));
         p.gemm_b = std::max(p.gemm_b, product_workspace(1, 0, 2 * F, K, M, type));
@@ -540,6 +544,8 @@ extern "C" isam_status_t isam_gated_ffn(int64_t M, int64_t K, int64_t F, int typ
     } else if (type == ISAM_BF16) {
         e = gated_copies(p, ws, a, s);
         if (e == hipSuccess) e = launch_gated_tiles(a, p.tile, false, s);
+    } else if (p.direct) {
+        e = launch_gated_f32(a, false, s);
     } else {
         a.gu = reinterpret_cast<float*>(ws);
         st = product(0, 1, M, 2 * F, K, type, x, ldx, W, ldw, ISAM_F32, a.gu, 2 * F, ws + p.pair_b, p.gemm_b, s, who);
@@ -610,6 +616,8 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
         if (type == ISAM_BF16) {
             e = gated_copies(p, ws, a, s);
             if (e == hipSuccess) e = launch_gated_tiles(a, p.tile, true, s);
+        } else if (p.direct) {
+            e = launch_gated_f32(a, true, s);
         } else {
             a.gu = reinterpret_cast<float*>(pairs);
             st = product(0, 1, M, 2 * F, K, type, x, ldx, W, ldw, ISAM_F32, a.gu, 2 * F, gemm_ws, p.gemm_b, s, who);
@@ -623,8 +631,7 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
     if (dW && (st = product(1, 0, 2 * F, K, M, type, pairs, 2 * F, x, M ? ldx : K, type, dW, lddw, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
         return st;
     if (dbias) {
-        const int64_t rows = M == 0 ? 0 : type == ISAM_BF16 ? gated_bias_rows(p.tile, M) : cdiv(M, kGatedRows);
-        const ColSum sum{bias_part, dbias, rows, 2 * F, 1, kF32};
+        const ColSum sum{bias_part, dbias, p.bias_rows, 2 * F, 1, kF32};
         e = launch_colsum(&sum, 1, s);
     }
     return e == hipSuccess ? ISAM_OK : hip_fail(e, who);

@@ -71,6 +71,122 @@ __global__ __launch_bounds__(512) void gated_token_kernel(GatedArgs a) {
     IO::put(a.out, (int64_t)li * a.ld_out + fo, s * Uv);
 }
 
+// fp32 blocks of few tiles: 32 rows x 32 values of f, gate and up, on the fp32 matrix
+// instructions, straight from memory (any alignment of 4 bytes) into their operand
+// registers.  The four waves take every fourth 16-deep K step (32 matrix instructions
+// on 6 loads, two steps in flight) and meet in LDS, each wave then holding one 16 x 16
+// quarter of G and U for the epilogue.  G and U never reach memory, and no operand is
+// copied or split into bf16 terms first, which is what bounds small products; larger
+// ones are bound by the fp32 matrix rate (an eighth of what the terms need of bf16's)
+// and go through the library's product.
+template <bool BWD>
+__global__ __launch_bounds__(256, 2) void gated_f32_kernel(GatedArgs a, TileMapArgs tmap) {
+    __shared__ float sums[4][32][64];
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, g = lane >> 4;
+    int tm, tn;
+    map_tile(tmap, tm, tn);
+    const int64_t m0 = (int64_t)tm * kGatedF32Tile, f0 = (int64_t)tn * kGatedF32Tile;
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.x, (uint32_t)(((a.M - 1) * a.ld_x + a.K) * 4));
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.W, (uint32_t)(((2 * a.F - 1) * a.ld_w + a.K) * 4));
+    // rows of x, then gate and up rows of W: byte offset of the lane's four values of step 0
+    uint32_t at[6];
+    static_for<2>([&](auto i) {
+        const int64_t m = m0 + 16 * i + li, f = f0 + 16 * i + li;
+        at[i] = m < a.M ? (uint32_t)((m * a.ld_x + 4 * g) * 4) : kOob;
+        at[2 + i] = f < a.F ? (uint32_t)((f * a.ld_w + 4 * g) * 4) : kOob;
+        at[4 + i] = f < a.F ? (uint32_t)(((a.F + f) * a.ld_w + 4 * g) * 4) : kOob;
+    });
+    f32x4_t acc[2][2][2];  // [rows][f][gate, up]
+    static_for<2>([&](auto i) {
+        static_for<2>([&](auto j) { static_for<2>([&](auto h) { acc[i][j][h] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }); });
+    });
+    const int steps = (int)(a.K / 16);
+    auto load = [&](uint4 (&v)[6], int s) {
+        static_for<6>([&](auto o) {
+            const uint32_t off = s < steps && at[o] != kOob ? at[o] + (uint32_t)s * 64u : kOob;
+            v[o] = buf_load16(o < 2 ? rx : rw, off);
+        });
+    };
+    auto multiply = [&](const uint4 (&v)[6]) {
+        static_for<2>([&](auto i) {
+            static_for<2>([&](auto j) {
+                mfma16_f32x4(acc[i][j][0], v[i], v[2 + j]);
+                mfma16_f32x4(acc[i][j][1], v[i], v[4 + j]);
+            });
+        });
+    };
+    uint4 b0[6], b1[6];
+    load(b0, wid);
+    load(b1, wid + 4);
+    for (int s = wid; s < steps; s += 8) {  // (steps past the end are zeros)
+        multiply(b0);
+        load(b0, s + 8);
+        multiply(b1);
+        load(b1, s + 12);
+    }
+    if (a.K % 16 && wid == (steps & 3)) {  // the last values of the rows, one by one
+        const int k = steps * 16 + 4 * g;
+        uint4 v[6];
+        static_for<6>([&](auto o) {
+            uint32_t w[4];
+            static_for<4>([&](auto e) {
+                w[e] = buf_load4(o < 2 ? rx : rw, k + e < a.K && at[o] != kOob ? at[o] + (uint32_t)steps * 64u + 4u * e : kOob);
+            });
+            v[o] = make_uint4(w[0], w[1], w[2], w[3]);
+        });
+        multiply(v);
+    }
+    static_for<2>([&](auto i) {
+        static_for<2>([&](auto j) {
+            static_for<2>([&](auto h) {
+                static_for<4>([&](auto v) { sums[wid][((i * 2 + j) * 2 + h) * 4 + v][lane] = acc[i][j][h][decltype(v)::value]; });
+            });
+        });
+    });
+    __syncthreads();
+    // this wave's quarter: rows mq + 4 g + v, column f
+    const int64_t mq = m0 + 16 * (wid >> 1), f = f0 + 16 * (wid & 1) + li;
+    const bool in = f < a.F;
+    const float bg = a.bias && in ? a.bias[f] : 0.0f, bu = a.bias && in ? a.bias[a.F + f] : 0.0f;
+    const int64_t cols = BWD ? 2 * a.F : a.F;
+    const __amdgpu_buffer_rsrc_t rp = make_rsrc(BWD ? a.dout : nullptr, BWD ? (uint32_t)(((a.M - 1) * a.ld_dout + a.F) * 4) : 0u);
+    const __amdgpu_buffer_rsrc_t ro = make_rsrc(a.out, (uint32_t)(((a.M - 1) * a.ld_out + cols) * 4));
+    float sg = 0.0f, su = 0.0f;
+    static_for<4>([&](auto v) {
+        const int64_t m = mq + 4 * g + v;
+        const bool on = in && m < a.M;
+        float G = bg, U = bu;
+        static_for<4>([&](auto w) {
+            G += sums[w][wid * 8 + v][lane];
+            U += sums[w][wid * 8 + 4 + v][lane];
+        });
+        float slope;
+        const float s = a.act == 0 ? gate_act<0>(G, slope) : a.act == 1 ? gate_act<1>(G, slope) : gate_act<2>(G, slope);
+        const uint32_t to = on ? (uint32_t)((m * a.ld_out + f) * 4) : kOob;
+        if constexpr (BWD) {
+            const float dp = __uint_as_float(buf_load4(rp, on ? (uint32_t)((m * a.ld_dout + f) * 4) : kOob));
+            const float dg = dp * U * slope, du = dp * s;
+            __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(dg), ro, (int)to, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(du), ro, (int)(on ? to + (uint32_t)(a.F * 4) : kOob), 0, 0);
+            sg += on ? dg : 0.0f;
+            su += on ? du : 0.0f;
+        } else {
+            __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(s * U), ro, (int)to, 0, 0);
+        }
+    });
+    if (BWD && a.bias_part) {  // one partial row for every 16 rows
+        static_for<2>([&](auto k) {
+            sg += __shfl_xor(sg, 16 << decltype(k)::value);
+            su += __shfl_xor(su, 16 << decltype(k)::value);
+        });
+        float* const part = a.bias_part + (int64_t)(tm * 2 + (wid >> 1)) * 2 * a.F;
+        if (in && g == 0) {
+            part[f] = sg;
+            part[a.F + f] = su;
+        }
+    }
+}
+
 // fp32: p, or (BWD) dG and dU in place, from G and U in memory ([M][2F] at
 // a.gu).  A workgroup takes 64 columns of f and kGatedRows rows, four at a time,
 // and leaves one partial row of the bias gradient.
@@ -152,6 +268,24 @@ hipError_t launch_gated_tokens(const GatedArgs& a, int type, hipStream_t s) {
     if (a.M > kGatedTokens || (a.F + 15) / 16 > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL((type == kBF16 ? gated_token_kernel<2> : gated_token_kernel<4>), dim3((unsigned)((a.F + 15) / 16)), dim3(512), 0,
                        s, a);
+    return hipGetLastError();
+}
+
+// Where gated_f32_kernel is taken: up to 24 rounds of 64 values of K on a compute unit.
+// us forward, this kernel / product and element-wise step (rounds): 32x64x64 7.3 / 10.1 (1),
+// 128x512x2048 10.2 / 17.8 (8), 64x1024x1024 15.7 / 15.6, 256x1024x1024 15.8 / 24.1 and
+// 500x511x771 16.0 / 27.7 (16), 100x333x5001 18.6 / 27.0 (18), 512x512x2048 28.3 / 27.6 (32),
+// 1000x1000x1000 41.3 / 42.2 and 32x4096x512 46.5 / 20.8 (64), 512x2048x2048 90 / 69 (128).
+bool gated_f32_direct(int64_t M, int64_t K, int64_t F, int cus) {
+    const int64_t tiles = ((M + kGatedF32Tile - 1) / kGatedF32Tile) * ((F + kGatedF32Tile - 1) / kGatedF32Tile);
+    return (K + 63) / 64 <= 24 && (K + 63) / 64 * ((tiles + cus - 1) / cus) <= 24;
+}
+
+hipError_t launch_gated_f32(const GatedArgs& a, bool backward, hipStream_t s) {
+    const int64_t tm = (a.M + kGatedF32Tile - 1) / kGatedF32Tile, tn = (a.F + kGatedF32Tile - 1) / kGatedF32Tile;
+    if (tm * tn > INT32_MAX || a.K <= 0) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((backward ? gated_f32_kernel<true> : gated_f32_kernel<false>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, a,
+                       tile_map(tm, tn));
     return hipGetLastError();
 }
 

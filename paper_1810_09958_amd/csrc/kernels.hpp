@@ -313,6 +313,7 @@ hipError_t launch_norm_backward(const NormArgs& a, int64_t grid, hipStream_t s);
 // element-wise step behind fp32 products.
 constexpr int64_t kGatedTokens = 16;
 constexpr int64_t kGatedRows = 16;   // rows of a workgroup of the element-wise step
+constexpr int64_t kGatedF32Tile = 32;  // rows and values of f of a tile of the fp32 kernel
 enum GatedTile : int { kGated256 = 0, kGated128 = 1, kGated64 = 2 };
 struct GatedArgs {
     int64_t M, K, F;
@@ -333,6 +334,9 @@ int gated_tile(int64_t M, int64_t F, int cus);
 int64_t gated_bias_rows(int tile, int64_t M);
 hipError_t launch_gated_tiles(const GatedArgs& a, int tile, bool backward, hipStream_t s);
 hipError_t launch_gated_tokens(const GatedArgs& a, int type, hipStream_t s);
+// fp32 without the library's product: whether it is taken, and its launch.
+bool gated_f32_direct(int64_t M, int64_t K, int64_t F, int cus);
+hipError_t launch_gated_f32(const GatedArgs& a, bool backward, hipStream_t s);
 hipError_t launch_gated_pairs(const GatedArgs& a, bool backward, hipStream_t s);
 
 // out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros), up to three such

@@ -102,6 +102,14 @@ def test_small_tiles(M, K, F, dtype):
         compare(inputs(M, K, F, dtype, seed=M + i, bias=i != 1), name)
 
 
+@pytest.mark.parametrize("M,K,F", [(600, 700, 900), (2000, 130, 1501), (40, 1700, 50), (333, 1537, 513), (1000, 24, 777),
+                                   (500, 511, 771), (1025, 80, 1031), (17, 1536, 3000)])
+def test_fp32_sizes(M, K, F):
+    # both sides of the rule between the block's own fp32 kernel and the library's product
+    for i, name in enumerate(ACTS):
+        compare(inputs(M, K, F, torch.float32, seed=M + i, bias=i != 1), name)
+
+
 @pytest.mark.parametrize("M,K,F", [(1024, 64, 2048), (1000, 200, 2111), (1100, 136, 2100), (1023, 65, 2050)])
 def test_middle_tiles(M, K, F):
     for i, name in enumerate(ACTS):
