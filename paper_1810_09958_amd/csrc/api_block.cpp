@@ -408,6 +408,7 @@ namespace {
 // what the matrix products use.
 struct GatedPlan {
     int64_t Kp;                       // row length of the copies
+    int64_t ld_pair;                  // of the projections or their gradients
     bool copy_x, copy_w;
     bool direct;                      // fp32 projections formed in the block's own kernel
     int tile;
@@ -417,6 +418,8 @@ struct GatedPlan {
 };
 
 bool rows_aligned(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+int64_t gated_ld_pair(int64_t F) { return cdiv(2 * F, 8) * 8; }
 
 GatedPlan gated_plan(int64_t M, int64_t K, int64_t F, int type, bool x_ok, bool w_ok, bool backward) {
     GatedPlan p{};
@@ -433,7 +436,9 @@ GatedPlan gated_plan(int64_t M, int64_t K, int64_t F, int type, bool x_ok, bool 
         p.tile = gated_tile(M, F, device_cus());
     }
     p.direct = type == ISAM_F32 && gated_f32_direct(M, K, F, device_cus());
-    if (backward || (type == ISAM_F32 && !p.direct)) p.pair_b = align256((size_t)(M * 2 * F) * es);
+    // (rows of whole 16-byte pieces, so that the products after it need no copy of them)
+    p.ld_pair = type == ISAM_F32 && !p.direct ? 2 * F : gated_ld_pair(F);
+    if (backward || (type == ISAM_F32 && !p.direct)) p.pair_b = align256((size_t)(M * p.ld_pair) * es);
     p.bias_rows = type == ISAM_BF16 ? gated_bias_rows(p.tile, M) : p.direct ? cdiv(M, kGatedF32Tile) * 2 : cdiv(M, kGatedRows);
     if (backward) p.bias_b = align256((size_t)(p.bias_rows * 2 * F) * sizeof(float));
     if (type == ISAM_F32 && !p.direct) p.gemm_b = product_workspace(0, 1, M, 2 * F, K, type);
@@ -469,7 +474,7 @@ isam_status_t gated_matrix(const char* name, const void* p, int64_t rows, int64_
 bool gated_sizes(int64_t M, int64_t K, int64_t F, int type) {
     const __int128 es = (__int128)dsize(type), most = kMaxExtent;
     const __int128 Kp = (__int128)K + 64;
-    return (__int128)M * 2 * F * es <= most && (__int128)M * Kp * es <= most && (__int128)2 * F * Kp * es <= most &&
+    return (__int128)M * gated_ld_pair(F) * es <= most && (__int128)M * Kp * es <= most && (__int128)2 * F * Kp * es <= most &&
            (type == ISAM_BF16 || M <= 65535 * kGatedRows);
 }
 
@@ -597,8 +602,8 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
     float* const bias_part = reinterpret_cast<float*>(pairs + p.pair_b);
     char* const gemm_ws = pairs + p.pair_b + p.bias_b;
     hipError_t e = hipSuccess;
+    GatedArgs a{};
     if (M > 0) {
-        GatedArgs a{};
         a.M = M;
         a.K = K;
         a.F = F;
@@ -609,7 +614,7 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
         a.ld_x = ldx;
         a.ld_w = ldw;
         a.out = pairs;
-        a.ld_out = 2 * F;
+        a.ld_out = p.ld_pair;
         a.dout = dout;
         a.ld_dout = lddo;
         a.bias_part = dbias ? bias_part : nullptr;
@@ -625,10 +630,12 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
             e = launch_gated_pairs(a, true, s);
         }
         if (e != hipSuccess) return hip_fail(e, who);
-        if (dx && (st = product(0, 0, M, K, 2 * F, type, pairs, 2 * F, W, ldw, type, dx, lddx, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
+        // (of x and W the aligned copies, where the plan has them)
+        if (dx && (st = product(0, 0, M, K, 2 * F, type, pairs, p.ld_pair, a.W, a.ld_w, type, dx, lddx, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
             return st;
     }
-    if (dW && (st = product(1, 0, 2 * F, K, M, type, pairs, 2 * F, x, M ? ldx : K, type, dW, lddw, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
+    if (dW && (st = product(1, 0, 2 * F, K, M, type, pairs, M ? p.ld_pair : 2 * F, a.x, M ? a.ld_x : K, type, dW, lddw, gemm_ws, p.gemm_b, s,
+                            who)) != ISAM_OK)
         return st;
     if (dbias) {
         const ColSum sum{bias_part, dbias, p.bias_rows, 2 * F, 1, kF32};

@@ -174,6 +174,7 @@ __global__ __launch_bounds__(256, 2) void gated_f32_kernel(GatedArgs a, TileMapA
             __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(s * U), ro, (int)to, 0, 0);
         }
     });
+    if (BWD && f0 + kGatedF32Tile >= a.F) gated_pad<4>(a, m0, (int)min(kGatedF32Tile, a.M - m0), threadIdx.x, 256);
     if (BWD && a.bias_part) {  // one partial row for every 16 rows
         static_for<2>([&](auto k) {
             sg += __shfl_xor(sg, 16 << decltype(k)::value);

@@ -84,6 +84,22 @@ __device__ __forceinline__ void gated_store8(__amdgpu_buffer_rsrc_t rs, uint32_t
 }
 __device__ __forceinline__ uint32_t gated_bytes(int64_t rows, int64_t cols, int64_t ld) { return (uint32_t)(((rows - 1) * ld + cols) * 2); }
 
+// Zeros after the 2F gradients of each of a tile's rows, up to the end of the last 16-byte piece (the products
+// that follow may multiply what they read there by zero).
+template <int ES>
+__device__ __forceinline__ void gated_pad(const GatedArgs& a, int64_t m0, int rows, int tid, int threads) {
+    const __amdgpu_buffer_rsrc_t ro = make_rsrc(a.out, (uint32_t)(a.M * a.ld_out * ES));
+    const int pad = (int)(a.ld_out - 2 * a.F);
+#pragma unroll 1
+    for (int r = tid; r < rows; r += threads) {
+        const uint32_t at = (uint32_t)(((m0 + r) * a.ld_out + 2 * a.F) * ES);
+        static_for<6>([&](auto e) {  // (2F is even)
+            if constexpr (ES == 2) __builtin_amdgcn_raw_buffer_store_b16((short)0, ro, (int)(e < pad ? at + 2u * e : kOob), 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b32(0, ro, (int)(e < pad ? at + 4u * e : kOob), 0, 0);
+        });
+    }
+}
+
 // Epilogue of a tile of BM rows and HB = BN / 2 values of f.  `smem` is idle.
 template <int ACT, bool BWD, bool WHOLE, int BM, int HB, int WM, int WTM, int MI, int NT>
 __device__ __forceinline__ void gated_epilogue(const GatedArgs& a, f32x16_t (&acc)[MI][2], char* smem, int64_t m0, int64_t f0,
@@ -163,6 +179,9 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& a, f32x16_t (&ac
         const int n = r < rows ? valid : 0;
         gated_store8<WHOLE>(ro, at + (uint32_t)r * step, n, *reinterpret_cast<const uint4*>(src));
         if constexpr (BWD) gated_store8<WHOLE>(ro, at + (uint32_t)r * step + half, n, *reinterpret_cast<const uint4*>(src + TILE));
+    }
+    if constexpr (BWD && !WHOLE) {
+        if (f0 + HB >= a.F) gated_pad<2>(a, m0, rows, tid, NT);
     }
 }
 
