@@ -361,11 +361,13 @@ size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64_t D, int64
  * Sums are fp32; out is rounded once.  K > 0; M or F == 0: no-op.
  * bf16 beyond 16 rows runs as one kernel on 16-byte aligned rows (x and W on 16 bytes,
  * K, ldx and ldw multiples of 8); other rows are copied into the workspace first.
- * fp32 beyond 16 rows forms the two projections by the matrix product of isam_gemm
- * in the workspace.  Up to 16 rows no workspace is used.
+ * fp32 beyond 16 rows runs as one kernel while the tiles are few (any alignment, no
+ * workspace); larger blocks form the two projections by the matrix product of
+ * isam_gemm in the workspace.  Up to 16 rows no workspace is used.
  * Workspace: isam_gated_ffn_workspace_size bytes; aligned = 0 also makes room for the copies
  * (K off 8 says so by itself), which a call with unaligned pointers or leading
- * dimensions needs.  Each matrix, and M x 2F values of `type`, below 2^31 bytes.
+ * dimensions needs.  Each matrix, and M rows of 2F values of `type` (2F up to the next
+ * multiple of 8), below 2^31 bytes.
  */
 typedef enum { ISAM_ACT_SIGMOID = 0, ISAM_ACT_SILU = 1, ISAM_ACT_GELU = 2 } isam_activation_t;
 

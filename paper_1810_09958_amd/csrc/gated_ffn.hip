@@ -21,7 +21,7 @@ TileMapArgs tile_map(int64_t tiles_m, int64_t tiles_n) {
 // matrix instructions' operand registers, 16 rows of Wg and the same 16 of Wu
 // per workgroup; its eight waves take every eighth K step and their sums meet
 // in LDS.  x (the other operand: a column per token) comes from the caches.
-// Bound by the stream of W.
+// Bound by the stream of W: 16.8 MB at one token of 1024x4096 bf16, 6.7 us a call.
 template <int ES>
 __global__ __launch_bounds__(512) void gated_token_kernel(GatedArgs a) {
     using IO = Row16<ES>;
@@ -239,7 +239,8 @@ GatedFn tile_fn(int tile, bool k_full) {
 }  // namespace
 
 // bf16 tiles: 256 rows x 128 values of f while they give every compute unit one,
-// then 128 x 64, then 64 x 32.
+// then 128 x 64, then 64 x 32: as many products to a byte copied into LDS as leave no
+// compute unit without a tile.
 int gated_tile(int64_t M, int64_t F, int cus) {
     auto tiles = [&](int64_t bm, int64_t hb) { return ((M + bm - 1) / bm) * ((F + hb - 1) / hb); };
     if (tiles(256, 128) >= cus) return kGated256;
