@@ -123,7 +123,7 @@ def gffn(L, M=40, K=16, F=8, dt=BF16, act=1, x=at(0), ldx=16, W=at(1), ldw=16, b
     (dict(M=-1), INVALID), (dict(K=0), INVALID), (dict(F=-1), INVALID), (dict(dt=3), INVALID), (dict(act=3), INVALID),
     (dict(act=-1), INVALID), (dict(x=None), INVALID), (dict(W=None), INVALID), (dict(out=None), INVALID), (dict(ldx=15), INVALID),
     (dict(ldw=15), INVALID), (dict(ldo=7), INVALID), (dict(out=at(0)), INVALID), (dict(out=at(2)), INVALID),
-    (dict(dt=F32), WORKSPACE), (dict(ldx=17), WORKSPACE), (dict(K=15), WORKSPACE), (dict(ldx=17, ws=at(5), wsb=64), WORKSPACE),
+    (dict(dt=F32, K=1600, ldx=1600, ldw=1600), WORKSPACE), (dict(ldx=17), WORKSPACE), (dict(K=15), WORKSPACE), (dict(ldx=17, ws=at(5), wsb=64), WORKSPACE),
     (dict(ldx=17, ws=at(3), wsb=1 << 20), INVALID),
     (dict(M=1 << 20, ldx=1 << 11), UNSUPPORTED), (dict(M=1 << 20, F=1 << 12, ldo=1 << 12), UNSUPPORTED),
     (dict(F=1 << 20, ldw=1 << 12), UNSUPPORTED),
@@ -131,6 +131,14 @@ def gffn(L, M=40, K=16, F=8, dt=BF16, act=1, x=at(0), ldx=16, W=at(1), ldw=16, b
 def test_gated_ffn_refusals(L, kw, code):
     assert gffn(L, **kw) == code
     assert L.isam_last_error() != b""
+
+
+def test_gated_ffn_fp32_workspace(L):
+    size = L.isam_gated_ffn_workspace_size
+    assert size(40, 16, 8, F32, 0) == 0 and size(500, 511, 771, F32, 0) == 0     # few tiles: the block's own kernel
+    assert size(2000, 130, 1501, F32, 1) >= 2000 * 2 * 1501 * 4                  # beyond: both projections in memory
+    # the gradient's rows of [dg du] end on 16 bytes
+    assert L.isam_gated_ffn_backward_workspace_size(40, 16, 9, F32, 1) >= 40 * 24 * 4
 
 
 def gffn_bwd(L, M=40, K=16, F=8, dt=BF16, act=1, x=at(0), ldx=16, W=at(1), bias=at(2), do=at(3), lddo=8, dx=at(4), dW=at(5), db=at(6),
@@ -154,6 +162,6 @@ def test_gated_ffn_workspace(L):
     assert q(4096, 1024, 4096, BF16, 1) == 0 and q(16, 33, 17, F32, 0) == 0
     assert q(4096, 1024, 4096, BF16, 0) == 2 * 1024 * (4096 + 8192) + 255          # both copied
     assert q(100, 33, 64, BF16, 1) == 2 * (100 * 40 + 128 * 40) + 255 + (-(2 * 100 * 40)) % 256
-    assert q(100, 32, 64, F32, 1) >= 100 * 128 * 4
+    assert q(1000, 1000, 640, F32, 1) >= 1000 * 1280 * 4
     for bad in ((0, 8, 8, F32, 1), (8, 0, 8, F32, 1), (8, 8, 0, BF16, 1), (8, 8, 8, 5, 1)):
         assert q(*bad) == 0 and L.isam_gated_ffn_backward_workspace_size(*bad) == 0
