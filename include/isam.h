@@ -384,8 +384,9 @@ size_t isam_gated_ffn_workspace_size(int64_t M, int64_t K, int64_t F, int type, 
  *   dx = dg . W[0:F] + du . W[F:2F],  dW = [dg du]^T . x,  dbias = column sums of [dg du]
  *   dx [M][K] (type) at lddx >= K, dW [2*F][K] (type) at lddw >= K, dbias [2*F] fp32;
  *   each may be NULL, not all
- * bf16: dg and du are rounded to bf16 as the operands of the products (dbias is summed
- * from the unrounded values).  Everything else is fp32.  Sums are in a fixed order.
+ * bf16: dg and du are rounded to bf16 as the operands of the products; over up to 16 rows,
+ * which do not average that out, they enter as two bf16 terms instead.  dbias is summed
+ * from the unrounded values.  Everything else is fp32.  Sums are in a fixed order.
  * M == 0: dW and dbias are 0.
  */
 isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F, int type, int act, const void* x, int64_t ldx,

@@ -410,11 +410,12 @@ struct GatedPlan {
     int64_t Kp;                       // row length of the copies
     int64_t ld_pair;                  // of the projections or their gradients
     bool copy_x, copy_w;
+    bool terms;                       // a gradient of few rows: [dG dU] in two bf16 terms, 2 M rows
     bool direct;                      // fp32 projections formed in the block's own kernel
     int tile;
     int64_t bias_rows;                // partial sums of the bias gradient
-    size_t x_b, w_b, pair_b, bias_b, gemm_b;
-    size_t total() const { return x_b + w_b + pair_b + bias_b + gemm_b; }
+    size_t x_b, w_b, pair_b, bias_b, join_b, gemm_b;
+    size_t total() const { return x_b + w_b + pair_b + bias_b + join_b + gemm_b; }
 };
 
 bool rows_aligned(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
@@ -425,6 +426,19 @@ GatedPlan gated_plan(int64_t M, int64_t K, int64_t F, int type, bool x_ok, bool 
     GatedPlan p{};
     const size_t es = dsize(type);
     if (M == 0 || (!backward && M <= kGatedTokens)) return p;
+    p.terms = backward && type == ISAM_BF16 && M <= kGatedTokens && (__int128)2 * M * gated_ld_pair(F) * 2 <= kMaxExtent &&
+              (__int128)2 * M * (K + 8) * 4 <= kMaxExtent;
+    if (p.terms) {
+        p.Kp = cdiv(K, 8) * 8;
+        p.x_b = align256((size_t)(2 * M * p.Kp) * es);  // x twice, a row for each row of the terms
+        p.ld_pair = gated_ld_pair(F);
+        p.pair_b = align256((size_t)(2 * M * p.ld_pair) * es);
+        p.bias_rows = 1;
+        p.bias_b = align256((size_t)(2 * F) * sizeof(float));
+        p.join_b = align256((size_t)(2 * M * K) * sizeof(float));
+        p.gemm_b = align256(std::max(product_workspace(0, 0, 2 * M, K, 2 * F, type), product_workspace(1, 0, 2 * F, K, 2 * M, type)));
+        return p;
+    }
     if (type == ISAM_BF16) {
         p.copy_x = !x_ok || K % 8;
         p.copy_w = !w_ok || K % 8;
@@ -545,7 +559,7 @@ extern "C" isam_status_t isam_gated_ffn(int64_t M, int64_t K, int64_t F, int typ
     a.ld_out = ldo;
     hipError_t e;
     if (M <= kGatedTokens) {
-        e = launch_gated_tokens(a, type, s);
+        e = launch_gated_tokens(a, type, false, s);
     } else if (type == ISAM_BF16) {
         e = gated_copies(p, ws, a, s);
         if (e == hipSuccess) e = launch_gated_tiles(a, p.tile, false, s);
@@ -600,7 +614,8 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
     char* ws = room_start(workspace);
     char* const pairs = ws + p.x_b + p.w_b;
     float* const bias_part = reinterpret_cast<float*>(pairs + p.pair_b);
-    char* const gemm_ws = pairs + p.pair_b + p.bias_b;
+    float* const join = reinterpret_cast<float*>(pairs + p.pair_b + p.bias_b);
+    char* const gemm_ws = pairs + p.pair_b + p.bias_b + p.join_b;
     hipError_t e = hipSuccess;
     GatedArgs a{};
     if (M > 0) {
@@ -618,7 +633,15 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
         a.dout = dout;
         a.ld_dout = lddo;
         a.bias_part = dbias ? bias_part : nullptr;
-        if (type == ISAM_BF16) {
+        if (p.terms) {
+            e = launch_gated_tokens(a, type, true, s);
+            if (e == hipSuccess && dW) {
+                const PackRows x1{static_cast<const uint16_t*>(x), M, K, ldx, reinterpret_cast<uint16_t*>(ws), p.Kp};
+                PackRows x2 = x1;
+                x2.dst += M * p.Kp;
+                e = launch_pack_rows(x1, x2, device_cus(), s);
+            }
+        } else if (type == ISAM_BF16) {
             e = gated_copies(p, ws, a, s);
             if (e == hipSuccess) e = launch_gated_tiles(a, p.tile, true, s);
         } else if (p.direct) {
@@ -630,11 +653,26 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
             e = launch_gated_pairs(a, true, s);
         }
         if (e != hipSuccess) return hip_fail(e, who);
+        if (p.terms && dx) {
+            st = product(0, 0, 2 * M, K, 2 * F, type, pairs, p.ld_pair, W, ldw, ISAM_F32, join, K, gemm_ws, p.gemm_b, s, who);
+            if (st != ISAM_OK) return st;
+            GatedArgs sum{};
+            sum.M = M;
+            sum.K = K;
+            sum.gu = join;
+            sum.out = dx;
+            sum.ld_out = lddx;
+            if ((e = launch_gated_join(sum, s)) != hipSuccess) return hip_fail(e, who);
+        }
         // (of x and W the aligned copies, where the plan has them)
-        if (dx && (st = product(0, 0, M, K, 2 * F, type, pairs, p.ld_pair, a.W, a.ld_w, type, dx, lddx, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
+        if (!p.terms && dx && (st = product(0, 0, M, K, 2 * F, type, pairs, p.ld_pair, a.W, a.ld_w, type, dx, lddx, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
             return st;
     }
-    if (dW && (st = product(1, 0, 2 * F, K, M, type, pairs, M ? p.ld_pair : 2 * F, a.x, M ? a.ld_x : K, type, dW, lddw, gemm_ws, p.gemm_b, s,
+    if (p.terms && dW) {
+        st = product(1, 0, 2 * F, K, 2 * M, type, pairs, p.ld_pair, ws, p.Kp, type, dW, lddw, gemm_ws, p.gemm_b, s, who);
+        if (st != ISAM_OK) return st;
+    }
+    if (!p.terms && dW && (st = product(1, 0, 2 * F, K, M, type, pairs, M ? p.ld_pair : 2 * F, a.x, M ? a.ld_x : K, type, dW, lddw, gemm_ws, p.gemm_b, s,
                             who)) != ISAM_OK)
         return st;
     if (dbias) {

@@ -22,7 +22,10 @@ TileMapArgs tile_map(int64_t tiles_m, int64_t tiles_n) {
 // per workgroup; its eight waves take every eighth K step and their sums meet
 // in LDS.  x (the other operand: a column per token) comes from the caches.
 // Bound by the stream of W: 16.8 MB at one token of 1024x4096 bf16, 6.7 us a call.
-template <int ES>
+// BWD (bf16): [dG dU] instead, in two bf16 terms, the high ones in rows 0 .. M - 1 and what they
+// leave in rows M .. 2M - 1: over so few rows one rounding of an operand is not averaged
+// out in dW (a norm error of 2.5e-3 and more, against 1.7e-3 of its own rounding).
+template <int ES, bool BWD>
 __global__ __launch_bounds__(512) void gated_token_kernel(GatedArgs a) {
     using IO = Row16<ES>;
     constexpr int E = IO::E, KS = 4 * E, U = 4;  // values of K of a lane, of a step; steps in flight
@@ -52,6 +55,11 @@ __global__ __launch_bounds__(512) void gated_token_kernel(GatedArgs a) {
     }
     static_for<2>([&](auto j) { static_for<4>([&](auto v) { sums[wid][j][v][lane] = acc[j][decltype(v)::value]; }); });
     __syncthreads();
+    if (BWD && f0 + 16 >= a.F) {
+        GatedArgs both = a;
+        both.M = 2 * a.M;
+        gated_pad<2>(both, 0, (int)both.M, threadIdx.x, 512);
+    }
     // thread (v, lane) of the first four waves: f = f0 + 4 g + v, token li
     if (wid >= 4) return;
     const int v = wid;
@@ -61,14 +69,45 @@ __global__ __launch_bounds__(512) void gated_token_kernel(GatedArgs a) {
         Uv += sums[w][1][v][lane];
     }
     const int64_t fo = f0 + 4 * g + v;
-    if (fo >= a.F || li >= a.M) return;
-    if (a.bias) {
+    if (!BWD && (fo >= a.F || li >= a.M)) return;
+    const bool on = fo < a.F && li < a.M;
+    if (a.bias && fo < a.F) {
         G += a.bias[fo];
         Uv += a.bias[a.F + fo];
     }
     float slope;
     const float s = a.act == 0 ? gate_act<0>(G, slope) : a.act == 1 ? gate_act<1>(G, slope) : gate_act<2>(G, slope);
-    IO::put(a.out, (int64_t)li * a.ld_out + fo, s * Uv);
+    if constexpr (!BWD) {
+        IO::put(a.out, (int64_t)li * a.ld_out + fo, s * Uv);
+    } else {
+        const float dp = on ? IO::get(a.dout, (int64_t)li * a.ld_dout + fo) : 0.0f;
+        float d[2] = {on ? dp * Uv * slope : 0.0f, on ? dp * s : 0.0f};
+        if (on) {
+            static_for<2>([&](auto h) {
+                const int64_t at = (int64_t)li * a.ld_out + h * a.F + fo;
+                const float high = bf16_to_f32((uint16_t)pack_bf16_rne(d[h], 0.0f)), low = d[h] - high;
+                IO::put(a.out, at, high);
+                // (nothing is left of what the high term cannot hold: infinities, NaN)
+                IO::put(a.out, at + a.M * a.ld_out, low - low == 0.0f ? low : 0.0f);
+            });
+        }
+        static_for<4>([&](auto k) {
+            static_for<2>([&](auto h) { d[h] += __shfl_xor(d[h], 1 << decltype(k)::value); });
+        });
+        if (a.bias_part && li == 0 && fo < a.F) {
+            a.bias_part[fo] = d[0];
+            a.bias_part[a.F + fo] = d[1];
+        }
+    }
+}
+
+// dx = the sum of the two terms' products, [2][M][K] fp32 at a.gu.
+__global__ __launch_bounds__(256) void gated_join_kernel(GatedArgs a) {
+    const int64_t n = a.M * a.K;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t m = i / a.K;
+        Row16<2>::put(a.out, m * a.ld_out + (i - m * a.K), a.gu[i] + a.gu[n + i]);
+    }
 }
 
 // fp32 blocks of few tiles: 32 rows x 32 values of f, gate and up, on the fp32 matrix
@@ -266,10 +305,16 @@ hipError_t launch_gated_tiles(const GatedArgs& a, int tile, bool backward, hipSt
     return hipGetLastError();
 }
 
-hipError_t launch_gated_tokens(const GatedArgs& a, int type, hipStream_t s) {
-    if (a.M > kGatedTokens || (a.F + 15) / 16 > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((type == kBF16 ? gated_token_kernel<2> : gated_token_kernel<4>), dim3((unsigned)((a.F + 15) / 16)), dim3(512), 0,
-                       s, a);
+hipError_t launch_gated_tokens(const GatedArgs& a, int type, bool backward, hipStream_t s) {
+    if (a.M > kGatedTokens || (a.F + 15) / 16 > INT32_MAX || (backward && type != kBF16)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((backward ? gated_token_kernel<2, true> : type == kBF16 ? gated_token_kernel<2, false> : gated_token_kernel<4, false>),
+                       dim3((unsigned)((a.F + 15) / 16)), dim3(512), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_gated_join(const GatedArgs& a, hipStream_t s) {
+    const int64_t blocks = (a.M * a.K + 255) / 256;
+    hipLaunchKernelGGL(gated_join_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

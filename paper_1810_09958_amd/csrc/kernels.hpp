@@ -333,7 +333,9 @@ struct GatedArgs {
 int gated_tile(int64_t M, int64_t F, int cus);
 int64_t gated_bias_rows(int tile, int64_t M);
 hipError_t launch_gated_tiles(const GatedArgs& a, int tile, bool backward, hipStream_t s);
-hipError_t launch_gated_tokens(const GatedArgs& a, int type, hipStream_t s);
+hipError_t launch_gated_tokens(const GatedArgs& a, int type, bool backward, hipStream_t s);
+// The sum of two [M][K] fp32 matrices at a.gu, as bf16 at a.out.
+hipError_t launch_gated_join(const GatedArgs& a, hipStream_t s);
 // fp32 without the library's product: whether it is taken, and its launch.
 bool gated_f32_direct(int64_t M, int64_t K, int64_t F, int cus);
 hipError_t launch_gated_f32(const GatedArgs& a, bool backward, hipStream_t s);
