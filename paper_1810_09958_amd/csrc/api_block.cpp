@@ -403,9 +403,9 @@ extern "C" size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64
 // ---------------------------------------------------------------------------
 namespace {
 
-// Parts of the workspace, in order: copies of x and W with aligned rows, the
-// projections (fp32) or their gradients, the bias gradient's partial sums, and
-// what the matrix products use.
+// Parts of the workspace, in order: copies of x (twice for the terms) and W with
+// aligned rows, the projections (fp32) or their gradients, the bias gradient's
+// partial sums, the terms' dx, and what the matrix products use.
 struct GatedPlan {
     int64_t Kp;                       // row length of the copies
     int64_t ld_pair;                  // of the projections or their gradients
