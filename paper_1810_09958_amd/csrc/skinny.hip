@@ -493,7 +493,9 @@ __global__ __launch_bounds__(64 * kF32Waves) void skinny_rows_f32_kernel(GemmArg
 // (B^T[n][k], zero past K; all lanes with the same j read the same
 // address): v_dot2_f32_bf16 for bf16, FMAs for fp32.  K runs in LDS-sized
 // slices; the next batch of A loads is always in flight during the
-// arithmetic.  At the end the 8 lanes of a row are summed (butterfly), then the
+// arithmetic.  What lies behind a row's last value is another row's or nobody's
+// (zero times its infinity or NaN would be NaN), so pieces past K are not loaded and
+// a piece that K ends inside is cut.  At the end the 8 lanes of a row are summed (butterfly), then the
 // 4 waves in wave order through LDS, and C is written.
 constexpr int kNarrowRows = 8;
 constexpr int kNarrowWaves = 4;
@@ -524,16 +526,25 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(GemmArgs a, i
     // loads of batch b+1 are issued before the arithmetic of batch b, and the
     // first batch of a slice before its B^T is staged.
     uint4 av[kNarrowUnroll][PIECES], nx[kNarrowUnroll][PIECES];
-    auto load_batch = [&](uint4 (&dst)[kNarrowUnroll][PIECES], int64_t k0, int blocks, int b) {
+    auto load_batch = [&](uint4 (&dst)[kNarrowUnroll][PIECES], int64_t k0, int len, int b) {
 #pragma unroll
         for (int u = 0; u < kNarrowUnroll; ++u) {
             const int blk = wid + kNarrowWaves * (b * kNarrowUnroll + u);
             const int kk = blk * 64 + j * 8;
-            const bool ok = row_ok && blk < blocks;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p)
-                dst[u][p] = buf_load16(rsA, ok ? a_row + (uint32_t)((k0 + kk) * sizeof(T)) + p * 16 : kOob);
+                dst[u][p] = buf_load16(rsA, row_ok && kk + p * 4 < len ? a_row + (uint32_t)((k0 + kk) * sizeof(T)) + p * 16 : kOob);
         }
+    };
+    // Zeros for the values from `valid` on of a piece.
+    auto cut = [](uint4& v, int valid) {
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (BF) w[q] = valid >= 2 * q + 2 ? w[q] : valid == 2 * q + 1 ? w[q] & 0xffffu : 0u;
+            else w[q] = valid > q ? w[q] : 0u;
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
     };
     for (int64_t k0 = 0; k0 < a.K; k0 += ks_len) {
         const int len = (int)min((int64_t)ks_len, a.K - k0);
@@ -551,19 +562,23 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(GemmArgs a, i
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[e] = v[e];
         }
-        load_batch(nx, k0, blocks, 0);
+        load_batch(nx, k0, len, 0);
         __syncthreads();
         for (int bb = 0; bb < batches; ++bb) {
 #pragma unroll
             for (int u = 0; u < kNarrowUnroll; ++u)
 #pragma unroll
                 for (int p = 0; p < PIECES; ++p) av[u][p] = nx[u][p];
-            if (bb + 1 < batches) load_batch(nx, k0, blocks, bb + 1);
+            if (bb + 1 < batches) load_batch(nx, k0, len, bb + 1);
 #pragma unroll
             for (int u = 0; u < kNarrowUnroll; ++u) {
                 const int blk = wid + kNarrowWaves * (bb * kNarrowUnroll + u);
                 if (blk >= blocks) break;
                 const int kk = blk * 64 + j * 8;
+                if (kk < len && kk + 8 > len) {
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) cut(av[u][p], len - kk - p * 4);
+                }
 #pragma unroll
                 for (int n = 0; n < 7; ++n) {
                     if (n >= N) break;

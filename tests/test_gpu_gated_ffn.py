@@ -287,3 +287,15 @@ def test_refusals():
     with pytest.raises(isam.IsamError) as e:     # copies need room
         isam.gated_ffn(y["x"], y["W"], workspace=torch.empty(8, device="cuda", dtype=torch.uint8))
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,K,F", [(130, 7, 9), (5, 7, 9), (130, 7, 40), (130, 1, 33), (300, 72, 41)])
+def test_bad_row_stays_with_itself_in_dx(M, K, F, dtype):
+    x = inputs(M, K, F, dtype, seed=2)
+    good = isam.gated_ffn_backward(x["x"], x["W"], x["dout"], bias=x["bias"])[0]
+    x["dout"][1] = float("nan")
+    bad = isam.gated_ffn_backward(x["x"], x["W"], x["dout"], bias=x["bias"])[0]
+    keep = [i for i in range(M) if i != 1]
+    assert torch.isnan(bad[1].float()).all()
+    assert torch.equal(bad[keep], good[keep])

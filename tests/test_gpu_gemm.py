@@ -650,3 +650,25 @@ def test_operand_at_the_extent_limit(dt, K):
     assert norm_err(got, ref, S) <= (TOL_BF16 if dt == "bf16" else TOL_F32)
     del A, C
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("K", [18, 72, 1000, 7200])
+@pytest.mark.parametrize("N", [1, 2, 3, 4, 5, 6, 7, 8])
+def test_few_columns_keep_rows_apart(N, K, dtype):
+    # what lies behind a row of A (padding, then the next row) stays out of its products, NaN and
+    # infinities too: dense rows and rows in a wider matrix, K on and off the vector width
+    g = torch.Generator().manual_seed(N + K)
+    M = 70
+    A, B = torch.randn((M, K), generator=g).to(dtype).cuda(), torch.randn((K, N), generator=g).to(dtype).cuda()
+    for ld in (K, -(-K // 8) * 8, -(-K // 8) * 8 + 72):
+        wide = torch.zeros((M, ld), device="cuda", dtype=dtype)
+        wide[:, :K] = A
+        good = isam.gemm(wide[:, :K], B)
+        for bad in (float("nan"), float("inf")):
+            wide[:, K:] = bad
+            wide[5] = bad
+            got = isam.gemm(wide[:, :K], B)
+            keep = torch.arange(M, device="cuda") != 5
+            assert torch.equal(got[keep], good[keep]), (ld, bad)
+            assert not torch.isfinite(got[5]).any()
