@@ -273,7 +273,9 @@ isam_status_t isam_conv1d(int64_t batch, int64_t L, int64_t Ki, int64_t D, int64
  *   states  [ceil(T / 128)][batch][hidden] fp32, or NULL: the state before steps
  *           0, 128, 256, ...: what the backward pass needs of the forward pass
  * At least one of h_seq, h_T and states.  T == 0: h_T = h0 (or zeros); batch or
- * hidden == 0: no-op.  The state is fp32 throughout; h_seq is rounded once.
+ * hidden == 0: no-op.  The state is fp32 throughout; h_seq is rounded once.  Gates and
+ * candidates are formed from the sum with the bias, to a few units of 2^-24 relative to
+ * themselves however small they are.
  * Results repeat bit for bit.  Tensors may pass 2^31 bytes here, as long as 32
  * steps of each stay below.
  * Workspace: isam_linear_gru_workspace_size bytes (0 up to 256 steps; beyond, the

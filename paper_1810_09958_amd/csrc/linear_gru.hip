@@ -179,25 +179,30 @@ __device__ __forceinline__ void store_channels(float* p, int64_t at, int64_t H, 
 
 constexpr float kLog2e = 1.44269504f;
 
-// z = sigmoid(v) and 1 - z from w = -v log2(e), each to fp32 accuracy also where it is
-// small (1 - z formed from z would lose the digits that decide how long a state
-// lives).  The bound on w keeps 2^w z finite; a NaN passes.
-__device__ __forceinline__ void gate_pair(float w, float& z, float& omz) {
-    const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(w, 126.0f));
+// z = sigmoid(v) and 1 - z, each to fp32 accuracy also where it is small (1 - z formed
+// from z would lose the digits that decide how long a state lives).  The bound on the
+// exponent keeps 2^w z finite; a NaN passes.
+__device__ __forceinline__ void gate_pair(float v, float& z, float& omz) {
+    const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(v * -kLog2e, 126.0f));
     z = __builtin_amdgcn_rcpf(1.0f + e);
     omz = e * z;
 }
-// tanh(v) from w = 2 v log2(e), absolute error of a few 2^-24.
+// tanh(v), relative error of some 8 x 2^-24.  Through the exponential alone the difference
+// from 1 would leave an absolute error (5e-5 of values of 1e-3), so below 1/4 it is v + v^3 P(v^2)
+// with P fitted to tanh for the least relative error (0.05 x 2^-24 before rounding).
 template <int ES>
-__device__ __forceinline__ float gate_tanh(float w) {
+__device__ __forceinline__ float gate_tanh(float v) {
+    const float y = v * v, p = __builtin_fmaf(__builtin_fmaf(-0.05143003f, y, 0.13324237f), y, -0.3333324f);
+    const float low = __builtin_fmaf(v, p * y, v);
+    float high;
     if constexpr (ES == 4) {
-        const float t = __builtin_amdgcn_exp2f(-__builtin_fabsf(w));
-        return __builtin_copysignf((1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), w);
+        const float t = __builtin_amdgcn_exp2f(__builtin_fabsf(v) * (-2.0f * kLog2e));
+        high = __builtin_copysignf((1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), v);
+    } else {
+        high = __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * (2.0f * kLog2e))), 1.0f);
     }
-    return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w)), 1.0f);
+    return __builtin_fabsf(v) < 0.25f ? low : high;
 }
-// Factor of the candidate's argument.
-__device__ __forceinline__ float candidate_scale(const LinGruArgs& a) { return a.candidate ? 2.0f * kLog2e : 1.0f; }
 
 // Inclusive scan over the wave's four groups in time order (UP) or against it.
 template <bool RESET, bool UP>
@@ -353,11 +358,6 @@ __global__ __launch_bounds__(NW * 64, 4) void lingru_fwd_kernel(LinGruArgs a) {
     float bz[4], bn[4];
     load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
     load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
-    const float scale = candidate_scale(a);
-    static_for<4>([&](auto e) {
-        bz[e] *= -kLog2e;
-        bn[e] *= scale;
-    });
 
     // (a step that does not exist leaves the state as it is, whatever the bias)
     float ca[R][4], cb[R][4], A[4], B[4];
@@ -366,11 +366,11 @@ __global__ __launch_bounds__(NW * 64, 4) void lingru_fwd_kernel(LinGruArgs a) {
         float gz[4], n[4];
         S::unpack(pz[r], gz);
         S::unpack(pn[r], n);
-        static_for<4>([&](auto e) { n[e] = __builtin_fmaf(n[e], scale, bn[e]); });
+        static_for<4>([&](auto e) { n[e] += bn[e]; });
         if (a.candidate) static_for<4>([&](auto e) { n[e] = gate_tanh<ES>(n[e]); });
         static_for<4>([&](auto e) {
             float z, omz;
-            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z, omz);
+            gate_pair(gz[e] + bz[e], z, omz);
             ca[r][e] = in ? z : 1.0f;
             cb[r][e] = in ? omz * n[e] : 0.0f;
             step<RESET>(drop, r == 0, ca[r][e], cb[r][e], A[e], B[e]);
@@ -445,12 +445,11 @@ __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
         }
     });
     if (a.states && T > 0) a.states[i] = h;
-    const float scale = candidate_scale(a);
     static_for<kFewSteps>([&](auto t) {
         if (t < T) {
             float z, omz;
-            gate_pair(__builtin_fmaf(gz[t], -kLog2e, bz * -kLog2e), z, omz);
-            const float v = __builtin_fmaf(gn[t], scale, bn * scale), n = a.candidate ? gate_tanh<ES>(v) : v;
+            gate_pair(gz[t] + bz, z, omz);
+            const float v = gn[t] + bn, n = a.candidate ? gate_tanh<ES>(v) : v;
             h = drop[t] ? omz * n : __builtin_fmaf(z, h, omz * n);
             if (a.h_seq) Row16<ES>::put(a.h_seq, b * a.h_b + t * a.h_t + c, h);
         }
@@ -488,11 +487,6 @@ __global__ __launch_bounds__(NW * 64, ES == 2 && VEC ? 3 : 2) void lingru_bwd_ke
     float bz[4], bn[4];
     load_channels<VEC>(a.bias, 0, a.H, c0, lane, bz);
     load_channels<VEC>(a.bias, a.H, a.H, c0, lane, bn);
-    const float scale = candidate_scale(a);
-    static_for<4>([&](auto e) {
-        bz[e] *= -kLog2e;
-        bn[e] *= scale;
-    });
 
     // z, 1 - z and n of each step; (A, B) composes the state, (Z, C) e
     float z[R][4], omz[R][4], n[R][4], A[4], B[4], Z[4], C[4];
@@ -501,10 +495,10 @@ __global__ __launch_bounds__(NW * 64, ES == 2 && VEC ? 3 : 2) void lingru_bwd_ke
         float gz[4];
         S::unpack(pz[r], gz);
         S::unpack(pn[r], n[r]);
-        static_for<4>([&](auto e) { n[r][e] = __builtin_fmaf(n[r][e], scale, bn[e]); });
+        static_for<4>([&](auto e) { n[r][e] += bn[e]; });
         if (a.candidate) static_for<4>([&](auto e) { n[r][e] = gate_tanh<ES>(n[r][e]); });
         static_for<4>([&](auto e) {
-            gate_pair(__builtin_fmaf(gz[e], -kLog2e, bz[e]), z[r][e], omz[r][e]);
+            gate_pair(gz[e] + bz[e], z[r][e], omz[r][e]);
             z[r][e] = in ? z[r][e] : 1.0f;
             omz[r][e] = in ? omz[r][e] : 0.0f;
             n[r][e] = in ? n[r][e] : 0.0f;
