@@ -279,7 +279,8 @@ isam_status_t isam_conv1d(int64_t batch, int64_t L, int64_t Ki, int64_t D, int64
  * Results repeat bit for bit.  Tensors may pass 2^31 bytes here, as long as 32
  * steps of each stay below.
  * Workspace: isam_linear_gru_workspace_size bytes (0 up to 256 steps; beyond, the
- * tiles of time hand the state on through it).
+ * tiles of time hand the state on through it, so two calls must not use it at the same
+ * time; where such a call destroys a state on its way, the states after it are NaN).
  */
 typedef enum { ISAM_LINEAR = 0, ISAM_TANH = 1 } isam_candidate_t;
 

@@ -238,7 +238,7 @@ hipError_t launch_gru_copy_state(const float* h0, float* h_T, int64_t n, hipStre
 constexpr int64_t kLinGruChunk = 128;  // steps between two rows of `states`
 constexpr int kLinGruSteps = 8;                              // steps of a group, four groups to a wave
 constexpr int kLinGruFwdWaves = 8, kLinGruBwdWaves = 4;      // waves of a tile
-constexpr uint64_t kLinGruTimeoutTicks = 200000000ull;   // bound of a wait for an earlier tile (2 s at 100 MHz)
+constexpr int kLinGruLooks = 1 << 22;                    // bound of a wait for an earlier tile, a microsecond or more each
 struct LinGruArgs {
     int64_t T, batch, H;
     int type;                // of gx, h_seq, dh_seq and dgx

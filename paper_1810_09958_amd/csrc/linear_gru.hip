@@ -239,13 +239,15 @@ __device__ __forceinline__ void chain_put(const LinGruArgs& a, int64_t id, int c
     __hip_atomic_store(chain_state(a, id, ch), chain_bits(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 // State that reaches the tile `id`, `before` tiles into its column (lane: channel;
-// whole wave).  `first`: the state before the column's first tile.  NaN if a word
-// should not arrive within 2 s (it is written by a running workgroup).
+// whole wave).  `first`: the state before the column's first tile.  The wait ends: a
+// column's first tile waits for nobody, and every other one for tiles drawn before it, which
+// running workgroups hold.  Only a foreign write to the workspace can take a word away
+// for good; so that this ends too, a wait gives up after some seconds, with NaN.  It counts
+// its looks, not the time: a queue that is taken off the device does not look.
 template <bool RESET>
 __device__ __forceinline__ float chain_in(const LinGruArgs& a, int64_t id, int64_t before, int64_t cols, int lane, float first) {
     constexpr int W = kChainWindow;  // tiles looked at together
-    const uint64_t t0 = wall_clock64();
-    for (;;) {
+    for (int looks = 0; looks < kLinGruLooks; ++looks) {
         uint64_t ab[W];
         uint32_t st[W];
         static_for<W>([&](auto i) {
@@ -275,9 +277,9 @@ __device__ __forceinline__ float chain_in(const LinGruArgs& a, int64_t id, int64
             });
             return v;
         }
-        if (wall_clock64() - t0 > kLinGruTimeoutTicks) return __builtin_nanf("");
         __builtin_amdgcn_s_sleep(1);
     }
+    return __builtin_nanf("");
 }
 
 // Which tile a workgroup has: number, place in its column (from the end if
