@@ -494,9 +494,10 @@ __global__ __launch_bounds__(64 * kF32Waves) void skinny_rows_f32_kernel(GemmArg
 // address): v_dot2_f32_bf16 for bf16, FMAs for fp32.  K runs in LDS-sized
 // slices; the next batch of A loads is always in flight during the
 // arithmetic.  What lies behind a row's last value is another row's or nobody's
-// (zero times its infinity or NaN would be NaN), so pieces past K are not loaded and
-// a piece that K ends inside is cut.  At the end the 8 lanes of a row are summed (butterfly), then the
-// 4 waves in wave order through LDS, and C is written.
+// (zero times its infinity or NaN would be NaN), so only whole pieces are loaded; the
+// last K % 8 values of a row are added one to a lane after the loop.  At the end
+// the 8 lanes of a row are summed (butterfly), then the 4 waves in wave order
+// through LDS, and C is written.
 constexpr int kNarrowRows = 8;
 constexpr int kNarrowWaves = 4;
 constexpr int kNarrowSliceBytes = 64 * 1024;  // B^T slice in LDS
@@ -531,20 +532,11 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(GemmArgs a, i
         for (int u = 0; u < kNarrowUnroll; ++u) {
             const int blk = wid + kNarrowWaves * (b * kNarrowUnroll + u);
             const int kk = blk * 64 + j * 8;
+            const bool ok = row_ok && kk + 8 <= len;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p)
-                dst[u][p] = buf_load16(rsA, row_ok && kk + p * 4 < len ? a_row + (uint32_t)((k0 + kk) * sizeof(T)) + p * 16 : kOob);
+                dst[u][p] = buf_load16(rsA, ok ? a_row + (uint32_t)((k0 + kk) * sizeof(T)) + p * 16 : kOob);
         }
-    };
-    // Zeros for the values from `valid` on of a piece.
-    auto cut = [](uint4& v, int valid) {
-        uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (BF) w[q] = valid >= 2 * q + 2 ? w[q] : valid == 2 * q + 1 ? w[q] & 0xffffu : 0u;
-            else w[q] = valid > q ? w[q] : 0u;
-        }
-        v = make_uint4(w[0], w[1], w[2], w[3]);
     };
     for (int64_t k0 = 0; k0 < a.K; k0 += ks_len) {
         const int len = (int)min((int64_t)ks_len, a.K - k0);
@@ -575,10 +567,6 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(GemmArgs a, i
                 const int blk = wid + kNarrowWaves * (bb * kNarrowUnroll + u);
                 if (blk >= blocks) break;
                 const int kk = blk * 64 + j * 8;
-                if (kk < len && kk + 8 > len) {
-#pragma unroll
-                    for (int p = 0; p < PIECES; ++p) cut(av[u][p], len - kk - p * 4);
-                }
 #pragma unroll
                 for (int n = 0; n < 7; ++n) {
                     if (n >= N) break;
@@ -604,6 +592,20 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(GemmArgs a, i
                         acc[n] = t;
                     }
                 }
+            }
+        }
+    }
+    if (a.K & 7) {  // (the last slice's B^T is still in LDS)
+        const int64_t k0 = (a.K - 1) / ks_len * ks_len;
+        const int kk = ((int)(a.K - k0) & ~7) + j;
+        if (wid == 0 && row_ok && k0 + kk < a.K) {
+            const T v = static_cast<const T*>(a.A)[row * a.lda + k0 + kk];
+#pragma unroll
+            for (int n = 0; n < 7; ++n) {
+                if (n >= N) break;
+                const T w = bt[n * ks_len + kk];
+                if constexpr (BF) acc[n] = fmaf(bf16_to_f32(v), bf16_to_f32(w), acc[n]);
+                else acc[n] = fmaf(v, w, acc[n]);
             }
         }
     }

@@ -672,3 +672,11 @@ def test_few_columns_keep_rows_apart(N, K, dtype):
             keep = torch.arange(M, device="cuda") != 5
             assert torch.equal(got[keep], good[keep]), (ld, bad)
             assert not torch.isfinite(got[5]).any()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 3, 7])
+def test_few_columns_last_values(dt, N):
+    # K off the vector width in aligned rows: within one piece, behind whole ones, in a second slice of B^T
+    for M, K, pad in [(1, 3, 5), (70, 18, 6), (129, 1001, 7), (33, 9367, 1), (40, 7175, 1), (65, 524, 4)]:
+        _run_case(M, N, K, dt, "f32", seed=M + K + N, pad_ld=pad)
