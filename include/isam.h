@@ -277,7 +277,7 @@ isam_status_t isam_conv1d(int64_t batch, int64_t L, int64_t Ki, int64_t D, int64
  * candidates are formed from the sum with the bias, to a few units of 2^-24 relative to
  * themselves however small they are.
  * Results repeat bit for bit.  Tensors may pass 2^31 bytes here, as long as 32
- * steps of each stay below.
+ * steps of each stay below (one step, and up to 8 without a gradient: any stride).
  * Workspace: isam_linear_gru_workspace_size bytes (0 up to 256 steps; beyond, the
  * tiles of time hand the state on through it, so two calls must not use it at the same
  * time; where such a call destroys a state on its way, the states after it are NaN).

@@ -100,13 +100,14 @@ extern "C" isam_status_t isam_linear_gru(int64_t T, int64_t batch, int64_t hidde
     if (need && (!workspace || workspace_bytes < room(need)))
         return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
                     room(need));
+    if (T == 1) gx_stride_t = h_stride_t = reset_stride_t = 0;  // (one step: no second one to stride to)
     size_t gx_b, h_b, r_b;
     if (!extent(T, gx_stride_t, batch, gx_stride_b, 2 * hidden, es, &gx_b) ||
         !extent(h_seq ? T : 0, h_stride_t, batch, h_stride_b, hidden, es, &h_b) ||
         !extent(reset ? T : 0, reset_stride_t, batch, reset_stride_b, 1, 1, &r_b))
         return fail(ISAM_ERR_UNSUPPORTED, "%s: a tensor spans more than 2^46 bytes", who);
-    if (!lingru_strides(gx_stride_t, 2 * hidden, es) || (h_seq && !lingru_strides(h_stride_t, hidden, es)) ||
-        (reset && !lingru_strides(reset_stride_t, 1, 1)))
+    if (T > kLinGruFew && (!lingru_strides(gx_stride_t, 2 * hidden, es) || (h_seq && !lingru_strides(h_stride_t, hidden, es)) ||
+                           (reset && !lingru_strides(reset_stride_t, 1, 1))))
         return fail(ISAM_ERR_UNSUPPORTED, "%s: 32 steps of a tensor span more than 2^31 bytes", who);
     const Tensor all[] = {{"gx", gx, gx_b, false},
                           {"bias", bias, (size_t)(2 * hidden) * 4, false},
@@ -170,6 +171,7 @@ extern "C" isam_status_t isam_linear_gru_backward(int64_t T, int64_t batch, int6
     if (need && (!workspace || workspace_bytes < room(need)))
         return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0,
                     room(need));
+    if (T == 1) gx_stride_t = dgx_stride_t = dh_stride_t = reset_stride_t = 0;
     size_t gx_b, dg_b, dh_b, r_b;
     if (!extent(T, gx_stride_t, batch, gx_stride_b, 2 * hidden, es, &gx_b) ||
         !extent(T, dgx_stride_t, batch, dgx_stride_b, 2 * hidden, es, &dg_b) ||

@@ -236,6 +236,7 @@ hipError_t launch_gru_copy_state(const float* h0, float* h_T, int64_t n, hipStre
 
 // Linear GRU (linear_gru.hip).  Strides in elements; rows are [2H] (gx, dgx) or [H].
 constexpr int64_t kLinGruChunk = 128;  // steps between two rows of `states`
+constexpr int kLinGruFew = 8;                                // steps forward up to which no tile is formed (64-bit offsets)
 constexpr int kLinGruSteps = 8;                              // steps of a group, four groups to a wave
 constexpr int kLinGruFwdWaves = 8, kLinGruBwdWaves = 4;      // waves of a tile
 constexpr int kLinGruLooks = 1 << 22;                    // bound of a wait for an earlier tile, a microsecond or more each

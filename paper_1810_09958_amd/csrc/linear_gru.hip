@@ -428,18 +428,17 @@ __global__ __launch_bounds__(NW * 64, 4) void lingru_fwd_kernel(LinGruArgs a) {
 
 // A few steps, one thread per channel: decoding (no tile to fill).  Bound by one
 // memory latency; a step of 32 x 1024 takes 7.7 us a call, most of it the host's.
-constexpr int kFewSteps = 8;
 template <int ES>
 __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x;
     if (i >= a.batch * a.H) return;
     const int64_t b = i / a.H, c = i - b * a.H;
     const int T = (int)a.T;
-    float gz[kFewSteps], gn[kFewSteps];
-    bool drop[kFewSteps];
+    float gz[kLinGruFew], gn[kLinGruFew];
+    bool drop[kLinGruFew];
     float h = a.h0 ? a.h0[i] : 0.0f;
     const float bz = a.bias ? a.bias[c] : 0.0f, bn = a.bias ? a.bias[a.H + c] : 0.0f;
-    static_for<kFewSteps>([&](auto t) {
+    static_for<kLinGruFew>([&](auto t) {
         if (t < T) {
             gz[t] = Row16<ES>::get(a.gx, b * a.gx_b + t * a.gx_t + c);
             gn[t] = Row16<ES>::get(a.gx, b * a.gx_b + t * a.gx_t + a.H + c);
@@ -447,7 +446,7 @@ __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
         }
     });
     if (a.states && T > 0) a.states[i] = h;
-    static_for<kFewSteps>([&](auto t) {
+    static_for<kLinGruFew>([&](auto t) {
         if (t < T) {
             float z, omz;
             gate_pair(gz[t] + bz, z, omz);
@@ -691,7 +690,7 @@ size_t lingru_chain_bytes(int64_t T, int64_t batch, int64_t H, bool backward) {
 
 hipError_t launch_lingru_forward(const LinGruArgs& a, hipStream_t s) {
     const int64_t n = a.batch * a.H;
-    if (a.T > kFewSteps) return a.type == kBF16 ? launch_tiles<2, false>(a, s) : launch_tiles<4, false>(a, s);
+    if (a.T > kLinGruFew) return a.type == kBF16 ? launch_tiles<2, false>(a, s) : launch_tiles<4, false>(a, s);
     if ((n + 63) / 64 > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL((a.type == kBF16 ? lingru_few_kernel<2> : lingru_few_kernel<4>), dim3((unsigned)((n + 63) / 64)), dim3(64), 0, s, a);
     return hipGetLastError();

@@ -95,3 +95,41 @@ def _near_steps(T, B, H, dtype, seed):
                                  (128, 66), (129, 66), (127, 40), (128, 40), (129, 40), (384, 40), (385, 40)])
 def test_overlapping_pieces_and_tile_ends(T, H, dtype):
     _near_steps(T, 2, H, dtype, T + H)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_one_step_has_no_stride(dtype):
+    # one step cut out of a tensor whose steps lie 2^29 values apart: forward and backward
+    from tests.test_gpu_linear_gru import check as check_bounds, inputs, reference as full
+    B, H, far = 3, 24, 1 << 29
+    x = inputs(1, B, H, dtype, seed=1, reset=0.5)
+    ref = full(x, "tanh", H)
+
+    def apart(w):
+        return torch.zeros((B, w), device="cuda", dtype=dtype).as_strided((1, B, w), (far, w, 1))
+
+    gx, dh, h, dgx = apart(2 * H), apart(H), apart(H), apart(2 * H)
+    gx.copy_(x["gx"])
+    dh.copy_(x["dh_seq"])
+    reset = x["reset"].contiguous().as_strided((1, B), (1 << 30, 1))
+    states = torch.empty(isam.linear_gru_states_shape(1, B, H), device="cuda")
+    _, h_T = isam.linear_gru(gx, bias=x["bias"], h0=x["h0"], reset=reset, h_seq=h, states=states)
+    _, dh0, db = isam.linear_gru_backward(gx, dh, states=states, bias=x["bias"], reset=reset, dh_T=x["dh_T"], dgx=dgx)
+    for k, v in (("h_seq", h), ("h_T", h_T), ("dgx", dgx), ("dh0", dh0), ("dbias", db)):
+        check_bounds(v, ref[k], k)
+
+
+def test_few_steps_far_apart():
+    # eight steps 2^25 values apart: 32 of them would pass 2^31 bytes
+    from tests.test_gpu_linear_gru import check as check_bounds, inputs, reference as full
+    T, B, H, far = 8, 2, 24, 1 << 25
+    x = inputs(T, B, H, torch.bfloat16, seed=2, train=False)
+    ref = full(x, "tanh", H)
+    gx = torch.empty(((T - 1) * far + 2 * B * H,), device="cuda", dtype=torch.bfloat16).as_strided((T, B, 2 * H), (far, 2 * H, 1))
+    gx.copy_(x["gx"])
+    h, h_T = isam.linear_gru(gx, bias=x["bias"], h0=x["h0"])
+    check_bounds(h, ref["h_seq"], "h_seq")
+    check_bounds(h_T, ref["h_T"], "h_T")
+    with pytest.raises(isam.IsamError) as e:       # a gradient forms tiles of time
+        isam.linear_gru_backward(gx, None, states=torch.empty((1, B, H), device="cuda"), bias=x["bias"])
+    assert e.value.status == 2
