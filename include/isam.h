@@ -390,7 +390,7 @@ size_t isam_gated_ffn_workspace_size(int64_t M, int64_t K, int64_t F, int type, 
  * bf16: dg and du are rounded to bf16 as the operands of the products; over up to 16 rows,
  * which do not average that out, they enter as two bf16 terms instead.  dbias is summed
  * from the unrounded values.  Everything else is fp32.  Sums are in a fixed order.
- * M == 0: dW and dbias are 0.
+ * M == 0: dW and dbias are 0.  F == 0: no-op (with rows and a dx, which would be zeros: an error).
  */
 isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F, int type, int act, const void* x, int64_t ldx,
                                       const void* W, int64_t ldw, const float* bias, const void* dout, int64_t lddo, void* dx,

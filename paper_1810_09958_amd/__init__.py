@@ -508,7 +508,7 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
                        dbias=None, workspace: torch.Tensor | None = None):
     """Gradient of ``gated_ffn`` from dout [M][F]: the projections are formed again, nothing is kept
     from the forward call.  Returns (dx [M][K], dW [2F][K] in x's dtype, dbias [2F] float32 or
-    None without a bias)."""
+    None without a bias).  F = 0: dx is zeros."""
     _on(x, W, dout, bias, dx, dW, dbias, workspace)
     M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
     act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
@@ -521,6 +521,9 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
     _want(dbias, "dbias", (2 * F,))
     lddo, lddx = _matrix(dout, "dout", (M, F), x.dtype), _matrix(dx, "dx", (M, K), x.dtype)
     lddw = _matrix(dW, "dW", (2 * F, K), x.dtype)
+    if F == 0:  # (a sum of nothing; the C entry takes no dx then)
+        dx.zero_()
+        return dx, dW, dbias
     if workspace is None:
         workspace = _room(gated_ffn_backward_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
     rc = lib().isam_gated_ffn_backward(M, K, F, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(dout), lddo, _ptr(dx), lddx,

@@ -299,3 +299,13 @@ def test_bad_row_stays_with_itself_in_dx(M, K, F, dtype):
     keep = [i for i in range(M) if i != 1]
     assert torch.isnan(bad[1].float()).all()
     assert torch.equal(bad[keep], good[keep])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_empty_block_has_zero_gradient(dtype):
+    # no hidden values: the block gives [M][0], and nothing comes back through it
+    for M in (0, 5, 40):
+        x = inputs(M, 24, 0, dtype)
+        dx = torch.full((M, 24), 7.0, device="cuda", dtype=dtype)
+        got, dW, db = isam.gated_ffn_backward(x["x"], x["W"], x["dout"], bias=x["bias"], dx=dx)
+        assert got is dx and (dx == 0).all() and dW.shape == (0, 24) and db.shape == (0,)
