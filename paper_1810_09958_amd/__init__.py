@@ -504,17 +504,18 @@ def gated_ffn(x: torch.Tensor, W: torch.Tensor, *, bias=None, activation="silu",
     return out
 
 
-def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, bias=None, activation="silu", dx=None, dW=None,
-                       dbias=None, workspace: torch.Tensor | None = None):
+def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, bias=None, activation="silu", return_dx=True,
+                       return_dW=True, dx=None, dW=None, dbias=None, workspace: torch.Tensor | None = None):
     """Gradient of ``gated_ffn`` from dout [M][F]: the projections are formed again, nothing is kept
     from the forward call.  Returns (dx [M][K], dW [2F][K] in x's dtype, dbias [2F] float32 or
-    None without a bias).  F = 0: dx is zeros."""
+    None without a bias).  return_dx or return_dW False (frozen inputs or weights): that product is
+    left out, and None stands for it.  F = 0: dx is zeros."""
     _on(x, W, dout, bias, dx, dW, dbias, workspace)
     M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
     act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
-    if dx is None:
+    if dx is None and return_dx:
         dx = torch.empty((M, K), device=dev, dtype=x.dtype)
-    if dW is None:
+    if dW is None and return_dW:
         dW = torch.empty((2 * F, K), device=dev, dtype=x.dtype)
     if dbias is None and bias is not None:
         dbias = torch.empty((2 * F,), device=dev, dtype=torch.float32)
@@ -522,7 +523,8 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
     lddo, lddx = _matrix(dout, "dout", (M, F), x.dtype), _matrix(dx, "dx", (M, K), x.dtype)
     lddw = _matrix(dW, "dW", (2 * F, K), x.dtype)
     if F == 0:  # (a sum of nothing; the C entry takes no dx then)
-        dx.zero_()
+        if dx is not None:
+            dx.zero_()
         return dx, dW, dbias
     if workspace is None:
         workspace = _room(gated_ffn_backward_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)

@@ -309,3 +309,21 @@ def test_empty_block_has_zero_gradient(dtype):
         dx = torch.full((M, 24), 7.0, device="cuda", dtype=dtype)
         got, dW, db = isam.gated_ffn_backward(x["x"], x["W"], x["dout"], bias=x["bias"], dx=dx)
         assert got is dx and (dx == 0).all() and dW.shape == (0, 24) and db.shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,K,F", [(5, 72, 41), (70, 72, 40), (600, 700, 900), (40, 24, 0)])
+def test_parts_of_the_gradient(M, K, F, dtype):
+    # what is asked for alone is what the whole call gives, bit for bit; the rest is None
+    x = inputs(M, K, F, dtype, seed=3)
+    call = lambda **kw: isam.gated_ffn_backward(x["x"], x["W"], x["dout"], bias=x["bias"], **kw)
+    dx, dW, db = call()
+    a, b, c = call(return_dW=False)
+    assert torch.equal(a, dx) and b is None and torch.equal(c, db)
+    a, b, c = call(return_dx=False)
+    assert a is None and torch.equal(b, dW) and torch.equal(c, db)
+    a, b, c = call(return_dx=False, return_dW=False)
+    assert a is None and b is None and torch.equal(c, db)
+    if F:
+        with pytest.raises(isam.IsamError):      # nothing left to form
+            isam.gated_ffn_backward(x["x"], x["W"], x["dout"], return_dx=False, return_dW=False)
