@@ -266,10 +266,12 @@ def _rows(t, name, shape, dtype):
 
 
 def _on(first, *ts):
-    """Checks that every tensor given is on the first one's GPU."""
+    """Checks that every tensor given is on the current GPU, whose stream the call runs on."""
     at = first.get_device()
     if at < 0:
         raise ValueError("tensors must be on the GPU")
+    if at != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current GPU (torch.cuda.set_device)")
     for t in ts:
         if t is not None and t.get_device() != at:
             raise ValueError("tensors must be on one GPU")
