@@ -277,14 +277,19 @@ GatedFn tile_fn(int tile, bool k_full) {
 
 }  // namespace
 
-// bf16 tiles: 256 rows x 128 values of f while they give every compute unit one,
-// then 128 x 64, then 64 x 32: as many products to a byte copied into LDS as leave no
-// compute unit without a tile.
+// bf16 tiles, by the rounds of workgroups they take on the compute units: 64 rows x 32 values of
+// f (two workgroups to a compute unit) while they need one round; else 128 x 64 or 256 x 128, whose
+// round does four times the work in 3.3 times the time. us forward of tiles of 256 / 128 / 64
+// rows (tiles): 512x4096x2048 66 / 34 / 28 (32, 128, 512), 576x4096x2048 64 / 34 / 45 (48, 160, 640),
+// 576x256x2048 10.3 / 6.9 / 8.3, 896x1024x2048 21.5 / 10.8 / 16.9 (64, 224, 896), 1024x1024x4096 25 / 20 / 35
+// (128, 512), 1792x1024x4096 31 / 33 (224, 896), 2048x1024x4096 33 / 36 (256, 1024), 2304x1024x4096
+// 51 / 43 (288, 1152), 2944x1024x4096 53 / 51 (384, 1472), 3328x1024x4096 55 / 58 (416, 1664), 5120x4096x4096
+// 275 / 302 (640, 2560). The backward kernel's times lie alike.
 int gated_tile(int64_t M, int64_t F, int cus) {
     auto tiles = [&](int64_t bm, int64_t hb) { return ((M + bm - 1) / bm) * ((F + hb - 1) / hb); };
-    if (tiles(256, 128) >= cus) return kGated256;
-    if (tiles(128, 64) >= cus) return kGated128;
-    return kGated64;
+    auto rounds = [&](int64_t n) { return (n + cus - 1) / cus; };
+    if (tiles(64, 32) <= 2 * (int64_t)cus) return kGated64;
+    return 10 * rounds(tiles(128, 64)) < 33 * rounds(tiles(256, 128)) ? kGated128 : kGated256;
 }
 
 int64_t gated_bias_rows(int tile, int64_t M) {

@@ -240,8 +240,8 @@ __global__ __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) void gated_dma_ker
     gated_finish<BWD, BM, HB, WM, WTM, MI, 64 * NW>(a, acc, smem, m0, f0, tm, wm, wn, true, tid, lane);
 }
 
-// Small tiles (64 rows, 32 values of f): grids below one 128-row tile per
-// compute unit, bound by the copies' latency.  An LDS ring of four 64-deep K
+// Small tiles (64 rows, 32 values of f): grids of up to two to a compute unit,
+// bound by the copies' latency.  An LDS ring of four 64-deep K
 // tiles; the four waves are two row blocks times two halves of each K tile's
 // steps, summed through LDS at the end, so that each wave still holds a pair of
 // column blocks.

@@ -327,3 +327,12 @@ def test_parts_of_the_gradient(M, K, F, dtype):
     if F:
         with pytest.raises(isam.IsamError):      # nothing left to form
             isam.gated_ffn_backward(x["x"], x["W"], x["dout"], return_dx=False, return_dW=False)
+
+
+# Both sides of the limits between the tiles: one round of small tiles or more, and large tiles whose rounds
+# are nearly full or nearly empty; whole and ragged rows, columns and K.
+@pytest.mark.parametrize("M,K,F", [(512, 72, 2048), (513, 72, 2048), (1000, 63, 1030), (2000, 64, 512), (1537, 64, 4096),
+                                   (1700, 65, 4095), (2047, 63, 4096), (2049, 128, 4096), (2900, 40, 4001), (3200, 64, 4097)])
+def test_tile_limits(M, K, F):
+    for i, name in enumerate(ACTS):
+        compare(inputs(M, K, F, torch.bfloat16, seed=M + i, bias=i != 1), name)
