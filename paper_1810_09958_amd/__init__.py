@@ -510,7 +510,8 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
                        return_dW=True, dx=None, dW=None, dbias=None, workspace: torch.Tensor | None = None):
     """Gradient of ``gated_ffn`` from dout [M][F]: the projections are formed again, nothing is kept
     from the forward call.  Returns (dx [M][K], dW [2F][K] in x's dtype, dbias [2F] float32 or
-    None without a bias).  return_dx or return_dW False (frozen inputs or weights): that product is
+    None without a bias).  bfloat16 beyond 16 rows: the projections' gradients are rounded as the
+    products' operands, so dx and dW carry two roundings.  return_dx or return_dW False (frozen inputs or weights): that product is
     left out, and None stands for it.  F = 0: dx is zeros."""
     _on(x, W, dout, bias, dx, dW, dbias, workspace)
     M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)

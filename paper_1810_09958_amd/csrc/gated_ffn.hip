@@ -23,8 +23,11 @@ TileMapArgs tile_map(int64_t tiles_m, int64_t tiles_n) {
 // in LDS.  x (the other operand: a column per token) comes from the caches.
 // Bound by the stream of W: 16.8 MB at one token of 1024x4096 bf16, 6.7 us a call.
 // BWD (bf16): [dG dU] instead, in two bf16 terms, the high ones in rows 0 .. M - 1 and what they
-// leave in rows M .. 2M - 1: over so few rows one rounding of an operand is not averaged
-// out in dW (a norm error of 2.5e-3 and more, against 1.7e-3 of its own rounding).
+// leave in rows M .. 2M - 1, so that dx and dW carry the rounding of the output alone: a norm error
+// of 1.66e-3, against 2.35e-3 with dG and dU rounded once (at any number of rows: terms and errors
+// grow alike). The price is twice the operations of both products: nothing while W's bytes bound
+// them (dx and dW 12.8 and 14.1 us with one term and 12.9 and 14.2 with two at 16x1024x4096), 95 to
+// 166 us for both at 2048x1024x4096, so blocks of more rows round dG and dU.
 template <int ES, bool BWD>
 __global__ __launch_bounds__(512) void gated_token_kernel(GatedArgs a) {
     using IO = Row16<ES>;

@@ -15,7 +15,8 @@
 // The backward kernel forms G and U again with the same main loop (4 M K F
 // operations, against writing and reading 2 M F values and keeping them from the
 // forward pass) and leaves dG and dU, rounded to bf16 as operands of the two
-// products that follow; the bias gradient is summed from the unrounded values.
+// products that follow (the second rounding in dx and dW; why not two terms stands at
+// gated_token_kernel); the bias gradient is summed from the unrounded values.
 // Bound by the rate of the large product: 8192x2048x8192 437-441 us, 1.25 PFLOP/s (8192^3
 // without an epilogue 1.28 on the same card).  Training step 2048x1024x4096: forward 36 us,
 // this backward kernel 44, dx 53 (128 tiles of 128x128 in two K slices), dW 39 and the
