@@ -44,9 +44,10 @@ except AttributeError:  # pragma: no cover - older torch
     _raw_stream = None
 
 
-def _stream():
+def _stream(device=None):
+    """The current stream of the current GPU (`device`, where the caller has asked for it already)."""
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(torch.cuda.current_device() if device is None else device)
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -266,7 +267,7 @@ def _rows(t, name, shape, dtype):
 
 
 def _on(first, *ts):
-    """Checks that every tensor given is on the current GPU, whose stream the call runs on."""
+    """Checks that every tensor given is on the current GPU, whose stream the call runs on; its number."""
     at = first.get_device()
     if at < 0:
         raise ValueError("tensors must be on the GPU")
@@ -275,6 +276,7 @@ def _on(first, *ts):
     for t in ts:
         if t is not None and t.get_device() != at:
             raise ValueError("tensors must be on one GPU")
+    return at
 
 
 def _room(nbytes, dev):
@@ -319,7 +321,7 @@ def linear_gru(gx: torch.Tensor, *, bias=None, h0=None, reset=None, candidate="t
     reset [T][batch] bool (the step starts from a zero state).  states
     (``linear_gru_states_shape``, float32) receives what ``linear_gru_backward`` needs.
     Returns (h_seq in gx's dtype, h_T in float32)."""
-    _on(gx, bias, h0, reset, h_seq, h_T, states, workspace)
+    at = _on(gx, bias, h0, reset, h_seq, h_T, states, workspace)
     T, B, H, dt, gs, rs = _linear_gru_args(gx, bias, reset)
     cand = _code(_CANDIDATES, candidate, "candidate")
     dev = gx.device
@@ -334,7 +336,7 @@ def linear_gru(gx: torch.Tensor, *, bias=None, h0=None, reset=None, candidate="t
     if workspace is None:
         workspace = _room(linear_gru_workspace_size(T, B, H, dt), dev)
     rc = lib().isam_linear_gru(T, B, H, dt, cand, _ptr(gx), *gs, _ptr(bias), _ptr(h0), _ptr(reset), *rs, _ptr(h_seq), *hs,
-                               _ptr(h_T), _ptr(states), _ptr(workspace), _bytes(workspace), _stream())
+                               _ptr(h_T), _ptr(states), _ptr(workspace), _bytes(workspace), _stream(at))
     _call(rc, "isam_linear_gru")
     return h_seq, h_T
 
@@ -344,7 +346,7 @@ def linear_gru_backward(gx: torch.Tensor, dh_seq: torch.Tensor | None, *, states
     """Gradient of ``linear_gru``: gx, bias, reset, candidate and states as in (and from) the forward
     call, dh_seq [T][batch][H] in gx's dtype or None, dh_T [batch][H] float32 or None.  Returns
     (dgx in gx's dtype, dh0, dbias in float32; dbias is None without a bias unless given)."""
-    _on(gx, dh_seq, states, bias, reset, dh_T, dgx, dh0, dbias, workspace)
+    at = _on(gx, dh_seq, states, bias, reset, dh_T, dgx, dh0, dbias, workspace)
     T, B, H, dt, gs, rs = _linear_gru_args(gx, bias, reset)
     cand = _code(_CANDIDATES, candidate, "candidate")
     dev = gx.device
@@ -364,7 +366,7 @@ def linear_gru_backward(gx: torch.Tensor, dh_seq: torch.Tensor | None, *, states
         workspace = _room(linear_gru_backward_workspace_size(T, B, H, dt), dev)
     rc = lib().isam_linear_gru_backward(T, B, H, dt, cand, _ptr(gx), *gs, _ptr(bias), _ptr(reset), *rs, _ptr(states),
                                         _ptr(dh_seq), *ds, _ptr(dh_T), _ptr(dgx), *dgs, _ptr(dh0), _ptr(dbias),
-                                        _ptr(workspace), _bytes(workspace), _stream())
+                                        _ptr(workspace), _bytes(workspace), _stream(at))
     _call(rc, "isam_linear_gru_backward")
     return dgx, dh0, dbias
 
@@ -410,7 +412,7 @@ def norm_residual(x: torch.Tensor | None, r: torch.Tensor, *, w_pre, w_post=None
     x, r [rows][D] (float32 or bfloat16; row strides may exceed D), gate [gates][D] in their
     dtype with gates a divisor of rows, w_post and w_pre [D] float32.  r_out may be r.
     x None: y = norm of r alone.  Returns (r_out, y); r_out is r without x."""
-    _on(r, x, w_pre, w_post, gate, r_out, y)
+    at = _on(r, x, w_pre, w_post, gate, r_out, y)
     R, D, G = _norm_args(r, gate, w_post, w_pre)
     dt, dev = _dt(r), r.device
     if r_out is None and x is not None:
@@ -421,7 +423,7 @@ def norm_residual(x: torch.Tensor | None, r: torch.Tensor, *, w_pre, w_post=None
     ldx, ldr = _matrix(x, "x", shape, ty), _matrix(r, "r", shape, ty)
     ldro, ldy = _matrix(r_out, "r_out", shape, ty), _matrix(y, "y", shape, ty)
     rc = lib().isam_norm_residual(R, D, G, dt, _ptr(x), ldx, _ptr(r), ldr, _ptr(gate), _ptr(w_post), _ptr(w_pre), scale, eps,
-                                  _ptr(r_out), ldro, _ptr(y), ldy, _stream())
+                                  _ptr(r_out), ldro, _ptr(y), ldy, _stream(at))
     _call(rc, "isam_norm_residual")
     return (r if x is None else r_out), y
 
@@ -432,7 +434,7 @@ def norm_residual_backward(x: torch.Tensor | None, r_out: torch.Tensor, dy: torc
     """Gradient of ``norm_residual``: x, gate, w_post, w_pre, scale and eps as in the forward call, r_out
     as it left it, dy and dr_out (None for zeros) the gradients of y and r_out.  dr may be dr_out.
     Returns (dx, dr, dgate, dw_post, dw_pre), None where the forward call had no such input."""
-    _on(r_out, x, dy, w_pre, w_post, gate, dr_out, dx, dr, dgate, dw_post, dw_pre, workspace)
+    at = _on(r_out, x, dy, w_pre, w_post, gate, dr_out, dx, dr, dgate, dw_post, dw_pre, workspace)
     R, D, G = _norm_args(r_out, gate, w_post, w_pre)
     dt, dev, shape, ty = _dt(r_out), r_out.device, (R, D), r_out.dtype
     if dx is None and x is not None:
@@ -454,7 +456,7 @@ def norm_residual_backward(x: torch.Tensor | None, r_out: torch.Tensor, dy: torc
         R, D, G, dt, _ptr(x), _matrix(x, "x", shape, ty), _ptr(r_out), _matrix(r_out, "r_out", shape, ty), _ptr(gate),
         _ptr(w_post), _ptr(w_pre), scale, eps, _ptr(dy), _matrix(dy, "dy", shape, ty), _ptr(dr_out),
         _matrix(dr_out, "dr_out", shape, ty), _ptr(dx), _matrix(dx, "dx", shape, ty), _ptr(dr), _matrix(dr, "dr", shape, ty),
-        _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(workspace), _bytes(workspace), _stream())
+        _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(workspace), _bytes(workspace), _stream(at))
     _call(rc, "isam_norm_residual_backward")
     return dx, dr, dgate, dw_post, dw_pre
 
@@ -492,7 +494,7 @@ def gated_ffn(x: torch.Tensor, W: torch.Tensor, *, bias=None, activation="silu",
     ("sigmoid", "silu" or "gelu") and the product together.  x [M][K], W [2F][K] (gate rows, then up
     rows; float32 or bfloat16; row strides may exceed K), bias [2F] float32.  Returns out [M][F] in
     x's dtype."""
-    _on(x, W, bias, out, workspace)
+    at = _on(x, W, bias, out, workspace)
     M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
     act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
     if out is None:
@@ -501,7 +503,7 @@ def gated_ffn(x: torch.Tensor, W: torch.Tensor, *, bias=None, activation="silu",
     if workspace is None:
         workspace = _room(gated_ffn_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
     rc = lib().isam_gated_ffn(M, K, F, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(out), ldo, _ptr(workspace),
-                              _bytes(workspace), _stream())
+                              _bytes(workspace), _stream(at))
     _call(rc, "isam_gated_ffn")
     return out
 
@@ -513,7 +515,7 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
     None without a bias).  bfloat16 beyond 16 rows: the projections' gradients are rounded as the
     products' operands, so dx and dW carry two roundings.  return_dx or return_dW False (frozen inputs or weights): that product is
     left out, and None stands for it.  F = 0: dx is zeros."""
-    _on(x, W, dout, bias, dx, dW, dbias, workspace)
+    at = _on(x, W, dout, bias, dx, dW, dbias, workspace)
     M, K, F, dt, ldx, ldw = _gated_args(x, W, bias)
     act, dev = _code(_ACTIVATIONS, activation, "activation"), x.device
     if dx is None and return_dx:
@@ -532,6 +534,6 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
     if workspace is None:
         workspace = _room(gated_ffn_backward_workspace_size(M, K, F, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
     rc = lib().isam_gated_ffn_backward(M, K, F, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(dout), lddo, _ptr(dx), lddx,
-                                       _ptr(dW), lddw, _ptr(dbias), _ptr(workspace), _bytes(workspace), _stream())
+                                       _ptr(dW), lddw, _ptr(dbias), _ptr(workspace), _bytes(workspace), _stream(at))
     _call(rc, "isam_gated_ffn_backward")
     return dx, dW, dbias
