@@ -5,7 +5,8 @@ their gradients, as hand-written HIP kernels behind the C ABI in ``include/isam.
 This module is argument marshalling only: it checks torch tensors (device, dtype,
 contiguity), sizes and allocates the workspace, and calls the C ABI on torch's current
 stream.  Every arithmetic step runs in the library's kernels.  If ``libisam.so`` is
-missing the calls raise; there is no fallback.
+missing the calls raise; there is no fallback.  No call is recorded by torch's autograd,
+whatever its inputs require: gradients come from the ``*_backward`` calls.
 """
 from __future__ import annotations
 

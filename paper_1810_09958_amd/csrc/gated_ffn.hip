@@ -21,7 +21,8 @@ TileMapArgs tile_map(int64_t tiles_m, int64_t tiles_n) {
 // matrix instructions' operand registers, 16 rows of Wg and the same 16 of Wu
 // per workgroup; its eight waves take every eighth K step and their sums meet
 // in LDS.  x (the other operand: a column per token) comes from the caches.
-// Bound by the stream of W: 16.8 MB at one token of 1024x4096 bf16, 6.7 us a call.
+// Bound by the stream of W: 16.8 MB at one token of 1024x4096 bf16, 6.7-7.0 us a call (16
+// tokens 6.4; fp32 8.0 and 8.9).
 // BWD (bf16): [dG dU] instead, in two bf16 terms, the high ones in rows 0 .. M - 1 and what they
 // leave in rows M .. 2M - 1, so that dx and dW carry the rounding of the output alone: a norm error
 // of 1.66e-3, against 2.35e-3 with dG and dU rounded once (at any number of rows: terms and errors

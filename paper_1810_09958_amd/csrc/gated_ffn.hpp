@@ -17,9 +17,9 @@
 // forward pass) and leaves dG and dU, rounded to bf16 as operands of the two
 // products that follow (the second rounding in dx and dW; why not two terms stands at
 // gated_token_kernel); the bias gradient is summed from the unrounded values.
-// Bound by the rate of the large product: 8192x2048x8192 437-441 us, 1.25 PFLOP/s (8192^3
-// without an epilogue 1.28 on the same card).  Training step 2048x1024x4096: forward 36 us,
-// this backward kernel 44, dx 53 (128 tiles of 128x128 in two K slices), dW 39 and the
+// Bound by the rate of the large product: 8192x2048x8192 436 us, 1.26 PFLOP/s (8192^3
+// without an epilogue 1.28-1.33 on the same cards).  Training step 2048x1024x4096: forward 35 us,
+// this backward kernel 44, dx 51 (128 tiles of 128x128 in two K slices), dW 38 and the
 // transposed copy of its operand 13.
 #pragma once
 

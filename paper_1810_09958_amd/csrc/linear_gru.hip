@@ -30,12 +30,14 @@
 //     state before every 128 steps, and each tile forms its states again in
 //     registers while it scans e from its end (5 values moved per element, 6 with
 //     stored states, which would have to be fp32 to give fp32 gradients).
-// Measured, bf16: 32768 steps of 1 x 2048 forward 99 us, 4.1 TB/s (a copy runs at 5.1);
-// forward and backward of 4096 x 8 x 1024 with resets 165 us, 3.3 TB/s, of which the
-// forward kernel 62 and the backward kernel 98.  The vector units are busy 44 % and 50 %
-// of that (30 and 54 instructions a value) and half of the waves' time is waiting: a
+// Measured, bf16: 32768 steps of 1 x 2048 forward 98-100 us, 4.1 TB/s (the residual norm streams
+// at 5.4); forward and backward of 4096 x 8 x 1024 with resets 164 us, 3.3 TB/s, of which the
+// forward kernel 62 and the backward kernel 98.  The vector units are busy 57 % of both
+// (40 and 64 instructions a value) and half of the waves' time is waiting: a
 // tile loads, computes, waits for the chain and stores, and only the two or three
-// workgroups that the registers let a compute unit hold cover for each other.  Of tile
+// workgroups that the registers let a compute unit hold cover for each other.  The chain by
+// itself, 32768 steps of a single column (1 x 64), takes 49 us forward and 97 backward.  fp32:
+// 32768 x 1 x 2048 forward 153 us (5.3 TB/s), 4096 x 8 x 1024 84 and 149.  Of tile
 // sizes: forward tiles of four waves (twice as many links) 122 us for the long sequence
 // against 99; backward tiles of eight waves at two waves a SIMD 123, of four at two 113,
 // of four at three 98 (a look of four tiles back instead of two takes the registers for
@@ -427,7 +429,7 @@ __global__ __launch_bounds__(NW * 64, 4) void lingru_fwd_kernel(LinGruArgs a) {
 }
 
 // A few steps, one thread per channel: decoding (no tile to fill).  Bound by one
-// memory latency; a step of 32 x 1024 takes 7.7 us a call, most of it the host's.
+// memory latency; a step of 32 x 1024 takes 7.7-8 us a call, most of it the host's.
 template <int ES>
 __global__ __launch_bounds__(64) void lingru_few_kernel(LinGruArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x;

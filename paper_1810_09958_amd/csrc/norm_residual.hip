@@ -17,9 +17,9 @@
 // in a fixed order by a second kernel (colsum.hip).  Everything is fp32 between
 // the loads and the stores: y is normalised from the unrounded r'.  Measured, bf16: forward
 // 32768 x 2048 99 us, 5.4 TB/s (a copy runs at 5.1); gradient of 8192 x 4096 with eight
-// gate rows 94-96 us, 4.2 TB/s: 85 and a second launch of 9 for the sums over rows; fp32 gradient of
-// 1001 x 1537 with a gate to each element 17 us; 32 x 1024 forward 7.7 us a call, most of it
-// the host's.
+// gate rows 94-97 us, 4.2 TB/s: 86 and a second launch of 9 for the sums over rows; fp32 gradient of
+// 1001 x 1537 with a gate to each element 17 us; 32 x 1024 forward 7.7-8.3 us a call, most of it
+// the host's.  fp32: 32768 x 2048 forward 201 us (5.3 TB/s), gradient of 8192 x 4096 186 us.
 #include "kernels.hpp"
 #include "rowio.hpp"
 

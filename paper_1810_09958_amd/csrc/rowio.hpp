@@ -1,6 +1,8 @@
-// Rows of bf16 or fp32 values moved 16 bytes per lane at the elements' own
-// alignment (gfx950 serves unaligned global accesses; a piece that passes the
-// end of its row is moved element by element), and the gate functions.
+// Rows of bf16 or fp32 values at the elements' own alignment, and the gate function of the
+// feed-forward block.  Row16: single values, and pieces of 16 bytes straight from memory
+// (gfx950 serves unaligned global accesses; a piece that passes the end of its row is loaded
+// value by value), for the kernels of a few rows.  RowBuf: whole rows as buffers of their own
+// length, for the norms.
 #pragma once
 
 #include "common.hpp"
