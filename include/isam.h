@@ -401,12 +401,70 @@ isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F, int type,
 
 size_t isam_gated_ffn_backward_workspace_size(int64_t M, int64_t K, int64_t F, int type, int aligned);
 
+/*
+ * Selective scan: a diagonal state space whose step, input and output weights depend on the token, over
+ * channels c < D and states n < N:
+ *   d_t = softplus(dt_t + dt_bias)
+ *   h_t[c][n] = exp(d_t[c] A[c][n]) * h_{t-1}[c][n] + d_t[c] * x_t[c] * B_t[n],  h_{-1} = h0
+ *   v_t[c] = sum_n C_t[n] h_t[c][n] + skip[c] * x_t[c],  y_t = v_t * z_t * sigmoid(z_t)  (v_t without z)
+ * Where reset is given and nonzero at (t, b), the token starts from a zero state; nothing from before it,
+ * infinities and NaN included, reaches a later state, nor any gradient an earlier token.
+ *
+ *   x, dt, z, y  row (t, b) of D values (type) at its own strides (elements, >= 0), as the linear GRU's
+ *           gx; B, C rows of N values.  Rows may be parts of wider ones (x and z halves of one
+ *           projection's rows, say), outputs too, as long as no element is shared.
+ *   A       [D][N] fp32, the finite values that the exponent takes (below 0: states that decay)
+ *   skip, dt_bias  [D] fp32, or NULL for zeros;  z NULL: no gate
+ *   h0      [batch][D][N] fp32, or NULL for zeros;  h_T  the same, or NULL; h_T may be h0 itself up to 8
+ *           tokens
+ *   states  [ceil(T / 16)][batch][D][N] fp32, or NULL: the state before tokens 0, 16, 32, ...: what
+ *           the backward pass needs of the forward pass
+ * At least one of y, h_T and states.  N up to 64.  T == 0: h_T = h0 (or zeros); batch or D == 0: no-op.
+ * The state, steps and sums are fp32; y is rounded once.  Results repeat bit for bit.  Tensors may pass
+ * 2^31 bytes, as long as 32 tokens of each stay below (up to 8 tokens without a gradient: any stride).
+ * Workspace: isam_selective_scan_workspace_size bytes (0 where the channels alone fill the chip).
+ */
+isam_status_t isam_selective_scan(int64_t T, int64_t batch, int64_t D, int64_t N, int type, const void* x, int64_t x_stride_t,
+                                  int64_t x_stride_b, const void* dt, int64_t dt_stride_t, int64_t dt_stride_b, const float* A,
+                                  const void* B, int64_t B_stride_t, int64_t B_stride_b, const void* C, int64_t C_stride_t,
+                                  int64_t C_stride_b, const float* skip, const void* z, int64_t z_stride_t, int64_t z_stride_b,
+                                  const float* dt_bias, const float* h0, const uint8_t* reset, int64_t reset_stride_t,
+                                  int64_t reset_stride_b, void* y, int64_t y_stride_t, int64_t y_stride_b, float* h_T,
+                                  float* states, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t isam_selective_scan_workspace_size(int64_t T, int64_t batch, int64_t D, int64_t N, int type);
+
+/*
+ * Gradient of isam_selective_scan from dy and dh_T, the gradients of y and h_T (NULL for zeros); the
+ * inputs as in the forward call, states as it left them (the first row stands for h0).
+ * With dv = dy * z * sigmoid(z), a = exp(d A) and g_t the gradient of h_t, h_{t-1} taken as 0 at a reset:
+ *   g_t = C_t dv_t + a_{t+1} g_{t+1}  (no second term before a reset; + dh_T at the last token)
+ *   dC_t = sum_c h_t dv_t,  dB_t = sum_c g_t d_t x_t,  dx_t = skip dv_t + d_t sum_n g_t B_t
+ *   ddt_t = (sum_n g_t a_t h_{t-1} A + x_t sum_n g_t B_t) sigmoid(dt_t + dt_bias),  dz_t = dy_t v_t silu'(z_t)
+ *   dA = sums of g_t a_t h_{t-1} d_t, dskip of dv_t x_t, ddt_bias of ddt_t, over t and b;  dh0 = a_0 g_0
+ *   dx, ddt, dz  rows of D values (type), dB, dC  of N, at their own strides; dz NULL without z
+ *   dA [D][N], dskip, ddt_bias [D], dh0 [batch][D][N] fp32; each of these, and dz, may be NULL
+ * Sums are fp32, in a fixed order.  T or batch == 0: dA, dskip and ddt_bias are 0, dh0 = dh_T (or zeros).
+ */
+isam_status_t isam_selective_scan_backward(
+    int64_t T, int64_t batch, int64_t D, int64_t N, int type, const void* x, int64_t x_stride_t, int64_t x_stride_b, const void* dt,
+    int64_t dt_stride_t, int64_t dt_stride_b, const float* A, const void* B, int64_t B_stride_t, int64_t B_stride_b, const void* C,
+    int64_t C_stride_t, int64_t C_stride_b, const float* skip, const void* z, int64_t z_stride_t, int64_t z_stride_b,
+    const float* dt_bias, const uint8_t* reset, int64_t reset_stride_t, int64_t reset_stride_b, const float* states, const void* dy,
+    int64_t dy_stride_t, int64_t dy_stride_b, const float* dh_T, void* dx, int64_t dx_stride_t, int64_t dx_stride_b, void* ddt,
+    int64_t ddt_stride_t, int64_t ddt_stride_b, float* dA, void* dB, int64_t dB_stride_t, int64_t dB_stride_b, void* dC,
+    int64_t dC_stride_t, int64_t dC_stride_b, float* dskip, void* dz, int64_t dz_stride_t, int64_t dz_stride_b, float* ddt_bias,
+    float* dh0, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t isam_selective_scan_backward_workspace_size(int64_t T, int64_t batch, int64_t D, int64_t N, int type);
+
 /* Static text for a status code. */
 const char* isam_status_string(int status);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */
 const char* isam_last_error(void);
 /* Library version, major*10000 + minor*100 + patch. */
-int isam_version(void);  /* 101: adds isam_conv1d; 102: the operators of a recurrent block */
+int isam_version(void);  /* 101: adds isam_conv1d; 102: the operators of a recurrent block;
+                           103: the operators of a state-space block and beam search */
 
 #ifdef __cplusplus
 }

@@ -22,7 +22,9 @@ __all__ = ["gemm", "conv1d", "dwsep_conv", "gru_forward", "gru_forward_noalloc",
            "linear_gru", "linear_gru_backward", "linear_gru_states_shape", "linear_gru_workspace_size",
            "linear_gru_backward_workspace_size", "norm_residual", "norm_residual_backward",
            "norm_residual_backward_workspace_size", "gated_ffn", "gated_ffn_backward", "gated_ffn_workspace_size",
-           "gated_ffn_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
+           "gated_ffn_backward_workspace_size",
+           "selective_scan", "selective_scan_backward", "selective_scan_states_shape", "selective_scan_workspace_size",
+           "selective_scan_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
 
 _DT = {torch.float32: ISAM_F32, torch.bfloat16: ISAM_BF16}
 
@@ -538,3 +540,114 @@ def gated_ffn_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, 
                                        _ptr(dW), lddw, _ptr(dbias), _ptr(workspace), _bytes(workspace), _stream(at))
     _call(rc, "isam_gated_ffn_backward")
     return dx, dW, dbias
+
+
+# ---------------------------------------------------------------------------------------
+# Selective scan
+# ---------------------------------------------------------------------------------------
+def selective_scan_workspace_size(T, batch, D, N, dtype) -> int:
+    return lib().isam_selective_scan_workspace_size(T, batch, D, N, dtype)
+
+
+def selective_scan_backward_workspace_size(T, batch, D, N, dtype) -> int:
+    return lib().isam_selective_scan_backward_workspace_size(T, batch, D, N, dtype)
+
+
+def selective_scan_states_shape(T, batch, D, N):
+    """Shape of the ``states`` tensor: the state before tokens 0, 16, 32, ..."""
+    return (T + 15) // 16, batch, D, N
+
+
+def _sequence(t, name, shape, dtype):
+    """Pointer and row strides of a [T][batch][width] tensor (None: no rows)."""
+    if t is None:
+        return None, 0, 0
+    return (t.data_ptr(), *_rows(t, name, shape, dtype))
+
+
+def _reset(reset, T, B):
+    if reset is not None and reset.dtype not in (torch.bool, torch.uint8):
+        raise TypeError("reset must be bool or uint8")
+    return _sequence(reset, "reset", (T, B), None if reset is None else reset.dtype)
+
+
+def _scan_args(x, dt, A, B, C, skip, z, dt_bias, reset):
+    if x.dim() != 3 or A.dim() != 2:
+        raise ValueError("x must be [T][batch][D] and A [D][N]")
+    T, b, D = x.shape
+    N, ty = A.shape[1], x.dtype
+    _want(A, "A", (D, N))
+    _want(skip, "skip", (D,))
+    _want(dt_bias, "dt_bias", (D,))
+    rows, few = (T, b, D), (T, b, N)
+    return T, b, D, N, _dt(x), (*_sequence(x, "x", rows, ty), *_sequence(dt, "dt", rows, ty), A.data_ptr(), *_sequence(B, "B", few, ty),
+                                *_sequence(C, "C", few, ty), _ptr(skip), *_sequence(z, "z", rows, ty), _ptr(dt_bias)), _reset(reset, T, b)
+
+
+def selective_scan(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor, *, skip=None, z=None,
+                   dt_bias=None, h0=None, reset=None, return_sequence=True, y=None, h_T=None, states=None,
+                   workspace: torch.Tensor | None = None):
+    """Selective scan: h_t = exp(d_t A) h_{t-1} + d_t x_t B_t over channels and states with d_t =
+    softplus(dt_t + dt_bias), y_t = (sum_n C_t h_t + skip x_t) silu(z_t).
+    x, dt, z [T][batch][D] and B, C [T][batch][N] (float32 or bfloat16, one dtype; any strides of the
+    first two dimensions, so batch-first tensors go in transposed and slices of wider rows as they are),
+    A [D][N] (below 0 for states that decay), skip, dt_bias [D] and h0 [batch][D][N] float32, reset
+    [T][batch] bool (the token starts from a zero state).  N up to 64.  states
+    (``selective_scan_states_shape``, float32) receives what ``selective_scan_backward`` needs.  h_T may
+    be h0 up to 8 tokens.  Returns (y in x's dtype, h_T in float32)."""
+    at = _on(x, dt, A, B, C, skip, z, dt_bias, h0, reset, y, h_T, states, workspace)
+    T, b, D, N, ty, seq, marks = _scan_args(x, dt, A, B, C, skip, z, dt_bias, reset)
+    dev = x.device
+    _want(h0, "h0", (b, D, N))
+    _want(states, "states", selective_scan_states_shape(T, b, D, N))
+    if y is None and return_sequence:
+        y = torch.empty((T, b, D), device=dev, dtype=x.dtype)
+    if h_T is None:
+        h_T = torch.empty((b, D, N), device=dev, dtype=torch.float32)
+    _want(h_T, "h_T", (b, D, N))
+    if workspace is None:
+        workspace = _room(selective_scan_workspace_size(T, b, D, N, ty), dev)
+    rc = lib().isam_selective_scan(T, b, D, N, ty, *seq, _ptr(h0), *marks, *_sequence(y, "y", (T, b, D), x.dtype), _ptr(h_T), _ptr(states),
+                                   _ptr(workspace), _bytes(workspace), _stream(at))
+    _call(rc, "isam_selective_scan")
+    return y, h_T
+
+
+def selective_scan_backward(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor,
+                            dy: torch.Tensor | None, *, states, skip=None, z=None, dt_bias=None, reset=None, dh_T=None, dx=None,
+                            ddt=None, dA=None, dB=None, dC=None, dskip=None, dz=None, ddt_bias=None, dh0=None,
+                            workspace: torch.Tensor | None = None):
+    """Gradient of ``selective_scan``: the inputs as in, and states from, the forward call; dy [T][batch][D] in
+    x's dtype or None, dh_T [batch][D][N] float32 or None.  dx, ddt, dB, dC and dz may be slices of wider
+    rows.  Returns (dx, ddt, dA, dB, dC, dskip, dz, ddt_bias, dh0), rows in x's dtype and the rest in
+    float32, None where the forward call had no such input (dskip, dz, ddt_bias; given ones are filled)."""
+    at = _on(x, dt, A, B, C, dy, states, skip, z, dt_bias, reset, dh_T, dx, ddt, dA, dB, dC, dskip, dz, ddt_bias, dh0, workspace)
+    T, b, D, N, ty, seq, marks = _scan_args(x, dt, A, B, C, skip, z, dt_bias, reset)
+    dev, rows, few = x.device, (T, b, D), (T, b, N)
+
+    def made(t, shape, dtype=torch.float32):
+        return torch.empty(shape, device=dev, dtype=dtype) if t is None else t
+
+    _want(states, "states", selective_scan_states_shape(T, b, D, N))
+    _want(dh_T, "dh_T", (b, D, N))
+    dx, ddt, dB, dC = made(dx, rows, x.dtype), made(ddt, rows, x.dtype), made(dB, few, x.dtype), made(dC, few, x.dtype)
+    if z is not None:
+        dz = made(dz, rows, x.dtype)
+    if skip is not None:
+        dskip = made(dskip, (D,))
+    if dt_bias is not None:
+        ddt_bias = made(ddt_bias, (D,))
+    dA, dh0 = made(dA, (D, N)), made(dh0, (b, D, N))
+    _want(dA, "dA", (D, N))
+    _want(dskip, "dskip", (D,))
+    _want(ddt_bias, "ddt_bias", (D,))
+    _want(dh0, "dh0", (b, D, N))
+    if workspace is None:
+        workspace = _room(selective_scan_backward_workspace_size(T, b, D, N, ty), dev)
+    rc = lib().isam_selective_scan_backward(
+        T, b, D, N, ty, *seq, *marks, _ptr(states), *_sequence(dy, "dy", rows, x.dtype), _ptr(dh_T),
+        *_sequence(dx, "dx", rows, x.dtype), *_sequence(ddt, "ddt", rows, x.dtype), _ptr(dA), *_sequence(dB, "dB", few, x.dtype),
+        *_sequence(dC, "dC", few, x.dtype), _ptr(dskip), *_sequence(dz, "dz", rows, x.dtype), _ptr(ddt_bias), _ptr(dh0),
+        _ptr(workspace), _bytes(workspace), _stream(at))
+    _call(rc, "isam_selective_scan_backward")
+    return dx, ddt, dA, dB, dC, dskip, dz, ddt_bias, dh0

@@ -9,6 +9,7 @@ ISAM_F32, ISAM_BF16 = 0, 1
 
 # name -> (restype, argtypes), mirroring include/isam.h
 i64, vp, sz, ci, cf = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
+row = (vp, i64, i64)  # rows of a [T][batch] tensor: pointer and two strides
 SIGNATURES = {
     "isam_gemm": (ci, [ci, ci, i64, i64, i64, ci, vp, i64, vp, i64, ci, ci, vp, i64, vp, sz, vp]),
     "isam_gemm_workspace_size": (sz, [ci, ci, i64, i64, i64, ci, ci]),
@@ -31,6 +32,11 @@ SIGNATURES = {
     "isam_gated_ffn_workspace_size": (sz, [i64, i64, i64, ci, ci]),
     "isam_gated_ffn_backward": (ci, [i64, i64, i64, ci, ci, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]),
     "isam_gated_ffn_backward_workspace_size": (sz, [i64, i64, i64, ci, ci]),
+    "isam_selective_scan": (ci, [i64] * 4 + [ci, *row, *row, vp, *row, *row, vp, *row, vp, vp, *row, *row, vp, vp, vp, sz, vp]),
+    "isam_selective_scan_workspace_size": (sz, [i64] * 4 + [ci]),
+    "isam_selective_scan_backward": (ci, [i64] * 4 + [ci, *row, *row, vp, *row, *row, vp, *row, vp, *row, vp, *row, vp, *row, *row, vp,
+                                          *row, *row, vp, *row, vp, vp, vp, sz, vp]),
+    "isam_selective_scan_backward_workspace_size": (sz, [i64] * 4 + [ci]),
     "isam_status_string": (ctypes.c_char_p, [ci]),
     "isam_last_error": (ctypes.c_char_p, []),
     "isam_version": (ci, []),

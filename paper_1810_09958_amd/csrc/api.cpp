@@ -1435,6 +1435,6 @@ const char* isam_status_string(int status) {
 
 const char* isam_last_error(void) { return last_error(); }
 
-int isam_version(void) { return 102; }
+int isam_version(void) { return 103; }
 
 }  // extern "C"

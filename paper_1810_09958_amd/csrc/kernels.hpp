@@ -342,6 +342,48 @@ bool gated_f32_direct(int64_t M, int64_t K, int64_t F, int cus);
 hipError_t launch_gated_f32(const GatedArgs& a, bool backward, hipStream_t s);
 hipError_t launch_gated_pairs(const GatedArgs& a, bool backward, hipStream_t s);
 
+// Selective scan (selective_scan.hpp).  Rows of a [T][batch] tensor, strides in elements.
+struct ScanRows {
+    const void* p;  // or null
+    int64_t st, sb;
+};
+constexpr int kScanChunk = 16;        // tokens between two rows of `states`
+constexpr int kScanFew = 8;           // tokens forward up to which no tile is formed (64-bit offsets)
+constexpr int64_t kScanMaxN = 64;
+constexpr int64_t kScanMaxSegments = 64;
+struct ScanArgs {
+    int64_t T, batch, D, N;
+    int type;                 // of the rows
+    ScanRows x, dt, z, B, C, y;
+    const float* A;           // [D][N]
+    const float* skip;        // [D] or null
+    const float* dt_bias;     // [D] or null
+    const float* h0;          // [batch][D][N] or null
+    const uint8_t* reset;     // or null
+    int64_t rs_t, rs_b;
+    float* h_T;               // [batch][D][N] or null
+    float* states;            // [ceil(T / 16)][batch][D][N]: state before tokens 0, 16, ...; or null (forward)
+    int64_t segs, seg_len;    // segments of time, tokens of each (a multiple of the tile)
+    float* seg_sum;           // [segs][batch][D]
+    float* seg_end;           // [segs][batch][D][N]
+    // backward
+    ScanRows dy, dx, ddt, dz, dB, dC;
+    const float* dh_T;        // [batch][D][N] or null
+    float* dA;                // [D][N] or null
+    float* dskip;             // [D] or null
+    float* ddt_bias;          // [D] or null
+    float* dh0;               // [batch][D][N] or null
+    float* bc_part;           // [blocks][T][batch][2N]: dB and dC of a workgroup's channels
+    float* par_part;          // [segs][batch][D N + 2 D]: dA, dskip, ddt_bias
+};
+int64_t scan_channels(int64_t N);     // of a workgroup
+int64_t scan_segments(int64_t T, int64_t batch, int64_t D, int64_t N, int cus);
+int64_t scan_segment_length(int64_t T, int64_t segs);
+bool scan_pieces(const ScanRows& r, int64_t D, int64_t N, int type);
+hipError_t launch_scan_copy(const float* src, float* dst, int64_t n, hipStream_t s);
+hipError_t launch_scan_forward(const ScanArgs& a, hipStream_t s);
+hipError_t launch_scan_backward(const ScanArgs& a, hipStream_t s);
+
 // out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros), up to three such
 // sums in one launch.
 struct ColSum {
