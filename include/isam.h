@@ -372,7 +372,7 @@ size_t isam_norm_residual_backward_workspace_size(int64_t rows, int64_t D, int64
  * dimensions needs.  Each matrix, and M rows of 2F values of `type` (2F up to the next
  * multiple of 8), below 2^31 bytes.
  */
-typedef enum { ISAM_ACT_SIGMOID = 0, ISAM_ACT_SILU = 1, ISAM_ACT_GELU = 2 } isam_activation_t;
+typedef enum { ISAM_ACT_SIGMOID = 0, ISAM_ACT_SILU = 1, ISAM_ACT_GELU = 2, ISAM_ACT_NONE = 3 } isam_activation_t;
 
 isam_status_t isam_gated_ffn(int64_t M, int64_t K, int64_t F, int type, int act, const void* x, int64_t ldx, const void* W,
                              int64_t ldw, const float* bias, void* out, int64_t ldo, void* workspace, size_t workspace_bytes,
@@ -457,6 +457,72 @@ isam_status_t isam_selective_scan_backward(
     float* dh0, void* workspace, size_t workspace_bytes, void* stream);
 
 size_t isam_selective_scan_backward_workspace_size(int64_t T, int64_t batch, int64_t D, int64_t N, int type);
+
+/*
+ * Short causal convolution over time, channels independent, as it stands before the selective scan:
+ *   y_t[c] = act(bias[c] + sum_{k < K} w[k][c] * x_{t-K+1+k}[c])
+ * Inputs before the first token come from `state` (zeros if NULL).  Where reset is given and nonzero at
+ * (t, b), the inputs before that token count as zeros from it on, infinities and NaN included.
+ *   x, y    row (t, b) of C values (type) at its own strides (elements, >= 0); y may be NULL
+ *   w       [K][C] fp32, K from 1 to 6             bias  [C] fp32, or NULL
+ *   act     ISAM_ACT_NONE or ISAM_ACT_SILU
+ *   state   [K-1][batch][C] (type): the inputs of tokens -(K-1) .. -1, or NULL
+ *   state_T the same for the next call, or NULL: the last K - 1 inputs, zeros where a reset lies after
+ *           them; may be state itself up to 8 tokens
+ * Sums are fp32; y is rounded once.  T == 0: state_T = state (or zeros); batch or C == 0: no-op.
+ */
+isam_status_t isam_causal_conv(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, const void* x, int64_t x_stride_t,
+                               int64_t x_stride_b, const float* w, const float* bias, const void* state, const uint8_t* reset,
+                               int64_t reset_stride_t, int64_t reset_stride_b, void* y, int64_t y_stride_t, int64_t y_stride_b,
+                               void* state_T, void* stream);
+
+/*
+ * Gradient of isam_causal_conv from dy and dstate_T, the gradients of y and state_T (NULL for zeros); x, w,
+ * bias, state, reset and act as in the forward call.  With e_t = dy_t act'(pre_t), pre formed again:
+ *   dx_s = sum_j w[K-1-j] e_{s+j}  (terms up to the next reset; + dstate_T's for the inputs kept)
+ *   dw[K-1-j] = sum_t e_t x_{t-j},  dbias = sum_t e_t
+ *   dx rows of C values (type), dstate [K-1][batch][C] (type), dw [K][C], dbias [C] fp32; each may be NULL,
+ *   not all.  Sums are fp32, in a fixed order.
+ * T or batch == 0: dw and dbias are 0, dstate = dstate_T (or zeros).
+ */
+isam_status_t isam_causal_conv_backward(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, const void* x,
+                                        int64_t x_stride_t, int64_t x_stride_b, const float* w, const float* bias,
+                                        const void* state, const uint8_t* reset, int64_t reset_stride_t, int64_t reset_stride_b,
+                                        const void* dy, int64_t dy_stride_t, int64_t dy_stride_b, const void* dstate_T, void* dx,
+                                        int64_t dx_stride_t, int64_t dx_stride_b, void* dstate, float* dw, float* dbias,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+size_t isam_causal_conv_backward_workspace_size(int64_t T, int64_t batch, int64_t C, int64_t K, int type);
+
+/*
+ * One step of beam search: of each text's beams x V candidates, of value
+ *   scores[b][i] + logits[b][i][v] - log(sum_w exp(logits[b][i][w])),
+ * the best `width`, the best first and equal ones by the lowest i * V + v.  Values are formed in 64 bits.
+ *   logits   row (b, i) of V values (type) at b*logits_stride_b + i*logits_stride_n
+ *   scores   [batch][beams] fp32
+ *   finished [batch][beams], or NULL: a nonzero beam's only candidate is the token `end` at its unchanged
+ *            score (the rest have -inf)
+ *   end      the token that ends a text, below V; negative for none (then finished must be NULL)
+ *   scores_out [batch][width] fp32, parent (i) and token (v) [batch][width] int32, finished_out
+ *            [batch][width] (finished[parent], or token == end), or NULL
+ * A logit of -inf is a candidate of -inf.  A beam with a score of -inf or NaN, or with logits that are all -inf or
+ * hold a NaN or +inf, has only such candidates.  beams and width up to 64, beams * V below 2^31, width at
+ * most beams * V.  batch == 0: no-op.  Workspace: isam_beam_step_workspace_size bytes.
+ */
+isam_status_t isam_beam_step(int64_t batch, int64_t beams, int64_t V, int64_t width, int type, const void* logits,
+                             int64_t logits_stride_b, int64_t logits_stride_n, const float* scores, const uint8_t* finished,
+                             int64_t end, float* scores_out, int32_t* parent, int32_t* token, uint8_t* finished_out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+size_t isam_beam_step_workspace_size(int64_t batch, int64_t beams, int64_t V, int64_t width, int type);
+
+/*
+ * The rows of the beams that go on: dst[o][b*width + k] = src[o][b*beams + parent[b][k]], rows of row_bytes
+ * bytes of any kind (recurrent states, kept inputs, tokens so far).  A parent outside 0 .. beams - 1 leaves zeros.
+ *   src [outer][batch*beams] rows, dst [outer][batch*width] rows, parent [batch][width] int32
+ */
+isam_status_t isam_beam_reorder(int64_t outer, int64_t batch, int64_t beams, int64_t width, int64_t row_bytes, const void* src,
+                                const int32_t* parent, void* dst, void* stream);
 
 /* Static text for a status code. */
 const char* isam_status_string(int status);

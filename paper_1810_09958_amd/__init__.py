@@ -24,7 +24,8 @@ __all__ = ["gemm", "conv1d", "dwsep_conv", "gru_forward", "gru_forward_noalloc",
            "norm_residual_backward_workspace_size", "gated_ffn", "gated_ffn_backward", "gated_ffn_workspace_size",
            "gated_ffn_backward_workspace_size",
            "selective_scan", "selective_scan_backward", "selective_scan_states_shape", "selective_scan_workspace_size",
-           "selective_scan_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
+           "selective_scan_backward_workspace_size", "causal_conv", "causal_conv_backward",
+           "causal_conv_backward_workspace_size", "beam_step", "beam_step_workspace_size", "beam_reorder", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
 
 _DT = {torch.float32: ISAM_F32, torch.bfloat16: ISAM_BF16}
 
@@ -468,6 +469,7 @@ def norm_residual_backward(x: torch.Tensor | None, r_out: torch.Tensor, dy: torc
 # Gated feed-forward block
 # ---------------------------------------------------------------------------------------
 _ACTIVATIONS = {"sigmoid": 0, "silu": 1, "gelu": 2}
+_NONE = 3  # no activation
 
 
 def gated_ffn_workspace_size(M, K, F, dtype, aligned=True) -> int:
@@ -651,3 +653,150 @@ def selective_scan_backward(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, 
         _ptr(workspace), _bytes(workspace), _stream(at))
     _call(rc, "isam_selective_scan_backward")
     return dx, ddt, dA, dB, dC, dskip, dz, ddt_bias, dh0
+
+
+# ---------------------------------------------------------------------------------------
+# Causal convolution
+# ---------------------------------------------------------------------------------------
+_CONV_ACTIVATIONS = {"none": _NONE, "silu": 1}
+
+
+def causal_conv_backward_workspace_size(T, batch, C, K, dtype) -> int:
+    return lib().isam_causal_conv_backward_workspace_size(T, batch, C, K, dtype)
+
+
+def _conv_args(x, w, bias, state, reset):
+    if x.dim() != 3 or w.dim() != 2 or w.shape[0] == 0:
+        raise ValueError("x must be [T][batch][C] and w [K][C]")
+    T, b, C = x.shape
+    K = w.shape[0]
+    _want(w, "w", (K, C))
+    _want(bias, "bias", (C,))
+    _want(state, "state", (K - 1, b, C), x.dtype)
+    return T, b, C, K, _dt(x), _sequence(x, "x", (T, b, C), x.dtype), (w.data_ptr(), _ptr(bias), _ptr(state), *_reset(reset, T, b))
+
+
+def causal_conv(x: torch.Tensor, w: torch.Tensor, *, bias=None, state=None, reset=None, activation="silu", return_state=True,
+                y=None, state_T=None):
+    """Short causal convolution over time, channels independent: y_t = act(bias + sum_k w[k] x_{t-K+1+k}).
+    x [T][batch][C] (float32 or bfloat16; any strides of the first two dimensions), w [K][C] (K up to 6,
+    the last row for the token itself) and bias [C] float32, state [K-1][batch][C] in x's dtype (the inputs
+    before the first token; zeros without), reset [T][batch] bool (the inputs before that token count as
+    zeros from it on), activation "silu" or "none".  Returns (y, state_T), state_T for the next call; it may
+    be state up to 8 tokens."""
+    at = _on(x, w, bias, state, reset, y, state_T)
+    T, b, C, K, ty, xs, rest = _conv_args(x, w, bias, state, reset)
+    act = _code(_CONV_ACTIVATIONS, activation, "activation")
+    if y is None:
+        y = torch.empty((T, b, C), device=x.device, dtype=x.dtype)
+    if state_T is None and return_state:
+        state_T = torch.empty((K - 1, b, C), device=x.device, dtype=x.dtype)
+    _want(state_T, "state_T", (K - 1, b, C), x.dtype)
+    rc = lib().isam_causal_conv(T, b, C, K, ty, act, *xs, *rest, *_sequence(y, "y", (T, b, C), x.dtype), _ptr(state_T), _stream(at))
+    _call(rc, "isam_causal_conv")
+    return y, state_T
+
+
+def causal_conv_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor | None, *, bias=None, state=None, reset=None,
+                         activation="silu", dstate_T=None, dx=None, dstate=None, dw=None, dbias=None,
+                         workspace: torch.Tensor | None = None):
+    """Gradient of ``causal_conv`` from dy [T][batch][C] and dstate_T [K-1][batch][C] in x's dtype (None for
+    zeros); the rest as in the forward call.  Returns (dx, dstate in x's dtype, dw, dbias in float32; dbias is
+    None without a bias unless given)."""
+    at = _on(x, w, dy, bias, state, reset, dstate_T, dx, dstate, dw, dbias, workspace)
+    T, b, C, K, ty, xs, rest = _conv_args(x, w, bias, state, reset)
+    act, dev, rows, kept = _code(_CONV_ACTIVATIONS, activation, "activation"), x.device, (T, b, C), (K - 1, b, C)
+    if dx is None:
+        dx = torch.empty(rows, device=dev, dtype=x.dtype)
+    if dstate is None:
+        dstate = torch.empty(kept, device=dev, dtype=x.dtype)
+    if dw is None:
+        dw = torch.empty((K, C), device=dev, dtype=torch.float32)
+    if dbias is None and bias is not None:
+        dbias = torch.empty((C,), device=dev, dtype=torch.float32)
+    _want(dstate_T, "dstate_T", kept, x.dtype)
+    _want(dstate, "dstate", kept, x.dtype)
+    _want(dw, "dw", (K, C))
+    _want(dbias, "dbias", (C,))
+    if workspace is None:
+        workspace = _room(causal_conv_backward_workspace_size(T, b, C, K, ty), dev)
+    rc = lib().isam_causal_conv_backward(T, b, C, K, ty, act, *xs, *rest, *_sequence(dy, "dy", rows, x.dtype), _ptr(dstate_T),
+                                         *_sequence(dx, "dx", rows, x.dtype), _ptr(dstate), _ptr(dw), _ptr(dbias), _ptr(workspace),
+                                         _bytes(workspace), _stream(at))
+    _call(rc, "isam_causal_conv_backward")
+    return dx, dstate, dw, dbias
+
+
+# ---------------------------------------------------------------------------------------
+# Beam search
+# ---------------------------------------------------------------------------------------
+def beam_step_workspace_size(batch, beams, V, width, dtype) -> int:
+    return lib().isam_beam_step_workspace_size(batch, beams, V, width, dtype)
+
+
+def beam_step(logits: torch.Tensor, scores: torch.Tensor, *, width=None, finished=None, end=-1, scores_out=None, parent=None,
+              token=None, finished_out=None, workspace: torch.Tensor | None = None):
+    """One step of beam search: of each text's candidates scores[b][i] + log_softmax(logits[b][i])[v] the best
+    `width` (beams unless given), the best first and equal ones by the lowest i * V + v.
+    logits [batch][beams][V] (float32 or bfloat16; any strides of the first two dimensions), scores
+    [batch][beams] float32, finished [batch][beams] bool (such a beam goes on unchanged, by the token
+    `end`).  beams and width up to 64.  Returns (scores [batch][width] float32, parent (the beam) and token
+    int32, finished bool)."""
+    at = _on(logits, scores, finished, scores_out, parent, token, finished_out, workspace)
+    if logits.dim() != 3:
+        raise ValueError("logits must be [batch][beams][V]")
+    b, n, V = logits.shape
+    w, ty, dev = n if width is None else width, _dt(logits), logits.device
+    _want(scores, "scores", (b, n))
+    if finished is not None and finished.dtype not in (torch.bool, torch.uint8):
+        raise TypeError("finished must be bool or uint8")
+    _want(finished, "finished", (b, n), None if finished is None else finished.dtype)
+    if scores_out is None:
+        scores_out = torch.empty((b, w), device=dev, dtype=torch.float32)
+    if parent is None:
+        parent = torch.empty((b, w), device=dev, dtype=torch.int32)
+    if token is None:
+        token = torch.empty((b, w), device=dev, dtype=torch.int32)
+    if finished_out is None:
+        finished_out = torch.empty((b, w), device=dev, dtype=torch.bool)
+    _want(scores_out, "scores_out", (b, w))
+    _want(parent, "parent", (b, w), torch.int32)
+    _want(token, "token", (b, w), torch.int32)
+    _want(finished_out, "finished_out", (b, w), torch.bool)
+    if workspace is None:
+        workspace = _room(beam_step_workspace_size(b, n, V, w, ty), dev)
+    rc = lib().isam_beam_step(b, n, V, w, ty, *_sequence(logits, "logits", (b, n, V), logits.dtype), _ptr(scores), _ptr(finished), end,
+                              _ptr(scores_out), _ptr(parent), _ptr(token), _ptr(finished_out), _ptr(workspace), _bytes(workspace),
+                              _stream(at))
+    _call(rc, "isam_beam_step")
+    return scores_out, parent, token, finished_out
+
+
+def beam_reorder(state: torch.Tensor, parent: torch.Tensor, *, dim=0, out=None):
+    """The rows of the beams that go on: along `dim`, of size batch * beams, row b * beams + parent[b][k] becomes row
+    b * width + k.  state contiguous, of any dtype; parent [batch][width] int32 as ``beam_step`` gives it (an index
+    outside leaves zeros).  Returns out (not state itself)."""
+    at = _on(state, parent, out)
+    if parent.dim() != 2:
+        raise ValueError("parent must be [batch][width]")
+    b, w = parent.shape
+    _want(parent, "parent", (b, w), torch.int32)
+    shape = list(state.shape)
+    if not -len(shape) <= dim < len(shape):
+        raise ValueError(f"state has no dimension {dim}")
+    dim %= len(shape)
+    if not state.is_contiguous() or b == 0 or w == 0 or shape[dim] % b or shape[dim] == 0:
+        raise ValueError("state must be contiguous, with batch * beams rows along dim")
+    beams, outer, inner = shape[dim] // b, 1, state.element_size()
+    for i, n in enumerate(shape):
+        if i < dim:
+            outer *= n
+        elif i > dim:
+            inner *= n
+    shape[dim] = b * w
+    if out is None:
+        out = torch.empty(shape, device=state.device, dtype=state.dtype)
+    _want(out, "out", tuple(shape), state.dtype)
+    rc = lib().isam_beam_reorder(outer, b, beams, w, inner, _ptr(state), _ptr(parent), _ptr(out), _stream(at))
+    _call(rc, "isam_beam_reorder")
+    return out

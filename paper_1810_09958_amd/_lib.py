@@ -37,6 +37,12 @@ SIGNATURES = {
     "isam_selective_scan_backward": (ci, [i64] * 4 + [ci, *row, *row, vp, *row, *row, vp, *row, vp, *row, vp, *row, vp, *row, *row, vp,
                                           *row, *row, vp, *row, vp, vp, vp, sz, vp]),
     "isam_selective_scan_backward_workspace_size": (sz, [i64] * 4 + [ci]),
+    "isam_causal_conv": (ci, [i64] * 4 + [ci, ci, *row, vp, vp, vp, *row, *row, vp, vp]),
+    "isam_causal_conv_backward": (ci, [i64] * 4 + [ci, ci, *row, vp, vp, vp, *row, *row, vp, *row, vp, vp, vp, vp, sz, vp]),
+    "isam_causal_conv_backward_workspace_size": (sz, [i64] * 4 + [ci]),
+    "isam_beam_step": (ci, [i64] * 4 + [ci, *row, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]),
+    "isam_beam_step_workspace_size": (sz, [i64] * 4 + [ci]),
+    "isam_beam_reorder": (ci, [i64] * 5 + [vp, vp, vp, vp]),
     "isam_status_string": (ctypes.c_char_p, [ci]),
     "isam_last_error": (ctypes.c_char_p, []),
     "isam_version": (ci, []),

@@ -290,3 +290,229 @@ extern "C" size_t isam_selective_scan_backward_workspace_size(int64_t T, int64_t
     if (T <= 0 || batch <= 0 || D <= 0 || N <= 0 || !valid_dtype(type) || !scan_sizes(T, batch, D, N)) return 0;
     return room(scan_plan(T, batch, D, N, true).total() * sizeof(float));
 }
+
+// ---------------------------------------------------------------------------
+// Causal convolution
+// ---------------------------------------------------------------------------
+namespace {
+
+bool conv_sizes(int64_t T, int64_t batch, int64_t C) {
+    return T < ((int64_t)1 << 40) && batch < ((int64_t)1 << 31) && C < ((int64_t)1 << 31) &&
+           (__int128)std::max<int64_t>(T, 1) * std::max<int64_t>(batch, 1) * std::max<int64_t>(C, 1) < ((__int128)1 << 42);
+}
+
+isam_status_t conv_check(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, const char* who) {
+    if (T < 0 || batch < 0 || C < 0 || K <= 0)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: bad size T=%lld batch=%lld C=%lld K=%lld", who, (long long)T, (long long)batch, (long long)C, (long long)K);
+    if (!valid_dtype(type)) return fail(ISAM_ERR_INVALID_ARG, "%s: dtype must be ISAM_F32 (0) or ISAM_BF16 (1)", who);
+    if (act != ISAM_ACT_NONE && act != ISAM_ACT_SILU)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: activation must be ISAM_ACT_NONE or ISAM_ACT_SILU", who);
+    if (K > kConvMaxK || !conv_sizes(T, batch, C))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: K=%lld above %lld, or sizes too large", who, (long long)K, (long long)kConvMaxK);
+    return ISAM_OK;
+}
+
+ConvArgs conv_args(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, bool backward) {
+    ConvArgs a{};
+    a.T = T;
+    a.batch = batch;
+    a.C = C;
+    a.K = K;
+    a.type = type;
+    a.act = act == ISAM_ACT_SILU;
+    conv_plan(a, backward, device_cus());
+    return a;
+}
+
+size_t conv_part_bytes(const ConvArgs& a) { return (size_t)(a.rows * (a.K + 1) * a.C) * sizeof(float); }
+
+}  // namespace
+
+extern "C" isam_status_t isam_causal_conv(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, const void* x,
+                                          int64_t x_stride_t, int64_t x_stride_b, const float* w, const float* bias,
+                                          const void* state, const uint8_t* reset, int64_t reset_stride_t,
+                                          int64_t reset_stride_b, void* y, int64_t y_stride_t, int64_t y_stride_b,
+                                          void* state_T, void* stream) {
+    clear_error();
+    const char* who = "isam_causal_conv";
+    isam_status_t st = conv_check(T, batch, C, K, type, act, who);
+    if (st != ISAM_OK || batch == 0 || C == 0) return st;
+    if (T > 0 && (!x || !w)) return fail(ISAM_ERR_INVALID_ARG, "%s: x or w is NULL", who);
+    if (!y && !state_T && T > 0 && K > 1) return fail(ISAM_ERR_INVALID_ARG, "%s: no output", who);
+    const size_t es = dsize(type), kept = (size_t)((K - 1) * batch * C) * es;
+    RowsArg r[] = {{"x", x, x_stride_t, x_stride_b, C, false}, {"y", y, y_stride_t, y_stride_b, C, true}};
+    size_t reset_b;
+    if ((st = reset_check(reset, T, &reset_stride_t, batch, &reset_stride_b, &reset_b, who)) != ISAM_OK) return st;
+    // (a few tokens: the state may be replaced in place, one thread reads a channel's before it writes it)
+    const bool in_place = state_T && state_T == state && T <= kConvFew;
+    const Tensor dense[] = {{"w", w, (size_t)(K * C) * 4, false},      {"bias", bias, (size_t)C * 4, false},
+                            {"state", in_place ? nullptr : state, kept, false}, {"reset", reset, reset_b, false},
+                            {"state_T", state_T, kept, true}};
+    if ((st = rows_check(r, dense, T, batch, es, who)) != ISAM_OK) return st;
+    ConvArgs a = conv_args(T, batch, C, K, type, act, false);
+    a.x = rows_of(r[0]);
+    a.y = rows_of(r[1]);
+    a.w = w;
+    a.bias = bias;
+    a.state = state;
+    a.reset = reset;
+    a.rs_t = reset_stride_t;
+    a.rs_b = reset_stride_b;
+    a.state_T = K > 1 ? state_T : nullptr;
+    const hipError_t e = launch_causal_conv(a, false, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" isam_status_t isam_causal_conv_backward(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, const void* x,
+                                                   int64_t x_stride_t, int64_t x_stride_b, const float* w, const float* bias,
+                                                   const void* state, const uint8_t* reset, int64_t reset_stride_t,
+                                                   int64_t reset_stride_b, const void* dy, int64_t dy_stride_t,
+                                                   int64_t dy_stride_b, const void* dstate_T, void* dx, int64_t dx_stride_t,
+                                                   int64_t dx_stride_b, void* dstate, float* dw, float* dbias,
+                                                   void* workspace, size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_causal_conv_backward";
+    isam_status_t st = conv_check(T, batch, C, K, type, act, who);
+    if (st != ISAM_OK || C == 0) return st;
+    const bool work = T > 0 && batch > 0;
+    if (work && (!x || !w)) return fail(ISAM_ERR_INVALID_ARG, "%s: x or w is NULL", who);
+    if (work && !dx && !dstate && !dw && !dbias) return fail(ISAM_ERR_INVALID_ARG, "%s: no output", who);
+    const size_t es = dsize(type), kept = (size_t)((K - 1) * batch * C) * es;
+    ConvArgs a = conv_args(T, batch, C, K, type, act, true);
+    const size_t need = work && (dw || dbias) ? conv_part_bytes(a) : 0;
+    if ((st = need_room(need, workspace, workspace_bytes, who)) != ISAM_OK) return st;
+    RowsArg r[] = {{"x", x, x_stride_t, x_stride_b, C, false},
+                   {"dy", dy, dy_stride_t, dy_stride_b, C, false},
+                   {"dx", dx, dx_stride_t, dx_stride_b, C, true}};
+    size_t reset_b;
+    if ((st = reset_check(reset, T, &reset_stride_t, batch, &reset_stride_b, &reset_b, who)) != ISAM_OK) return st;
+    const Tensor dense[] = {{"w", w, (size_t)(K * C) * 4, false},  {"bias", bias, (size_t)C * 4, false},
+                            {"state", state, kept, false},         {"reset", reset, reset_b, false},
+                            {"dstate_T", dstate_T, kept, false},   {"dstate", dstate, kept, true},
+                            {"dw", dw, (size_t)(K * C) * 4, true}, {"dbias", dbias, (size_t)C * 4, true},
+                            {"workspace", workspace, room(need), true}};
+    if ((st = rows_check(r, dense, T, batch, es, who)) != ISAM_OK) return st;
+    a.x = rows_of(r[0]);
+    a.dy = rows_of(r[1]);
+    a.dx = rows_of(r[2]);
+    a.w = w;
+    a.bias = bias;
+    a.state = state;
+    a.reset = reset;
+    a.rs_t = reset_stride_t;
+    a.rs_b = reset_stride_b;
+    a.dstate_T = dstate_T;
+    a.dstate = K > 1 ? dstate : nullptr;
+    a.dw = dw;
+    a.dbias = dbias;
+    a.part = reinterpret_cast<float*>(room_start(workspace));
+    const hipError_t e = launch_causal_conv(a, true, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_causal_conv_backward_workspace_size(int64_t T, int64_t batch, int64_t C, int64_t K, int type) {
+    if (T <= 0 || batch <= 0 || C <= 0 || K <= 0 || K > kConvMaxK || !valid_dtype(type) || !conv_sizes(T, batch, C)) return 0;
+    return room(conv_part_bytes(conv_args(T, batch, C, K, type, ISAM_ACT_NONE, true)));
+}
+
+// ---------------------------------------------------------------------------
+// Beam search
+// ---------------------------------------------------------------------------
+namespace {
+
+isam_status_t beam_check(int64_t batch, int64_t beams, int64_t V, int64_t width, const char* who) {
+    if (batch < 0 || beams <= 0 || V <= 0 || width <= 0)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: bad size batch=%lld beams=%lld V=%lld width=%lld", who, (long long)batch, (long long)beams, (long long)V, (long long)width);
+    if (beams > kBeamMax || width > kBeamMax)
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: beams=%lld or width=%lld above %lld", who, (long long)beams, (long long)width, (long long)kBeamMax);
+    if (V > INT32_MAX / beams || batch > ((int64_t)1 << 40) / (beams * V))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: beams x V passes 2^31, or sizes too large", who);
+    if (width > beams * V) return fail(ISAM_ERR_INVALID_ARG, "%s: width=%lld above the %lld candidates", who, (long long)width, (long long)(beams * V));
+    return ISAM_OK;
+}
+
+size_t beam_bytes(int64_t batch, int64_t beams, int64_t V, int64_t width) {
+    return (size_t)(batch * beams * cdiv(V, kBeamPart)) * (16 + 8 * (size_t)width);
+}
+
+}  // namespace
+
+extern "C" isam_status_t isam_beam_step(int64_t batch, int64_t beams, int64_t V, int64_t width, int type, const void* logits,
+                                        int64_t logits_stride_b, int64_t logits_stride_n, const float* scores,
+                                        const uint8_t* finished, int64_t end, float* scores_out, int32_t* parent,
+                                        int32_t* token, uint8_t* finished_out, void* workspace, size_t workspace_bytes,
+                                        void* stream) {
+    clear_error();
+    const char* who = "isam_beam_step";
+    isam_status_t st = beam_check(batch, beams, V, width, who);
+    if (st != ISAM_OK) return st;
+    if (!valid_dtype(type)) return fail(ISAM_ERR_INVALID_ARG, "%s: dtype must be ISAM_F32 (0) or ISAM_BF16 (1)", who);
+    if (end >= V) return fail(ISAM_ERR_INVALID_ARG, "%s: end=%lld is not below V=%lld", who, (long long)end, (long long)V);
+    if (finished && end < 0) return fail(ISAM_ERR_INVALID_ARG, "%s: finished needs an end token", who);
+    if (batch == 0) return ISAM_OK;
+    if (!logits || !scores || !scores_out || !parent || !token)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: logits, scores, scores_out, parent or token is NULL", who);
+    if (logits_stride_b < 0 || logits_stride_n < 0) return fail(ISAM_ERR_INVALID_ARG, "%s: negative stride", who);
+    const size_t es = dsize(type), need = beam_bytes(batch, beams, V, width);
+    if ((st = need_room(need, workspace, workspace_bytes, who)) != ISAM_OK) return st;
+    size_t lg_b;
+    if (!extent(batch, logits_stride_b, beams, logits_stride_n, V, es, &lg_b))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: logits span more than 2^46 bytes", who);
+    const size_t in = (size_t)(batch * beams), out = (size_t)(batch * width);
+    const Tensor all[] = {{"logits", logits, lg_b, false},       {"scores", scores, in * 4, false},
+                          {"finished", finished, in, false},     {"scores_out", scores_out, out * 4, true},
+                          {"parent", parent, out * 4, true},     {"token", token, out * 4, true},
+                          {"finished_out", finished_out, out, true}, {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    BeamArgs a{};
+    a.batch = batch;
+    a.beams = beams;
+    a.V = V;
+    a.width = width;
+    a.type = type;
+    a.logits = logits;
+    a.lg_b = logits_stride_b;
+    a.lg_n = logits_stride_n;
+    a.scores = scores;
+    a.finished = finished;
+    a.end = end;
+    a.scores_out = scores_out;
+    a.parent = parent;
+    a.token = token;
+    a.finished_out = finished_out;
+    a.parts = cdiv(V, kBeamPart);
+    a.sums = reinterpret_cast<double2*>(room_start(workspace));
+    a.best = reinterpret_cast<uint64_t*>(a.sums + batch * beams * a.parts);
+    const hipError_t e = launch_beam_step(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_beam_step_workspace_size(int64_t batch, int64_t beams, int64_t V, int64_t width, int type) {
+    if (batch <= 0 || !valid_dtype(type) || beams <= 0 || V <= 0 || width <= 0 || beams > kBeamMax || width > kBeamMax ||
+        V > INT32_MAX / beams || batch > ((int64_t)1 << 40) / (beams * V))
+        return 0;
+    return room(beam_bytes(batch, beams, V, width));
+}
+
+extern "C" isam_status_t isam_beam_reorder(int64_t outer, int64_t batch, int64_t beams, int64_t width, int64_t row_bytes,
+                                           const void* src, const int32_t* parent, void* dst, void* stream) {
+    clear_error();
+    const char* who = "isam_beam_reorder";
+    if (outer < 0 || batch < 0 || beams <= 0 || width <= 0 || row_bytes < 0)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: bad size outer=%lld batch=%lld beams=%lld width=%lld row_bytes=%lld", who, (long long)outer,
+                    (long long)batch, (long long)beams, (long long)width, (long long)row_bytes);
+    if (outer == 0 || batch == 0 || row_bytes == 0) return ISAM_OK;
+    if (!src || !parent || !dst) return fail(ISAM_ERR_INVALID_ARG, "%s: src, parent or dst is NULL", who);
+    size_t in, out;
+    const int64_t lim = (int64_t)1 << 40;
+    if (outer > lim || batch > lim || beams > lim || width > lim || row_bytes > lim ||
+        (__int128)batch * std::max(beams, width) > lim || !extent(outer, batch * beams * row_bytes, 1, 0, batch * beams * row_bytes, 1, &in) ||
+        !extent(outer, batch * width * row_bytes, 1, 0, batch * width * row_bytes, 1, &out))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: sizes too large", who);
+    const Tensor all[] = {{"src", src, in, false}, {"parent", parent, (size_t)(batch * width) * 4, false}, {"dst", dst, out, true}};
+    const isam_status_t st = disjoint(all, who);
+    if (st != ISAM_OK) return st;
+    const ReorderArgs a{outer, batch, beams, width, row_bytes, src, parent, dst};
+    const hipError_t e = launch_beam_reorder(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}

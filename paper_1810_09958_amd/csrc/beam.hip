@@ -1,0 +1,270 @@
+// One step of beam search.  Of each text's beams x vocabulary candidates, of value
+//   score_i + logits_i[v] - log(sum_w exp(logits_i[w])),
+// the best `width`, equal ones by the lowest place i V + v.
+//
+// Bound by one pass over the logits.  Within a beam the order is that of the logits themselves, so
+// the first kernel reads each once: a workgroup takes 4096 of a row into registers, sums their
+// exponentials from their maximum, and leaves its best `width`.  To find them without sorting,
+// each thread takes its own best; of these 256 the width-th is a bound that at most width threads pass,
+// so at most 16 width values are left to order, by counting for each how many are better.  Every key holds
+// the place too, so no two are equal and ties need no care.
+// The second kernel forms the values of the candidates that are left, in 64 bits (the difference of two
+// beams' sums decides, and an fp32 sum of scores and logits would make ties of what is none), and
+// takes the best in the same way.
+#include "kernels.hpp"
+#include "rowio.hpp"
+
+namespace isam {
+
+namespace {
+
+// A value's order as unsigned; both zeros are one.
+__device__ __forceinline__ uint32_t order32(float v) {
+    const uint32_t u = __float_as_uint(v + 0.0f);
+    return (int)u < 0 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value32(uint32_t o) { return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ uint64_t order64(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
+    return (int64_t)u < 0 ? ~u : u | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double value64(uint64_t o) {
+    return __longlong_as_double((long long)((int64_t)o < 0 ? o & 0x7fffffffffffffffull : ~o));
+}
+
+// exp(x) for x <= 0, to 2^-23 of itself: the product with log2 e in two parts.
+__device__ __forceinline__ float exp_of(float x) {
+    const float p = x * 1.44269502f, lo = __builtin_fmaf(x, 1.44269502f, -p) + x * 1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(p);
+    return p > -126.0f ? __builtin_fmaf(e, lo * 0.69314718f, e) : 0.0f;
+}
+
+constexpr int kEach = (int)(kBeamPart / 256);  // logits of a thread
+
+template <int ES>
+__global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
+    constexpr int E = 16 / ES, Q = kEach / E;  // values of a 16-byte piece, pieces of a thread
+    __shared__ uint64_t firsts[256];
+    __shared__ uint64_t list[kEach * kBeamMax];
+    __shared__ double wsum[4];
+    __shared__ float wmax[4];
+    __shared__ uint64_t bound;
+    __shared__ int count;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    const int64_t row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, b = row / a.beams, i = row - b * a.beams;
+    const int64_t base = b * a.lg_b + i * a.lg_n, v0 = part * kBeamPart;
+    const int W = (int)a.width;
+    float v[kEach];
+    static_for<Q>([&](auto q) {
+        const int64_t at = v0 + (int64_t)(q * 256 + tid) * E;
+        const int n = (int)max((int64_t)0, min((int64_t)E, a.V - at));
+        const uint4 w = Row16<ES>::load(a.logits, base + at, n);
+        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+        static_for<E>([&](auto e) {
+            float f;
+            if constexpr (ES == 4) f = __uint_as_float(ws[e]);
+            else if constexpr (e & 1) f = bf16hi(ws[e / 2]);
+            else f = bf16lo(ws[e / 2]);
+            v[q * E + e] = f;
+        });
+    });
+    // value k of the thread: place v0 + ((k / E) 256 + tid) E + k % E
+    auto place = [&](int k) { return v0 + (int64_t)((k / E) * 256 + tid) * E + k % E; };
+    auto key = [&](int k) { return place(k) < a.V ? (uint64_t)order32(v[k]) << 32 | (uint32_t)~(uint32_t)place(k) : 0ull; };
+    uint64_t first = 0;
+    float most = -INFINITY;
+    bool bad = false;
+    static_for<kEach>([&](auto k) {
+        const bool on = place(k) < a.V;
+        const uint64_t u = key(k);
+        first = u > first ? u : first;
+        most = on ? fmaxf(most, v[k]) : most;
+        bad = bad || (on && v[k] != v[k]);
+    });
+    firsts[tid] = first;
+    for (int m = 32; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+    if (lane == 0) wmax[wid] = most;
+    if (tid == 0) {
+        count = 0;
+        bound = 0;
+    }
+    __syncthreads();
+    most = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
+    // the sum (an infinite maximum leaves NaN, which the second kernel takes as a row without candidates)
+    float few = 0.0f;
+    static_for<kEach>([&](auto k) { few += place(k) < a.V ? (v[k] == -INFINITY ? 0.0f : exp_of(v[k] - most)) : 0.0f; });
+    double sum = bad ? __builtin_nan("") : (double)few;
+    for (int m = 32; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
+    if (lane == 0) wsum[wid] = sum;
+    // the width-th of the threads' best
+    int better = 0;
+    for (int k = 0; k < 256; k += 2) {
+        better += firsts[k] > first;
+        better += firsts[k + 1] > first;
+    }
+    if (better == W - 1 && first) bound = first;
+    __syncthreads();
+    const uint64_t least = bound;  // 0: fewer than width threads have any
+    static_for<kEach>([&](auto k) {
+        const uint64_t u = key(k);
+        if (u && u >= least) list[atomicAdd(&count, 1)] = u;
+    });
+    __syncthreads();
+    const int n = count;
+    uint64_t* const out = a.best + (row * a.parts + part) * W;
+    for (int k = tid; k < n; k += 256) {
+        const uint64_t u = list[k];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += list[j] > u;
+        if (rank < W) out[rank] = u;
+    }
+    for (int k = n + tid; k < W; k += 256) out[k] = 0;
+    if (tid == 0) a.sums[row * a.parts + part] = make_double2((double)most, (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]));
+}
+
+// A candidate: its value's order (0: none) and its place, lowest first.
+struct Cand {
+    uint64_t order;
+    uint32_t place;
+};
+__device__ __forceinline__ bool ahead(const Cand& x, const Cand& y) {
+    return x.order > y.order || (x.order == y.order && x.order && x.place < y.place);
+}
+
+constexpr int kAtOnce = 8;  // candidates of a thread
+
+__global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
+    __shared__ double offset[kBeamMax];       // score - log sum; -inf: no candidate but of -inf
+    __shared__ Cand firsts[256];
+    __shared__ Cand list[(kAtOnce + 1) * kBeamMax];
+    __shared__ Cand best[kBeamMax];
+    __shared__ Cand bound;
+    __shared__ int count;
+    const int tid = threadIdx.x, W = (int)a.width;
+    const int64_t b = blockIdx.x;
+    for (int64_t i = tid; i < a.beams; i += 256) {
+        const int64_t row = b * a.beams + i;
+        const double2* const s = a.sums + row * a.parts;
+        double most = -INFINITY, sum = 0.0;
+        bool bad = false;
+        for (int64_t p = 0; p < a.parts; ++p) {
+            most = s[p].x > most ? s[p].x : most;
+            bad = bad || s[p].y != s[p].y;
+        }
+        for (int64_t p = 0; p < a.parts; ++p) sum += s[p].x == -INFINITY ? 0.0 : s[p].y * exp(s[p].x - most);
+        double o = (double)a.scores[row] - (most + log(sum));
+        if (a.finished && a.finished[row]) o = (double)a.scores[row];
+        else if (bad || most == -INFINITY || most == INFINITY) o = -INFINITY;
+        offset[i] = o == o ? o : -INFINITY;
+    }
+    for (int k = tid; k < W; k += 256) best[k] = Cand{0, 0};
+    __syncthreads();
+    // candidate c: of beam c / each; of a beam that can go on the parts' best, else the first tokens
+    const int64_t each = a.parts * W, all = a.beams * each;
+    const double none = -INFINITY;
+    auto candidate = [&](int64_t c) {
+        const int64_t i = c / each, k = c - i * each, row = b * a.beams + i;
+        const double o = offset[i];
+        const bool over = a.finished && a.finished[row];
+        if (over || o == none) {
+            // (a finished beam: its end token, then the others)
+            if (k >= W || k >= a.V) return Cand{0, 0};
+            if (over && o != none) {
+                const int64_t v = k == 0 ? a.end : k - 1 < a.end ? k - 1 : k;
+                return Cand{order64(k == 0 ? o : none), (uint32_t)(i * a.V + v)};
+            }
+            return Cand{order64(none), (uint32_t)(i * a.V + k)};
+        }
+        const uint64_t u = a.best[row * each + k];
+        if (!u) return Cand{0, 0};
+        const double v = o + (double)value32((uint32_t)(u >> 32));
+        return Cand{order64(v == v ? v : none), (uint32_t)(i * a.V) + ~(uint32_t)u};
+    };
+    for (int64_t c0 = 0; c0 < all; c0 += 256 * kAtOnce) {
+        Cand mine[kAtOnce + 1];
+        static_for<kAtOnce>([&](auto k) {
+            const int64_t c = c0 + k * 256 + tid;
+            mine[k] = c < all ? candidate(c) : Cand{0, 0};
+        });
+        mine[kAtOnce] = tid < W ? best[tid] : Cand{0, 0};
+        Cand first{0, 0};
+        static_for<kAtOnce + 1>([&](auto k) { first = ahead(mine[k], first) ? mine[k] : first; });
+        firsts[tid] = first;
+        if (tid == 0) {
+            count = 0;
+            bound = Cand{0, 0};
+        }
+        __syncthreads();
+        int better = 0;
+        for (int k = 0; k < 256; ++k) better += ahead(firsts[k], first);
+        if (better == W - 1 && first.order) bound = first;
+        __syncthreads();
+        const Cand least = bound;
+        static_for<kAtOnce + 1>([&](auto k) {
+            if (mine[k].order && !ahead(least, mine[k])) list[atomicAdd(&count, 1)] = mine[k];
+        });
+        __syncthreads();
+        const int n = count;
+        for (int k = tid; k < n; k += 256) {
+            const Cand u = list[k];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += ahead(list[j], u);
+            if (rank < W) best[rank] = u;
+        }
+        __syncthreads();
+    }
+    for (int k = tid; k < W; k += 256) {
+        const Cand u = best[k];
+        const int64_t i = u.place / a.V, v = u.place - i * a.V, at = b * W + k;
+        a.scores_out[at] = (float)value64(u.order);
+        a.parent[at] = (int32_t)i;
+        a.token[at] = (int32_t)v;
+        if (a.finished_out) a.finished_out[at] = v == a.end || (a.finished && a.finished[b * a.beams + i]);
+    }
+}
+
+// Rows of the beams that go on; a parent that is none of the beams leaves zeros.
+template <typename V>
+__global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
+    constexpr int U = 4;
+    const int64_t n = a.bytes / (int64_t)sizeof(V), blocks = (n + 256 * U - 1) / (256 * U);
+    const int64_t row = blockIdx.x / blocks, at = (blockIdx.x - row * blocks) * 256 * U + threadIdx.x;
+    const int64_t o = row / (a.batch * a.width), r = row - o * a.batch * a.width, b = r / a.width;
+    const int64_t from = a.parent[r];
+    const bool in = from >= 0 && from < a.beams;
+    const V* const src = static_cast<const V*>(a.src) + ((o * a.batch + b) * a.beams + (in ? from : 0)) * n;
+    V* const dst = static_cast<V*>(a.dst) + row * n;
+    V v[U];
+    static_for<U>([&](auto k) {
+        const int64_t i = at + 256 * k;
+        if (i < n) v[k] = src[i];
+    });
+    static_for<U>([&](auto k) {
+        const int64_t i = at + 256 * k;
+        if (i < n) dst[i] = in ? v[k] : V{};
+    });
+}
+
+}  // namespace
+
+hipError_t launch_beam_step(const BeamArgs& a, hipStream_t s) {
+    const int64_t rows = a.batch * a.beams;
+    if (rows * a.parts > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((a.type == kBF16 ? beam_part_kernel<2> : beam_part_kernel<4>), dim3((unsigned)(rows * a.parts)), dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)a.batch), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_beam_reorder(const ReorderArgs& a, hipStream_t s) {
+    const uintptr_t both = (uintptr_t)a.src | (uintptr_t)a.dst | (uintptr_t)a.bytes;
+    const int64_t size = both % 16 == 0 ? 16 : both % 4 == 0 ? 4 : 1;
+    const int64_t blocks = a.outer * a.batch * a.width * ((a.bytes / size + 1023) / 1024);
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((size == 16 ? beam_reorder_kernel<uint4> : size == 4 ? beam_reorder_kernel<uint32_t> : beam_reorder_kernel<uint8_t>),
+                       dim3((unsigned)blocks), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace isam

@@ -384,6 +384,62 @@ hipError_t launch_scan_copy(const float* src, float* dst, int64_t n, hipStream_t
 hipError_t launch_scan_forward(const ScanArgs& a, hipStream_t s);
 hipError_t launch_scan_backward(const ScanArgs& a, hipStream_t s);
 
+// Causal convolution (causal_conv.hip): K taps over time, channels independent.
+constexpr int64_t kConvMaxK = 6;
+constexpr int64_t kConvFew = 8;   // tokens up to which one thread owns a channel's whole sequence
+struct ConvArgs {
+    int64_t T, batch, C, K;
+    int type;                 // of the rows and states
+    int act;                  // 0 none, 1 silu
+    ScanRows x, y;
+    const float* w;           // [K][C], the last row for the token itself
+    const float* bias;        // [C] or null
+    const void* state;        // [K-1][batch][C]: the inputs before the first token; or null
+    const uint8_t* reset;     // or null
+    int64_t rs_t, rs_b;
+    void* state_T;            // or null
+    // backward
+    ScanRows dy, dx;
+    const void* dstate_T;     // or null
+    void* dstate;             // or null
+    float* dw;                // [K][C] or null
+    float* dbias;             // [C] or null
+    float* part;              // [rows][K C], then [rows][C]
+    // set by conv_plan
+    int lanes;                // of a workgroup along the channels, a power of two
+    int64_t run, rows;        // tokens of a thread, rows of partial sums (workgroups of one channel block)
+};
+void conv_plan(ConvArgs& a, bool backward, int cus);
+hipError_t launch_causal_conv(const ConvArgs& a, bool backward, hipStream_t s);
+
+// Beam search (beam.hip): rows of V logits, `beams` to a text, of which `width` candidates go on.
+constexpr int64_t kBeamMax = 64;        // beams and width
+constexpr int64_t kBeamPart = 4096;     // logits of a workgroup
+struct BeamArgs {
+    int64_t batch, beams, V, width;
+    int type;                  // of the logits
+    const void* logits;
+    int64_t lg_b, lg_n;        // strides of a text and of a beam, in elements
+    const float* scores;       // [batch][beams]
+    const uint8_t* finished;   // [batch][beams] or null
+    int64_t end;               // the token that ends a text; negative: none
+    float* scores_out;         // [batch][width]
+    int32_t* parent;
+    int32_t* token;
+    uint8_t* finished_out;     // or null
+    int64_t parts;             // workgroups of a row
+    double2* sums;             // [batch][beams][parts]: largest logit, sum of exponentials from it
+    uint64_t* best;            // [batch][beams][parts][width]: order of the logit, then of the token
+};
+hipError_t launch_beam_step(const BeamArgs& a, hipStream_t s);
+struct ReorderArgs {
+    int64_t outer, batch, beams, width, bytes;   // of a row
+    const void* src;           // [outer][batch][beams] rows
+    const int32_t* parent;     // [batch][width]
+    void* dst;                 // [outer][batch][width] rows
+};
+hipError_t launch_beam_reorder(const ReorderArgs& a, hipStream_t s);
+
 // out[g][c] = sum over r of part[g][r][c] (rows may be 0: zeros), up to three such
 // sums in one launch.
 struct ColSum {
