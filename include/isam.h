@@ -524,6 +524,38 @@ size_t isam_beam_step_workspace_size(int64_t batch, int64_t beams, int64_t V, in
 isam_status_t isam_beam_reorder(int64_t outer, int64_t batch, int64_t beams, int64_t width, int64_t row_bytes, const void* src,
                                 const int32_t* parent, void* dst, void* stream);
 
+/*
+ * Projection with its epilogue:
+ *   out[m][n] = act(sum_k x[m][k] W[n][k] + bias[n]) + residual[m][n]
+ *   x [M][K], W [N][K], residual and out [M][N] (type) at leading dimensions ld* >= the row; bias [N] fp32 or
+ *   NULL; residual NULL for none, or out itself (same address and leading dimension)
+ *   act  sigmoid, silu, gelu (as isam_gated_ffn's) or ISAM_ACT_NONE
+ * Sums and epilogue are fp32; out is rounded once.  K > 0; M or N == 0: no-op.  Each matrix below 2^31 bytes.
+ * Workspace: isam_linear_workspace_size bytes (whatever the epilogue); aligned = 0 also makes room for copies of
+ * bf16 rows off 16 bytes (K off 8 says so by itself), which a call with unaligned pointers or leading
+ * dimensions (not multiples of 8) needs.  Up to 16 rows none is used.
+ */
+isam_status_t isam_linear(int64_t M, int64_t K, int64_t N, int type, int act, const void* x, int64_t ldx, const void* W, int64_t ldw,
+                          const float* bias, const void* residual, int64_t ldr, void* out, int64_t ldo, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+size_t isam_linear_workspace_size(int64_t M, int64_t K, int64_t N, int type, int aligned);
+
+/*
+ * Gradient of isam_linear from dout, the gradient of out (which is also that of residual).  With P the product and
+ * bias (formed again where there is an activation) and dP = dout * act'(P):
+ *   dx = dP . W [M][K] (type),  dW = dP^T . x [N][K] (type),  dbias = column sums of dP [N] fp32
+ *   each may be NULL, not all
+ * bf16 with an activation, beyond 16 rows: dP is rounded to bf16 as the operand of the products, so dx and dW carry
+ * two roundings (up to 16 rows it enters in two bf16 terms); dbias is summed from the unrounded values.  Everything else is fp32, in a fixed order.
+ * M == 0: dW and dbias are 0.  N == 0: no-op (with rows and a dx, which would be zeros: an error).
+ */
+isam_status_t isam_linear_backward(int64_t M, int64_t K, int64_t N, int type, int act, const void* x, int64_t ldx, const void* W,
+                                   int64_t ldw, const float* bias, const void* dout, int64_t lddo, void* dx, int64_t lddx, void* dW,
+                                   int64_t lddw, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t isam_linear_backward_workspace_size(int64_t M, int64_t K, int64_t N, int type, int aligned);
+
 /* Static text for a status code. */
 const char* isam_status_string(int status);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */

@@ -25,7 +25,8 @@ __all__ = ["gemm", "conv1d", "dwsep_conv", "gru_forward", "gru_forward_noalloc",
            "gated_ffn_backward_workspace_size",
            "selective_scan", "selective_scan_backward", "selective_scan_states_shape", "selective_scan_workspace_size",
            "selective_scan_backward_workspace_size", "causal_conv", "causal_conv_backward",
-           "causal_conv_backward_workspace_size", "beam_step", "beam_step_workspace_size", "beam_reorder", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
+           "causal_conv_backward_workspace_size", "beam_step", "beam_step_workspace_size", "beam_reorder", "linear", "linear_backward", "linear_workspace_size",
+           "linear_backward_workspace_size", "lib", "lib_path", "ISAM_F32", "ISAM_BF16", "version"]
 
 _DT = {torch.float32: ISAM_F32, torch.bfloat16: ISAM_BF16}
 
@@ -800,3 +801,75 @@ def beam_reorder(state: torch.Tensor, parent: torch.Tensor, *, dim=0, out=None):
     rc = lib().isam_beam_reorder(outer, b, beams, w, inner, _ptr(state), _ptr(parent), _ptr(out), _stream(at))
     _call(rc, "isam_beam_reorder")
     return out
+
+
+# ---------------------------------------------------------------------------------------
+# Projection with its epilogue
+# ---------------------------------------------------------------------------------------
+_LINEAR_ACTIVATIONS = {**_ACTIVATIONS, "none": _NONE}
+
+
+def linear_workspace_size(M, K, N, dtype, aligned=True) -> int:
+    return lib().isam_linear_workspace_size(M, K, N, dtype, int(aligned))
+
+
+def linear_backward_workspace_size(M, K, N, dtype, aligned=True) -> int:
+    return lib().isam_linear_backward_workspace_size(M, K, N, dtype, int(aligned))
+
+
+def _linear_args(x, W, bias):
+    if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
+        raise ValueError("x must be [M][K] and W [N][K]")
+    M, K = x.shape
+    N = W.shape[0]
+    _want(bias, "bias", (N,))
+    return M, K, N, _dt(x), _matrix(x, "x", (M, K), x.dtype), _matrix(W, "W", (N, K), x.dtype)
+
+
+def linear(x: torch.Tensor, W: torch.Tensor, *, bias=None, activation="none", residual=None, out=None,
+           workspace: torch.Tensor | None = None):
+    """Projection with its epilogue: act(x W^T + bias) + residual.  x [M][K], W [N][K], residual and out [M][N]
+    (float32 or bfloat16, one dtype; row strides may exceed the row), bias [N] float32, activation "none",
+    "sigmoid", "silu" or "gelu".  residual may be out.  Returns out."""
+    at = _on(x, W, bias, residual, out, workspace)
+    M, K, N, dt, ldx, ldw = _linear_args(x, W, bias)
+    act, dev = _code(_LINEAR_ACTIVATIONS, activation, "activation"), x.device
+    if out is None:
+        out = torch.empty((M, N), device=dev, dtype=x.dtype)
+    ldr, ldo = _matrix(residual, "residual", (M, N), x.dtype), _matrix(out, "out", (M, N), x.dtype)
+    if workspace is None:
+        workspace = _room(linear_workspace_size(M, K, N, dt, _aligned(x, ldx) and _aligned(W, ldw)), dev)
+    rc = lib().isam_linear(M, K, N, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(out), ldo, _ptr(workspace),
+                           _bytes(workspace), _stream(at))
+    _call(rc, "isam_linear")
+    return out
+
+
+def linear_backward(x: torch.Tensor, W: torch.Tensor, dout: torch.Tensor, *, bias=None, activation="none", return_dx=True,
+                    return_dW=True, dx=None, dW=None, dbias=None, workspace: torch.Tensor | None = None):
+    """Gradient of ``linear`` from dout [M][N] (which is also the residual's).  Returns (dx [M][K], dW [N][K] in x's
+    dtype, dbias [N] float32 or None without a bias); with an activation the product is formed again, nothing is
+    kept from the forward call (bfloat16 beyond 16 rows: its gradient is rounded as the products' operand, so dx and dW carry
+    two roundings).  return_dx or return_dW False: that product is left out, and None stands for it.  N = 0: dx
+    is zeros."""
+    at = _on(x, W, dout, bias, dx, dW, dbias, workspace)
+    M, K, N, dt, ldx, ldw = _linear_args(x, W, bias)
+    act, dev = _code(_LINEAR_ACTIVATIONS, activation, "activation"), x.device
+    if dx is None and return_dx:
+        dx = torch.empty((M, K), device=dev, dtype=x.dtype)
+    if dW is None and return_dW:
+        dW = torch.empty((N, K), device=dev, dtype=x.dtype)
+    if dbias is None and bias is not None:
+        dbias = torch.empty((N,), device=dev, dtype=torch.float32)
+    _want(dbias, "dbias", (N,))
+    lddo, lddx, lddw = _matrix(dout, "dout", (M, N), x.dtype), _matrix(dx, "dx", (M, K), x.dtype), _matrix(dW, "dW", (N, K), x.dtype)
+    if N == 0:  # (a sum of nothing; the C entry takes no dx then)
+        if dx is not None:
+            dx.zero_()
+        return dx, dW, dbias
+    if workspace is None:
+        workspace = _room(linear_backward_workspace_size(M, K, N, dt, _aligned(x, ldx) and _aligned(W, ldw) and _aligned(dout, lddo)), dev)
+    rc = lib().isam_linear_backward(M, K, N, dt, act, _ptr(x), ldx, _ptr(W), ldw, _ptr(bias), _ptr(dout), lddo, _ptr(dx), lddx, _ptr(dW),
+                                    lddw, _ptr(dbias), _ptr(workspace), _bytes(workspace), _stream(at))
+    _call(rc, "isam_linear_backward")
+    return dx, dW, dbias

@@ -43,6 +43,10 @@ SIGNATURES = {
     "isam_beam_step": (ci, [i64] * 4 + [ci, *row, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]),
     "isam_beam_step_workspace_size": (sz, [i64] * 4 + [ci]),
     "isam_beam_reorder": (ci, [i64] * 5 + [vp, vp, vp, vp]),
+    "isam_linear": (ci, [i64] * 3 + [ci, ci, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, sz, vp]),
+    "isam_linear_workspace_size": (sz, [i64] * 3 + [ci, ci]),
+    "isam_linear_backward": (ci, [i64] * 3 + [ci, ci, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]),
+    "isam_linear_backward_workspace_size": (sz, [i64] * 3 + [ci, ci]),
     "isam_status_string": (ctypes.c_char_p, [ci]),
     "isam_last_error": (ctypes.c_char_p, []),
     "isam_version": (ci, []),

@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libisam.so")
-SOURCES = ["api.cpp", "api_block.cpp", "api_space.cpp", "launch_cache.cpp", "gemm.hip", "gemm_bf16.hip", "gemm_f32.hip", "gemm_dma.hip", "gemm_dma_sk.hip", "gemm_ring.hip", "gemm_f32x.hip", "gemm_small.hip", "gemm_stream.hip", "pack.hip", "skinny.hip", "dwconv.hip", "dwsep_fused.hip", "dwsep_fused_f32.hip", "gru.hip", "linear_gru.hip", "norm_residual.hip", "gated_ffn.hip", "colsum.hip", "selective_scan.hip", "selective_scan_bwd.hip", "causal_conv.hip", "beam.hip"]
+SOURCES = ["api.cpp", "api_block.cpp", "api_space.cpp", "launch_cache.cpp", "gemm.hip", "gemm_bf16.hip", "gemm_f32.hip", "gemm_dma.hip", "gemm_dma_sk.hip", "gemm_ring.hip", "gemm_f32x.hip", "gemm_small.hip", "gemm_stream.hip", "pack.hip", "skinny.hip", "dwconv.hip", "dwsep_fused.hip", "dwsep_fused_f32.hip", "gru.hip", "linear_gru.hip", "norm_residual.hip", "gated_ffn.hip", "colsum.hip", "selective_scan.hip", "selective_scan_bwd.hip", "causal_conv.hip", "beam.hip", "linear.hip"]
 HOST_SOURCES = ["api.cpp", "api_block.cpp", "api_space.cpp"]  # argument checks and dispatch, no kernels
 ARCH = "gfx950"
 

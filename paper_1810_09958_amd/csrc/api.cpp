@@ -973,8 +973,8 @@ namespace api {
 
 isam_status_t product(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int ab_type, const void* A, int64_t lda,
                       const void* B, int64_t ldb, int c_type, void* C, int64_t ldc, void* workspace, size_t workspace_bytes,
-                      hipStream_t stream, const char* who) {
-    return run_gemm(trans_a, trans_b, M, N, K, ab_type, A, lda, B, ldb, 0, c_type, C, ldc, nullptr, workspace,
+                      hipStream_t stream, const char* who, int accumulate, const float* bias) {
+    return run_gemm(trans_a, trans_b, M, N, K, ab_type, A, lda, B, ldb, accumulate, c_type, C, ldc, bias, workspace,
                     workspace_bytes, stream, who);
 }
 

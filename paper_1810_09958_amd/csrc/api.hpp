@@ -26,10 +26,11 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 constexpr int64_t kMaxExtent = (int64_t(1) << 31) - 1;
 
-// The library's matrix product on validated operands (as isam_gemm, C overwritten).
+// The library's matrix product on validated operands (as isam_gemm; C overwritten unless accumulate), with a bias
+// per column of C or none.
 isam_status_t product(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int ab_type, const void* A, int64_t lda,
                       const void* B, int64_t ldb, int c_type, void* C, int64_t ldc, void* workspace, size_t workspace_bytes,
-                      hipStream_t stream, const char* who);
+                      hipStream_t stream, const char* who, int accumulate = 0, const float* bias = nullptr);
 size_t product_workspace(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int ab_type);
 
 }  // namespace api

@@ -370,8 +370,6 @@ struct GatedPlan {
     size_t total() const { return x_b + w_b + pair_b + bias_b + join_b + gemm_b; }
 };
 
-bool rows_aligned(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
-
 int64_t gated_ld_pair(int64_t F) { return cdiv(2 * F, 8) * 8; }
 
 GatedPlan gated_plan(int64_t M, int64_t K, int64_t F, int type, bool x_ok, bool w_ok, bool backward) {
@@ -425,17 +423,6 @@ isam_status_t gated_check(int64_t M, int64_t K, int64_t F, int type, int act, co
     return ISAM_OK;
 }
 
-// A matrix operand whose extent must stay below 2^31 bytes; a null one has none.
-isam_status_t gated_matrix(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, size_t es, size_t* bytes,
-                           const char* who) {
-    *bytes = 0;
-    if (!p || rows == 0 || cols == 0) return ISAM_OK;
-    if (ld < cols) return fail(ISAM_ERR_INVALID_ARG, "%s: leading dimension %lld of %s below %lld", who, (long long)ld, name, (long long)cols);
-    if (!extent(rows, ld, 1, 0, cols, es, bytes) || *bytes > (size_t)kMaxExtent)
-        return fail(ISAM_ERR_UNSUPPORTED, "%s: %s spans more than 2^31 bytes", who, name);
-    return ISAM_OK;
-}
-
 // Sizes for which every buffer the plan adds stays below 2^31 bytes as well.
 bool gated_sizes(int64_t M, int64_t K, int64_t F, int type) {
     const __int128 es = (__int128)dsize(type), most = kMaxExtent;
@@ -479,9 +466,9 @@ extern "C" isam_status_t isam_gated_ffn(int64_t M, int64_t K, int64_t F, int typ
     if (!x || !W || !out) return fail(ISAM_ERR_INVALID_ARG, "%s: x, W or out is NULL", who);
     const size_t es = dsize(type);
     size_t x_b, w_b, o_b;
-    if ((st = gated_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
-        (st = gated_matrix("W", W, 2 * F, K, ldw, es, &w_b, who)) != ISAM_OK ||
-        (st = gated_matrix("out", out, M, F, ldo, es, &o_b, who)) != ISAM_OK)
+    if ((st = small_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
+        (st = small_matrix("W", W, 2 * F, K, ldw, es, &w_b, who)) != ISAM_OK ||
+        (st = small_matrix("out", out, M, F, ldo, es, &o_b, who)) != ISAM_OK)
         return st;
     if (!gated_sizes(M, K, F, type)) return fail(ISAM_ERR_UNSUPPORTED, "%s: M x 2F, M x K or 2F x K passes 2^31 bytes", who);
     const GatedPlan p = gated_plan(M, K, F, type, rows_aligned(x, ldx), rows_aligned(W, ldw), false);
@@ -545,11 +532,11 @@ extern "C" isam_status_t isam_gated_ffn_backward(int64_t M, int64_t K, int64_t F
     if (M > 0 && (!x || !W || !dout)) return fail(ISAM_ERR_INVALID_ARG, "%s: x, W or dout is NULL", who);
     const size_t es = dsize(type);
     size_t x_b, w_b, do_b, dx_b, dw_b;
-    if ((st = gated_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
-        (st = gated_matrix("W", W, 2 * F, K, ldw, es, &w_b, who)) != ISAM_OK ||
-        (st = gated_matrix("dout", dout, M, F, lddo, es, &do_b, who)) != ISAM_OK ||
-        (st = gated_matrix("dx", dx, M, K, lddx, es, &dx_b, who)) != ISAM_OK ||
-        (st = gated_matrix("dW", dW, 2 * F, K, lddw, es, &dw_b, who)) != ISAM_OK)
+    if ((st = small_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
+        (st = small_matrix("W", W, 2 * F, K, ldw, es, &w_b, who)) != ISAM_OK ||
+        (st = small_matrix("dout", dout, M, F, lddo, es, &do_b, who)) != ISAM_OK ||
+        (st = small_matrix("dx", dx, M, K, lddx, es, &dx_b, who)) != ISAM_OK ||
+        (st = small_matrix("dW", dW, 2 * F, K, lddw, es, &dw_b, who)) != ISAM_OK)
         return st;
     if (!gated_sizes(M, K, F, type)) return fail(ISAM_ERR_UNSUPPORTED, "%s: M x 2F, M x K or 2F x K passes 2^31 bytes", who);
     const GatedPlan p = gated_plan(M, K, F, type, rows_aligned(x, ldx), rows_aligned(W, ldw), true);

@@ -56,5 +56,25 @@ inline bool matrix(const void* p, int64_t rows, int64_t D, int64_t ld, size_t es
     return ld >= D && extent(rows, ld, 1, 0, D, es, bytes);
 }
 
+// A matrix operand whose extent must stay below 2^31 bytes; a null one has none.
+inline isam_status_t small_matrix(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, size_t es, size_t* bytes,
+                           const char* who) {
+    *bytes = 0;
+    if (!p || rows == 0 || cols == 0) return ISAM_OK;
+    if (ld < cols) return fail(ISAM_ERR_INVALID_ARG, "%s: leading dimension %lld of %s below %lld", who, (long long)ld, name, (long long)cols);
+    if (!extent(rows, ld, 1, 0, cols, es, bytes) || *bytes > (size_t)kMaxExtent)
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: %s spans more than 2^31 bytes", who, name);
+    return ISAM_OK;
+}
+
+inline bool rows_aligned(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+// What a workspace has to hold.
+inline isam_status_t need_room(size_t need, const void* workspace, size_t workspace_bytes, const char* who) {
+    if (need && (!workspace || workspace_bytes < room(need)))
+        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0, room(need));
+    return ISAM_OK;
+}
+
 }  // namespace api
 }  // namespace isam

@@ -125,12 +125,6 @@ ScanPlan scan_plan(int64_t T, int64_t batch, int64_t D, int64_t N, bool backward
     return p;
 }
 
-isam_status_t need_room(size_t need, const void* workspace, size_t workspace_bytes, const char* who) {
-    if (need && (!workspace || workspace_bytes < room(need)))
-        return fail(ISAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0, room(need));
-    return ISAM_OK;
-}
-
 }  // namespace
 
 extern "C" isam_status_t isam_selective_scan(int64_t T, int64_t batch, int64_t D, int64_t N, int type, const void* x,
@@ -515,4 +509,347 @@ extern "C" isam_status_t isam_beam_reorder(int64_t outer, int64_t batch, int64_t
     const ReorderArgs a{outer, batch, beams, width, row_bytes, src, parent, dst};
     const hipError_t e = launch_beam_reorder(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+// ---------------------------------------------------------------------------
+// Projection with its epilogue
+// ---------------------------------------------------------------------------
+namespace {
+
+enum LinearWay { kLinearTokens, kLinearTiles, kLinearF32, kLinearProduct, kLinearDirect };
+
+// Parts of the workspace, in order: copies of x (twice for the terms), W and dout with aligned rows, P or dP, the bias
+// gradient's partial sums, the terms' dx, and what the matrix products use.
+struct LinearPlan {
+    LinearWay way;
+    int tile;
+    int64_t Kp, ld_pre, bias_rows;
+    bool copy_x, copy_w, copy_d;
+    size_t x_b, w_b, d_b, pre_b, bias_b, join_b, gemm_b;
+    size_t total() const { return x_b + w_b + d_b + pre_b + bias_b + join_b + gemm_b; }
+};
+
+int64_t round8(int64_t v) { return cdiv(v, 8) * 8; }
+
+void linear_copies(LinearPlan& p, int64_t M, int64_t K, int64_t N) {
+    p.Kp = K;
+    if (p.copy_x || p.copy_w) {
+        // whole 64-deep tiles where that adds at most an eighth and both are copied (no range checks in the kernel)
+        const int64_t K64 = cdiv(K, 64) * 64;
+        p.Kp = p.copy_x && p.copy_w && (K64 - K) * 8 <= K ? K64 : round8(K);
+    }
+    if (p.copy_x) p.x_b = align256((size_t)(M * p.Kp) * 2);
+    if (p.copy_w) p.w_b = align256((size_t)(N * p.Kp) * 2);
+}
+
+// Forward.  plain: no activation, and no residual but out itself: the library's product has that epilogue in every
+// one of its plans.
+LinearPlan linear_forward_plan(int64_t M, int64_t K, int64_t N, int type, bool plain, bool x_ok, bool w_ok) {
+    LinearPlan p{};
+    if (M <= kGatedTokens) {
+        p.way = kLinearTokens;
+    } else if (type == ISAM_F32 && gated_f32_direct(M, K, cdiv(N, 2), device_cus())) {
+        p.way = kLinearF32;
+    } else if (plain && (type == ISAM_F32 || (x_ok && w_ok))) {
+        p.way = kLinearDirect;
+        p.gemm_b = align256(product_workspace(0, 1, M, N, K, type));
+    } else if (type == ISAM_BF16) {
+        p.way = kLinearTiles;
+        p.copy_x = !x_ok || K % 8;
+        p.copy_w = !w_ok || K % 8;
+        linear_copies(p, M, K, N);
+        p.tile = gated_tile(M, cdiv(N, 2), device_cus());
+    } else {
+        p.way = kLinearProduct;
+        p.ld_pre = N;
+        p.pre_b = align256((size_t)(M * N) * sizeof(float));
+        p.gemm_b = align256(product_workspace(0, 1, M, N, K, type));
+    }
+    return p;
+}
+
+// Gradient.  act: there is an activation, P is formed again and dP stands in the workspace; without one dP is dout.
+LinearPlan linear_backward_plan(int64_t M, int64_t K, int64_t N, int type, bool act, bool x_ok, bool w_ok, bool d_ok) {
+    LinearPlan p{};
+    const size_t es = dsize(type);
+    p.gemm_b = std::max(product_workspace(0, 0, M, K, N, type), product_workspace(1, 0, N, K, M, type));
+    p.Kp = K;
+    p.ld_pre = round8(N);
+    if (!act) {
+        p.way = kLinearDirect;
+        if (type == ISAM_BF16) {  // (rows off 16 bytes by size alone are the products' own matter)
+            p.copy_x = !x_ok && K % 8 == 0;
+            p.copy_w = !w_ok && K % 8 == 0;
+            p.copy_d = !d_ok && N % 8 == 0;
+            if (p.copy_x) p.x_b = align256((size_t)(M * K) * es);
+            if (p.copy_w) p.w_b = align256((size_t)(N * K) * es);
+            if (p.copy_d) p.d_b = align256((size_t)(M * N) * es);
+        }
+        p.bias_rows = cdiv(M, kLinearRows);
+    } else if (type == ISAM_BF16 && M <= kGatedTokens && (__int128)2 * M * p.ld_pre * 2 <= kMaxExtent &&
+               (__int128)2 * M * (K + 8) * 4 <= kMaxExtent) {
+        p.way = kLinearTokens;  // dP in two bf16 terms, 2 M rows
+        p.Kp = round8(K);
+        p.x_b = align256((size_t)(2 * M * p.Kp) * es);
+        p.pre_b = align256((size_t)(2 * M * p.ld_pre) * es);
+        p.bias_rows = 1;
+        p.join_b = align256((size_t)(2 * M * K) * sizeof(float));
+        p.gemm_b = std::max(product_workspace(0, 0, 2 * M, K, N, type), product_workspace(1, 0, N, K, 2 * M, type));
+    } else if (type == ISAM_BF16) {
+        p.way = kLinearTiles;
+        p.copy_x = !x_ok || K % 8;
+        p.copy_w = !w_ok || K % 8;
+        linear_copies(p, M, K, N);
+        p.tile = gated_tile(M, cdiv(N, 2), device_cus());
+        p.bias_rows = gated_bias_rows(p.tile, M);
+        p.pre_b = align256((size_t)(M * p.ld_pre) * es);
+    } else if (gated_f32_direct(M, K, cdiv(N, 2), device_cus())) {
+        p.way = kLinearF32;
+        p.bias_rows = cdiv(M, 32) * 2;
+        p.pre_b = align256((size_t)(M * p.ld_pre) * es);
+    } else {
+        p.way = kLinearProduct;
+        p.bias_rows = cdiv(M, kLinearRows);
+        p.ld_pre = N;
+        p.pre_b = align256((size_t)(M * N) * es);
+        p.gemm_b = std::max(p.gemm_b, product_workspace(0, 1, M, N, K, type));
+    }
+    p.bias_b = align256((size_t)(p.bias_rows * N) * sizeof(float));
+    p.gemm_b = align256(p.gemm_b);
+    return p;
+}
+
+isam_status_t linear_check(int64_t M, int64_t K, int64_t N, int type, int act, const char* who) {
+    if (M < 0 || K <= 0 || N < 0)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: bad size M=%lld K=%lld N=%lld", who, (long long)M, (long long)K, (long long)N);
+    if (!valid_dtype(type)) return fail(ISAM_ERR_INVALID_ARG, "%s: dtype must be ISAM_F32 (0) or ISAM_BF16 (1)", who);
+    if (act < ISAM_ACT_SIGMOID || act > ISAM_ACT_NONE)
+        return fail(ISAM_ERR_INVALID_ARG, "%s: activation must be 0 (sigmoid), 1 (silu), 2 (gelu) or 3 (none)", who);
+    return ISAM_OK;
+}
+
+// Sizes for which every buffer a plan adds stays below 2^31 bytes as well.
+bool linear_sizes(int64_t M, int64_t K, int64_t N, int type) {
+    const __int128 es = (__int128)dsize(type), most = kMaxExtent, Kp = (__int128)K + 64, Np = (__int128)N + 8;
+    return (__int128)M * Np * es <= most && (__int128)M * Kp * es <= most && Np * Kp * es <= most;
+}
+
+// The copies of the plan, and the operands then read.
+hipError_t linear_copy(const LinearPlan& p, char* ws, LinearArgs& a, hipStream_t s) {
+    if (!p.copy_x && !p.copy_w) return hipSuccess;
+    PackRows cx{}, cw{};
+    if (p.copy_x) cx = PackRows{static_cast<const uint16_t*>(a.x), a.M, a.K, a.ld_x, reinterpret_cast<uint16_t*>(ws), p.Kp};
+    if (p.copy_w) cw = PackRows{static_cast<const uint16_t*>(a.W), a.N, a.K, a.ld_w, reinterpret_cast<uint16_t*>(ws + p.x_b), p.Kp};
+    const hipError_t e = launch_pack_rows(cx, cw, device_cus(), s);
+    if (e != hipSuccess) return e;
+    if (p.copy_x) {
+        a.x = cx.dst;
+        a.ld_x = p.Kp;
+    }
+    if (p.copy_w) {
+        a.W = cw.dst;
+        a.ld_w = p.Kp;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+extern "C" isam_status_t isam_linear(int64_t M, int64_t K, int64_t N, int type, int act, const void* x, int64_t ldx, const void* W,
+                                     int64_t ldw, const float* bias, const void* residual, int64_t ldr, void* out, int64_t ldo,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_linear";
+    isam_status_t st = linear_check(M, K, N, type, act, who);
+    if (st != ISAM_OK || M == 0 || N == 0) return st;
+    if (!x || !W || !out) return fail(ISAM_ERR_INVALID_ARG, "%s: x, W or out is NULL", who);
+    const size_t es = dsize(type);
+    size_t x_b, w_b, r_b, o_b;
+    if ((st = small_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
+        (st = small_matrix("W", W, N, K, ldw, es, &w_b, who)) != ISAM_OK ||
+        (st = small_matrix("residual", residual, M, N, ldr, es, &r_b, who)) != ISAM_OK ||
+        (st = small_matrix("out", out, M, N, ldo, es, &o_b, who)) != ISAM_OK)
+        return st;
+    if (!linear_sizes(M, K, N, type)) return fail(ISAM_ERR_UNSUPPORTED, "%s: M x N, M x K or N x K passes 2^31 bytes", who);
+    const bool in_place = residual == out && (ldr == ldo || M == 1);
+    const LinearPlan p = linear_forward_plan(M, K, N, type, act == ISAM_ACT_NONE && (!residual || in_place), rows_aligned(x, ldx),
+                                             rows_aligned(W, ldw));
+    const size_t need = p.total();
+    if ((st = need_room(need, workspace, workspace_bytes, who)) != ISAM_OK) return st;
+    const Tensor all[] = {{"x", x, x_b, false},
+                          {"W", W, w_b, false},
+                          {"bias", bias, (size_t)N * 4, false},
+                          {"residual", in_place ? nullptr : residual, r_b, false},
+                          {"out", out, o_b, true},
+                          {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* const ws = room_start(workspace);
+    if (p.way == kLinearDirect)
+        return product(0, 1, M, N, K, type, x, ldx, W, ldw, type, out, ldo, ws, p.gemm_b, s, who, residual ? 1 : 0, bias);
+    LinearArgs a{};
+    a.M = M;
+    a.K = K;
+    a.N = N;
+    a.act = act;
+    a.x = x;
+    a.W = W;
+    a.bias = bias;
+    a.ld_x = ldx;
+    a.ld_w = ldw;
+    a.side = residual;
+    a.ld_side = ldr;
+    a.out = out;
+    a.ld_out = ldo;
+    hipError_t e;
+    if (p.way == kLinearTokens) {
+        e = launch_linear_tokens(a, type, false, s);
+    } else if (p.way == kLinearF32) {
+        e = launch_linear_f32(a, false, s);
+    } else if (p.way == kLinearTiles) {
+        e = linear_copy(p, ws, a, s);
+        a.K = p.Kp;
+        if (e == hipSuccess) e = launch_linear_tiles(a, p.tile, false, s);
+    } else {
+        float* const pre = reinterpret_cast<float*>(ws);
+        st = product(0, 1, M, N, K, type, x, ldx, W, ldw, ISAM_F32, pre, N, ws + p.pre_b, p.gemm_b, s, who);
+        if (st != ISAM_OK) return st;
+        a.pre = pre;
+        a.ld_pre = N;
+        e = launch_linear_pass(a, type, false, s);
+    }
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_linear_workspace_size(int64_t M, int64_t K, int64_t N, int type, int aligned) {
+    if (M <= 0 || K <= 0 || N <= 0 || !valid_dtype(type) || !linear_sizes(M, K, N, type)) return 0;
+    size_t most = 0;
+    for (const bool plain : {false, true}) most = std::max(most, linear_forward_plan(M, K, N, type, plain, aligned != 0, aligned != 0).total());
+    return room(most);
+}
+
+extern "C" isam_status_t isam_linear_backward(int64_t M, int64_t K, int64_t N, int type, int act, const void* x, int64_t ldx,
+                                              const void* W, int64_t ldw, const float* bias, const void* dout, int64_t lddo, void* dx,
+                                              int64_t lddx, void* dW, int64_t lddw, float* dbias, void* workspace,
+                                              size_t workspace_bytes, void* stream) {
+    clear_error();
+    const char* who = "isam_linear_backward";
+    isam_status_t st = linear_check(M, K, N, type, act, who);
+    if (st != ISAM_OK) return st;
+    if (N == 0 && M > 0 && dx) return fail(ISAM_ERR_INVALID_ARG, "%s: N is 0", who);
+    if (N == 0) return ISAM_OK;
+    if (!dx && !dW && !dbias) return fail(ISAM_ERR_INVALID_ARG, "%s: no output", who);
+    if (M > 0 && (!x || !W || !dout)) return fail(ISAM_ERR_INVALID_ARG, "%s: x, W or dout is NULL", who);
+    const size_t es = dsize(type);
+    size_t x_b, w_b, do_b, dx_b, dw_b;
+    if ((st = small_matrix("x", x, M, K, ldx, es, &x_b, who)) != ISAM_OK ||
+        (st = small_matrix("W", W, N, K, ldw, es, &w_b, who)) != ISAM_OK ||
+        (st = small_matrix("dout", dout, M, N, lddo, es, &do_b, who)) != ISAM_OK ||
+        (st = small_matrix("dx", dx, M, K, lddx, es, &dx_b, who)) != ISAM_OK ||
+        (st = small_matrix("dW", dW, N, K, lddw, es, &dw_b, who)) != ISAM_OK)
+        return st;
+    if (!linear_sizes(M, K, N, type)) return fail(ISAM_ERR_UNSUPPORTED, "%s: M x N, M x K or N x K passes 2^31 bytes", who);
+    const LinearPlan p = linear_backward_plan(M, K, N, type, act != ISAM_ACT_NONE, rows_aligned(x, ldx), rows_aligned(W, ldw),
+                                              rows_aligned(dout, lddo));
+    const size_t need = p.total();
+    if ((st = need_room(need, workspace, workspace_bytes, who)) != ISAM_OK) return st;
+    const size_t b_b = (size_t)N * 4;
+    const Tensor all[] = {{"x", x, x_b, false},       {"W", W, w_b, false},   {"bias", bias, b_b, false},
+                          {"dout", dout, do_b, false}, {"dx", dx, dx_b, true}, {"dW", dW, dw_b, true},
+                          {"dbias", dbias, b_b, true}, {"workspace", workspace, room(need), true}};
+    if ((st = disjoint(all, who)) != ISAM_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* const ws = room_start(workspace);
+    char* const copy_d = ws + p.x_b + p.w_b;
+    char* const pre = copy_d + p.d_b;
+    float* const bias_part = reinterpret_cast<float*>(pre + p.pre_b);
+    float* const join = reinterpret_cast<float*>(pre + p.pre_b + p.bias_b);
+    char* const gemm_ws = pre + p.pre_b + p.bias_b + p.join_b;
+    const void* dP = dout;
+    int64_t ld_dP = lddo;
+    LinearArgs a{};
+    hipError_t e = hipSuccess;
+    if (M > 0) {
+        a.M = M;
+        a.K = K;
+        a.N = N;
+        a.act = act;
+        a.x = x;
+        a.W = W;
+        a.bias = bias;
+        a.ld_x = ldx;
+        a.ld_w = ldw;
+        a.side = dout;
+        a.ld_side = lddo;
+        a.out = pre;
+        a.ld_out = p.ld_pre;
+        a.bias_part = dbias ? bias_part : nullptr;
+        if ((e = linear_copy(p, ws, a, s)) != hipSuccess) return hip_fail(e, who);
+        if (p.way != kLinearDirect) {
+            dP = pre;
+            ld_dP = p.ld_pre;
+        }
+        if (p.way == kLinearTokens) {
+            e = launch_linear_tokens(a, type, true, s);
+            if (e == hipSuccess && dW) {
+                const PackRows x1{static_cast<const uint16_t*>(x), M, K, ldx, reinterpret_cast<uint16_t*>(ws), p.Kp};
+                PackRows x2 = x1;
+                x2.dst += M * p.Kp;
+                e = launch_pack_rows(x1, x2, device_cus(), s);
+            }
+        } else if (p.way == kLinearTiles) {
+            LinearArgs t = a;
+            t.K = p.Kp;
+            e = launch_linear_tiles(t, p.tile, true, s);
+        } else if (p.way == kLinearF32) {
+            e = launch_linear_f32(a, true, s);
+        } else if (p.way == kLinearProduct) {
+            st = product(0, 1, M, N, K, type, x, ldx, W, ldw, ISAM_F32, pre, N, gemm_ws, p.gemm_b, s, who);
+            if (st != ISAM_OK) return st;
+            a.pre = reinterpret_cast<const float*>(pre);
+            a.ld_pre = N;
+            e = launch_linear_pass(a, type, true, s);
+        } else {
+            if (p.copy_d) {
+                const PackRows cd{static_cast<const uint16_t*>(dout), M, N, lddo, reinterpret_cast<uint16_t*>(copy_d), N};
+                e = launch_pack_rows(cd, PackRows{}, device_cus(), s);
+                dP = copy_d;
+                ld_dP = N;
+            }
+            if (e == hipSuccess && dbias) e = launch_linear_pass(a, type, true, s);  // (column sums of dout)
+        }
+        if (e != hipSuccess) return hip_fail(e, who);
+        if (p.way == kLinearTokens) {  // both terms' rows in one product, then their sum
+            if (dx) {
+                st = product(0, 0, 2 * M, K, N, type, dP, ld_dP, W, ldw, ISAM_F32, join, K, gemm_ws, p.gemm_b, s, who);
+                if (st != ISAM_OK) return st;
+                GatedArgs sum{};
+                sum.M = M;
+                sum.K = K;
+                sum.gu = join;
+                sum.out = dx;
+                sum.ld_out = lddx;
+                if ((e = launch_gated_join(sum, s)) != hipSuccess) return hip_fail(e, who);
+            }
+            if (dW) st = product(1, 0, N, K, 2 * M, type, dP, ld_dP, ws, p.Kp, type, dW, lddw, gemm_ws, p.gemm_b, s, who);
+            if (st != ISAM_OK) return st;
+            dx = dW = nullptr;
+        }
+        if (dx && (st = product(0, 0, M, K, N, type, dP, ld_dP, a.W, a.ld_w, type, dx, lddx, gemm_ws, p.gemm_b, s, who)) != ISAM_OK) return st;
+    }
+    if (dW && (st = product(1, 0, N, K, M, type, dP, M ? ld_dP : N, a.x, M ? a.ld_x : K, type, dW, lddw, gemm_ws, p.gemm_b, s, who)) != ISAM_OK)
+        return st;
+    if (dbias) {
+        const ColSum sum{bias_part, dbias, M ? p.bias_rows : 0, N, 1, kF32};
+        e = launch_colsum(&sum, 1, s);
+    }
+    return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+}
+
+extern "C" size_t isam_linear_backward_workspace_size(int64_t M, int64_t K, int64_t N, int type, int aligned) {
+    if (M <= 0 || K <= 0 || N <= 0 || !valid_dtype(type) || !linear_sizes(M, K, N, type)) return 0;
+    const bool ok = aligned != 0;
+    size_t most = 0;
+    for (const bool act : {false, true}) most = std::max(most, linear_backward_plan(M, K, N, type, act, ok, ok, ok).total());
+    return room(most);
 }

@@ -342,6 +342,30 @@ bool gated_f32_direct(int64_t M, int64_t K, int64_t F, int cus);
 hipError_t launch_gated_f32(const GatedArgs& a, bool backward, hipStream_t s);
 hipError_t launch_gated_pairs(const GatedArgs& a, bool backward, hipStream_t s);
 
+// Projection with its epilogue (linear.hip): bf16 tiles over 16-byte aligned rows (GatedTile's, each as wide as
+// high), up to kGatedTokens rows of x and fp32 grids of few tiles at any alignment, and the element-wise pass.
+constexpr int64_t kLinearRows = 32;  // rows of a workgroup of the element-wise pass
+struct LinearArgs {
+    int64_t M, K, N;
+    int act;                  // 0 sigmoid, 1 silu, 2 gelu, 3 none
+    const void* x;            // [M][K]
+    const void* W;            // [N][K]
+    const float* bias;        // [N] or null
+    int64_t ld_x, ld_w;
+    const void* side;         // residual [M][N] or null; backward: dout
+    int64_t ld_side;
+    void* out;                // [M][N]; backward: dP
+    int64_t ld_out;
+    float* bias_part;         // backward: partial sums [rows][N], or null
+    int whole;                // rows of out and side on 4 bytes, N a multiple of 8 (set by the launch)
+    const float* pre;         // the pass: P, [M][ld_pre]; null: column sums of side alone
+    int64_t ld_pre;
+};
+hipError_t launch_linear_tiles(const LinearArgs& a, int tile, bool backward, hipStream_t s);
+hipError_t launch_linear_tokens(const LinearArgs& a, int type, bool backward, hipStream_t s);
+hipError_t launch_linear_f32(const LinearArgs& a, bool backward, hipStream_t s);
+hipError_t launch_linear_pass(const LinearArgs& a, int type, bool backward, hipStream_t s);
+
 // Selective scan (selective_scan.hpp).  Rows of a [T][batch] tensor, strides in elements.
 struct ScanRows {
     const void* p;  // or null
