@@ -306,7 +306,7 @@ isam_status_t conv_check(int64_t T, int64_t batch, int64_t C, int64_t K, int typ
     return ISAM_OK;
 }
 
-ConvArgs conv_args(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, bool backward) {
+ConvArgs conv_args(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, bool packed) {
     ConvArgs a{};
     a.T = T;
     a.batch = batch;
@@ -314,7 +314,8 @@ ConvArgs conv_args(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int
     a.K = K;
     a.type = type;
     a.act = act == ISAM_ACT_SILU;
-    conv_plan(a, backward, device_cus());
+    a.packed = packed;
+    conv_plan(a, device_cus());
     return a;
 }
 
@@ -343,7 +344,7 @@ extern "C" isam_status_t isam_causal_conv(int64_t T, int64_t batch, int64_t C, i
                             {"state", in_place ? nullptr : state, kept, false}, {"reset", reset, reset_b, false},
                             {"state_T", state_T, kept, true}};
     if ((st = rows_check(r, dense, T, batch, es, who)) != ISAM_OK) return st;
-    ConvArgs a = conv_args(T, batch, C, K, type, act, false);
+    ConvArgs a = conv_args(T, batch, C, K, type, act, conv_packs(rows_of(r[0]), C, type) && conv_packs(rows_of(r[1]), C, type));
     a.x = rows_of(r[0]);
     a.y = rows_of(r[1]);
     a.w = w;
@@ -372,12 +373,14 @@ extern "C" isam_status_t isam_causal_conv_backward(int64_t T, int64_t batch, int
     if (work && (!x || !w)) return fail(ISAM_ERR_INVALID_ARG, "%s: x or w is NULL", who);
     if (work && !dx && !dstate && !dw && !dbias) return fail(ISAM_ERR_INVALID_ARG, "%s: no output", who);
     const size_t es = dsize(type), kept = (size_t)((K - 1) * batch * C) * es;
-    ConvArgs a = conv_args(T, batch, C, K, type, act, true);
-    const size_t need = work && (dw || dbias) ? conv_part_bytes(a) : 0;
-    if ((st = need_room(need, workspace, workspace_bytes, who)) != ISAM_OK) return st;
     RowsArg r[] = {{"x", x, x_stride_t, x_stride_b, C, false},
                    {"dy", dy, dy_stride_t, dy_stride_b, C, false},
                    {"dx", dx, dx_stride_t, dx_stride_b, C, true}};
+    bool packed = true;
+    for (const RowsArg& v : r) packed = packed && conv_packs(ScanRows{v.p, 0, batch > 1 ? v.sb : 0}, C, type);
+    ConvArgs a = conv_args(T, batch, C, K, type, act, packed);
+    const size_t need = work && (dw || dbias) ? conv_part_bytes(a) : 0;
+    if ((st = need_room(need, workspace, workspace_bytes, who)) != ISAM_OK) return st;
     size_t reset_b;
     if ((st = reset_check(reset, T, &reset_stride_t, batch, &reset_stride_b, &reset_b, who)) != ISAM_OK) return st;
     const Tensor dense[] = {{"w", w, (size_t)(K * C) * 4, false},  {"bias", bias, (size_t)C * 4, false},
@@ -406,7 +409,9 @@ extern "C" isam_status_t isam_causal_conv_backward(int64_t T, int64_t batch, int
 
 extern "C" size_t isam_causal_conv_backward_workspace_size(int64_t T, int64_t batch, int64_t C, int64_t K, int type) {
     if (T <= 0 || batch <= 0 || C <= 0 || K <= 0 || K > kConvMaxK || !valid_dtype(type) || !conv_sizes(T, batch, C)) return 0;
-    return room(conv_part_bytes(conv_args(T, batch, C, K, type, ISAM_ACT_NONE, true)));
+    // (the rows' strides decide whether a wave has several sequences, and that how long its runs are)
+    return room(std::max(conv_part_bytes(conv_args(T, batch, C, K, type, ISAM_ACT_NONE, true)),
+                         conv_part_bytes(conv_args(T, batch, C, K, type, ISAM_ACT_NONE, false))));
 }
 
 // ---------------------------------------------------------------------------

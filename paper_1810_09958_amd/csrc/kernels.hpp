@@ -429,11 +429,12 @@ struct ConvArgs {
     float* dw;                // [K][C] or null
     float* dbias;             // [C] or null
     float* part;              // [rows][K C], then [rows][C]
+    bool packed;              // a wave may have several sequences
     // set by conv_plan
-    int lanes;                // of a workgroup along the channels, a power of two
-    int64_t run, rows;        // tokens of a thread, rows of partial sums (workgroups of one channel block)
+    int64_t run, rows;        // tokens of a wave, rows of partial sums
 };
-void conv_plan(ConvArgs& a, bool backward, int cus);
+bool conv_packs(const ScanRows& r, int64_t C, int type);
+void conv_plan(ConvArgs& a, int cus);
 hipError_t launch_causal_conv(const ConvArgs& a, bool backward, hipStream_t s);
 
 // Beam search (beam.hip): rows of V logits, `beams` to a text, of which `width` candidates go on.

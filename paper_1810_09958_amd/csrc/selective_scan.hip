@@ -49,22 +49,28 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
         bias[e] = a.dt_bias && e < valid ? a.dt_bias[c0 + pc + e] : 0.0f;
         skip[e] = a.skip && e < valid ? a.skip[c0 + pc + e] : 0.0f;
     });
-    auto offset = [&](const ScanRows& r, int left) {
-        return tr < left && valid > 0 ? (uint32_t)tr * (uint32_t)(r.st * ES) + (uint32_t)((c0 + pc) * ES) : kOob;
+    TileRows<ES> rx(a.x, b, tbeg), rd(a.dt, b, tbeg), rz(a.z, b, tbeg), rB(a.B, b, tbeg), rC(a.C, b, tbeg), ry(a.y, b, tbeg);
+    auto offset = [&](const TileRows<ES>& r, int left) {
+        return tr < left && valid > 0 ? (uint32_t)tr * r.row + (uint32_t)((c0 + pc) * ES) : kOob;
     };
     P px, pd, pz;
     ScanWeights<ES, NP> wb, wc;
-    uint32_t marks;
+    ScanMarks marks;
     auto fetch = [&](int64_t t0) {
         const int left = (int)max((int64_t)0, min((int64_t)TT, tend - t0));
-        px.load(scan_rows<ES>(a.x, b, t0), offset(a.x, left), valid);
-        pd.load(scan_rows<ES>(a.dt, b, t0), offset(a.dt, left), valid);
-        wb.load(scan_rows<ES>(a.B, b, t0), a.B.st, N, left, tid);
+        px.load(rx.buffer(), offset(rx, left), valid);
+        pd.load(rd.buffer(), offset(rd, left), valid);
+        wb.load(rB.buffer(), rB.row, N, left, tid);
+        rx.forth();
+        rd.forth();
+        rB.forth();
         if constexpr (!SUM) {
-            pz.load(scan_rows<ES>(a.z, b, t0), a.z.p ? offset(a.z, left) : kOob, valid);
-            wc.load(scan_rows<ES>(a.C, b, t0), a.C.st, N, left, tid);
+            pz.load(rz.buffer(), rz.p ? offset(rz, left) : kOob, valid);
+            wc.load(rC.buffer(), rC.row, N, left, tid);
+            rz.forth();
+            rC.forth();
         }
-        marks = scan_resets(a, b, t0, left, lane);
+        marks.load(a, b, t0, left, lane);
     };
     fetch(tbeg);
     float total = 0.0f;
@@ -86,14 +92,23 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
             wc.template put<R>(bc, 1, tid);
             pz.unpack(zs);
         }
-        const uint32_t reset = marks;
+        const uint32_t reset = marks.bits();
         fetch(t0 + TT);  // (past the end: zeros)
         __syncthreads();
-        // FAST: a whole tile without a reset.
+        // FAST: a whole tile without a reset.  The next four tokens' values are on their way from LDS while
+        // four are walked.
         auto walk = [&](auto fast) {
             constexpr bool FAST = decltype(fast)::value;
+            using Token = ScanToken<L, R, !SUM>;
+            Token next[4];
+            auto ahead = [&](int q) { static_for<4>([&](auto i) { next[i].get(dd[q + i][cl], bc, q + i, g); }); };
+            ahead(0);
 #pragma unroll 2
             for (int q = 0; q < TT; q += 4) {
+                Token now[4];
+                static_for<4>([&](auto i) { now[i] = next[i]; });
+                ahead(q + 4 < TT ? q + 4 : q);
+                __builtin_amdgcn_sched_barrier(0);
                 if (!SUM && (q & (kScanChunk - 1)) == 0 && a.states && (FAST || q < left)) {
                     float* const to = a.states + (((t0 + q) / kScanChunk * a.batch + b) * a.D + ch) * N + g * R;
                     static_for<R>([&](auto r) {
@@ -103,22 +118,19 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
                 float p[4];
                 static_for<4>([&](auto i) {
                     const int t = q + i;
-                    const float2 s = dd[t][cl];
-                    float Bv[R], Cv[R];
-                    lds_get<R>(bc + (t * L + g) * 2 * R, Bv);
-                    if constexpr (!SUM) lds_get<R>(bc + (t * L + g) * 2 * R + R, Cv);
+                    const Token& v = now[i];
                     const bool drop = !FAST && (reset >> t & 1), live = FAST || t < left;
                     float acc = 0.0f;
                     static_for<R>([&](auto r) {
-                        const float av = __builtin_amdgcn_exp2f(s.x * A2[r]);
+                        const float av = __builtin_amdgcn_exp2f(v.s.x * A2[r]);
                         const float hb = drop ? 0.0f : h[r];
-                        const float hn = __builtin_fmaf(av, hb, s.y * Bv[r]);
+                        const float hn = __builtin_fmaf(av, hb, v.s.y * v.B[r]);
                         h[r] = live ? hn : h[r];
-                        if constexpr (!SUM) acc = r == 0 ? Cv[0] * h[0] : __builtin_fmaf(Cv[r], h[r], acc);
+                        if constexpr (!SUM) acc = r == 0 ? v.C[0] * h[0] : __builtin_fmaf(v.C[r], h[r], acc);
                     });
                     p[i] = acc;
                     if constexpr (SUM) {
-                        total = drop ? s.x : total + s.x;
+                        total = drop ? v.s.x : total + v.s.x;
                         dropped = dropped || drop;
                     }
                 });
@@ -142,7 +154,8 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
                     y[e] *= zs[e] * z;
                 }
             });
-            if (a.y.p) P::store(scan_rows<ES>(a.y, b, t0), offset(a.y, left), valid, y);
+            P::store(ry.buffer(), ry.p ? offset(ry, left) : kOob, valid, y);
+            ry.forth();
         }
     }
     if (!in) return;
@@ -252,14 +265,16 @@ bool scan_pieces(const ScanRows& r, int64_t D, int64_t N, int type) {
     return !r.p || (D % e == 0 && (type == kF32 || ((uintptr_t)r.p % 4 == 0 && r.st % 2 == 0 && r.sb % 2 == 0)));
 }
 
-// Segments of time: tiles of 32 tokens shared out over them.
+// Segments of time, tiles of 32 tokens shared out over them: as many as make four workgroups to a compute unit, of two
+// tiles at least, where the channels alone make fewer than two.  us forward / backward of 1, 2, 4, 8, 16 segments
+// (workgroups of one; bf16, N 16): 512x2x1024 (64) 43, 39, 25, 21, 25 / 131, 93, 58, 48, 54; 4096x1x1024 (32)
+// 301, -, 133, 73, 55 / 922, -, 309, 169, 122; 4096x2x2048 (128) 301, 255, 174, 156, 150 / 973, 633, 414, 404, 409;
+// 2048x8x1024 (256) 161, 166, 150, 146 / 524, 419, 404, 412; 2048x8x2048 (512) 245, 257, 264, 277 / 678, 737, 745, 770.
 int64_t scan_segments(int64_t T, int64_t batch, int64_t D, int64_t N, int cus) {
     if (T <= kScanFew) return 1;
     const int64_t groups = batch * ((D + scan_channels(N) - 1) / scan_channels(N)), tiles = (T + kScanTile - 1) / kScanTile;
-    if (groups >= cus || tiles <= 4) return 1;
-    int64_t segs = std::min<int64_t>((4 * (int64_t)cus + groups - 1) / groups, std::max<int64_t>(1, tiles / 4));
-    segs = std::min<int64_t>(segs, kScanMaxSegments);
-    if (segs < 2) return 1;
+    if (groups >= 2 * (int64_t)cus || tiles < 4) return 1;
+    const int64_t segs = std::min({(4 * (int64_t)cus + groups - 1) / groups, tiles / 2, kScanMaxSegments});
     const int64_t per = (tiles + segs - 1) / segs;
     return (tiles + per - 1) / per;
 }

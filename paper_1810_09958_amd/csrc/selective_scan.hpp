@@ -106,11 +106,19 @@ struct Piece {
     }
 };
 
-// Rows of one sequence in a [T][batch] tensor from token t0 on, as a buffer.
+// Rows of one sequence in a [T][batch] tensor, a tile at a time: from token t0 on, as a buffer.
 template <int ES>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t scan_rows(const ScanRows& r, int64_t b, int64_t t0) {
-    return make_rsrc(r.p ? static_cast<const char*>(r.p) + (b * r.sb + t0 * r.st) * ES : nullptr, r.p ? 0x7fffffffu : 0u);
-}
+struct TileRows {
+    const char* p;       // null: no rows
+    uint32_t row;        // bytes from a token to the next (a tile stays below 2^31)
+    __device__ __forceinline__ TileRows(const ScanRows& r, int64_t b, int64_t t0) {
+        p = r.p ? static_cast<const char*>(r.p) + (b * r.sb + t0 * r.st) * ES : nullptr;
+        row = r.p ? (uint32_t)(r.st * ES) : 0u;
+    }
+    __device__ __forceinline__ void forth() { p += row * (uint32_t)kScanTile; }
+    __device__ __forceinline__ void back() { p -= row * (uint32_t)kScanTile; }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const { return make_rsrc(p, p ? 0x7fffffffu : 0u); }
+};
 
 // How a workgroup's lanes stand to its channels, states and tiles.
 template <int ES, bool VEC, int L, int R>
@@ -131,10 +139,10 @@ struct ScanWeights {
     static constexpr int BE = (kScanTile * NP + 255) / 256;
     uint16_t h[ES == 2 ? BE : 1];
     float f[ES == 4 ? BE : 1];
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int64_t stride, int N, int left, int tid) {
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, uint32_t row, int N, int left, int tid) {
         static_for<BE>([&](auto i) {
             const int idx = tid + 256 * i, t = idx / NP, n = idx % NP;
-            const uint32_t off = t < left && t < kScanTile && n < N ? (uint32_t)t * (uint32_t)(stride * ES) + (uint32_t)(n * ES) : kOob;
+            const uint32_t off = t < left && n < N ? (uint32_t)t * row + (uint32_t)(n * ES) : kOob;  // (left <= the tile)
             if constexpr (ES == 4) f[i] = __uint_as_float(buf_load4(rs, off));
             else h[i] = (uint16_t)buf_load2(rs, off);
         });
@@ -168,6 +176,18 @@ __device__ __forceinline__ void lds_get(const float* p, float (&f)[R]) {
     }
 }
 
+// What a token brings to a lane: d, d x and the lane's values of B and C.
+template <int L, int R, bool WITH_C>
+struct ScanToken {
+    float2 s;
+    float B[R], C[WITH_C ? R : 1];
+    __device__ __forceinline__ void get(const float2& at, const float* bc, int t, int g) {
+        s = at;
+        lds_get<R>(bc + (t * L + g) * 2 * R, B);
+        if constexpr (WITH_C) lds_get<R>(bc + (t * L + g) * 2 * R + R, C);
+    }
+};
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
@@ -194,13 +214,17 @@ __device__ __forceinline__ float sum_lanes4(const float (&p)[4]) {
     return s;
 }
 
-// Reset marks of a tile's tokens, a bit each (uniform).
-__device__ __forceinline__ uint32_t scan_resets(const ScanArgs& a, int64_t b, int64_t t0, int left, int lane) {
-    if (!a.reset) return 0u;
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.reset + b * a.rs_b + t0 * a.rs_t, 0x7fffffffu);
-    const uint32_t v = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(lane < left && lane < kScanTile ? (uint32_t)lane * (uint32_t)a.rs_t : kOob), 0, 0);
-    return (uint32_t)__ballot((v & 0xffu) != 0);
-}
+// Reset marks of a tile's tokens: a byte to a lane, turned into a bit each where they are used (the loads of a
+// tile are on their way during the one before).
+struct ScanMarks {
+    uint32_t byte = 0;
+    __device__ __forceinline__ void load(const ScanArgs& a, int64_t b, int64_t t0, int left, int lane) {
+        if (!a.reset) return;
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.reset + b * a.rs_b + t0 * a.rs_t, 0x7fffffffu);
+        byte = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(lane < left ? (uint32_t)lane * (uint32_t)a.rs_t : kOob), 0, 0);
+    }
+    __device__ __forceinline__ uint32_t bits() const { return (uint32_t)__ballot((byte & 0xffu) != 0); }  // (left <= the tile)
+};
 
 // Segments: [segment][batch][D] sums of steps (sign bit set: a reset lies inside, nothing passes),
 // and [segment][batch][D][N] end states from zero.

@@ -53,9 +53,11 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
     constexpr int CH = S::CH, E = S::E, NP = S::NP, TT = kScanTile, CK = kScanChunk, CW = S::CW;
     constexpr bool KEEP = R < 4;  // a of each token kept (R = 4: no registers left, formed again)
     constexpr int BITS = CW == 16 ? 4 : CW == 8 ? 3 : 2, LEFT = 2 * R > CW ? 2 * R / CW : 1;
-    __shared__ __attribute__((aligned(16))) float4 dd[TT][CH];  // d, d x, dv, v; then sum q A, sum g B, dv, v
+    constexpr int BUF = NP <= 32 ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) float4 dd[TT][CH];                    // d, d x, dv, v
+    __shared__ __attribute__((aligned(16))) float2 back_sums[SUM ? 1 : TT][CH];   // sum q A, sum g B
     __shared__ __attribute__((aligned(16))) float bc[TT * NP * 2];
-    __shared__ __attribute__((aligned(16))) float part[SUM ? 1 : kScanWaves][SUM ? 1 : CK][2 * NP];
+    __shared__ __attribute__((aligned(16))) float part[BUF][SUM ? 1 : kScanWaves][SUM ? 1 : CK][2 * NP];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane / CW, cl = wid * CW + lane % CW;
     const int64_t blocks = (a.D + CH - 1) / CH;
@@ -90,50 +92,70 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         skip[e] = a.skip && e < valid ? a.skip[c0 + pc + e] : 0.0f;
         sum_skip[e] = sum_bias[e] = 0.0f;
     });
-    auto offset = [&](const ScanRows& r, int left) {
-        return tr < left && valid > 0 ? (uint32_t)tr * (uint32_t)(r.st * ES) + (uint32_t)((c0 + pc) * ES) : kOob;
+    const int64_t tlast = tbeg + (tend - tbeg - 1) / TT * TT;
+    TileRows<ES> rx(a.x, b, tlast), rd(a.dt, b, tlast), rz(a.z, b, tlast), ry(a.dy, b, tlast), rB(a.B, b, tlast), rC(a.C, b, tlast),
+        rdx(a.dx, b, tlast), rdt(a.ddt, b, tlast), rdz(a.dz, b, tlast);
+    auto offset = [&](const TileRows<ES>& r, int left) {
+        return r.p && tr < left && valid > 0 ? (uint32_t)tr * r.row + (uint32_t)((c0 + pc) * ES) : kOob;
     };
     P px, pd, pz, py;
     ScanWeights<ES, NP> wb, wc;
-    uint32_t marks;
-    auto fetch = [&](int64_t t0) {
+    ScanMarks marks;
+    auto fetch = [&](int64_t t0) {  // (tiles before the segment: nothing is read)
         const int left = t0 >= tbeg ? (int)min((int64_t)TT, tend - t0) : 0;
-        const int64_t at = max(t0, (int64_t)0);
-        pd.load(scan_rows<ES>(a.dt, b, at), offset(a.dt, left), valid);
-        pz.load(scan_rows<ES>(a.z, b, at), a.z.p ? offset(a.z, left) : kOob, valid);
-        py.load(scan_rows<ES>(a.dy, b, at), a.dy.p ? offset(a.dy, left) : kOob, valid);
-        wc.load(scan_rows<ES>(a.C, b, at), a.C.st, N, left, tid);
+        pd.load(rd.buffer(), offset(rd, left), valid);
+        pz.load(rz.buffer(), offset(rz, left), valid);
+        py.load(ry.buffer(), offset(ry, left), valid);
+        wc.load(rC.buffer(), rC.row, N, left, tid);
+        rd.back();
+        rz.back();
+        ry.back();
+        rC.back();
         if constexpr (!SUM) {
-            px.load(scan_rows<ES>(a.x, b, at), offset(a.x, left), valid);
-            wb.load(scan_rows<ES>(a.B, b, at), a.B.st, N, left, tid);
+            px.load(rx.buffer(), offset(rx, left), valid);
+            wb.load(rB.buffer(), rB.row, N, left, tid);
+            rx.back();
+            rB.back();
         }
-        marks = scan_resets(a, b, at, left, lane);
+        marks.load(a, b, max(t0, (int64_t)0), left, lane);
     };
     float total = 0.0f;
     bool dropped = false;
-    const int64_t tlast = tbeg + (tend - tbeg - 1) / TT * TT;
     fetch(tlast);
+    using Token = ScanToken<L, R, true>;
+    // the state kept before the next 16 tokens to be walked
+    float hnext[R];
+    auto kept = [&](int64_t t) {
+        const float* const from = a.states + ((t / CK * a.batch + b) * a.D + ch) * N + g * R;
+        static_for<R>([&](auto r) { hnext[r] = t >= tbeg && in && g * R + r < N ? from[r] : 0.0f; });
+    };
+    if constexpr (!SUM) kept(tbeg + (tend - tbeg - 1) / CK * CK);
+    // the first value that sum_channels leaves in this lane: the bits that halved the values, the highest first
+    constexpr int USED = 2 * R >= CW ? BITS : (R == 1 ? 1 : 2);
+    const int first = ((lane & (CW - 1)) >> (BITS - USED)) * LEFT;
     for (int64_t t0 = tlast; t0 >= tbeg; t0 -= TT) {
         const int left = (int)min((int64_t)TT, tend - t0);
-        float x[E], raw[E], step[E], zs[E], dys[E], gate[E], ogate[E], dv[E];
-        if constexpr (!SUM) px.unpack(x);
-        pd.unpack(raw);
-        pz.unpack(zs);
-        py.unpack(dys);
-        static_for<E>([&](auto e) {
-            raw[e] += bias[e];
-            step[e] = tr < left && e < valid ? softplus(raw[e]) : 0.0f;
-            dv[e] = dys[e];
-            gate[e] = ogate[e] = 0.0f;
-            if (a.z.p) {
-                sigmoid_pair(zs[e], gate[e], ogate[e]);
-                dv[e] *= zs[e] * gate[e];
-            }
-            dd[tr][pc + e] = make_float4(step[e], SUM ? 0.0f : step[e] * x[e], dv[e], 0.0f);
-        });
+        // (the pieces stay as they came; what the last step needs of them is formed again there)
+        const P qx = px, qd = pd, qz = pz, qy = py;
+        {
+            float x[E], raw[E], zs[E], dv[E];
+            if constexpr (!SUM) qx.unpack(x);
+            qd.unpack(raw);
+            qz.unpack(zs);
+            qy.unpack(dv);
+            static_for<E>([&](auto e) {
+                const float step = tr < left && e < valid ? softplus(raw[e] + bias[e]) : 0.0f;
+                if (a.z.p) {
+                    float gate, omz;
+                    sigmoid_pair(zs[e], gate, omz);
+                    dv[e] *= zs[e] * gate;
+                }
+                dd[tr][pc + e] = make_float4(step, SUM ? 0.0f : step * x[e], dv[e], 0.0f);
+            });
+        }
         wc.template put<R>(bc, 1, tid);
         if constexpr (!SUM) wb.template put<R>(bc, 0, tid);
-        const uint32_t reset = marks;
+        const uint32_t reset = marks.bits();
         fetch(t0 - TT);  // (before the segment: zeros)
         __syncthreads();
         auto walk = [&](auto fast) {
@@ -159,83 +181,90 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                     const int tc = k * CK;
                     if (!FAST && tc >= left) continue;
                     float h[CK + 1][R], av[KEEP ? CK : 1][R];  // h[i]: the state before token i (reset or not)
-                    const float* const from = a.states + (((t0 + tc) / CK * a.batch + b) * a.D + ch) * N + g * R;
-                    static_for<R>([&](auto r) { h[0][r] = in && g * R + r < N ? from[r] : 0.0f; });
-                    static_for<CK / 4>([&](auto q) {
-                        float p[4];
-                        static_for<4>([&](auto j) {
-                            constexpr int i = decltype(q)::value * 4 + decltype(j)::value;
-                            const int t = tc + i;
-                            const float2 s = *reinterpret_cast<const float2*>(&dd[t][cl]);
-                            float Bv[R], Cv[R];
-                            lds_get<R>(bc + (t * L + g) * 2 * R, Bv);
-                            lds_get<R>(bc + (t * L + g) * 2 * R + R, Cv);
-                            const bool drop = !FAST && (reset >> t & 1), live = FAST || t < left;
-                            float acc = 0.0f;
-                            static_for<R>([&](auto r) {
-                                const float aw = live ? __builtin_amdgcn_exp2f(s.x * A2[r]) : 1.0f;
-                                if constexpr (KEEP) av[i][r] = aw;
-                                const float hn = __builtin_fmaf(aw, drop ? 0.0f : h[i][r], s.y * Bv[r]);
-                                h[i + 1][r] = live ? hn : h[i][r];
-                                acc = __builtin_fmaf(Cv[r], h[i + 1][r], acc);
-                            });
-                            p[j] = acc;
+                    static_for<R>([&](auto r) { h[0][r] = hnext[r]; });
+                    kept(t0 + tc - CK);
+                    float(*const to)[CK][2 * NP] = part[BUF == 2 ? k & 1 : 0];
+                    // Tokens' values on their way from LDS: two ahead of the one walked.
+                    Token tok[4];
+                    float dvs[4];
+                    auto get = [&](auto ic) {
+                        constexpr int i = decltype(ic)::value;
+                        tok[i & 3].get(*reinterpret_cast<const float2*>(&dd[tc + i][cl]), bc, tc + i, g);
+                    };
+                    get(std::integral_constant<int, 0>{});
+                    get(std::integral_constant<int, 1>{});
+                    float p[4];
+                    static_for<CK>([&](auto ic) {
+                        constexpr int i = decltype(ic)::value;
+                        if constexpr (i + 2 < CK) get(std::integral_constant<int, (i + 2 < CK ? i + 2 : 0)>{});
+                        __builtin_amdgcn_sched_barrier(0);
+                        const Token& s = tok[i & 3];
+                        const bool drop = !FAST && (reset >> (tc + i) & 1), live = FAST || tc + i < left;
+                        float acc = 0.0f;
+                        static_for<R>([&](auto r) {
+                            const float aw = live ? __builtin_amdgcn_exp2f(s.s.x * A2[r]) : 1.0f;
+                            if constexpr (KEEP) av[i][r] = aw;
+                            const float hn = __builtin_fmaf(aw, drop ? 0.0f : h[i][r], s.s.y * s.B[r]);
+                            h[i + 1][r] = live ? hn : h[i][r];
+                            acc = r == 0 ? s.C[0] * h[i + 1][0] : __builtin_fmaf(s.C[r], h[i + 1][r], acc);
                         });
-                        if (a.z.p) {
-                            const float v = sum_lanes4<L>(p);
-                            dd[tc + q * 4 + (lane >> 4)][cl].w = v;
+                        p[i & 3] = acc;
+                        if constexpr ((i & 3) == 3) {
+                            if (a.z.p) {
+                                const float v = sum_lanes4<L>(p);
+                                dd[tc + i - 3 + (lane >> 4)][cl].w = v;
+                            }
                         }
-                        // (what was read from LDS is read again on the way back, not held in registers)
-                        asm volatile("" ::: "memory");
                     });
-                    static_for<CK / 4>([&](auto qr) {
-                        constexpr int q = CK / 4 - 1 - decltype(qr)::value;
-                        float pq[4], pg[4];
-                        static_for<4>([&](auto jr) {
-                            constexpr int j = 3 - decltype(jr)::value, i = q * 4 + j;
-                            const int t = tc + i;
-                            const float4 s = dd[t][cl];
-                            float Bv[R], Cv[R], sums[2 * R];
-                            lds_get<R>(bc + (t * L + g) * 2 * R, Bv);
-                            lds_get<R>(bc + (t * L + g) * 2 * R + R, Cv);
-                            const bool drop = !FAST && (reset >> t & 1), live = FAST || t < left;
-                            float aq = 0.0f, gb = 0.0f;
-                            static_for<R>([&](auto r) {
-                                G[r] = __builtin_fmaf(Cv[r], s.z, G[r]);
-                                sums[r] = G[r] * s.y;
-                                sums[R + r] = h[i + 1][r] * s.z;
-                                gb = __builtin_fmaf(G[r], Bv[r], gb);
-                                float aw;
-                                if constexpr (KEEP) aw = av[i][r];
-                                else aw = live ? __builtin_amdgcn_exp2f(s.x * A2[r]) : 1.0f;
-                                const float back = aw * G[r];
-                                float qv = back * (drop ? 0.0f : h[i][r]);
-                                if (!FAST) qv = live ? qv : 0.0f;
-                                dA[r] = __builtin_fmaf(qv, s.x, dA[r]);
-                                aq = __builtin_fmaf(qv, A2[r], aq);
-                                G[r] = drop ? 0.0f : back;
-                            });
-                            pq[j] = aq;
-                            pg[j] = gb;
-                            sum_channels<BITS - 1, 2 * R>(sums, lane);
-                            // the lane's first value: the bits that halved the values, the highest first
-                            constexpr int USED = 2 * R >= CW ? BITS : (R == 1 ? 1 : 2);
-                            const int first = ((lane & (CW - 1)) >> (BITS - USED)) * LEFT;
-                            static_for<LEFT>([&](auto e) { part[wid][i][g * 2 * R + first + e] = sums[e]; });
+                    // (what was read from LDS is read again on the way back, not held in registers)
+                    asm volatile("" ::: "memory");
+                    auto get_back = [&](auto ic) {
+                        get(ic);
+                        dvs[ic & 3] = dd[tc + ic][cl].z;
+                    };
+                    get_back(std::integral_constant<int, CK - 1>{});
+                    get_back(std::integral_constant<int, CK - 2>{});
+                    float pq[4], pg[4];
+                    static_for<CK>([&](auto ir) {
+                        constexpr int i = CK - 1 - decltype(ir)::value;
+                        if constexpr (i >= 2) get_back(std::integral_constant<int, (i >= 2 ? i - 2 : 0)>{});
+                        __builtin_amdgcn_sched_barrier(0);
+                        const Token& s = tok[i & 3];
+                        const float dv = dvs[i & 3];
+                        const bool drop = !FAST && (reset >> (tc + i) & 1), live = FAST || tc + i < left;
+                        float aq = 0.0f, gb = 0.0f, sums[2 * R];
+                        static_for<R>([&](auto r) {
+                            G[r] = __builtin_fmaf(s.C[r], dv, G[r]);
+                            sums[r] = G[r] * s.s.y;
+                            sums[R + r] = h[i + 1][r] * dv;
+                            gb = r == 0 ? G[0] * s.B[0] : __builtin_fmaf(G[r], s.B[r], gb);
+                            float aw;
+                            if constexpr (KEEP) aw = av[i][r];
+                            else aw = live ? __builtin_amdgcn_exp2f(s.s.x * A2[r]) : 1.0f;
+                            const float back = aw * G[r];
+                            float qv = back * (drop ? 0.0f : h[i][r]);
+                            if (!FAST) qv = live ? qv : 0.0f;
+                            dA[r] = __builtin_fmaf(qv, s.s.x, dA[r]);
+                            aq = r == 0 ? qv * A2[0] : __builtin_fmaf(qv, A2[r], aq);
+                            G[r] = drop ? 0.0f : back;
                         });
-                        // (the wave's lanes have read these four tokens)
-                        const float sq = sum_lanes4<L>(pq), sg = sum_lanes4<L>(pg);
-                        *reinterpret_cast<float2*>(&dd[tc + q * 4 + (lane >> 4)][cl]) = make_float2(sq, sg);
-                        asm volatile("" ::: "memory");
+                        pq[i & 3] = aq;
+                        pg[i & 3] = gb;
+                        sum_channels<BITS - 1, 2 * R>(sums, lane);
+                        static_for<LEFT>([&](auto e) { to[wid][i][g * 2 * R + first + e] = sums[e]; });
+                        if constexpr ((i & 3) == 0) {
+                            const float sq = sum_lanes4<L>(pq), sg = sum_lanes4<L>(pg);
+                            back_sums[tc + i + (lane >> 4)][cl] = make_float2(sq, sg);
+                        }
                     });
                     __syncthreads();
                     for (int idx = tid; idx < CK * 2 * NP; idx += 256) {
                         const int i = idx / (2 * NP), at = idx % (2 * NP), gg = at / (2 * R), w = at % (2 * R) / R, n = gg * R + at % R;
-                        float s = part[0][i][at];
-                        static_for<kScanWaves - 1>([&](auto k1) { s += part[k1 + 1][i][at]; });
+                        float s = to[0][i][at];
+                        static_for<kScanWaves - 1>([&](auto k1) { s += to[k1 + 1][i][at]; });
                         if (n < N && tc + i < left) a.bc_part[((blk * a.T + t0 + tc + i) * a.batch + b) * 2 * N + w * N + n] = s;
                     }
-                    __syncthreads();
+                    if constexpr (BUF == 1) __syncthreads();
                 }
             }
         };
@@ -244,23 +273,33 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         if constexpr (SUM) {
             __syncthreads();
         } else {
-            float odx[E], odt[E], odz[E];
+            float x[E], raw[E], zs[E], dys[E], odx[E], odt[E], odz[E];
+            qx.unpack(x);
+            qd.unpack(raw);
+            qz.unpack(zs);
+            qy.unpack(dys);
             static_for<E>([&](auto e) {
                 const float4 s = dd[tr][pc + e];
+                const float2 q = back_sums[tr][pc + e];
                 float z, omz;
-                sigmoid_pair(raw[e], z, omz);
-                const float d = __builtin_fmaf(s.y, x[e], s.x * 0.69314718f);
-                odt[e] = d * z;
-                odx[e] = __builtin_fmaf(skip[e], dv[e], step[e] * s.y);
-                const float v = __builtin_fmaf(skip[e], x[e], s.w);
-                odz[e] = dys[e] * v * (gate[e] * __builtin_fmaf(zs[e], ogate[e], 1.0f));
+                sigmoid_pair(raw[e] + bias[e], z, omz);
+                odt[e] = __builtin_fmaf(q.y, x[e], q.x * 0.69314718f) * z;
+                odx[e] = __builtin_fmaf(skip[e], s.z, s.x * q.y);
+                odz[e] = 0.0f;
+                if (a.dz.p) {
+                    sigmoid_pair(zs[e], z, omz);
+                    odz[e] = dys[e] * __builtin_fmaf(skip[e], x[e], s.w) * (z * __builtin_fmaf(zs[e], omz, 1.0f));
+                }
                 const bool live = tr < left && e < valid;
-                sum_skip[e] += live ? dv[e] * x[e] : 0.0f;
+                sum_skip[e] += live ? s.z * x[e] : 0.0f;
                 sum_bias[e] += live ? odt[e] : 0.0f;
             });
-            P::store(scan_rows<ES>(a.dx, b, t0), offset(a.dx, left), valid, odx);
-            P::store(scan_rows<ES>(a.ddt, b, t0), offset(a.ddt, left), valid, odt);
-            if (a.dz.p) P::store(scan_rows<ES>(a.dz, b, t0), offset(a.dz, left), valid, odz);
+            P::store(rdx.buffer(), offset(rdx, left), valid, odx);
+            P::store(rdt.buffer(), offset(rdt, left), valid, odt);
+            P::store(rdz.buffer(), offset(rdz, left), valid, odz);
+            rdx.back();
+            rdt.back();
+            rdz.back();
         }
     }
     if constexpr (SUM) {
