@@ -5,9 +5,9 @@
 // Bound by one pass over the logits.  Within a beam the order is that of the logits themselves, so
 // the first kernel reads each once: a workgroup takes 4096 of a row into registers, sums their
 // exponentials from their maximum, and leaves its best `width`.  To find them without sorting,
-// each thread takes its own best; of these 256 the width-th is a bound that at most width threads pass,
-// so at most 16 width values are left to order, by counting for each how many are better.  Every key holds
-// the place too, so no two are equal and ties need no care.
+// each lane takes its own best; of a wave's 64 the width-th is a bound that at most width lanes pass, so
+// at most 16 width values of a wave are left to order (a few more than width, mostly), by counting for each how
+// many are better.  Every key holds the place too, so no two are equal and ties need no care.
 // The second kernel forms the values of the candidates that are left, in 64 bits (the difference of two
 // beams' sums decides, and an fp32 sum of scores and logits would make ties of what is none), and
 // takes the best in the same way.
@@ -32,23 +32,25 @@ __device__ __forceinline__ double value64(uint64_t o) {
     return __longlong_as_double((long long)((int64_t)o < 0 ? o & 0x7fffffffffffffffull : ~o));
 }
 
-// exp(x) for x <= 0, to 2^-23 of itself: the product with log2 e in two parts.
+// exp(x) for x <= 0, to 2^-23 of itself: the product with log2 e in two parts.  NaN passes.
 __device__ __forceinline__ float exp_of(float x) {
     const float p = x * 1.44269502f, lo = __builtin_fmaf(x, 1.44269502f, -p) + x * 1.92596299e-8f;
     const float e = __builtin_amdgcn_exp2f(p);
-    return p > -126.0f ? __builtin_fmaf(e, lo * 0.69314718f, e) : 0.0f;
+    return p < -126.0f ? 0.0f : __builtin_fmaf(e, lo * 0.69314718f, e);
 }
 
 constexpr int kEach = (int)(kBeamPart / 256);  // logits of a thread
 
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int k) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), k) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, k);
+}
+
 template <int ES>
 __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     constexpr int E = 16 / ES, Q = kEach / E;  // values of a 16-byte piece, pieces of a thread
-    __shared__ uint64_t firsts[256];
-    __shared__ uint64_t list[kEach * kBeamMax];
+    __shared__ __attribute__((aligned(16))) uint64_t list[4 * kEach * kBeamMax];
     __shared__ double wsum[4];
     __shared__ float wmax[4];
-    __shared__ uint64_t bound;
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     const int64_t row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, b = row / a.beams, i = row - b * a.beams;
@@ -65,50 +67,45 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
             if constexpr (ES == 4) f = __uint_as_float(ws[e]);
             else if constexpr (e & 1) f = bf16hi(ws[e / 2]);
             else f = bf16lo(ws[e / 2]);
-            v[q * E + e] = f;
+            v[q * E + e] = e < n ? f : -INFINITY;
         });
     });
     // value k of the thread: place v0 + ((k / E) 256 + tid) E + k % E
     auto place = [&](int k) { return v0 + (int64_t)((k / E) * 256 + tid) * E + k % E; };
-    auto key = [&](int k) { return place(k) < a.V ? (uint64_t)order32(v[k]) << 32 | (uint32_t)~(uint32_t)place(k) : 0ull; };
-    uint64_t first = 0;
-    float most = -INFINITY;
-    bool bad = false;
-    static_for<kEach>([&](auto k) {
-        const bool on = place(k) < a.V;
-        const uint64_t u = key(k);
-        first = u > first ? u : first;
-        most = on ? fmaxf(most, v[k]) : most;
-        bad = bad || (on && v[k] != v[k]);
+    auto key = [&](int k) { return (uint64_t)order32(v[k]) << 32 | (uint32_t)~(uint32_t)place(k); };
+    // (places rise with k: the first of equal values is the best)
+    float most = v[0];
+    int at = 0;
+    static_for<kEach - 1>([&](auto k1) {
+        constexpr int k = decltype(k1)::value + 1;
+        const bool up = v[k] > most || (k == 1 && most != most);  // (a NaN makes the row one without candidates)
+        at = up ? k : at;
+        most = up ? v[k] : most;
     });
-    firsts[tid] = first;
+    const uint64_t first = place(0) < a.V ? (uint64_t)order32(most) << 32 | (uint32_t)~(uint32_t)place(at) : 0ull;
     for (int m = 32; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
     if (lane == 0) wmax[wid] = most;
-    if (tid == 0) {
-        count = 0;
-        bound = 0;
-    }
+    if (tid == 0) count = 0;
     __syncthreads();
     most = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
-    // the sum (an infinite maximum leaves NaN, which the second kernel takes as a row without candidates)
+    // the width-th of the wave's firsts; 0: fewer lanes have any
+    int better = 0;
+    static_for<64>([&](auto k) { better += of_lane(first, decltype(k)::value) > first; });
+    const uint64_t hit = __ballot(better == W - 1 && first != 0);
+    const uint64_t least = hit ? of_lane(first, __builtin_ctzll(hit)) : 0;
+    const float bound = value32((uint32_t)(least >> 32));
+    static_for<kEach>([&](auto k) {
+        if (place(k) < a.V && (least == 0 || v[k] >= bound)) {
+            const uint64_t u = key(k);
+            if (u >= least) list[atomicAdd(&count, 1)] = u;
+        }
+    });
+    // the sum; a NaN or an infinite maximum leaves NaN, which the second kernel takes as a row without candidates
     float few = 0.0f;
-    static_for<kEach>([&](auto k) { few += place(k) < a.V ? (v[k] == -INFINITY ? 0.0f : exp_of(v[k] - most)) : 0.0f; });
-    double sum = bad ? __builtin_nan("") : (double)few;
+    static_for<kEach>([&](auto k) { few += exp_of(v[k] - most); });
+    double sum = most == -INFINITY ? 0.0 : (double)few;
     for (int m = 32; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) wsum[wid] = sum;
-    // the width-th of the threads' best
-    int better = 0;
-    for (int k = 0; k < 256; k += 2) {
-        better += firsts[k] > first;
-        better += firsts[k + 1] > first;
-    }
-    if (better == W - 1 && first) bound = first;
-    __syncthreads();
-    const uint64_t least = bound;  // 0: fewer than width threads have any
-    static_for<kEach>([&](auto k) {
-        const uint64_t u = key(k);
-        if (u && u >= least) list[atomicAdd(&count, 1)] = u;
-    });
     __syncthreads();
     const int n = count;
     uint64_t* const out = a.best + (row * a.parts + part) * W;
@@ -133,73 +130,86 @@ __device__ __forceinline__ bool ahead(const Cand& x, const Cand& y) {
 
 constexpr int kAtOnce = 8;  // candidates of a thread
 
+__device__ __forceinline__ Cand of_lane(const Cand& v, int k) {
+    return Cand{of_lane(v.order, k), (uint32_t)__builtin_amdgcn_readlane((int)v.place, k)};
+}
+
 __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
     __shared__ double offset[kBeamMax];       // score - log sum; -inf: no candidate but of -inf
-    __shared__ Cand firsts[256];
-    __shared__ Cand list[(kAtOnce + 1) * kBeamMax];
+    __shared__ bool over[kBeamMax];           // finished
+    __shared__ Cand list[4 * (kAtOnce + 1) * kBeamMax];
     __shared__ Cand best[kBeamMax];
-    __shared__ Cand bound;
     __shared__ int count;
-    const int tid = threadIdx.x, W = (int)a.width;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, W = (int)a.width, parts = (int)a.parts, beams = (int)a.beams;
     const int64_t b = blockIdx.x;
-    for (int64_t i = tid; i < a.beams; i += 256) {
-        const int64_t row = b * a.beams + i;
-        const double2* const s = a.sums + row * a.parts;
+    const uint32_t each = (uint32_t)parts * (uint32_t)W, all = (uint32_t)beams * each, V = (uint32_t)a.V, end = (uint32_t)a.end;
+    const uint64_t* const from = a.best + b * (int64_t)all;
+    const uint64_t early = tid < all ? from[tid] : 0ull;  // (on its way during the sums)
+    int lanes = 1;
+    while (lanes < 64 && lanes < parts) lanes *= 2;
+    // a wave to a beam, a lane to a part
+    for (int i = wid; i < beams; i += 4) {
+        const int64_t row = b * beams + i;
+        const double2* const s = a.sums + row * parts;
+        const double score = (double)a.scores[row];
+        const bool done = a.finished && a.finished[row];
         double most = -INFINITY, sum = 0.0;
-        bool bad = false;
-        for (int64_t p = 0; p < a.parts; ++p) {
-            most = s[p].x > most ? s[p].x : most;
-            bad = bad || s[p].y != s[p].y;
+        for (int p = lane; p < parts; p += 64) most = s[p].x > most ? s[p].x : most;
+        for (int m = lanes / 2; m > 0; m >>= 1) {
+            const double o = __shfl_xor(most, m);
+            most = o > most ? o : most;
         }
-        for (int64_t p = 0; p < a.parts; ++p) sum += s[p].x == -INFINITY ? 0.0 : s[p].y * exp(s[p].x - most);
-        double o = (double)a.scores[row] - (most + log(sum));
-        if (a.finished && a.finished[row]) o = (double)a.scores[row];
-        else if (bad || most == -INFINITY || most == INFINITY) o = -INFINITY;
-        offset[i] = o == o ? o : -INFINITY;
+        // (a part without a finite logit has no sum)
+        for (int p = lane; p < parts; p += 64) sum += s[p].x == -INFINITY ? s[p].y : s[p].y * exp(s[p].x - most);
+        for (int m = lanes / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
+        const double o = done ? score : most == -INFINITY || most == INFINITY ? -INFINITY : score - (most + log(sum));
+        if (lane == 0) {
+            offset[i] = o == o ? o : -INFINITY;
+            over[i] = done;
+        }
     }
     for (int k = tid; k < W; k += 256) best[k] = Cand{0, 0};
     __syncthreads();
     // candidate c: of beam c / each; of a beam that can go on the parts' best, else the first tokens
-    const int64_t each = a.parts * W, all = a.beams * each;
     const double none = -INFINITY;
-    auto candidate = [&](int64_t c) {
-        const int64_t i = c / each, k = c - i * each, row = b * a.beams + i;
+    auto candidate = [&](uint32_t c) {
+        const uint32_t i = c / each, k = c - i * each;
         const double o = offset[i];
-        const bool over = a.finished && a.finished[row];
-        if (over || o == none) {
+        if (over[i] || o == none) {
             // (a finished beam: its end token, then the others)
-            if (k >= W || k >= a.V) return Cand{0, 0};
-            if (over && o != none) {
-                const int64_t v = k == 0 ? a.end : k - 1 < a.end ? k - 1 : k;
-                return Cand{order64(k == 0 ? o : none), (uint32_t)(i * a.V + v)};
+            if (k >= (uint32_t)W || k >= V) return Cand{0, 0};
+            if (over[i] && o != none) {
+                const uint32_t v = k == 0 ? end : k - 1 < end ? k - 1 : k;
+                return Cand{order64(k == 0 ? o : none), i * V + v};
             }
-            return Cand{order64(none), (uint32_t)(i * a.V + k)};
+            return Cand{order64(none), i * V + k};
         }
-        const uint64_t u = a.best[row * each + k];
+        const uint64_t u = c < 256 ? early : from[c];
         if (!u) return Cand{0, 0};
         const double v = o + (double)value32((uint32_t)(u >> 32));
-        return Cand{order64(v == v ? v : none), (uint32_t)(i * a.V) + ~(uint32_t)u};
+        return Cand{order64(v == v ? v : none), i * V + ~(uint32_t)u};
     };
-    for (int64_t c0 = 0; c0 < all; c0 += 256 * kAtOnce) {
+    for (uint32_t c0 = 0; c0 < all; c0 += 256 * kAtOnce) {
         Cand mine[kAtOnce + 1];
         static_for<kAtOnce>([&](auto k) {
-            const int64_t c = c0 + k * 256 + tid;
-            mine[k] = c < all ? candidate(c) : Cand{0, 0};
+            const uint32_t c = c0 + k * 256 + tid;
+            mine[k] = Cand{0, 0};
+            if (c0 + k * 256 < all && c < all) mine[k] = candidate(c);
         });
         mine[kAtOnce] = tid < W ? best[tid] : Cand{0, 0};
+        if (tid == 0) count = 0;
         Cand first{0, 0};
         static_for<kAtOnce + 1>([&](auto k) { first = ahead(mine[k], first) ? mine[k] : first; });
-        firsts[tid] = first;
-        if (tid == 0) {
-            count = 0;
-            bound = Cand{0, 0};
+        // the width-th of the wave's firsts, as above; a wave without candidates has none to pass on
+        Cand least{0, 0};
+        const uint64_t with = __ballot(first.order != 0);
+        if (with) {
+            int better = 0;
+            for (int k = 0; k <= 63 - __builtin_clzll(with); ++k) better += ahead(of_lane(first, k), first);
+            const uint64_t hit = __ballot(better == W - 1 && first.order != 0);
+            if (hit) least = of_lane(first, __builtin_ctzll(hit));
         }
-        __syncthreads();
-        int better = 0;
-        for (int k = 0; k < 256; ++k) better += ahead(firsts[k], first);
-        if (better == W - 1 && first.order) bound = first;
-        __syncthreads();
-        const Cand least = bound;
+        __syncthreads();  // (best has been read, count is clear)
         static_for<kAtOnce + 1>([&](auto k) {
             if (mine[k].order && !ahead(least, mine[k])) list[atomicAdd(&count, 1)] = mine[k];
         });
@@ -215,11 +225,12 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
     }
     for (int k = tid; k < W; k += 256) {
         const Cand u = best[k];
-        const int64_t i = u.place / a.V, v = u.place - i * a.V, at = b * W + k;
+        const uint32_t i = u.place / V, v = u.place - i * V;
+        const int64_t at = b * W + k;
         a.scores_out[at] = (float)value64(u.order);
         a.parent[at] = (int32_t)i;
         a.token[at] = (int32_t)v;
-        if (a.finished_out) a.finished_out[at] = v == a.end || (a.finished && a.finished[b * a.beams + i]);
+        if (a.finished_out) a.finished_out[at] = (int64_t)v == a.end || over[i];
     }
 }
 
