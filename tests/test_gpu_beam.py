@@ -142,3 +142,72 @@ def test_reorder(shape, dim, dtype):
     got = isam.beam_reorder(s, p, dim=dim).cpu()
     assert (got.select(dim, 1) == 0).all() and (got.select(dim, 2) == 0).all()
     assert torch.equal(got.select(dim, 3), s.cpu().select(dim, 5))
+
+
+def test_streams_repeats_and_graph_replays():
+    logits, scores = inputs(3, 4, 9000, torch.float32, 5)
+    state = torch.randn((2, 12, 33), device="cuda")
+    out = dict(scores_out=torch.empty((3, 4), device="cuda"), parent=torch.empty((3, 4), device="cuda", dtype=torch.int32),
+               token=torch.empty((3, 4), device="cuda", dtype=torch.int32), finished_out=torch.empty((3, 4), device="cuda", dtype=torch.bool),
+               workspace=torch.empty(isam.beam_step_workspace_size(3, 4, 9000, 4, isam.ISAM_F32), device="cuda", dtype=torch.uint8))
+    moved = torch.empty_like(state)
+
+    def step():
+        isam.beam_step(logits, scores, end=2, **out)
+        isam.beam_reorder(state, out["parent"], dim=1, out=moved)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        logits.copy_(inputs(3, 4, 9000, torch.float32, 10 + i)[0])
+        want = compare(logits, scores, end=2)
+        other = isam.beam_reorder(state, want[1], dim=1)
+        for _ in range(2):
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip((out["scores_out"], out["parent"], out["token"], out["finished_out"], moved), (*want, other)):
+                assert torch.equal(a, b)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = isam.beam_step(logits, scores, end=2)
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_refusals():
+    logits, scores = inputs(2, 3, 50, torch.float32)
+    fin = torch.zeros((2, 3), device="cuda", dtype=torch.bool)
+    with pytest.raises(ValueError):
+        isam.beam_step(logits[0], scores)
+    with pytest.raises(ValueError):
+        isam.beam_step(logits, scores[:, :2])
+    with pytest.raises(TypeError):
+        isam.beam_step(logits, scores.double())
+    with pytest.raises(TypeError):
+        isam.beam_step(logits.half(), scores)
+    with pytest.raises(TypeError):
+        isam.beam_step(logits, scores, finished=fin.float(), end=1)
+    with pytest.raises(ValueError):
+        isam.beam_step(logits.cpu(), scores.cpu())
+    for kw in (dict(width=65), dict(width=0), dict(end=50), dict(finished=fin), dict(width=200)):
+        with pytest.raises((isam.IsamError, RuntimeError)):
+            isam.beam_step(logits, scores, **kw)
+    with pytest.raises(isam.IsamError) as e:
+        isam.beam_step(logits, scores, workspace=torch.empty(16, device="cuda", dtype=torch.uint8))
+    assert e.value.status == 3
+    p = torch.zeros((2, 3), device="cuda", dtype=torch.int32)
+    state = torch.zeros((4, 6, 5), device="cuda")
+    for bad in (lambda: isam.beam_reorder(state, p, dim=2), lambda: isam.beam_reorder(state.transpose(0, 1), p),
+                lambda: isam.beam_reorder(state, p[0], dim=1), lambda: isam.beam_reorder(state, p, dim=3),
+                lambda: isam.beam_reorder(state, p, dim=1, out=torch.zeros((4, 5, 5), device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        isam.beam_reorder(state, p.long(), dim=1)
+    with pytest.raises(isam.IsamError):
+        isam.beam_reorder(state, p, dim=1, out=state)

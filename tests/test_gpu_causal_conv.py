@@ -149,3 +149,185 @@ def test_optional_arguments():
     compare(x)
     y, kept = isam.causal_conv(x["x"], x["w"], return_state=False)
     assert kept is None
+
+
+@DTYPES
+@pytest.mark.parametrize("T", [2, 30, 200])
+def test_slices(T, dtype):
+    B, C, K = 3, 21, 4
+    x = inputs(T, B, C, K, dtype, seed=T, reset=0.05)
+    ref = reference(x, "silu")
+    wide = torch.zeros((T, B, C + 9), device="cuda", dtype=dtype)
+    wide[..., 3:3 + C] = x["x"]
+    x["x"] = wide[..., 3:3 + C]
+    y, dx = (torch.full((T, B, C + 5), 7.0, device="cuda", dtype=dtype) for _ in range(2))
+    opt = {k: x[k] for k in ("bias", "state", "reset")}
+    isam.causal_conv(x["x"], x["w"], y=y[..., 1:1 + C], **opt)
+    isam.causal_conv_backward(x["x"], x["w"], x["dy"], dstate_T=x["dstate_T"], dx=dx[..., 2:2 + C], **opt)
+    check(y[..., 1:1 + C], ref["y"], "y")
+    check(dx[..., 2:2 + C], ref["dx"], "dx")
+    for t, lo in ((y, 1), (dx, 2)):
+        assert (t[..., :lo] == 7).all() and (t[..., lo + C:] == 7).all()
+
+
+@DTYPES
+@pytest.mark.parametrize("T", [6, 60, 300])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_reset_cuts_off_bad_values(T, dtype, bad):
+    B, C, K = 2, 12, 4
+    a, b = T // 3, 2 * T // 3
+    x = inputs(T, B, C, K, dtype, seed=T)
+    x["reset"] = torch.zeros((T, B), dtype=torch.bool, device="cuda")
+    x["reset"][a] = x["reset"][b] = True
+    ref = reference(x, "silu")
+    x["x"][a:b] = bad
+    x["dy"][a:b] = bad
+    out = run(x, "silu")
+    for part in (slice(0, a), slice(b, T)):
+        for k in ("y", "dx"):
+            check(out[k][part], (ref[k][0][part], ref[k][1][part]), f"{k} {part}")
+    check(out["dstate"], ref["dstate"], "dstate")
+    if T - b >= K - 1:
+        check(out["state_T"], ref["state_T"], "state_T")
+
+
+def test_reset_in_the_kept_inputs():
+    # a reset within the last K - 1 tokens: the next call does not see what lies before it
+    x = inputs(20, 2, 8, 4, torch.float32, seed=1)
+    x["reset"] = torch.zeros((20, 2), dtype=torch.bool, device="cuda")
+    x["reset"][18, 0] = x["reset"][19, 1] = True
+    whole, _ = isam.causal_conv(torch.cat((x["x"], x["x"])), x["w"], bias=x["bias"], state=x["state"],
+                                reset=torch.cat((x["reset"], torch.zeros_like(x["reset"]))))
+    _, kept = isam.causal_conv(x["x"], x["w"], bias=x["bias"], state=x["state"], reset=x["reset"])
+    assert (kept[:2, 0] != 0).any(-1).tolist() == [False, True] and (kept[:, 1] != 0).any(-1).tolist() == [False, False, True]
+    y, _ = isam.causal_conv(x["x"], x["w"], bias=x["bias"], state=kept)
+    assert torch.equal(y, whole[20:])
+
+
+@pytest.mark.parametrize("C", [1, 3, 5, 24, 261])
+@pytest.mark.parametrize("T", [1, 2, 8])
+def test_state_in_place(T, C):
+    x = inputs(T, 5, C, 4, torch.bfloat16, seed=T)
+    y, kept = isam.causal_conv(x["x"], x["w"], bias=x["bias"], state=x["state"])
+    state = x["state"].clone()
+    y2, s2 = isam.causal_conv(x["x"], x["w"], bias=x["bias"], state=state, state_T=state)
+    assert s2 is state and torch.equal(y, y2) and torch.equal(kept, state)
+
+
+def test_tokens_one_by_one():
+    x = inputs(30, 3, 20, 4, torch.float32, seed=5, reset=0.1)
+    ref = reference(x, "silu")
+    state, ys = x["state"].clone(), []
+    for t in range(30):
+        y, _ = isam.causal_conv(x["x"][t:t + 1], x["w"], bias=x["bias"], state=state, state_T=state, reset=x["reset"][t:t + 1])
+        ys.append(y)
+    check(torch.cat(ys), ref["y"], "y")
+    check(state, ref["state_T"], "state_T")
+
+
+def test_empty():
+    x = inputs(0, 3, 16, 4, torch.bfloat16)
+    y, kept = isam.causal_conv(x["x"], x["w"], bias=x["bias"], state=x["state"])
+    assert y.shape == (0, 3, 16) and torch.equal(kept, x["state"])
+    assert (isam.causal_conv(x["x"], x["w"])[1] == 0).all()
+    dx, ds, dw, db = isam.causal_conv_backward(x["x"], x["w"], x["dy"], bias=x["bias"], state=x["state"], dstate_T=x["dstate_T"])
+    assert torch.equal(ds, x["dstate_T"]) and (dw == 0).all() and (db == 0).all()
+    x = inputs(4, 0, 16, 3, torch.float32)
+    assert isam.causal_conv(x["x"], x["w"])[0].shape == (4, 0, 16)
+    assert (isam.causal_conv_backward(x["x"], x["w"], x["dy"])[2] == 0).all()
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_gradient_against_differences(T):
+    # central differences, step 2^-7: third-order terms below 2^-14 of the terms, rounding 2^-24 2^7 of the sums
+    x = inputs(T, 2, 6, 4, torch.float32, seed=T, reset=0.1)
+    out, g, step = run(x, "silu"), torch.Generator(device="cuda").manual_seed(5), 2.0 ** -7
+
+    def loss(v):
+        y, kept = isam.causal_conv(v["x"], v["w"], bias=v["bias"], state=v["state"], reset=v["reset"])
+        return float((y.double() * x["dy"].double()).sum() + (kept.double() * x["dstate_T"].double()).sum())
+
+    size = float((out["y"].double() * x["dy"].double()).abs().sum() + (out["state_T"].double() * x["dstate_T"].double()).abs().sum())
+    for name in ("x", "w", "bias", "state"):
+        v = torch.randn(x[name].shape, generator=g, device="cuda")
+        hi, lo = dict(x), dict(x)
+        hi[name], lo[name] = x[name] + step * v, x[name] - step * v
+        diff = (loss(hi) - loss(lo)) / (2 * step)
+        terms = out["d" + name].double() * v.double()
+        assert abs(diff - float(terms.sum())) <= 2.0 ** -9 * float(terms.abs().sum()) + 2.0 ** -14 * size, name
+
+
+def test_repeats_and_streams():
+    x = inputs(900, 2, 70, 4, torch.bfloat16, seed=2, reset=0.01)
+    ref = run(x, "silu")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        out = run(x, "silu")
+    torch.cuda.current_stream().wait_stream(s)
+    for k in ref:
+        assert torch.equal(out[k], ref[k]), k
+
+
+def test_graph_replays():
+    x = inputs(300, 2, 40, 4, torch.bfloat16, seed=4, reset=0.01)
+    opt = {k: x[k] for k in ("bias", "state", "reset")}
+    like = lambda t, dt=None: torch.empty(t.shape, device="cuda", dtype=dt or t.dtype)  # noqa: E731
+    fwd = dict(y=like(x["x"]), state_T=like(x["state"]))
+    bwd = dict(dx=like(x["x"]), dstate=like(x["state"]), dw=like(x["w"]), dbias=like(x["bias"]))
+    ws = torch.empty(isam.causal_conv_backward_workspace_size(300, 2, 40, 4, 1), device="cuda", dtype=torch.uint8)
+
+    def both():
+        isam.causal_conv(x["x"], x["w"], **opt, **fwd)
+        isam.causal_conv_backward(x["x"], x["w"], x["dy"], dstate_T=x["dstate_T"], workspace=ws, **opt, **bwd)
+
+    both()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for i in range(3):
+        x["x"].copy_(torch.randn(x["x"].shape, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16))
+        ref = run(x, "silu")
+        g.replay()
+        torch.cuda.synchronize()
+        for k, v in {**fwd, **bwd}.items():
+            assert torch.equal(v, ref[k]), k
+
+
+def test_long_offsets():
+    # sequences whose places pass 2^31 elements: waves of one sequence each, and the last tokens of a long one
+    B, C, K = 3, 8, 4
+    x = inputs(40, B, C, K, torch.bfloat16, seed=6, reset=0.1)
+    big = torch.empty((2 * ((1 << 30) + 7) + 40 * C,), device="cuda", dtype=torch.bfloat16)
+    v = big.as_strided((40, B, C), (C, (1 << 30) + 7, 1))
+    v.copy_(x["x"])
+    x["x"] = v
+    compare(x)
+    x = inputs(300, 1, C, K, torch.bfloat16, seed=7)
+    stride = (1 << 31) // 256
+    v = torch.empty((300 * stride,), device="cuda", dtype=torch.bfloat16).as_strided((300, 1, C), (stride, stride, 1))
+    v.copy_(x["x"])
+    x["x"] = v
+    compare(x)
+
+
+def test_refusals():
+    x = inputs(10, 2, 16, 4, torch.float32)
+    for kw in (dict(bias=x["bias"][:5]), dict(state=x["state"][:2]), dict(activation="gelu"), dict(y=torch.empty((10, 2, 17), device="cuda"))):
+        with pytest.raises(ValueError):
+            isam.causal_conv(x["x"], x["w"], **kw)
+    for kw in (dict(bias=x["bias"].double()), dict(state=x["state"].bfloat16()), dict(reset=torch.zeros((10, 2), device="cuda"))):
+        with pytest.raises(TypeError):
+            isam.causal_conv(x["x"], x["w"], **kw)
+    with pytest.raises(ValueError):
+        isam.causal_conv(x["x"].cpu(), x["w"])
+    with pytest.raises(isam.IsamError):
+        isam.causal_conv(x["x"], torch.zeros((7, 16), device="cuda"))
+    with pytest.raises(isam.IsamError):
+        isam.causal_conv(x["x"], x["w"], y=x["x"])
+    with pytest.raises(isam.IsamError):
+        isam.causal_conv(x["x"], x["w"], state=x["state"], state_T=x["state"])
+    with pytest.raises(isam.IsamError) as e:
+        isam.causal_conv_backward(x["x"], x["w"], x["dy"], workspace=torch.empty(16, device="cuda", dtype=torch.uint8))
+    assert e.value.status == 3

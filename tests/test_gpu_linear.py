@@ -120,3 +120,140 @@ def test_gradient_of_few_rows_rounds_once(M, K, N):
         for k, v in zip(("dx", "dW"), isam.linear_backward(x["x"], x["W"], x["dout"], bias=x["bias"], activation=name)):
             val = ref[k][0]
             assert float((v.double() - val).norm()) <= (2.0 ** -9 + 2.0 ** -13) * float(val.norm()), k
+
+
+@DTYPES
+@pytest.mark.parametrize("M,K,N", [(5, 72, 40), (70, 72, 40), (300, 200, 65), (500, 511, 77), (1500, 130, 1100)])
+def test_strided_rows(M, K, N, dtype):
+    # every matrix as a slice of wider rows, off 16 bytes; nothing beside the rows is touched
+    for name in ("gelu", "none"):
+        x = inputs(M, K, N, dtype, seed=M)
+        ref = reference(x, name)
+
+        def wide(t, off, fill):
+            w = torch.full((t.shape[0], t.shape[1] + 11), fill, device="cuda", dtype=t.dtype)
+            w[:, off:off + t.shape[1]] = t
+            return w, w[:, off:off + t.shape[1]]
+
+        xs, ws, rs, ds = (wide(x[k], o, float("nan"))[1] for k, o in (("x", 3), ("W", 1), ("residual", 5), ("dout", 2)))
+        out_w, out = wide(torch.zeros_like(x["dout"]), 3, 7.0)
+        dx_w, dx = wide(torch.zeros_like(x["x"]), 1, 7.0)
+        dW_w, dW = wide(torch.zeros_like(x["W"]), 4, 7.0)
+        isam.linear(xs, ws, bias=x["bias"], activation=name, residual=rs, out=out)
+        _, _, db = isam.linear_backward(xs, ws, ds, bias=x["bias"], activation=name, dx=dx, dW=dW)
+        for k, v in (("out", out), ("dx", dx), ("dW", dW), ("dbias", db)):
+            check(v, ref[k], f"{name} {k}")
+        for w, off, n in ((out_w, 3, N), (dx_w, 1, K), (dW_w, 4, K)):
+            assert (w[:, :off] == 7).all() and (w[:, off + n:] == 7).all()
+
+
+@DTYPES
+def test_parts_of_the_gradient(dtype):
+    x = inputs(100, 64, 72, dtype)
+    for name in ("silu", "none"):
+        ref = reference(x, name)
+        dx, dW, db = isam.linear_backward(x["x"], x["W"], x["dout"], activation=name, return_dW=False)
+        assert dW is None and db is None
+        check(dx, ref["dx"] if x["bias"] is None else reference({**x, "bias": None}, name)["dx"], "dx")
+        dx, dW, db = isam.linear_backward(x["x"], x["W"], x["dout"], bias=x["bias"], activation=name, return_dx=False)
+        assert dx is None
+        check(dW, ref["dW"], "dW")
+        check(db, ref["dbias"], "dbias")
+
+
+def test_empty():
+    for dtype in (torch.float32, torch.bfloat16):
+        e = torch.empty((0, 16), device="cuda", dtype=dtype)
+        W = torch.ones((8, 16), device="cuda", dtype=dtype)
+        assert isam.linear(e, W).shape == (0, 8)
+        dx, dW, db = isam.linear_backward(e, W, torch.empty((0, 8), device="cuda", dtype=dtype), bias=torch.ones(8, device="cuda"))
+        assert dx.shape == (0, 16) and (dW == 0).all() and (db == 0).all()
+        x, none = torch.ones((5, 16), device="cuda", dtype=dtype), torch.empty((0, 16), device="cuda", dtype=dtype)
+        assert isam.linear(x, none).shape == (5, 0)
+        assert (isam.linear_backward(x, none, torch.empty((5, 0), device="cuda", dtype=dtype))[0] == 0).all()
+
+
+@pytest.mark.parametrize("name", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("M,K,N", [(5, 40, 30), (100, 40, 30)])
+def test_gradient_against_differences(M, K, N, name):
+    # central differences, step 2^-6: third-order terms below 2^-12 of the terms, rounding 2^-22 2^6 of the sums
+    x = inputs(M, K, N, torch.float32, seed=M)
+    grads = dict(zip(("x", "W", "bias"), isam.linear_backward(x["x"], x["W"], x["dout"], bias=x["bias"], activation=name)))
+    g, step = torch.Generator(device="cuda").manual_seed(5), 2.0 ** -6
+    for k, d in grads.items():
+        v = torch.randn(x[k].shape, generator=g, device="cuda")
+        side = []
+        for s in (step, -step):
+            y = {**x, k: x[k] + s * v}
+            side.append(float((isam.linear(y["x"], y["W"], bias=y["bias"], activation=name).double() * x["dout"].double()).sum()))
+        terms = d.double() * v.double()
+        size = float((isam.linear(x["x"], x["W"], bias=x["bias"], activation=name).double() * x["dout"].double()).abs().sum())
+        assert abs((side[0] - side[1]) / (2 * step) - float(terms.sum())) <= 2.0 ** -10 * float(terms.abs().sum()) + 2.0 ** -16 * size, k
+
+
+@DTYPES
+def test_infinite_values_stay_in_their_rows(dtype):
+    x = inputs(130, 64, 72, dtype)
+    x["x"][7] = float("nan")
+    x["x"][100, 3] = float("inf")
+    out = isam.linear(x["x"], x["W"], bias=x["bias"], activation="silu", residual=x["residual"])
+    rows = torch.ones(130, dtype=torch.bool, device="cuda")
+    rows[7] = rows[100] = False
+    assert torch.isnan(out[7]).all() and torch.isfinite(out[rows].float()).all()
+
+
+def test_streams_and_graph_replays():
+    for M in (4, 200):
+        x = inputs(M, 72, 80, torch.bfloat16, seed=M)
+        code = isam.ISAM_BF16
+        out, dx, dW, db = (torch.empty_like(x[k]) for k in ("dout", "x", "W", "bias"))
+        w1 = torch.empty(max(1, isam.linear_workspace_size(M, 72, 80, code)), device="cuda", dtype=torch.uint8)
+        w2 = torch.empty(isam.linear_backward_workspace_size(M, 72, 80, code), device="cuda", dtype=torch.uint8)
+
+        def both(out, dx, dW, db):
+            isam.linear(x["x"], x["W"], bias=x["bias"], activation="gelu", residual=x["residual"], out=out, workspace=w1)
+            isam.linear_backward(x["x"], x["W"], x["dout"], bias=x["bias"], activation="gelu", dx=dx, dW=dW, dbias=db, workspace=w2)
+
+        both(out, dx, dW, db)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            both(out, dx, dW, db)
+        for i in range(3):
+            x["x"].copy_(torch.randn((M, 72), generator=torch.Generator().manual_seed(i)).to(torch.bfloat16))
+            ref = tuple(torch.empty_like(t) for t in (out, dx, dW, db))
+            both(*ref)
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip((out, dx, dW, db), ref):
+                assert torch.equal(a, b)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            other = isam.linear(x["x"], x["W"], bias=x["bias"], activation="gelu", residual=x["residual"])
+        torch.cuda.current_stream().wait_stream(s)
+        assert torch.equal(other, out)
+
+
+def test_refusals():
+    x = inputs(40, 64, 72, torch.float32)
+    for kw in (dict(bias=x["bias"][:5]), dict(residual=x["residual"][:5]), dict(activation="relu"), dict(out=torch.empty((40, 71), device="cuda"))):
+        with pytest.raises(ValueError):
+            isam.linear(x["x"], x["W"], **kw)
+    for kw in (dict(bias=x["bias"].double()), dict(residual=x["residual"].bfloat16())):
+        with pytest.raises(TypeError):
+            isam.linear(x["x"], x["W"], **kw)
+    with pytest.raises(ValueError):
+        isam.linear(x["x"][:, :5], x["W"])
+    with pytest.raises(TypeError):
+        isam.linear(x["x"].half(), x["W"].half())
+    with pytest.raises(ValueError):
+        isam.linear(x["x"].cpu(), x["W"].cpu())
+    with pytest.raises(isam.IsamError):          # a residual that is out shifted by a row
+        r = torch.zeros((41, 72), device="cuda")
+        isam.linear(x["x"], x["W"], residual=r[1:], out=r[:40])
+    with pytest.raises(isam.IsamError):
+        isam.linear_backward(x["x"], x["W"], x["dout"], dx=x["x"])
+    with pytest.raises(isam.IsamError) as e:
+        isam.linear_backward(x["x"], x["W"], x["dout"], workspace=torch.empty(16, device="cuda", dtype=torch.uint8))
+    assert e.value.status == 3

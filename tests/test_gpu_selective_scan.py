@@ -183,3 +183,247 @@ def test_widths(D, dtype):
                                            (640, 3, 16, 64, 0.004), (1030, 1, 16, 32, None)])
 def test_time_in_segments(T, B, D, N, reset, dtype):
     compare(inputs(T, B, D, N, dtype, seed=T, reset=reset))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [6, 70, 400])
+def test_slices_and_batch_first(T, dtype):
+    # x and z halves of one tensor's rows, B and C of another's, at odd offsets; gradients into slices alike
+    B, D, N = 3, 37, 11
+    for first in (False, True):
+        x = inputs(T, B, D, N, dtype, seed=T, batch_first=first, reset=0.02)
+        ref = reference(x)
+
+        def wide(w, fill=7.0):
+            t = torch.full((B, T, w) if first else (T, B, w), fill, device="cuda", dtype=dtype)
+            return t.transpose(0, 1) if first else t
+
+        xz, bc, y = wide(2 * D + 5), wide(2 * N + 3), wide(D + 2)
+        xz[..., 1:1 + D], xz[..., 3 + D:3 + 2 * D] = x["x"], x["z"]
+        bc[..., :N], bc[..., N + 1:2 * N + 1] = x["B"], x["C"]
+        x["x"], x["z"], x["B"], x["C"] = xz[..., 1:1 + D], xz[..., 3 + D:3 + 2 * D], bc[..., :N], bc[..., N + 1:2 * N + 1]
+        states = torch.empty(isam.selective_scan_states_shape(T, B, D, N), device="cuda")
+        seq, opt = tuple(x[k] for k in ("x", "dt", "A", "B", "C")), {k: x[k] for k in ("skip", "z", "dt_bias", "reset")}
+        isam.selective_scan(*seq, h0=x["h0"], y=y[..., 1:1 + D], states=states, **opt)
+        dxz, dbc = wide(2 * D + 5), wide(2 * N + 3)
+        isam.selective_scan_backward(*seq, x["dy"], states=states, dh_T=x["dh_T"], dx=dxz[..., 1:1 + D], dz=dxz[..., 3 + D:3 + 2 * D],
+                                     dB=dbc[..., :N], dC=dbc[..., N + 1:2 * N + 1], **opt)
+        torch.cuda.synchronize()
+        check(y[..., 1:1 + D], ref["y"], "y")
+        check(dxz[..., 1:1 + D], ref["dx"], "dx")
+        check(dxz[..., 3 + D:3 + 2 * D], ref["dz"], "dz")
+        check(dbc[..., :N], ref["dB"], "dB")
+        check(dbc[..., N + 1:2 * N + 1], ref["dC"], "dC")
+        for t, used in ((y, [(1, 1 + D)]), (dxz, [(1, 1 + D), (3 + D, 3 + 2 * D)]), (dbc, [(0, N), (N + 1, 2 * N + 1)])):
+            rest = torch.ones(t.shape[-1], dtype=torch.bool, device="cuda")
+            for lo, hi in used:
+                rest[lo:hi] = False
+            assert (t[..., rest] == 7).all()          # nothing beside the rows is touched
+
+
+@pytest.mark.parametrize("T", [5, 40, 300])
+def test_optional_arguments(T):
+    x = inputs(T, 2, 24, 16, torch.float32, seed=T, gate=False)
+    x["skip"] = x["dt_bias"] = x["h0"] = x["dh_T"] = None
+    out = compare(x)
+    assert not {"dskip", "dz", "ddt_bias"} & set(out)
+    x = inputs(T, 2, 24, 16, torch.float32, seed=T)
+    x["dy"] = None
+    compare(x)
+    seq, opt = tuple(x[k] for k in ("x", "dt", "A", "B", "C")), {k: x[k] for k in ("skip", "z", "dt_bias")}
+    y, h = isam.selective_scan(*seq, h0=x["h0"], return_sequence=False, **opt)
+    assert y is None
+    check(h, reference(x)["h_T"], "h_T")
+
+
+def test_empty():
+    x = inputs(0, 3, 16, 8, torch.float32)
+    seq, opt = tuple(x[k] for k in ("x", "dt", "A", "B", "C")), {k: x[k] for k in ("skip", "z", "dt_bias")}
+    y, h = isam.selective_scan(*seq, h0=x["h0"], **opt)
+    assert y.shape == (0, 3, 16) and torch.equal(h, x["h0"])
+    assert (isam.selective_scan(*seq, **opt)[1] == 0).all()
+    states = torch.empty(isam.selective_scan_states_shape(0, 3, 16, 8), device="cuda")
+    out = dict(zip(NAMES, isam.selective_scan_backward(*seq, x["dy"], states=states, dh_T=x["dh_T"], **opt)))
+    assert torch.equal(out["dh0"], x["dh_T"]) and all((out[k] == 0).all() for k in ("dA", "dskip", "ddt_bias"))
+    x = inputs(5, 0, 16, 8, torch.float32)
+    seq, opt = tuple(x[k] for k in ("x", "dt", "A", "B", "C")), {k: x[k] for k in ("skip", "z", "dt_bias")}
+    assert isam.selective_scan(*seq, **opt)[0].shape == (5, 0, 16)
+    states = torch.empty(isam.selective_scan_states_shape(5, 0, 16, 8), device="cuda")
+    out = dict(zip(NAMES, isam.selective_scan_backward(*seq, x["dy"], states=states, **opt)))
+    assert all((out[k] == 0).all() for k in ("dA", "dskip", "ddt_bias"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [6, 60, 500])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_reset_cuts_off_bad_values(T, dtype, bad):
+    # a text of bad values between two good ones, and bad gradients likewise: neither the states after it nor
+    # the gradients before it see them
+    B, D, N = 2, 20, 9
+    a, b = T // 3, 2 * T // 3
+    for key in ("x", "dt", "B", "C", "z"):
+        x = inputs(T, B, D, N, dtype, seed=T)
+        r = torch.zeros((T, B), dtype=torch.bool, device="cuda")
+        r[a], r[b] = True, True
+        x["reset"] = r
+        ref = reference(x)
+        x[key][a:b] = bad
+        x["dy"][a:b] = bad
+        out = run(x)
+        for part in (slice(0, a), slice(b, T)):
+            for k in ("y", "dx", "ddt", "dB", "dC", "dz"):
+                check(out[k][part], (ref[k][0][part], ref[k][1][part]), f"{key} {k} {part}")
+        check(out["h_T"], ref["h_T"], "h_T")
+        check(out["dh0"], ref["dh0"], "dh0")
+    # without resets a NaN stays in the state to the end
+    if bad != bad:
+        x["reset"] = None
+        x["x"][a:b] = bad
+        assert torch.isnan(run(x)["h_T"]).all()
+
+
+def test_steps_of_all_sizes():
+    # steps from 1e-30 to 1e4: softplus far into both tails
+    x = inputs(40, 1, 64, 4, torch.float32, seed=1)
+    x["dt_bias"] = None
+    x["dt"][:] = torch.linspace(-70, 20, 64, device="cuda")
+    x["dt"][20:, :, 40:] = 1e4
+    compare(x)
+
+
+@pytest.mark.parametrize("T,B,D,N", [(40, 2, 40, 16), (500, 1, 64, 16), (5, 3, 33, 7)])
+def test_repeats_bit_for_bit(T, B, D, N):
+    x = inputs(T, B, D, N, torch.bfloat16, seed=9, reset=0.01)
+    first = run(x)
+    for _ in range(3):
+        for k, v in run(x).items():
+            assert torch.equal(v, first[k]), k
+
+
+@pytest.mark.parametrize("T", [5, 40, 200])
+def test_gradient_against_differences(T):
+    # central differences of the 32-bit forward pass along random directions of one norm: step 2^-7, whose
+    # third-order term is below 2^-14 of the terms and whose rounding is about 2^-24 2^7 of the sum's magnitudes
+    x = inputs(T, 2, 12, 6, torch.float32, seed=T, reset=0.05)
+    out = run(x)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    step = 2.0 ** -7
+
+    def loss(v):
+        y, h = isam.selective_scan(*(v[k] for k in ("x", "dt", "A", "B", "C")), h0=v["h0"], **{k: v[k] for k in ("skip", "z", "dt_bias", "reset")})
+        return float((y.double() * x["dy"].double()).sum() + (h.double() * x["dh_T"].double()).sum())
+
+    size = float((reference(x)["y"][0].cuda() * x["dy"].double()).abs().sum() + (reference(x)["h_T"][0].cuda() * x["dh_T"].double()).abs().sum())
+    for name in ("x", "dt", "A", "B", "C", "skip", "z", "dt_bias", "h0"):
+        v = torch.randn(x[name].shape, generator=g, device="cuda")
+        hi, lo = dict(x), dict(x)
+        hi[name], lo[name] = x[name] + step * v, x[name] - step * v
+        diff = (loss(hi) - loss(lo)) / (2 * step)
+        terms = out["d" + name].double() * v.double()
+        assert abs(diff - float(terms.sum())) <= 2.0 ** -9 * float(terms.abs().sum()) + 2.0 ** -14 * size, name
+
+
+@pytest.mark.parametrize("T", [1, 4, 8])
+def test_state_in_place(T):
+    x = inputs(T, 2, 24, 16, torch.bfloat16, seed=T, train=False)
+    seq, opt = tuple(x[k] for k in ("x", "dt", "A", "B", "C")), {k: x[k] for k in ("skip", "z", "dt_bias")}
+    y, h = isam.selective_scan(*seq, h0=x["h0"], **opt)
+    state = x["h0"].clone()
+    y2, h2 = isam.selective_scan(*seq, h0=state, h_T=state, **opt)
+    assert h2 is state and torch.equal(y, y2) and torch.equal(h, state)
+
+
+def test_tokens_one_by_one():
+    # decoding: a call for each token, the state handed on, gives what one call over all gives
+    x = inputs(40, 3, 24, 16, torch.float32, seed=3, train=False, reset=0.1)
+    ref = reference(x)
+    state, ys = x["h0"].clone(), []
+    for t in range(40):
+        seq = [x[k] if k == "A" else x[k][t:t + 1] for k in ("x", "dt", "A", "B", "C")]
+        y, _ = isam.selective_scan(*seq, h0=state, h_T=state, skip=x["skip"], z=x["z"][t:t + 1], dt_bias=x["dt_bias"], reset=x["reset"][t:t + 1])
+        ys.append(y)
+    check(torch.cat(ys), ref["y"], "y")
+    check(state, ref["h_T"], "h_T")
+
+
+def test_other_stream():
+    x = inputs(700, 1, 64, 16, torch.bfloat16, seed=2)
+    ref = run(x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        out = run(x)
+    torch.cuda.current_stream().wait_stream(s)
+    for k in ref:
+        assert torch.equal(out[k], ref[k])
+
+
+def test_graph_replays():
+    T, B, D, N = 300, 1, 40, 16
+    x = inputs(T, B, D, N, torch.bfloat16, seed=4, reset=0.01)
+    seq, opt = tuple(x[k] for k in ("x", "dt", "A", "B", "C")), {k: x[k] for k in ("skip", "z", "dt_bias", "reset")}
+    f32 = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
+    like = lambda t: torch.empty(t.shape, device="cuda", dtype=t.dtype)  # noqa: E731
+    states = f32(*isam.selective_scan_states_shape(T, B, D, N))
+    fwd = dict(y=like(x["x"]), h_T=f32(B, D, N))
+    bwd = dict(dx=like(x["x"]), ddt=like(x["x"]), dA=f32(D, N), dB=like(x["B"]), dC=like(x["B"]), dskip=f32(D), dz=like(x["x"]),
+               ddt_bias=f32(D), dh0=f32(B, D, N))
+    w1 = torch.empty(max(1, isam.selective_scan_workspace_size(T, B, D, N, 1)), device="cuda", dtype=torch.uint8)
+    w2 = torch.empty(isam.selective_scan_backward_workspace_size(T, B, D, N, 1), device="cuda", dtype=torch.uint8)
+
+    def both():
+        isam.selective_scan(*seq, h0=x["h0"], states=states, workspace=w1, **opt, **fwd)
+        isam.selective_scan_backward(*seq, x["dy"], states=states, dh_T=x["dh_T"], workspace=w2, **opt, **bwd)
+
+    both()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for i in range(3):
+        x["x"].copy_(torch.randn(x["x"].shape, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16))
+        ref = run(x)
+        g.replay()
+        torch.cuda.synchronize()
+        for k, v in {**fwd, **bwd}.items():
+            assert torch.equal(v, ref[k]), k
+
+
+def test_long_offsets():
+    # rows whose offsets pass 2^31 elements: the last tokens of a long strided tensor
+    T, B, D, N = 300, 1, 32, 8
+    stride = (1 << 31) // 256
+    x = inputs(T, B, D, N, torch.bfloat16, seed=6)
+    for k in ("x", "dt"):
+        big = torch.empty((T * stride,), device="cuda", dtype=torch.bfloat16).as_strided((T, B, D), (stride, stride, 1))
+        big.copy_(x[k])
+        x[k] = big
+    compare(x)
+
+
+def test_refusals():
+    T, B, D, N = 10, 2, 16, 8
+    x = inputs(T, B, D, N, torch.float32)
+    seq = [x[k] for k in ("x", "dt", "A", "B", "C")]
+    for kw in (dict(skip=x["skip"][:5]), dict(h0=x["h0"][..., :4]), dict(z=x["z"][:5]), dict(reset=torch.zeros((T, B + 1), device="cuda", dtype=torch.bool)),
+               dict(y=torch.empty((T, B, D + 1), device="cuda")), dict(states=torch.empty((1, B, D, N + 1), device="cuda"))):
+        with pytest.raises(ValueError):
+            isam.selective_scan(*seq, **kw)
+    for kw in (dict(skip=x["skip"].double()), dict(reset=torch.zeros((T, B), device="cuda")), dict(z=x["z"].bfloat16())):
+        with pytest.raises(TypeError):
+            isam.selective_scan(*seq, **kw)
+    with pytest.raises(ValueError):
+        isam.selective_scan(seq[0], seq[1], seq[2], seq[3][..., :5], seq[4])
+    with pytest.raises(ValueError):
+        isam.selective_scan(*(t.cpu() for t in seq))
+    with pytest.raises(isam.IsamError):          # output over input
+        isam.selective_scan(*seq, y=seq[0])
+    with pytest.raises(isam.IsamError):          # more states than a lane group holds
+        isam.selective_scan(*seq[:2], torch.zeros((D, 65), device="cuda"), *(torch.zeros((T, B, 65), device="cuda"),) * 2)
+    long = inputs(500, 1, 16, 8, torch.float32)
+    with pytest.raises(isam.IsamError) as e:
+        isam.selective_scan(*(long[k] for k in ("x", "dt", "A", "B", "C")), workspace=torch.empty(16, device="cuda", dtype=torch.uint8))
+    assert e.value.status == 3
+    state = long["h0"].clone()
+    with pytest.raises(isam.IsamError):          # the state in place beyond a few tokens
+        isam.selective_scan(*(long[k] for k in ("x", "dt", "A", "B", "C")), h0=state, h_T=state)
