@@ -12,7 +12,7 @@ layer's state, [batch][H] in fp32, however long the text has become.
     python examples/recurrent_lm.py [--steps N] [--dtype bf16|f32]
 
 trains on synthetic texts (each repeats a random phrase of its own) and prints the loss, then reads a
-prompt in one pass and continues it token by token.
+prompt in one pass and continues it token by token; ``beam_decode`` continues it by beam search.
 """
 from __future__ import annotations
 
@@ -141,6 +141,22 @@ def decode(p, tokens, count):
         out.append(seen[-1].argmax(1))
         logits, state, _ = forward(p, out[-1][None], state)
     return torch.stack(out), torch.stack(seen)
+
+
+def beam_decode(p, tokens, count, beams, end=-1):
+    """As ``decode``, with the best `beams` texts of each prompt; a text that has reached the token `end` goes on
+    unchanged.  Returns (tokens [batch][beams][count], the best first, their log probabilities [batch][beams])."""
+    B = tokens.shape[1]
+    logits, state, _ = forward(p, tokens)
+    logits = logits[-B:].view(B, 1, -1)
+    scores, finished, out = torch.zeros((B, 1), device=tokens.device), None, None
+    for _ in range(count):
+        scores, parent, token, finished = isam.beam_step(logits, scores, width=beams, finished=finished if end >= 0 else None, end=end)
+        new = token.view(B * beams, 1)
+        out = new if out is None else torch.cat((isam.beam_reorder(out, parent), new), 1)
+        logits, state, _ = forward(p, token.view(1, B * beams), isam.beam_reorder(state, parent, dim=1))
+        logits = logits.view(B, beams, -1)
+    return out.view(B, beams, count), scores
 
 
 def texts(T, B, vocab, phrase, generator, device):
