@@ -417,8 +417,8 @@ size_t isam_gated_ffn_backward_workspace_size(int64_t M, int64_t K, int64_t F, i
  *   skip, dt_bias  [D] fp32, or NULL for zeros;  z NULL: no gate
  *   h0      [batch][D][N] fp32, or NULL for zeros;  h_T  the same, or NULL; h_T may be h0 itself up to 8
  *           tokens
- *   states  [ceil(T / 16)][batch][D][N] fp32, or NULL: the state before tokens 0, 16, 32, ...: what
- *           the backward pass needs of the forward pass
+ *   states  [ceil(T / k)][batch][D][N] fp32, or NULL: the state before tokens 0, k, 2k, ... with k = 16 (8 for N
+ *           above 32): what the backward pass needs of the forward pass
  * At least one of y, h_T and states.  N up to 64.  T == 0: h_T = h0 (or zeros); batch or D == 0: no-op.
  * The state, steps and sums are fp32; y is rounded once.  Results repeat bit for bit.  Tensors may pass
  * 2^31 bytes, as long as 32 tokens of each stay below (up to 8 tokens without a gradient: any stride).

@@ -557,8 +557,9 @@ def selective_scan_backward_workspace_size(T, batch, D, N, dtype) -> int:
 
 
 def selective_scan_states_shape(T, batch, D, N):
-    """Shape of the ``states`` tensor: the state before tokens 0, 16, 32, ..."""
-    return (T + 15) // 16, batch, D, N
+    """Shape of the ``states`` tensor: the state before tokens 0, 16, 32, ... (0, 8, 16, ... for N above 32)."""
+    every = 8 if N > 32 else 16
+    return (T + every - 1) // every, batch, D, N
 
 
 def _sequence(t, name, shape, dtype):

@@ -159,7 +159,7 @@ extern "C" isam_status_t isam_selective_scan(int64_t T, int64_t batch, int64_t D
                             {"h0", in_place ? nullptr : h0, state, false},
                             {"reset", reset, reset_b, false},
                             {"h_T", h_T, state, true},
-                            {"states", states, (size_t)cdiv(T, kScanChunk) * state, true},
+                            {"states", states, (size_t)cdiv(T, scan_chunk(N)) * state, true},
                             {"workspace", workspace, room(need), true}};
     if ((st = rows_check(r, dense, T, batch, es, who)) != ISAM_OK) return st;
     if (T > kScanFew && (st = rows_near(r, es, reset, reset_stride_t, who)) != ISAM_OK) return st;
@@ -231,7 +231,7 @@ extern "C" isam_status_t isam_selective_scan_backward(
                             {"skip", skip, (size_t)D * 4, false},
                             {"dt_bias", dt_bias, (size_t)D * 4, false},
                             {"reset", reset, reset_b, false},
-                            {"states", states, (size_t)cdiv(T, kScanChunk) * state, false},
+                            {"states", states, (size_t)cdiv(T, scan_chunk(N)) * state, false},
                             {"dh_T", dh_T, state, false},
                             {"dA", dA, (size_t)(D * N) * 4, true},
                             {"dskip", dskip, (size_t)D * 4, true},

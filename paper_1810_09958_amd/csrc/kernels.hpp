@@ -371,7 +371,8 @@ struct ScanRows {
     const void* p;  // or null
     int64_t st, sb;
 };
-constexpr int kScanChunk = 16;        // tokens between two rows of `states`
+// Tokens between two rows of `states`: what the backward pass holds of them in registers.
+constexpr int scan_chunk(int64_t N) { return N > 32 ? 8 : 16; }
 constexpr int kScanFew = 8;           // tokens forward up to which no tile is formed (64-bit offsets)
 constexpr int64_t kScanMaxN = 64;
 constexpr int64_t kScanMaxSegments = 64;
@@ -386,7 +387,7 @@ struct ScanArgs {
     const uint8_t* reset;     // or null
     int64_t rs_t, rs_b;
     float* h_T;               // [batch][D][N] or null
-    float* states;            // [ceil(T / 16)][batch][D][N]: state before tokens 0, 16, ...; or null (forward)
+    float* states;            // [ceil(T / scan_chunk)][batch][D][N]: state before tokens 0, 16, ...; or null (forward)
     int64_t segs, seg_len;    // segments of time, tokens of each (a multiple of the tile)
     float* seg_sum;           // [segs][batch][D]
     float* seg_end;           // [segs][batch][D][N]

@@ -109,8 +109,8 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
                 static_for<4>([&](auto i) { now[i] = next[i]; });
                 ahead(q + 4 < TT ? q + 4 : q);
                 __builtin_amdgcn_sched_barrier(0);
-                if (!SUM && (q & (kScanChunk - 1)) == 0 && a.states && (FAST || q < left)) {
-                    float* const to = a.states + (((t0 + q) / kScanChunk * a.batch + b) * a.D + ch) * N + g * R;
+                if (!SUM && (q & (S::CK - 1)) == 0 && a.states && (FAST || q < left)) {
+                    float* const to = a.states + (((t0 + q) / S::CK * a.batch + b) * a.D + ch) * N + g * R;
                     static_for<R>([&](auto r) {
                         if (in && g * R + r < N) to[r] = h[r];
                     });
@@ -202,17 +202,32 @@ __global__ __launch_bounds__(256) void scan_few_kernel(ScanArgs a) {
     else static_for<4>([&](auto r) { h[r] = 0.0f; });
     if (a.states && T > 0) put4(a.states + at);
     const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f, skip = a.skip ? a.skip[ch] : 0.0f;
+    auto row_get4 = [&](const ScanRows& r, int64_t at, float (&f)[4]) {
+        const char* const p = static_cast<const char*>(r.p) + (at + n0) * ES;
+        if (n0 + 4 <= N) {
+            uint32_t w[ES];
+            __builtin_memcpy(w, p, 4 * ES);
+            static_for<4>([&](auto e) {
+                if constexpr (ES == 4) f[e] = __uint_as_float(w[e]);
+                else f[e] = e & 1 ? bf16hi(w[e / 2]) : bf16lo(w[e / 2]);
+            });
+        } else {
+            static_for<4>([&](auto e) { f[e] = n0 + e < N ? Row16<ES>::get(r.p, at + n0 + e) : 0.0f; });
+        }
+    };
     for (int t = 0; t < T; ++t) {
         auto row_at = [&](const ScanRows& r) { return b * r.sb + t * r.st; };
-        const float x = Row16<ES>::get(a.x.p, row_at(a.x) + ch), d = softplus(Row16<ES>::get(a.dt.p, row_at(a.dt) + ch) + bias);
+        float Bv[4], Cv[4];
+        row_get4(a.B, row_at(a.B), Bv);
+        row_get4(a.C, row_at(a.C), Cv);
+        const float x = Row16<ES>::get(a.x.p, row_at(a.x) + ch), raw = Row16<ES>::get(a.dt.p, row_at(a.dt) + ch);
+        const float zv = a.z.p ? Row16<ES>::get(a.z.p, row_at(a.z) + ch) : 0.0f;
         const bool drop = a.reset && a.reset[t * a.rs_t + b * a.rs_b];
+        const float d = softplus(raw + bias);
         float v = 0.0f;
         static_for<4>([&](auto r) {
-            const bool on = n0 + r < N;
-            const float Bv = on ? Row16<ES>::get(a.B.p, row_at(a.B) + n0 + r) : 0.0f;
-            const float Cv = on ? Row16<ES>::get(a.C.p, row_at(a.C) + n0 + r) : 0.0f;
-            h[r] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * A2[r]), drop ? 0.0f : h[r], d * x * Bv);
-            v = __builtin_fmaf(Cv, on ? h[r] : 0.0f, v);
+            h[r] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * A2[r]), drop ? 0.0f : h[r], d * x * Bv[r]);
+            v = n0 + r < N ? __builtin_fmaf(Cv[r], h[r], v) : v;
         });
         static_for<4>([&](auto k) {
             constexpr int m = 1 << decltype(k)::value;
@@ -220,7 +235,6 @@ __global__ __launch_bounds__(256) void scan_few_kernel(ScanArgs a) {
         });
         v = __builtin_fmaf(skip, x, v);
         if (a.z.p) {
-            const float zv = Row16<ES>::get(a.z.p, row_at(a.z) + ch);
             float z, omz;
             sigmoid_pair(zv, z, omz);
             v *= zv * z;

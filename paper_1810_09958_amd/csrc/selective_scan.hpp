@@ -128,6 +128,7 @@ struct ScanShape {
     static constexpr int E = CH * kScanTile / 256; // values of a tile that a thread loads: one piece of a row
     static constexpr int PPR = CH / E;             // pieces of a row
     static constexpr int NP = L * R;               // N, padded
+    static constexpr int CK = scan_chunk(NP);      // (the same for every N of this instance)
     static constexpr int BE = kScanTile * NP / 256;  // values of B (and of C) of a tile that a thread loads
     static_assert(PPR * kScanTile == 256, "one piece a thread");
     using P = Piece<ES, VEC, E>;

@@ -5,7 +5,7 @@
 //   dd_t = sum_n g_t a_t h_{t-1} A + x_t sum_n g_t B_t,  ddt_t = dd_t sigmoid(dt_t + dt_bias)
 //   dA = sum g_t a_t h_{t-1} d_t,  dskip = sum dv x,  dz_t = dy_t v_t silu'(z_t),  dh0 = a_0 g_0
 //
-// Tiles from the end of time.  The states of 16 tokens are formed again in registers from the one
+// Tiles from the end of time.  The states of 16 tokens (8 for N above 32) are formed again in registers from the one
 // kept before them, with their a; then the tokens are walked backwards.  Running back by dividing by
 // a would lose every digit where a is small, and keeping each state would move 4 N bytes a value.
 // dB and dC are sums over channels: a wave halves its values lane bit by lane bit, the waves meet in
@@ -50,14 +50,14 @@ template <int ES, bool VEC, int L, int R, bool SUM>
 __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
     using S = ScanShape<ES, VEC, L, R>;
     using P = typename S::P;
-    constexpr int CH = S::CH, E = S::E, NP = S::NP, TT = kScanTile, CK = kScanChunk, CW = S::CW;
-    constexpr bool KEEP = R < 4;  // a of each token kept (R = 4: no registers left, formed again)
+    constexpr int CH = S::CH, E = S::E, NP = S::NP, TT = kScanTile, CK = S::CK, CW = S::CW;
     constexpr int BITS = CW == 16 ? 4 : CW == 8 ? 3 : 2, LEFT = 2 * R > CW ? 2 * R / CW : 1;
-    constexpr int BUF = NP <= 32 ? 2 : 1;
     __shared__ __attribute__((aligned(16))) float4 dd[TT][CH];                    // d, d x, dv, v
     __shared__ __attribute__((aligned(16))) float2 back_sums[SUM ? 1 : TT][CH];   // sum q A, sum g B
     __shared__ __attribute__((aligned(16))) float bc[TT * NP * 2];
-    __shared__ __attribute__((aligned(16))) float part[BUF][SUM ? 1 : kScanWaves][SUM ? 1 : CK][2 * NP];
+    __shared__ float2 par[CH];                            // dt_bias, skip
+    __shared__ float2 own_sums[SUM ? 1 : E][SUM ? 1 : 256];  // a thread's sums of dv x and ddt
+    __shared__ __attribute__((aligned(16))) float part[2][SUM ? 1 : kScanWaves][SUM ? 1 : CK][2 * NP];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane / CW, cl = wid * CW + lane % CW;
     const int64_t blocks = (a.D + CH - 1) / CH;
@@ -84,36 +84,49 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         }
     });
 
-    const int tr = tid / S::PPR, pc = (tid % S::PPR) * E;
-    const int valid = (int)max((int64_t)0, min((int64_t)E, a.D - (c0 + pc)));
-    float bias[E], skip[E], sum_skip[E], sum_bias[E];
-    static_for<E>([&](auto e) {
-        bias[e] = a.dt_bias && e < valid ? a.dt_bias[c0 + pc + e] : 0.0f;
-        skip[e] = a.skip && e < valid ? a.skip[c0 + pc + e] : 0.0f;
-        sum_skip[e] = sum_bias[e] = 0.0f;
-    });
+    // This thread's piece of a tile: row tr, channels c0 + pc .. + E.  LEAN: the index goes through an empty asm wherever it
+    // is used, so that what is computed from it is not held in registers across the walk (N above 32: 218 us with some
+    // 45 spilled, 180 without; where they suffice, forming the places again costs more, N = 16: 430 against 400).
+    constexpr bool LEAN = R >= 4;
+    struct Mine {
+        int tr, pc, valid;
+    };
+    auto mine = [&]() {
+        int id = tid;
+        if constexpr (LEAN) asm volatile("" : "+v"(id));
+        const int pc = id % S::PPR * E;
+        return Mine{id / S::PPR, pc, (int)max((int64_t)0, min((int64_t)E, a.D - (c0 + pc)))};
+    };
+    for (int i = tid; i < CH; i += 256) {
+        const bool on = c0 + i < a.D;
+        par[i] = make_float2(on && a.dt_bias ? a.dt_bias[c0 + i] : 0.0f, on && a.skip ? a.skip[c0 + i] : 0.0f);
+    }
+    if constexpr (!SUM) static_for<E>([&](auto e) { own_sums[e][tid] = make_float2(0.0f, 0.0f); });
     const int64_t tlast = tbeg + (tend - tbeg - 1) / TT * TT;
     TileRows<ES> rx(a.x, b, tlast), rd(a.dt, b, tlast), rz(a.z, b, tlast), ry(a.dy, b, tlast), rB(a.B, b, tlast), rC(a.C, b, tlast),
         rdx(a.dx, b, tlast), rdt(a.ddt, b, tlast), rdz(a.dz, b, tlast);
-    auto offset = [&](const TileRows<ES>& r, int left) {
-        return r.p && tr < left && valid > 0 ? (uint32_t)tr * r.row + (uint32_t)((c0 + pc) * ES) : kOob;
+    auto offset = [&](const TileRows<ES>& r, const Mine& m, int left) {
+        return r.p && m.tr < left && m.valid > 0 ? (uint32_t)m.tr * r.row + (uint32_t)((c0 + m.pc) * ES) : kOob;
     };
     P px, pd, pz, py;
     ScanWeights<ES, NP> wb, wc;
     ScanMarks marks;
     auto fetch = [&](int64_t t0) {  // (tiles before the segment: nothing is read)
         const int left = t0 >= tbeg ? (int)min((int64_t)TT, tend - t0) : 0;
-        pd.load(rd.buffer(), offset(rd, left), valid);
-        pz.load(rz.buffer(), offset(rz, left), valid);
-        py.load(ry.buffer(), offset(ry, left), valid);
-        wc.load(rC.buffer(), rC.row, N, left, tid);
+        const Mine m = mine();
+        int id = tid;
+        if constexpr (LEAN) asm volatile("" : "+v"(id));
+        pd.load(rd.buffer(), offset(rd, m, left), m.valid);
+        pz.load(rz.buffer(), offset(rz, m, left), m.valid);
+        py.load(ry.buffer(), offset(ry, m, left), m.valid);
+        wc.load(rC.buffer(), rC.row, N, left, id);
         rd.back();
         rz.back();
         ry.back();
         rC.back();
         if constexpr (!SUM) {
-            px.load(rx.buffer(), offset(rx, left), valid);
-            wb.load(rB.buffer(), rB.row, N, left, tid);
+            px.load(rx.buffer(), offset(rx, m, left), m.valid);
+            wb.load(rB.buffer(), rB.row, N, left, id);
             rx.back();
             rB.back();
         }
@@ -122,8 +135,9 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
     float total = 0.0f;
     bool dropped = false;
     fetch(tlast);
+    __syncthreads();  // (par)
     using Token = ScanToken<L, R, true>;
-    // the state kept before the next 16 tokens to be walked
+    // the state kept before the next tokens to be walked
     float hnext[R];
     auto kept = [&](int64_t t) {
         const float* const from = a.states + ((t / CK * a.batch + b) * a.D + ch) * N + g * R;
@@ -138,23 +152,28 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         // (the pieces stay as they came; what the last step needs of them is formed again there)
         const P qx = px, qd = pd, qz = pz, qy = py;
         {
+            const Mine m = mine();
             float x[E], raw[E], zs[E], dv[E];
             if constexpr (!SUM) qx.unpack(x);
             qd.unpack(raw);
             qz.unpack(zs);
             qy.unpack(dv);
             static_for<E>([&](auto e) {
-                const float step = tr < left && e < valid ? softplus(raw[e] + bias[e]) : 0.0f;
+                const float step = m.tr < left && e < m.valid ? softplus(raw[e] + par[m.pc + e].x) : 0.0f;
                 if (a.z.p) {
                     float gate, omz;
                     sigmoid_pair(zs[e], gate, omz);
                     dv[e] *= zs[e] * gate;
                 }
-                dd[tr][pc + e] = make_float4(step, SUM ? 0.0f : step * x[e], dv[e], 0.0f);
+                dd[m.tr][m.pc + e] = make_float4(step, SUM ? 0.0f : step * x[e], dv[e], 0.0f);
             });
         }
-        wc.template put<R>(bc, 1, tid);
-        if constexpr (!SUM) wb.template put<R>(bc, 0, tid);
+        {
+            int id = tid;
+            if constexpr (LEAN) asm volatile("" : "+v"(id));
+            wc.template put<R>(bc, 1, id);
+            if constexpr (!SUM) wb.template put<R>(bc, 0, id);
+        }
         const uint32_t reset = marks.bits();
         fetch(t0 - TT);  // (before the segment: zeros)
         __syncthreads();
@@ -180,10 +199,10 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                 for (int k = TT / CK - 1; k >= 0; --k) {
                     const int tc = k * CK;
                     if (!FAST && tc >= left) continue;
-                    float h[CK + 1][R], av[KEEP ? CK : 1][R];  // h[i]: the state before token i (reset or not)
+                    float h[CK + 1][R], av[CK][R];  // h[i]: the state before token i (reset or not)
                     static_for<R>([&](auto r) { h[0][r] = hnext[r]; });
                     kept(t0 + tc - CK);
-                    float(*const to)[CK][2 * NP] = part[BUF == 2 ? k & 1 : 0];
+                    float(*const to)[CK][2 * NP] = part[k & 1];
                     // Tokens' values on their way from LDS: two ahead of the one walked.
                     Token tok[4];
                     float dvs[4];
@@ -203,7 +222,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                         float acc = 0.0f;
                         static_for<R>([&](auto r) {
                             const float aw = live ? __builtin_amdgcn_exp2f(s.s.x * A2[r]) : 1.0f;
-                            if constexpr (KEEP) av[i][r] = aw;
+                            av[i][r] = aw;
                             const float hn = __builtin_fmaf(aw, drop ? 0.0f : h[i][r], s.s.y * s.B[r]);
                             h[i + 1][r] = live ? hn : h[i][r];
                             acc = r == 0 ? s.C[0] * h[i + 1][0] : __builtin_fmaf(s.C[r], h[i + 1][r], acc);
@@ -238,10 +257,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                             sums[r] = G[r] * s.s.y;
                             sums[R + r] = h[i + 1][r] * dv;
                             gb = r == 0 ? G[0] * s.B[0] : __builtin_fmaf(G[r], s.B[r], gb);
-                            float aw;
-                            if constexpr (KEEP) aw = av[i][r];
-                            else aw = live ? __builtin_amdgcn_exp2f(s.s.x * A2[r]) : 1.0f;
-                            const float back = aw * G[r];
+                            const float back = av[i][r] * G[r];
                             float qv = back * (drop ? 0.0f : h[i][r]);
                             if (!FAST) qv = live ? qv : 0.0f;
                             dA[r] = __builtin_fmaf(qv, s.s.x, dA[r]);
@@ -258,13 +274,14 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                         }
                     });
                     __syncthreads();
-                    for (int idx = tid; idx < CK * 2 * NP; idx += 256) {
+                    int id = tid;
+                    if constexpr (LEAN) asm volatile("" : "+v"(id));
+                    for (int idx = id; idx < CK * 2 * NP; idx += 256) {
                         const int i = idx / (2 * NP), at = idx % (2 * NP), gg = at / (2 * R), w = at % (2 * R) / R, n = gg * R + at % R;
                         float s = to[0][i][at];
                         static_for<kScanWaves - 1>([&](auto k1) { s += to[k1 + 1][i][at]; });
                         if (n < N && tc + i < left) a.bc_part[((blk * a.T + t0 + tc + i) * a.batch + b) * 2 * N + w * N + n] = s;
                     }
-                    if constexpr (BUF == 1) __syncthreads();
                 }
             }
         };
@@ -273,30 +290,33 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         if constexpr (SUM) {
             __syncthreads();
         } else {
+            const Mine m = mine();
             float x[E], raw[E], zs[E], dys[E], odx[E], odt[E], odz[E];
             qx.unpack(x);
             qd.unpack(raw);
             qz.unpack(zs);
             qy.unpack(dys);
             static_for<E>([&](auto e) {
-                const float4 s = dd[tr][pc + e];
-                const float2 q = back_sums[tr][pc + e];
+                const float4 s = dd[m.tr][m.pc + e];
+                const float2 q = back_sums[m.tr][m.pc + e], w = par[m.pc + e];
                 float z, omz;
-                sigmoid_pair(raw[e] + bias[e], z, omz);
+                sigmoid_pair(raw[e] + w.x, z, omz);
                 odt[e] = __builtin_fmaf(q.y, x[e], q.x * 0.69314718f) * z;
-                odx[e] = __builtin_fmaf(skip[e], s.z, s.x * q.y);
+                odx[e] = __builtin_fmaf(w.y, s.z, s.x * q.y);
                 odz[e] = 0.0f;
                 if (a.dz.p) {
                     sigmoid_pair(zs[e], z, omz);
-                    odz[e] = dys[e] * __builtin_fmaf(skip[e], x[e], s.w) * (z * __builtin_fmaf(zs[e], omz, 1.0f));
+                    odz[e] = dys[e] * __builtin_fmaf(w.y, x[e], s.w) * (z * __builtin_fmaf(zs[e], omz, 1.0f));
                 }
-                const bool live = tr < left && e < valid;
-                sum_skip[e] += live ? s.z * x[e] : 0.0f;
-                sum_bias[e] += live ? odt[e] : 0.0f;
+                const bool live = m.tr < left && e < m.valid;
+                float2 own = own_sums[e][tid];
+                own.x += live ? s.z * x[e] : 0.0f;
+                own.y += live ? odt[e] : 0.0f;
+                own_sums[e][tid] = own;
             });
-            P::store(rdx.buffer(), offset(rdx, left), valid, odx);
-            P::store(rdt.buffer(), offset(rdt, left), valid, odt);
-            P::store(rdz.buffer(), offset(rdz, left), valid, odz);
+            P::store(rdx.buffer(), offset(rdx, m, left), m.valid, odx);
+            P::store(rdt.buffer(), offset(rdt, m, left), m.valid, odt);
+            P::store(rdz.buffer(), offset(rdz, m, left), m.valid, odz);
             rdx.back();
             rdt.back();
             rdz.back();
@@ -321,16 +341,13 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         if (!a.dskip && !a.ddt_bias) return;
         // the threads with the same channels: 32 rows of the tile
         __syncthreads();
-        float* const sums = &dd[0][0].x;  // [2][32][CH]
-        static_for<E>([&](auto e) {
-            sums[tr * CH + pc + e] = sum_skip[e];
-            sums[TT * CH + tr * CH + pc + e] = sum_bias[e];
-        });
-        __syncthreads();
         for (int i = tid; i < 2 * CH; i += 256) {
             const int which = i / CH, c = i % CH;
             float s = 0.0f;
-            for (int t = 0; t < TT; ++t) s += sums[which * TT * CH + t * CH + c];
+            for (int t = 0; t < TT; ++t) {
+                const float2 v = own_sums[c % E][t * S::PPR + c / E];
+                s += which ? v.y : v.x;
+            }
             if (c0 + c < a.D) a.par_part[rows * a.D * N + (which * rows + row) * a.D + c0 + c] = s;
         }
     }
