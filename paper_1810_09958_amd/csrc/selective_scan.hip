@@ -78,6 +78,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
     for (int64_t t0 = tbeg; t0 < tend; t0 += TT) {
         const int left = (int)min((int64_t)TT, tend - t0);
         float x[E], zs[E];
+        bool wild = false;
         px.unpack(x);
         {
             float d[E];
@@ -85,6 +86,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
             static_for<E>([&](auto e) {
                 const float step = tr < left && e < valid ? softplus(d[e] + bias[e]) : 0.0f;
                 dd[tr][pc + e] = make_float2(step, step * x[e]);
+                wild = wild || not_finite(step * x[e]);
             });
         }
         wb.template put<R>(bc, 0, tid);
@@ -94,8 +96,8 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
         }
         const uint32_t reset = marks.bits();
         fetch(t0 + TT);  // (past the end: zeros)
-        __syncthreads();
-        // FAST: a whole tile without a reset.  The next four tokens' values are on their way from LDS while
+        wild = meet<NP>(N, wild);
+        // FAST: a whole tile without a reset (or an infinity that would reach the padding of N).  The next four tokens' values are on their way from LDS while
         // four are walked.
         auto walk = [&](auto fast) {
             constexpr bool FAST = decltype(fast)::value;
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
                         const float av = __builtin_amdgcn_exp2f(v.s.x * A2[r]);
                         const float hb = drop ? 0.0f : h[r];
                         const float hn = __builtin_fmaf(av, hb, v.s.y * v.B[r]);
-                        h[r] = live ? hn : h[r];
+                        h[r] = FAST || (live && g * R + r < N) ? hn : h[r];
                         if constexpr (!SUM) acc = r == 0 ? v.C[0] * h[0] : __builtin_fmaf(v.C[r], h[r], acc);
                     });
                     p[i] = acc;
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
                 }
             }
         };
-        if (left == TT && reset == 0) walk(std::true_type{});
+        if (left == TT && reset == 0 && !wild) walk(std::true_type{});
         else walk(std::false_type{});
         __syncthreads();
         if constexpr (!SUM) {

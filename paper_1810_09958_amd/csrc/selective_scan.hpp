@@ -227,10 +227,21 @@ struct ScanMarks {
     __device__ __forceinline__ uint32_t bits() const { return (uint32_t)__ballot((byte & 0xffu) != 0); }  // (left <= the tile)
 };
 
+__device__ __forceinline__ bool not_finite(float v) { return !(__builtin_fabsf(v) < __builtin_inff()); }
+
+// A barrier; and whether a thread before it had an infinity or NaN that meets the zeros which pad N.
+template <int NP>
+__device__ __forceinline__ bool meet(int N, bool wild) {
+    if (N != NP) return __syncthreads_or(wild);
+    __syncthreads();
+    return false;
+}
+
 // Segments: [segment][batch][D] sums of steps (sign bit set: a reset lies inside, nothing passes),
-// and [segment][batch][D][N] end states from zero.
+// and [segment][batch][D][N] end states from zero.  What passes is at least 2^-126 of h, so that an infinity stays one
+// where the tokens' factors are above zero and their product is not.
 __device__ __forceinline__ float pass_on(float sum, float a2, float h, float end) {
-    return (int)__float_as_uint(sum) < 0 ? end : __builtin_fmaf(__builtin_amdgcn_exp2f(sum * a2), h, end);
+    return (int)__float_as_uint(sum) < 0 ? end : __builtin_fmaf(fmaxf(__builtin_amdgcn_exp2f(sum * a2), 0x1p-126f), h, end);
 }
 
 // Instances by N and type: (lanes to a channel, values to a lane).

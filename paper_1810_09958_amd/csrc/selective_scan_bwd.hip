@@ -151,6 +151,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         const int left = (int)min((int64_t)TT, tend - t0);
         // (the pieces stay as they came; what the last step needs of them is formed again there)
         const P qx = px, qd = pd, qz = pz, qy = py;
+        bool wild = false;
         {
             const Mine m = mine();
             float x[E], raw[E], zs[E], dv[E];
@@ -165,7 +166,9 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                     sigmoid_pair(zs[e], gate, omz);
                     dv[e] *= zs[e] * gate;
                 }
-                dd[m.tr][m.pc + e] = make_float4(step, SUM ? 0.0f : step * x[e], dv[e], 0.0f);
+                const float dx = SUM ? 0.0f : step * x[e];
+                dd[m.tr][m.pc + e] = make_float4(step, dx, dv[e], 0.0f);
+                wild = wild || not_finite(dx) || not_finite(dv[e]);
             });
         }
         {
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         }
         const uint32_t reset = marks.bits();
         fetch(t0 - TT);  // (before the segment: zeros)
-        __syncthreads();
+        wild = meet<NP>(N, wild);
         auto walk = [&](auto fast) {
             constexpr bool FAST = decltype(fast)::value;
             if constexpr (SUM) {
@@ -218,13 +221,14 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                         if constexpr (i + 2 < CK) get(std::integral_constant<int, (i + 2 < CK ? i + 2 : 0)>{});
                         __builtin_amdgcn_sched_barrier(0);
                         const Token& s = tok[i & 3];
-                        const bool drop = !FAST && (reset >> (tc + i) & 1), live = FAST || tc + i < left;
+                        const bool drop = !FAST && (reset >> (tc + i) & 1), live = tc + i < left;
                         float acc = 0.0f;
                         static_for<R>([&](auto r) {
-                            const float aw = live ? __builtin_amdgcn_exp2f(s.s.x * A2[r]) : 1.0f;
+                            const bool on = FAST || (live && g * R + r < N);
+                            const float aw = on ? __builtin_amdgcn_exp2f(s.s.x * A2[r]) : 1.0f;
                             av[i][r] = aw;
                             const float hn = __builtin_fmaf(aw, drop ? 0.0f : h[i][r], s.s.y * s.B[r]);
-                            h[i + 1][r] = live ? hn : h[i][r];
+                            h[i + 1][r] = on ? hn : h[i][r];
                             acc = r == 0 ? s.C[0] * h[i + 1][0] : __builtin_fmaf(s.C[r], h[i + 1][r], acc);
                         });
                         p[i & 3] = acc;
@@ -253,7 +257,8 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                         const bool drop = !FAST && (reset >> (tc + i) & 1), live = FAST || tc + i < left;
                         float aq = 0.0f, gb = 0.0f, sums[2 * R];
                         static_for<R>([&](auto r) {
-                            G[r] = __builtin_fmaf(s.C[r], dv, G[r]);
+                            const float gn = __builtin_fmaf(s.C[r], dv, G[r]);
+                            G[r] = FAST || g * R + r < N ? gn : 0.0f;
                             sums[r] = G[r] * s.s.y;
                             sums[R + r] = h[i + 1][r] * dv;
                             gb = r == 0 ? G[0] * s.B[0] : __builtin_fmaf(G[r], s.B[r], gb);
@@ -285,7 +290,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                 }
             }
         };
-        if (left == TT && reset == 0) walk(std::true_type{});
+        if (left == TT && reset == 0 && !wild) walk(std::true_type{});
         else walk(std::false_type{});
         if constexpr (SUM) {
             __syncthreads();

@@ -282,6 +282,41 @@ def test_reset_cuts_off_bad_values(T, dtype, bad):
         assert torch.isnan(run(x)["h_T"]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [6, 70, 500])
+@pytest.mark.parametrize("N", [1, 3, 6, 13, 16, 21, 33])
+def test_infinity_stays_one(N, T, dtype):
+    """An infinite input with positive weights makes infinite outputs from its token on, whatever N is padded to, and
+    its neighbours keep theirs.  A factor exp(d A) below 2^-126 is zero in 32 bits (subnormal results of the exponential
+    are flushed), and zero times infinity is NaN: past such a token either may stand."""
+    x = inputs(T, 2, 21, N, dtype, gate=False)
+    for k in ("B", "C", "dy"):
+        x[k] = x[k].abs() + 0.5
+    x["dh_T"] = None
+    x["skip"][5] = 1.0
+    plain = run(x)
+    at = T // 2
+    step = torch.nn.functional.softplus(x["dt"][:, 1, 5].double() + x["dt_bias"][5].double(), threshold=1000)
+    none = torch.exp2(step * x["A"][5].double().min() / math.log(2)) < 2.0 ** -125
+    x["x"][at, 1, 5] = float("inf")
+    got = run(x)
+    hit = torch.zeros((T, 2, 21), dtype=torch.bool, device="cuda")
+    hit[at:, 1, 5] = True
+    gone = torch.zeros_like(hit)
+    gone[at + 1:, 1, 5] = none[at + 1:].cumsum(0) > 0
+    assert (got["y"][hit & ~gone] == float("inf")).all() and not torch.isfinite(got["y"][hit]).any()
+    assert torch.equal(got["y"][~hit], plain["y"][~hit])
+    assert torch.equal(got["dx"], plain["dx"])
+    x["x"][at, 1, 5] = 1.0
+    x["dy"][at, 1, 5] = float("inf")
+    got = run(x)
+    hit = torch.zeros((T, 2, 21), dtype=torch.bool, device="cuda")
+    hit[:at + 1, 1, 5] = True
+    gone = torch.zeros_like(hit)
+    gone[:at, 1, 5] = none[1:at + 1].flip(0).cumsum(0).flip(0) > 0
+    assert (got["dx"][hit & ~gone] == float("inf")).all() and torch.isfinite(got["dx"][~hit]).all()
+
+
 def test_steps_of_all_sizes():
     # steps from 1e-30 to 1e4: softplus far into both tails
     x = inputs(40, 1, 64, 4, torch.float32, seed=1)
