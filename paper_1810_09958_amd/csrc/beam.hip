@@ -41,14 +41,22 @@ __device__ __forceinline__ float exp_of(float x) {
 
 constexpr int kEach = (int)(kBeamPart / 256);  // logits of a thread
 
-__device__ __forceinline__ uint64_t of_lane(uint64_t v, int k) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), k) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, k);
+// The n-th largest of the values of the lanes in `of` (0: there are fewer), bit by bit from the highest: one
+// comparison of the wave and a count of its lanes each, the counts in scalar registers.
+__device__ __forceinline__ uint32_t nth(uint32_t v, uint64_t of, int n) {
+    uint32_t t = 0;
+    if ((of & (of - 1)) == 0 && n == 1 && of) return (uint32_t)__builtin_amdgcn_readlane((int)v, __builtin_ctzll(of));
+    static_for<32>([&](auto k) {
+        const uint32_t more = t | 0x80000000u >> decltype(k)::value;
+        if (__builtin_popcountll(__ballot(v >= more) & of) >= n) t = more;
+    });
+    return t;
 }
 
 template <int ES>
 __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     constexpr int E = 16 / ES, Q = kEach / E;  // values of a 16-byte piece, pieces of a thread
-    __shared__ __attribute__((aligned(16))) uint64_t list[4 * kEach * kBeamMax];
+    extern __shared__ __attribute__((aligned(16))) uint64_t list[];  // 4 kEach width
     __shared__ double wsum[4];
     __shared__ float wmax[4];
     __shared__ int count;
@@ -89,10 +97,12 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     __syncthreads();
     most = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
     // the width-th of the wave's firsts; 0: fewer lanes have any
-    int better = 0;
-    static_for<64>([&](auto k) { better += of_lane(first, decltype(k)::value) > first; });
-    const uint64_t hit = __ballot(better == W - 1 && first != 0);
-    const uint64_t least = hit ? of_lane(first, __builtin_ctzll(hit)) : 0;
+    uint32_t low = nth((uint32_t)(first >> 32), ~0ull, W), rest = 0;
+    if (low) {
+        const uint64_t above = __ballot((uint32_t)(first >> 32) > low), ties = __ballot((uint32_t)(first >> 32) == low);
+        rest = nth((uint32_t)first, ties, W - __builtin_popcountll(above));
+    }
+    const uint64_t least = (uint64_t)low << 32 | rest;
     const float bound = value32((uint32_t)(least >> 32));
     static_for<kEach>([&](auto k) {
         if (place(k) < a.V && (least == 0 || v[k] >= bound)) {
@@ -112,6 +122,7 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     for (int k = tid; k < n; k += 256) {
         const uint64_t u = list[k];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) rank += list[j] > u;
         if (rank < W) out[rank] = u;
     }
@@ -130,10 +141,6 @@ __device__ __forceinline__ bool ahead(const Cand& x, const Cand& y) {
 
 constexpr int kAtOnce = 8;  // candidates of a thread
 
-__device__ __forceinline__ Cand of_lane(const Cand& v, int k) {
-    return Cand{of_lane(v.order, k), (uint32_t)__builtin_amdgcn_readlane((int)v.place, k)};
-}
-
 __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
     __shared__ double offset[kBeamMax];       // score - log sum; -inf: no candidate but of -inf
     __shared__ bool over[kBeamMax];           // finished
@@ -147,23 +154,31 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
     const uint64_t early = tid < all ? from[tid] : 0ull;  // (on its way during the sums)
     int lanes = 1;
     while (lanes < 64 && lanes < parts) lanes *= 2;
-    // a wave to a beam, a lane to a part
-    for (int i = wid; i < beams; i += 4) {
+    // a lane to a part, 64 / lanes beams to a wave
+    const int at = lane & (lanes - 1), one = 64 / lanes;
+    for (int i0 = wid * one; i0 < beams; i0 += 4 * one) {
+        const int i = min(i0 + lane / lanes, beams - 1);
         const int64_t row = b * beams + i;
         const double2* const s = a.sums + row * parts;
         const double score = (double)a.scores[row];
         const bool done = a.finished && a.finished[row];
-        double most = -INFINITY, sum = 0.0;
-        for (int p = lane; p < parts; p += 64) most = s[p].x > most ? s[p].x : most;
+        const double2 own = at < parts ? s[at] : make_double2(-INFINITY, 0.0);
+        double most = own.x;
+        for (int p = at + 64; p < parts; p += 64) most = s[p].x > most ? s[p].x : most;
         for (int m = lanes / 2; m > 0; m >>= 1) {
             const double o = __shfl_xor(most, m);
             most = o > most ? o : most;
         }
         // (a part without a finite logit has no sum)
-        for (int p = lane; p < parts; p += 64) sum += s[p].x == -INFINITY ? s[p].y : s[p].y * exp(s[p].x - most);
+        double2 v = own;
+        double sum = 0.0;
+        for (int p = at; p < parts;) {
+            sum += v.x == -INFINITY ? v.y : v.y * exp(v.x - most);
+            if ((p += 64) < parts) v = s[p];
+        }
         for (int m = lanes / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
         const double o = done ? score : most == -INFINITY || most == INFINITY ? -INFINITY : score - (most + log(sum));
-        if (lane == 0) {
+        if (at == 0) {
             offset[i] = o == o ? o : -INFINITY;
             over[i] = done;
         }
@@ -200,24 +215,32 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
         if (tid == 0) count = 0;
         Cand first{0, 0};
         static_for<kAtOnce + 1>([&](auto k) { first = ahead(mine[k], first) ? mine[k] : first; });
-        // the width-th of the wave's firsts, as above; a wave without candidates has none to pass on
-        Cand least{0, 0};
+        // the width-th of the wave's firsts, as above: its order in two halves, then (where that many are equal) its place
+        const uint32_t hi = (uint32_t)(first.order >> 32), lo = (uint32_t)first.order;
         const uint64_t with = __ballot(first.order != 0);
-        if (with) {
-            int better = 0;
-            for (int k = 0; k <= 63 - __builtin_clzll(with); ++k) better += ahead(of_lane(first, k), first);
-            const uint64_t hit = __ballot(better == W - 1 && first.order != 0);
-            if (hit) least = of_lane(first, __builtin_ctzll(hit));
+        const uint32_t t1 = with ? nth(hi, with, W) : 0u;
+        uint32_t t2 = 0, t3 = 0;
+        if (t1) {
+            const uint64_t tie = __ballot(hi == t1);
+            const int n2 = W - __builtin_popcountll(__ballot(hi > t1));
+            if (__builtin_popcountll(tie) > n2) {
+                t2 = nth(lo, tie, n2);
+                const uint64_t both = tie & __ballot(lo == t2);
+                const int n3 = n2 - __builtin_popcountll(tie & __ballot(lo > t2));
+                if (__builtin_popcountll(both) > n3) t3 = nth(~first.place, both, n3);
+            }
         }
+        const uint64_t least = (uint64_t)t1 << 32 | t2;
         __syncthreads();  // (best has been read, count is clear)
         static_for<kAtOnce + 1>([&](auto k) {
-            if (mine[k].order && !ahead(least, mine[k])) list[atomicAdd(&count, 1)] = mine[k];
+            if (mine[k].order > least || (mine[k].order == least && least && ~mine[k].place >= t3)) list[atomicAdd(&count, 1)] = mine[k];
         });
         __syncthreads();
         const int n = count;
         for (int k = tid; k < n; k += 256) {
             const Cand u = list[k];
             int rank = 0;
+#pragma unroll 4
             for (int j = 0; j < n; ++j) rank += ahead(list[j], u);
             if (rank < W) best[rank] = u;
         }
@@ -261,7 +284,8 @@ __global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
 hipError_t launch_beam_step(const BeamArgs& a, hipStream_t s) {
     const int64_t rows = a.batch * a.beams;
     if (rows * a.parts > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((a.type == kBF16 ? beam_part_kernel<2> : beam_part_kernel<4>), dim3((unsigned)(rows * a.parts)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((a.type == kBF16 ? beam_part_kernel<2> : beam_part_kernel<4>), dim3((unsigned)(rows * a.parts)), dim3(256),
+                       (size_t)(4 * kEach * a.width) * sizeof(uint64_t), s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)a.batch), dim3(256), 0, s, a);
