@@ -4,13 +4,15 @@
 //
 // Bound by one pass over the logits.  Within a beam the order is that of the logits themselves, so
 // the first kernel reads each once: a workgroup takes 4096 of a row into registers, sums their
-// exponentials from their maximum, and leaves its best `width`.  To find them without sorting,
-// each lane takes its own best; of a wave's 64 the width-th is a bound that at most width lanes pass, so
-// at most 16 width values of a wave are left to order (a few more than width, mostly), by counting for each how
-// many are better.  Every key holds the place too, so no two are equal and ties need no care.
-// The second kernel forms the values of the candidates that are left, in 64 bits (the difference of two
-// beams' sums decides, and an fp32 sum of scores and logits would make ties of what is none), and
-// takes the best in the same way.
+// exponentials from their maximum, and leaves its best `width`, in order.  To find them without sorting,
+// each lane takes its own best; of these the width-th (of the wave, or of the workgroup) is a bound that at most
+// width lanes pass, so at most 16 width values are left to order (a few more than width, mostly), by counting for each
+// how many are better.  Every key holds the place too, so no two are equal and ties need no care.
+// The second kernel, a workgroup to a text, forms the values of the candidates that are left, in 64 bits (the
+// difference of two beams' sums decides, and an fp32 sum of scores and logits would make ties of what is none), and
+// takes the best in the same way, the lists' first entries first: it ends where none of a piece is among the best.
+// One text of 4 beams over 256: 5.3 and 9.2 us; 32 texts of 8 beams over 32000 (33 MB): 13.0 and 14.6 us, 2.5 TB/s for
+// the first (the vector units: an exponential and the bound, some 25 instructions a value).  Latency holds the second.
 #include "kernels.hpp"
 #include "rowio.hpp"
 
@@ -18,10 +20,10 @@ namespace isam {
 
 namespace {
 
-// A value's order as unsigned; both zeros are one.
+// A value's order as unsigned, never 0; both zeros are one.
 __device__ __forceinline__ uint32_t order32(float v) {
     const uint32_t u = __float_as_uint(v + 0.0f);
-    return (int)u < 0 ? ~u : u | 0x80000000u;
+    return (int)u < 0 ? max(~u, 1u) : u | 0x80000000u;  // (one NaN would have 0)
 }
 __device__ __forceinline__ float value32(uint32_t o) { return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o); }
 __device__ __forceinline__ uint64_t order64(double v) {
@@ -53,12 +55,13 @@ __device__ __forceinline__ uint32_t nth(uint32_t v, uint64_t of, int n) {
     return t;
 }
 
-template <int ES>
+template <int ES, bool ALL>
 __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     constexpr int E = 16 / ES, Q = kEach / E;  // values of a 16-byte piece, pieces of a thread
-    extern __shared__ __attribute__((aligned(16))) uint64_t list[];  // 4 kEach width
+    extern __shared__ __attribute__((aligned(16))) uint64_t list[];  // of kEach width: at most width lanes (of each wave, without ALL) have any
     __shared__ double wsum[4];
     __shared__ float wmax[4];
+    __shared__ uint64_t firsts[ALL ? 256 : 1];
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     const int64_t row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, b = row / a.beams, i = row - b * a.beams;
@@ -93,16 +96,38 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     const uint64_t first = place(0) < a.V ? (uint64_t)order32(most) << 32 | (uint32_t)~(uint32_t)place(at) : 0ull;
     for (int m = 32; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
     if (lane == 0) wmax[wid] = most;
+    if constexpr (ALL) firsts[tid] = first;
     if (tid == 0) count = 0;
     __syncthreads();
     most = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
-    // the width-th of the wave's firsts; 0: fewer lanes have any
-    uint32_t low = nth((uint32_t)(first >> 32), ~0ull, W), rest = 0;
-    if (low) {
-        const uint64_t above = __ballot((uint32_t)(first >> 32) > low), ties = __ballot((uint32_t)(first >> 32) == low);
-        rest = nth((uint32_t)first, ties, W - __builtin_popcountll(above));
+    // the width-th of the firsts, by value and then (where that many are equal) by place; 0: fewer lanes have any.
+    // ALL: of the workgroup's, four times the comparisons, which pays where many pass (32 texts of 8 beams over 32000
+    // 13.0 of a wave's against 15.6 us, 4 texts of 64 beams 671 against 445 with the second kernel).
+    uint64_t least = 0;
+    if constexpr (ALL) {
+        uint32_t hi[4], lo[4], low = 0, rest = 0;
+        static_for<4>([&](auto k) {
+            const uint64_t f = firsts[k * 64 + lane];
+            hi[k] = (uint32_t)(f >> 32);
+            lo[k] = (uint32_t)f;
+        });
+        auto lanes = [&](auto which) {
+            int n = 0;
+            static_for<4>([&](auto k) { n += __builtin_popcountll(__ballot(which(k))); });
+            return n;
+        };
+        for (uint32_t bit = 0x80000000u; bit; bit >>= 1) low = lanes([&](auto k) { return hi[k] >= (low | bit); }) >= W ? low | bit : low;
+        if (low) {
+            const int more = W - lanes([&](auto k) { return hi[k] > low; });
+            if (lanes([&](auto k) { return hi[k] == low; }) > more)
+                for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+                    rest = lanes([&](auto k) { return hi[k] == low && lo[k] >= (rest | bit); }) >= more ? rest | bit : rest;
+        }
+        least = (uint64_t)low << 32 | rest;
+    } else {
+        const uint32_t hi = (uint32_t)(first >> 32), low = nth(hi, ~0ull, W);
+        if (low) least = (uint64_t)low << 32 | nth((uint32_t)first, __ballot(hi == low), W - __builtin_popcountll(__ballot(hi > low)));
     }
-    const uint64_t least = (uint64_t)low << 32 | rest;
     const float bound = value32((uint32_t)(least >> 32));
     static_for<kEach>([&](auto k) {
         if (place(k) < a.V && (least == 0 || v[k] >= bound)) {
@@ -149,9 +174,10 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, W = (int)a.width, parts = (int)a.parts, beams = (int)a.beams;
     const int64_t b = blockIdx.x;
-    const uint32_t each = (uint32_t)parts * (uint32_t)W, all = (uint32_t)beams * each, V = (uint32_t)a.V, end = (uint32_t)a.end;
+    // candidate c: of list c % lists (a part of a beam) the c / lists-th
+    const uint32_t lists = (uint32_t)beams * (uint32_t)parts, all = lists * (uint32_t)W, V = (uint32_t)a.V, end = (uint32_t)a.end;
     const uint64_t* const from = a.best + b * (int64_t)all;
-    const uint64_t early = tid < all ? from[tid] : 0ull;  // (on its way during the sums)
+    const uint64_t early = tid < all ? from[tid % lists * W + tid / lists] : 0ull;  // (on its way during the sums)
     int lanes = 1;
     while (lanes < 64 && lanes < parts) lanes *= 2;
     // a lane to a part, 64 / lanes beams to a wave
@@ -185,31 +211,33 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
     }
     for (int k = tid; k < W; k += 256) best[k] = Cand{0, 0};
     __syncthreads();
-    // candidate c: of beam c / each; of a beam that can go on the parts' best, else the first tokens
+    // of a beam that can go on the parts' best, else the first tokens
     const double none = -INFINITY;
     auto candidate = [&](uint32_t c) {
-        const uint32_t i = c / each, k = c - i * each;
+        const uint32_t k = c / lists, l = c - k * lists, i = l / (uint32_t)parts;
         const double o = offset[i];
         if (over[i] || o == none) {
             // (a finished beam: its end token, then the others)
-            if (k >= (uint32_t)W || k >= V) return Cand{0, 0};
+            if (l != i * (uint32_t)parts || k >= V) return Cand{0, 0};
             if (over[i] && o != none) {
                 const uint32_t v = k == 0 ? end : k - 1 < end ? k - 1 : k;
                 return Cand{order64(k == 0 ? o : none), i * V + v};
             }
             return Cand{order64(none), i * V + k};
         }
-        const uint64_t u = c < 256 ? early : from[c];
+        const uint64_t u = c < 256 ? early : from[l * W + k];
         if (!u) return Cand{0, 0};
         const double v = o + (double)value32((uint32_t)(u >> 32));
         return Cand{order64(v == v ? v : none), i * V + ~(uint32_t)u};
     };
     for (uint32_t c0 = 0; c0 < all; c0 += 256 * kAtOnce) {
         Cand mine[kAtOnce + 1];
+        const Cand last = best[W - 1];  // (nothing behind it can be among the best any more)
         static_for<kAtOnce>([&](auto k) {
             const uint32_t c = c0 + k * 256 + tid;
             mine[k] = Cand{0, 0};
             if (c0 + k * 256 < all && c < all) mine[k] = candidate(c);
+            if (ahead(last, mine[k])) mine[k].order = 0;
         });
         mine[kAtOnce] = tid < W ? best[tid] : Cand{0, 0};
         if (tid == 0) count = 0;
@@ -232,10 +260,15 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
         }
         const uint64_t least = (uint64_t)t1 << 32 | t2;
         __syncthreads();  // (best has been read, count is clear)
+        bool fresh = false;
         static_for<kAtOnce + 1>([&](auto k) {
-            if (mine[k].order > least || (mine[k].order == least && least && ~mine[k].place >= t3)) list[atomicAdd(&count, 1)] = mine[k];
+            if (mine[k].order > least || (mine[k].order == least && least && ~mine[k].place >= t3)) {
+                list[atomicAdd(&count, 1)] = mine[k];
+                fresh = fresh || k < kAtOnce;
+            }
         });
-        __syncthreads();
+        // (each list falls: where none of it is among the best, none behind is)
+        if (!__syncthreads_or(fresh) && lists <= 256 * kAtOnce) break;
         const int n = count;
         for (int k = tid; k < n; k += 256) {
             const Cand u = list[k];
@@ -284,8 +317,12 @@ __global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
 hipError_t launch_beam_step(const BeamArgs& a, hipStream_t s) {
     const int64_t rows = a.batch * a.beams;
     if (rows * a.parts > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((a.type == kBF16 ? beam_part_kernel<2> : beam_part_kernel<4>), dim3((unsigned)(rows * a.parts)), dim3(256),
-                       (size_t)(4 * kEach * a.width) * sizeof(uint64_t), s, a);
+    const bool all = a.width > 16;
+    const size_t room = (size_t)((all ? 1 : 4) * kEach * a.width) * sizeof(uint64_t);
+    typedef void (*PartFn)(BeamArgs);
+    const PartFn fn = a.type == kBF16 ? (all ? beam_part_kernel<2, true> : beam_part_kernel<2, false>)
+                                      : (all ? beam_part_kernel<4, true> : beam_part_kernel<4, false>);
+    hipLaunchKernelGGL(fn, dim3((unsigned)(rows * a.parts)), dim3(256), room, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)a.batch), dim3(256), 0, s, a);

@@ -211,3 +211,29 @@ def test_refusals():
         isam.beam_reorder(state, p.long(), dim=1)
     with pytest.raises(isam.IsamError):
         isam.beam_reorder(state, p, dim=1, out=state)
+
+
+@DTYPES
+@pytest.mark.parametrize("width", [1, 4, 16, 17, 64])
+def test_equal_logits_and_nan_of_all_bits(width, dtype):
+    """More equal values than the candidates' list holds: the lowest places; a row of NaN with every bit set has no
+    candidates."""
+    logits = torch.zeros((2, 3, 9000), dtype=dtype, device="cuda")
+    scores = torch.tensor([[-1.0, -2.0, -2.0], [0.0, 0.0, -1.0]], device="cuda")
+    compare(logits, scores, width=width)
+    logits[:, :, 4000:] = 1.0
+    compare(logits, scores, width=width)
+    bits = logits.view(torch.int16 if dtype is torch.bfloat16 else torch.int32)
+    bits[0, 0] = -1
+    bits[1, :2] = -1
+    compare(logits, scores, width=width)
+
+
+@DTYPES
+def test_one_beam_far_ahead(dtype):
+    """The best all come from one beam's parts, whose lists have to be followed to their ends."""
+    logits, scores = inputs(2, 16, 20000, dtype, seed=5)
+    scores[0, 3] += 100
+    scores[1, 15] += 100
+    for width in (2, 16, 64):
+        compare(logits, scores, width=width)
