@@ -533,7 +533,7 @@ isam_status_t isam_beam_reorder(int64_t outer, int64_t batch, int64_t beams, int
  * Sums and epilogue are fp32; out is rounded once.  K > 0; M or N == 0: no-op.  Each matrix below 2^31 bytes.
  * Workspace: isam_linear_workspace_size bytes (whatever the epilogue); aligned = 0 also makes room for copies of
  * bf16 rows off 16 bytes (K off 8 says so by itself), which a call with unaligned pointers or leading
- * dimensions (not multiples of 8) needs.  Up to 16 rows none is used.
+ * dimensions (not multiples of 8) needs (it is room for aligned rows too).  Up to 16 rows none is used.
  */
 isam_status_t isam_linear(int64_t M, int64_t K, int64_t N, int type, int act, const void* x, int64_t ldx, const void* W, int64_t ldw,
                           const float* bias, const void* residual, int64_t ldr, void* out, int64_t ldo, void* workspace,

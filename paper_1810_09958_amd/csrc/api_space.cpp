@@ -547,18 +547,38 @@ void linear_copies(LinearPlan& p, int64_t M, int64_t K, int64_t N) {
     if (p.copy_w) p.w_b = align256((size_t)(N * p.Kp) * 2);
 }
 
+// Whether the kernel for a few rows takes them: always up to 16, and up to 64 where its work, in units of 16 rows of x
+// and 1024 values of K to a round of its workgroups (16 columns each), is small.  It takes some 6 us and 1 (bf16) or 2.2
+// (fp32) for each unit, the tiles (their copies of unaligned rows included) and the product with its pass, us of 17, 32, 64
+// rows against it, gelu: bf16 1024x4096 (K x N) 11.4, 11.3, 11.5 against 7.2, 7.1, 8.4; 4096x1024 21.9, 21.6, 21.7 against
+// 10.7, 13.6, 21.5; 4096x16384 36, 35, 36 against 41, 53, 84; fp32 1024x4096 18.5, 19.1, 18.9 against 9.3, 9.6, 15.4;
+// 4096x1024 21, 24, 23 against 24, 27, 49.  Unaligned: bf16 6683x3905 57, 57, 57 against 37, 51, 83; fp32 92, 92, 91 against
+// 44, 57, 90.
+bool linear_few(int64_t M, int64_t K, int64_t N, bool aligned) {
+    if (M <= kGatedTokens) return true;
+    const int64_t rounds = cdiv(N, 16 * (int64_t)device_cus());
+    return M <= kLinearFew && (__int128)M * K * rounds <= (aligned ? 4 : 16) * 16 * 1024;
+}
+
+// Whether the bf16 tiles would be too few and too deep: the product in slices of K and a pass take less than one round
+// of 64 x 64 tiles, whose copies' latency costs 3.5 us for 1024 of K.  us of 64, 128, 256, 512 rows, tiles / product
+// and pass, gelu: 2048x2048 (K x N) 15, 15, 15, 16 / 16, 17, 19, 21; 4096x1024 22, 22, 22, 23 / 18, 18, 20, 23; 4096x4096
+// 24, 24, 26, 35 / 21, 24, 30, 38; 8192x2048 38, 38, 38, 40 / 23, 23, 32, 41; 16384x512 64, 64, 65, 64 / 24, 24, 27, 33.
+bool linear_deep(int64_t M, int64_t K, int64_t N) { return K >= 4096 && 2 * cdiv(M, 64) * cdiv(N, 64) <= (int64_t)device_cus(); }
+
 // Forward.  plain: no activation, and no residual but out itself: the library's product has that epilogue in every
 // one of its plans.
 LinearPlan linear_forward_plan(int64_t M, int64_t K, int64_t N, int type, bool plain, bool x_ok, bool w_ok) {
     LinearPlan p{};
-    if (M <= kGatedTokens) {
+    const bool aligned = x_ok && w_ok && K % 8 == 0;
+    if (linear_few(M, K, N, aligned)) {
         p.way = kLinearTokens;
     } else if (type == ISAM_F32 && gated_f32_direct(M, K, cdiv(N, 2), device_cus())) {
         p.way = kLinearF32;
     } else if (plain && (type == ISAM_F32 || (x_ok && w_ok))) {
         p.way = kLinearDirect;
         p.gemm_b = align256(product_workspace(0, 1, M, N, K, type));
-    } else if (type == ISAM_BF16) {
+    } else if (type == ISAM_BF16 && !(aligned && linear_deep(M, K, N))) {
         p.way = kLinearTiles;
         p.copy_x = !x_ok || K % 8;
         p.copy_w = !w_ok || K % 8;
@@ -729,7 +749,10 @@ extern "C" isam_status_t isam_linear(int64_t M, int64_t K, int64_t N, int type, 
 extern "C" size_t isam_linear_workspace_size(int64_t M, int64_t K, int64_t N, int type, int aligned) {
     if (M <= 0 || K <= 0 || N <= 0 || !valid_dtype(type) || !linear_sizes(M, K, N, type)) return 0;
     size_t most = 0;
-    for (const bool plain : {false, true}) most = std::max(most, linear_forward_plan(M, K, N, type, plain, aligned != 0, aligned != 0).total());
+    for (const bool plain : {false, true}) {
+        most = std::max(most, linear_forward_plan(M, K, N, type, plain, true, true).total());
+        if (!aligned) most = std::max(most, linear_forward_plan(M, K, N, type, plain, false, false).total());
+    }
     return room(most);
 }
 

@@ -343,8 +343,10 @@ hipError_t launch_gated_f32(const GatedArgs& a, bool backward, hipStream_t s);
 hipError_t launch_gated_pairs(const GatedArgs& a, bool backward, hipStream_t s);
 
 // Projection with its epilogue (linear.hip): bf16 tiles over 16-byte aligned rows (GatedTile's, each as wide as
-// high), up to kGatedTokens rows of x and fp32 grids of few tiles at any alignment, and the element-wise pass.
+// high), up to kLinearFew rows of x (backward kGatedTokens) and fp32 grids of few tiles at any alignment, and the
+// element-wise pass.
 constexpr int64_t kLinearRows = 32;  // rows of a workgroup of the element-wise pass
+constexpr int64_t kLinearFew = 64;   // most rows of the kernel for a few of them
 struct LinearArgs {
     int64_t M, K, N;
     int act;                  // 0 sigmoid, 1 silu, 2 gelu, 3 none

@@ -8,14 +8,38 @@
 // formed again (2 M N K operations, against keeping M N values) and dP leaves rounded to bf16, as the
 // operand of the two products after it, so that dx and dW carry two roundings (beyond 16 rows).  The
 // bias' gradient is summed before that rounding.
-// Up to 16 rows the weights are streamed once, straight into the matrix instructions' operand registers.
-// fp32 grids of few tiles run on the fp32 matrix instructions, straight from memory; larger ones go
-// through the library's product and an element-wise pass.
+// Up to 16 rows (64 over little work) the weights are streamed once, straight into the matrix instructions' operand
+// registers: 1x1024x4096 (M x K x N) 4.2 us, 2 TB/s between start and end of one launch.  bf16 tiles: 8192x8192x2048
+// with a residual 212 us, 1.30 PFLOP/s, power, as the large product; 8192x2048x8192 280 us without an activation and 308
+// with gelu, whose epilogue (67 M values on the vector units) nothing covers.  Gradient of 2048x1024x4096 with gelu 100 us:
+// dP about 31, dx 31, dW 24 and the transposed copy of its operand 13.
+// fp32 grids of few tiles run on the fp32 matrix instructions, straight from memory; larger ones, and deep bf16 products
+// of few tiles, go through the library's product and an element-wise pass.
 #include "gated_ffn.hpp"
 
 namespace isam {
 
 namespace {
+
+// p Phi(p) and its derivative Phi(p) + p phi(p).  Both halves need exp(-p^2 / 2) once: Phi(-|p|) = exp(-x^2) erfcx(x) / 2
+// with x = |p| / sqrt 2, and erfcx(x) / (2 t) is a polynomial of t = 1 / (1 + 0.4 x) to 1.3e-7 of itself for all
+// x >= 0 (a least-squares fit to it weighted towards its largest error, over the zeros of a Chebyshev polynomial).
+__device__ __forceinline__ float gelu(float p, float& slope) {
+    const float e = __builtin_amdgcn_exp2f(p * p * -0.72134752f), t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(p), 0.28284271f, 1.0f));
+    float q = 0.0251324625f;
+    q = __builtin_fmaf(q, t, -0.0914563082f);
+    q = __builtin_fmaf(q, t, 0.0845517834f);
+    q = __builtin_fmaf(q, t, -0.00281151942f);
+    q = __builtin_fmaf(q, t, 0.0707194487f);
+    q = __builtin_fmaf(q, t, 0.0842699833f);
+    q = __builtin_fmaf(q, t, 0.103921491f);
+    q = __builtin_fmaf(q, t, 0.11283479f);
+    q = __builtin_fmaf(q, t, 0.112837931f);
+    q *= t * e;
+    const float cdf = p > 0.0f ? 1.0f - q : q;
+    slope = __builtin_fmaf(p * 0.39894228f, e, cdf);
+    return p * cdf;
+}
 
 // act(p) and its derivative.  ACT: 0 sigmoid, 1 silu, 2 gelu (erf form), 3 none.
 template <int ACT>
@@ -23,6 +47,8 @@ __device__ __forceinline__ float linear_act(float p, float& slope) {
     if constexpr (ACT == 3) {
         slope = 1.0f;
         return p;
+    } else if constexpr (ACT == 2) {
+        return gelu(p, slope);
     } else {
         return gate_act<ACT>(p, slope);
     }
@@ -227,64 +253,70 @@ __global__ __launch_bounds__(256, 2) void linear_ring_kernel(LinearArgs a, TileM
     linear_finish<BWD, BM, BN, 2, 32, 1, 256>(a, acc, smem, m0, n0, tm, wm, 0, kw == 0, tid, lane);
 }
 
-// A few rows (M <= 16): 16 rows of W per workgroup, streamed once into the operand registers; its
+// A few rows (MB blocks of 16): 16 rows of W per workgroup, streamed once into the operand registers; its
 // eight waves take every eighth K step and their sums meet in LDS.  x (a column per row of it) comes from the
-// caches.
-// BWD (bf16): dP instead, in two bf16 terms, the high ones in rows 0 .. M - 1 and what they leave in rows
+// caches, once for every 16 columns.
+// BWD (bf16, one block): dP instead, in two bf16 terms, the high ones in rows 0 .. M - 1 and what they leave in rows
 // M .. 2M - 1: over few rows the rounding of an operand is not averaged out, and twice the operations of both
 // products cost nothing while W's bytes bound them.
-template <int ES, bool BWD>
+template <int ES, bool BWD, int MB>
 __global__ __launch_bounds__(512) void linear_token_kernel(LinearArgs a) {
     using IO = Row16<ES>;
     constexpr int E = IO::E, KS = 4 * E, U = 4;  // values of K of a lane, of a step; steps in flight
-    __shared__ float sums[8][4][64];
+    static_assert(!BWD || MB == 1, "the gradient's terms are those of one block");
+    __shared__ float sums[8][4 * MB][64];
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + li;
     const int nk = (int)((a.K + KS - 1) / KS);
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    f32x4_t acc[MB];
+    static_for<MB>([&](auto m) { acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
     for (int s0 = wid; s0 < nk; s0 += 8 * U) {
-        uint4 w[U], x[U];
+        uint4 w[U], x[U][MB];
         static_for<U>([&](auto u) {
             const int64_t k = (int64_t)(s0 + 8 * u) * KS + g * E;
             const int valid = (int)max((int64_t)0, min((int64_t)E, a.K - k));
             w[u] = IO::load(a.W, n * a.ld_w + k, n < a.N ? valid : 0);
-            x[u] = IO::load(a.x, li * a.ld_x + k, li < a.M ? valid : 0);
+            static_for<MB>([&](auto m) { x[u][m] = IO::load(a.x, (16 * m + li) * a.ld_x + k, 16 * m + li < a.M ? valid : 0); });
         });
         static_for<U>([&](auto u) {
-            if constexpr (ES == 2) mfma16_bf16(acc, w[u], x[u]);
-            else mfma16_f32x4(acc, w[u], x[u]);
+            static_for<MB>([&](auto m) {
+                if constexpr (ES == 2) mfma16_bf16(acc[m], w[u], x[u][m]);
+                else mfma16_f32x4(acc[m], w[u], x[u][m]);
+            });
         });
     }
-    static_for<4>([&](auto v) { sums[wid][v][lane] = acc[decltype(v)::value]; });
+    static_for<MB>([&](auto m) { static_for<4>([&](auto v) { sums[wid][4 * m + v][lane] = acc[m][decltype(v)::value]; }); });
     __syncthreads();
     if (BWD && n0 + 16 >= a.N) {
         LinearArgs both = a;
         both.M = 2 * a.M;
         linear_pad<2>(both, 0, (int)both.M, threadIdx.x, 512);
     }
-    // thread (v, lane) of the first four waves: n = n0 + 4 g + v, row li
-    if (wid >= 4) return;
-    const int64_t no = n0 + 4 * g + wid;
-    const bool on = no < a.N && li < a.M;
-    if (!BWD && !on) return;
-    float p = a.bias && no < a.N ? a.bias[no] : 0.0f;
-    for (int w = 0; w < 8; ++w) p += sums[w][wid][lane];
-    float slope;
-    const float s = linear_act(a.act, p, slope);
-    const float other = on && a.side ? IO::get(a.side, (int64_t)li * a.ld_side + no) : 0.0f;
-    if constexpr (!BWD) {
-        IO::put(a.out, (int64_t)li * a.ld_out + no, s + other);
-    } else {
-        float d = on ? other * slope : 0.0f;
-        if (on) {
-            const int64_t at = (int64_t)li * a.ld_out + no;
-            const float high = bf16_to_f32((uint16_t)pack_bf16_rne(d, 0.0f)), low = d - high;
-            IO::put(a.out, at, high);
-            // (nothing is left of what the high term cannot hold: infinities, NaN)
-            IO::put(a.out, at + a.M * a.ld_out, low - low == 0.0f ? low : 0.0f);
+    // thread (4 m + v, lane): n = n0 + 4 g + v, row 16 m + li
+    for (int i = wid; i < 4 * MB; i += 8) {
+        const int64_t no = n0 + 4 * g + (i & 3);
+        const int row = 16 * (i >> 2) + li;
+        const bool on = no < a.N && row < a.M;
+        if (!BWD && !on) continue;
+        float p = a.bias && no < a.N ? a.bias[no] : 0.0f;
+        for (int w = 0; w < 8; ++w) p += sums[w][i][lane];
+        float slope;
+        const float s = linear_act(a.act, p, slope);
+        const float other = on && a.side ? IO::get(a.side, (int64_t)row * a.ld_side + no) : 0.0f;
+        if constexpr (!BWD) {
+            IO::put(a.out, (int64_t)row * a.ld_out + no, s + other);
+        } else {
+            float d = on ? other * slope : 0.0f;
+            if (on) {
+                const int64_t at = (int64_t)row * a.ld_out + no;
+                const float high = bf16_to_f32((uint16_t)pack_bf16_rne(d, 0.0f)), low = d - high;
+                IO::put(a.out, at, high);
+                // (nothing is left of what the high term cannot hold: infinities, NaN)
+                IO::put(a.out, at + a.M * a.ld_out, low - low == 0.0f ? low : 0.0f);
+            }
+            static_for<4>([&](auto k) { d += __shfl_xor(d, 1 << decltype(k)::value); });
+            if (a.bias_part && li == 0 && no < a.N) a.bias_part[no] = d;
         }
-        static_for<4>([&](auto k) { d += __shfl_xor(d, 1 << decltype(k)::value); });
-        if (a.bias_part && li == 0 && no < a.N) a.bias_part[no] = d;
     }
 }
 
@@ -445,8 +477,14 @@ hipError_t launch_linear_tiles(const LinearArgs& a, int tile, bool backward, hip
 }
 
 hipError_t launch_linear_tokens(const LinearArgs& a, int type, bool backward, hipStream_t s) {
-    if (a.M > kGatedTokens || (a.N + 15) / 16 > INT32_MAX || (backward && type != kBF16)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((backward ? linear_token_kernel<2, true> : type == kBF16 ? linear_token_kernel<2, false> : linear_token_kernel<4, false>), dim3((unsigned)((a.N + 15) / 16)), dim3(512), 0, s, a);
+    if (a.M > (backward ? kGatedTokens : kLinearFew) || (a.N + 15) / 16 > INT32_MAX || (backward && type != kBF16)) return hipErrorInvalidValue;
+    typedef void (*TokenFn)(LinearArgs);
+    TokenFn fn;
+    if (backward) fn = linear_token_kernel<2, true, 1>;
+    else if (a.M <= 16) fn = type == kBF16 ? linear_token_kernel<2, false, 1> : linear_token_kernel<4, false, 1>;
+    else if (a.M <= 32) fn = type == kBF16 ? linear_token_kernel<2, false, 2> : linear_token_kernel<4, false, 2>;
+    else fn = type == kBF16 ? linear_token_kernel<2, false, 4> : linear_token_kernel<4, false, 4>;
+    hipLaunchKernelGGL(fn, dim3((unsigned)((a.N + 15) / 16)), dim3(512), 0, s, a);
     return hipGetLastError();
 }
 

@@ -18,6 +18,10 @@
 // Where the channels are too few for the chip, time is cut into segments: a first kernel leaves
 // each segment's end state from zero and the sum of its steps (its map is h -> exp(A sum d) h + end),
 // and each workgroup of the scan composes those before its own.
+// A token and wave (8 channels, N 16) costs the forward walk some 57 cycles of the vector units and 48 of the compute
+// unit's LDS (B, C, d and d x of every lane, four waves): both bound it.  2048x8x1024 (tokens, sequences, channels), N 16,
+// bf16: summaries 52 us and scan 97; backward summaries 53, gradient 325, sums of dB
+// and dC 17.
 #pragma once
 
 #include "kernels.hpp"

@@ -257,3 +257,22 @@ def test_refusals():
     with pytest.raises(isam.IsamError) as e:
         isam.linear_backward(x["x"], x["W"], x["dout"], workspace=torch.empty(16, device="cuda", dtype=torch.uint8))
     assert e.value.status == 3
+
+
+@DTYPES
+@pytest.mark.parametrize("M,K,N", [(17, 1024, 96), (31, 130, 50), (32, 1000, 4001), (33, 512, 17), (47, 33, 129), (48, 1365, 15), (49, 200, 333),
+                                   (63, 1024, 100), (64, 1024, 512), (64, 1023, 70), (50, 2048, 40), (64, 4096, 200), (130, 4100, 72),
+                                   (65, 8192, 64), (20, 6001, 333)])
+def test_rows_between_few_and_tiles(M, K, N, dtype):
+    """Up to 64 rows over little work, and deep products of few tiles: their own ways."""
+    for i, name in enumerate(ACTS):
+        compare(inputs(M, K, N, dtype, seed=M + i, bias=i != 1, residual=i != 2), name, backward=i == 3)
+
+
+@DTYPES
+@pytest.mark.parametrize("M,K,N", [(17, 1024, 96), (64, 1024, 512), (64, 4096, 200), (33, 1001, 65)])
+def test_workspace_for_unaligned_rows_serves_aligned_ones(M, K, N, dtype):
+    x = inputs(M, K, N, dtype, seed=K)
+    code = 1 if dtype is torch.bfloat16 else 0
+    room = torch.empty(max(isam.linear_workspace_size(M, K, N, code, aligned=False), 1), dtype=torch.uint8, device="cuda")
+    check(isam.linear(x["x"], x["W"], bias=x["bias"], activation="gelu", residual=x["residual"], workspace=room), reference(x, "gelu")["out"], "out")
