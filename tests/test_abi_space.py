@@ -125,8 +125,8 @@ def linear(L, M=40, K=16, N=8, dt=BF16, act=1, x=at(0), ldx=16, W=at(1), ldw=16,
     (dict(M=-1), INVALID), (dict(K=0), INVALID), (dict(N=-1), INVALID), (dict(dt=3), INVALID), (dict(act=4), INVALID), (dict(act=-1), INVALID),
     (dict(x=None), INVALID), (dict(W=None), INVALID), (dict(out=None), INVALID), (dict(ldx=15), INVALID), (dict(ldw=15), INVALID),
     (dict(ldo=7), INVALID), (dict(ldr=7), INVALID), (dict(out=at(0)), INVALID), (dict(out=at(2)), INVALID), (dict(out=at(3), ldo=9), INVALID),
-    (dict(out=at(3, 2)), INVALID), (dict(ldx=17), WORKSPACE), (dict(K=15), WORKSPACE), (dict(dt=F32, M=4000, K=2000, N=4000, ldx=2000, ldw=2000, ldr=4000, ldo=4000), WORKSPACE),
-    (dict(ldx=17, ws=at(5), wsb=64), WORKSPACE), (dict(ldx=17, ws=at(4), wsb=1 << 20), INVALID),
+    (dict(out=at(3, 2)), INVALID), (dict(M=100, ldx=17), WORKSPACE), (dict(M=100, K=15), WORKSPACE), (dict(dt=F32, M=4000, K=2000, N=4000, ldx=2000, ldw=2000, ldr=4000, ldo=4000), WORKSPACE),
+    (dict(M=100, ldx=17, ws=at(5), wsb=64), WORKSPACE), (dict(M=100, ldx=17, ws=at(4), wsb=1 << 20), INVALID),
     (dict(M=1 << 20, ldx=1 << 11), UNSUPPORTED), (dict(M=1 << 20, N=1 << 12, ldo=1 << 12, ldr=1 << 12), UNSUPPORTED),
     (dict(N=1 << 20, ldw=1 << 12, ldr=1 << 20, ldo=1 << 20), UNSUPPORTED),
 ])
