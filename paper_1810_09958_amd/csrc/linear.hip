@@ -321,11 +321,13 @@ __global__ __launch_bounds__(512) void linear_token_kernel(LinearArgs a) {
 }
 
 // fp32 grids of few tiles: 32 rows x 64 columns on the fp32 matrix instructions, straight from memory
-// (any alignment of 4 bytes) into their operand registers.  The four waves take every fourth 16-deep K step (32
-// matrix instructions on 6 loads, two steps in flight) and meet in LDS, each wave then holding a 16 x 32 quarter.
+// (any alignment of 4 bytes) into their operand registers.  The eight waves take every eighth 16-deep K step (32
+// matrix instructions on 6 loads, two steps in flight) and meet in LDS, each wave then holding a 16 x 16 block.
+// 500x511x771 (M x K x N, 208 tiles) 13.3 us (four waves 15.5, four steps in flight 14.6; the matrix instructions 4).
 template <bool BWD>
-__global__ __launch_bounds__(256, 2) void linear_f32_kernel(LinearArgs a, TileMapArgs tmap) {
-    __shared__ float sums[4][32][64];
+__global__ __launch_bounds__(512) void linear_f32_kernel(LinearArgs a, TileMapArgs tmap) {
+    constexpr int NW = 8, U = 2;  // waves, steps loaded together
+    __shared__ float sums[NW][32][64];
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, g = lane >> 4;
     int tm, tn;
     map_tile(tmap, tm, tn);
@@ -350,26 +352,25 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(LinearArgs a, TileMa
     auto multiply = [&](const uint4 (&v)[6]) {
         static_for<2>([&](auto i) { static_for<4>([&](auto j) { mfma16_f32x4(acc[i][j], v[i], v[2 + j]); }); });
     };
-    uint4 b0[6], b1[6];
-    load(b0, wid);
-    load(b1, wid + 4);
-    for (int s = wid; s < steps; s += 8) {  // (steps past the end are zeros)
-        multiply(b0);
-        load(b0, s + 8);
-        multiply(b1);
-        load(b1, s + 12);
+    uint4 b[U][6];
+    static_for<U>([&](auto u) { load(b[u], wid + NW * u); });
+    for (int s = wid; s < steps; s += NW * U) {  // (steps past the end are zeros)
+        static_for<U>([&](auto u) {
+            multiply(b[u]);
+            load(b[u], s + NW * (U + u));
+        });
     }
-    if (a.K % 16 && wid == (steps & 3)) {  // the last values of the rows, one by one
+    if (a.K % 16 && wid == (steps & (NW - 1))) {  // the last values of the rows, one by one
         const int k = steps * 16 + 4 * g;
-        uint4 v[6];
+        uint4 tail[6];
         static_for<6>([&](auto o) {
             uint32_t w[4];
             static_for<4>([&](auto e) {
                 w[e] = buf_load4(o < 2 ? rx : rw, k + e < a.K && at[o] != kOob ? at[o] + (uint32_t)steps * 64u + 4u * e : kOob);
             });
-            v[o] = make_uint4(w[0], w[1], w[2], w[3]);
+            tail[o] = make_uint4(w[0], w[1], w[2], w[3]);
         });
-        multiply(v);
+        multiply(tail);
     }
     static_for<2>([&](auto i) {
         static_for<4>([&](auto j) {
@@ -377,34 +378,30 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(LinearArgs a, TileMa
         });
     });
     __syncthreads();
-    // this wave's quarter: row block wid / 2, column blocks 2 (wid % 2) and the next; rows 4 g + v, column li
-    const int64_t mq = m0 + 16 * (wid >> 1);
+    // this wave's eighth: row block wid / 4, column block wid % 4; rows 4 g + v, column li
+    const int64_t mq = m0 + 16 * (wid >> 2), n = n0 + 16 * (wid & 3) + li;
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.side, a.side ? (uint32_t)(((a.M - 1) * a.ld_side + a.N) * 4) : 0u);
     const __amdgpu_buffer_rsrc_t ro = make_rsrc(a.out, (uint32_t)(((a.M - 1) * a.ld_out + a.N) * 4));
-    static_for<2>([&](auto jj) {
-        const int j = 2 * (wid & 1) + jj, blk = (wid >> 1) * 4 + j;
-        const int64_t n = n0 + 16 * j + li;
-        const bool in = n < a.N;
-        const float bias = a.bias && in ? a.bias[n] : 0.0f;
-        float sum = 0.0f;
-        static_for<4>([&](auto v) {
-            const int64_t m = mq + 4 * g + v;
-            const bool on = in && m < a.M;
-            float p = bias;
-            static_for<4>([&](auto w) { p += sums[w][blk * 4 + v][lane]; });
-            float slope;
-            const float s = linear_act(a.act, p, slope);
-            const float other = __uint_as_float(buf_load4(rs, on && a.side ? (uint32_t)((m * a.ld_side + n) * 4) : kOob));
-            const float out = BWD ? other * slope : s + other;
-            __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(out), ro, (int)(on ? (uint32_t)((m * a.ld_out + n) * 4) : kOob), 0, 0);
-            sum += on ? out : 0.0f;
-        });
-        if (BWD && a.bias_part) {  // one partial row for every 16 rows
-            static_for<2>([&](auto k) { sum += __shfl_xor(sum, 16 << decltype(k)::value); });
-            if (in && g == 0) a.bias_part[(int64_t)(tm * 2 + (wid >> 1)) * a.N + n] = sum;
-        }
+    const bool in = n < a.N;
+    const float bias = a.bias && in ? a.bias[n] : 0.0f;
+    float sum = 0.0f;
+    static_for<4>([&](auto v) {
+        const int64_t m = mq + 4 * g + v;
+        const bool on = in && m < a.M;
+        float p = bias;
+        static_for<NW>([&](auto w) { p += sums[w][wid * 4 + v][lane]; });
+        float slope;
+        const float s = linear_act(a.act, p, slope);
+        const float other = __uint_as_float(buf_load4(rs, on && a.side ? (uint32_t)((m * a.ld_side + n) * 4) : kOob));
+        const float out = BWD ? other * slope : s + other;
+        __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint(out), ro, (int)(on ? (uint32_t)((m * a.ld_out + n) * 4) : kOob), 0, 0);
+        sum += on ? out : 0.0f;
     });
-    if (BWD && n0 + 64 >= a.N) linear_pad<4>(a, m0, (int)min((int64_t)32, a.M - m0), threadIdx.x, 256);
+    if (BWD && a.bias_part) {  // one partial row for every 16 rows
+        static_for<2>([&](auto k) { sum += __shfl_xor(sum, 16 << decltype(k)::value); });
+        if (in && g == 0) a.bias_part[(int64_t)(tm * 2 + (wid >> 2)) * a.N + n] = sum;
+    }
+    if (BWD && n0 + 64 >= a.N) linear_pad<4>(a, m0, (int)min((int64_t)32, a.M - m0), threadIdx.x, 512);
 }
 
 // The element-wise pass: out = act(P + b) + residual, or (BWD) dP, from P in memory ([M][ld_pre] fp32, which dP
@@ -491,7 +488,7 @@ hipError_t launch_linear_tokens(const LinearArgs& a, int type, bool backward, hi
 hipError_t launch_linear_f32(const LinearArgs& a, bool backward, hipStream_t s) {
     const int64_t tm = (a.M + 31) / 32, tn = (a.N + 63) / 64;
     if (tm * tn > INT32_MAX || a.K <= 0) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((backward ? linear_f32_kernel<true> : linear_f32_kernel<false>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, a,
+    hipLaunchKernelGGL((backward ? linear_f32_kernel<true> : linear_f32_kernel<false>), dim3((unsigned)(tm * tn)), dim3(512), 0, s, a,
                        linear_map(tm, tn));
     return hipGetLastError();
 }
