@@ -979,6 +979,7 @@ isam_status_t product(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K,
 }
 
 size_t product_workspace(int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int ab_type) {
+    if (M <= 0 || N <= 0 || K <= 0) return 0;  // (as isam_gemm_workspace_size: no plan of an empty product is asked for)
     return gemm_query(trans_a, trans_b, M, N, K, ab_type);
 }
 

@@ -597,6 +597,10 @@ LinearPlan linear_forward_plan(int64_t M, int64_t K, int64_t N, int type, bool p
 LinearPlan linear_backward_plan(int64_t M, int64_t K, int64_t N, int type, bool act, bool x_ok, bool w_ok, bool d_ok) {
     LinearPlan p{};
     const size_t es = dsize(type);
+    if (M == 0) {  // (zeros in dW and dbias; nothing is copied, formed or summed)
+        p.way = kLinearDirect;
+        return p;
+    }
     p.gemm_b = std::max(product_workspace(0, 0, M, K, N, type), product_workspace(1, 0, N, K, M, type));
     p.Kp = K;
     p.ld_pre = round8(N);

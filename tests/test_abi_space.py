@@ -148,6 +148,15 @@ def test_linear_backward_refusals(L, kw, code):
     refused(L, code, linear_bwd(L, **kw))
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("act", [0, 1, 2, NONE])
+@pytest.mark.parametrize("K,N", [(16, 8), (15, 7), (300, 300), (512, 512), (4096, 1024)])
+def test_linear_backward_of_no_rows(L, K, N, act, dt):
+    # the plan of an empty batch needs no workspace, as its query says; dx has no values, so nothing is launched
+    assert L.isam_linear_backward_workspace_size(0, K, N, dt, 1) == 0
+    assert L.isam_linear_backward(0, K, N, dt, act, at(0), K, at(1), K, at(2), at(3), N, at(4), K, None, K, None, None, 0, None) == OK
+
+
 def test_linear_no_op_and_workspace(L):
     assert linear(L, M=0) == OK and linear(L, N=0) == OK
     q, qb = L.isam_linear_workspace_size, L.isam_linear_backward_workspace_size

@@ -173,6 +173,17 @@ def test_empty():
         assert (isam.linear_backward(x, none, torch.empty((5, 0), device="cuda", dtype=dtype))[0] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("name", ["none", "sigmoid", "silu", "gelu"])
+@pytest.mark.parametrize("K,N", [(16, 8), (15, 7), (300, 300), (512, 512), (4096, 1024)])
+def test_gradient_of_no_rows(K, N, name, dtype):
+    e, W = torch.empty((0, K), device="cuda", dtype=dtype), torch.ones((N, K), device="cuda", dtype=dtype)
+    dW, db = torch.full((N, K), 7.0, device="cuda", dtype=dtype), torch.full((N,), 7.0, device="cuda")
+    dx, _, _ = isam.linear_backward(e, W, torch.empty((0, N), device="cuda", dtype=dtype), bias=torch.ones(N, device="cuda"), activation=name,
+                                    dW=dW, dbias=db)
+    assert dx.shape == (0, K) and (dW == 0).all() and (db == 0).all()
+
+
 @pytest.mark.parametrize("name", ["none", "silu", "gelu"])
 @pytest.mark.parametrize("M,K,N", [(5, 40, 30), (100, 40, 30)])
 def test_gradient_against_differences(M, K, N, name):
