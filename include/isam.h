@@ -547,7 +547,8 @@ size_t isam_linear_workspace_size(int64_t M, int64_t K, int64_t N, int type, int
  *   dx = dP . W [M][K] (type),  dW = dP^T . x [N][K] (type),  dbias = column sums of dP [N] fp32
  *   each may be NULL, not all
  * bf16 with an activation, beyond 16 rows: dP is rounded to bf16 as the operand of the products, so dx and dW carry
- * two roundings (up to 16 rows it enters in two bf16 terms); dbias is summed from the unrounded values.  Everything else is fp32, in a fixed order.
+ * two roundings, a norm error of 2.35e-3 instead of 1.66e-3 (up to 16 rows it enters in two bf16 terms, and ISAM_F32
+ * operands have no such rounding); dbias is summed from the unrounded values.  Everything else is fp32, in a fixed order.
  * M == 0: dW and dbias are 0.  N == 0: no-op (with rows and a dx, which would be zeros: an error).
  */
 isam_status_t isam_linear_backward(int64_t M, int64_t K, int64_t N, int type, int act, const void* x, int64_t ldx, const void* W,
