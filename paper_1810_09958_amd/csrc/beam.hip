@@ -84,13 +84,14 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     // value k of the thread: place v0 + ((k / E) 256 + tid) E + k % E
     auto place = [&](int k) { return v0 + (int64_t)((k / E) * 256 + tid) * E + k % E; };
     auto key = [&](int k) { return (uint64_t)order32(v[k]) << 32 | (uint32_t)~(uint32_t)place(k); };
-    // (places rise with k: the first of equal values is the best)
-    float most = v[0];
+    // The thread's best: places rise with k, so the first of equal values is.  A NaN is above nothing, so whatever its bits
+    // it hides none of the thread's values from the bound, which is what the list's size rests on (a NaN that passes for
+    // want of a bound makes the row one without candidates).
+    float most = -INFINITY;
     int at = 0;
-    static_for<kEach - 1>([&](auto k1) {
-        constexpr int k = decltype(k1)::value + 1;
-        const bool up = v[k] > most || (k == 1 && most != most);  // (a NaN makes the row one without candidates)
-        at = up ? k : at;
+    static_for<kEach>([&](auto k) {
+        const bool up = v[k] > most;
+        at = up ? (int)k : at;
         most = up ? v[k] : most;
     });
     const uint64_t first = place(0) < a.V ? (uint64_t)order32(most) << 32 | (uint32_t)~(uint32_t)place(at) : 0ull;

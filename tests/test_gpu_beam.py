@@ -237,3 +237,22 @@ def test_one_beam_far_ahead(dtype):
     scores[1, 15] += 100
     for width in (2, 16, 64):
         compare(logits, scores, width=width)
+
+
+@DTYPES
+@pytest.mark.parametrize("width", [1, 4, 16, 17, 64])
+@pytest.mark.parametrize("V", [4096, 9000])
+def test_nan_before_finite_values(V, width, dtype):
+    """NaN of both signs in the first values that most threads of a workgroup hold, finite ones behind: the row has no
+    candidates, and its neighbours keep theirs."""
+    logits, scores = inputs(2, 4, V, dtype, seed=V)
+    bits = logits.view(torch.int16 if dtype is torch.bfloat16 else torch.int32)
+    low, high = (-64, 0x7fc0) if dtype is torch.bfloat16 else (-4194304, 0x7fc00000)     # NaN below -inf and above inf by their bits
+    rising = torch.arange(V, device="cuda", dtype=torch.float32).to(dtype)
+    for b, i, first in ((0, 0, low), (0, 2, high), (1, 3, low)):
+        logits[b, i] = rising
+        bits[b, i, :1024] = low
+        bits[b, i, 0:2048:8] = first
+        bits[b, i, 1:2048:8] = first
+        logits[b, i, 96:104] = 2.0                        # one thread that has a value among them
+    compare(logits, scores, width=width)
