@@ -136,10 +136,12 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
             if (u >= least) list[atomicAdd(&count, 1)] = u;
         }
     });
-    // the sum; a NaN or an infinite maximum leaves NaN, which the second kernel takes as a row without candidates
+    // the sum; a NaN or an infinite maximum leaves NaN, which the second kernel takes as a row without candidates.  A part
+    // of -inf has none, but a NaN may stand among them.
     float few = 0.0f;
-    static_for<kEach>([&](auto k) { few += exp_of(v[k] - most); });
-    double sum = most == -INFINITY ? 0.0 : (double)few;
+    if (most == -INFINITY) static_for<kEach>([&](auto k) { few = v[k] == v[k] ? few : v[k]; });
+    else static_for<kEach>([&](auto k) { few += exp_of(v[k] - most); });
+    double sum = (double)few;
     for (int m = 32; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) wsum[wid] = sum;
     __syncthreads();
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
             const double o = __shfl_xor(most, m);
             most = o > most ? o : most;
         }
-        // (a part without a finite logit has no sum)
+        // (a part without a finite logit has the sum 0, or NaN)
         double2 v = own;
         double sum = 0.0;
         for (int p = at; p < parts;) {

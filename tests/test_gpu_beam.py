@@ -256,3 +256,21 @@ def test_nan_before_finite_values(V, width, dtype):
         bits[b, i, 1:2048:8] = first
         logits[b, i, 96:104] = 2.0                        # one thread that has a value among them
     compare(logits, scores, width=width)
+
+
+@DTYPES
+@pytest.mark.parametrize("width", [1, 4, 16, 17, 64])
+@pytest.mark.parametrize("V", [4097, 8193, 12000])
+def test_nan_among_masked_logits(V, width, dtype):
+    """A NaN whose neighbours are all -inf, or the row's last logit: the beam has no candidates."""
+    logits, scores = inputs(2, 4, V, dtype, seed=V)
+    scores[:, 1:3] += 50                                  # the beams with a NaN would win
+    logits[0, 1, V - 1] = float("nan")
+    logits[1, 2, V - 1] = -float("nan")
+    compare(logits, scores, width=width)
+    logits, scores = inputs(2, 4, V, dtype, seed=V)
+    scores[:, 1:3] += 50
+    logits[:, :, 4096:] = -math.inf                       # a part masked to -inf, with and without a NaN in it
+    for b, i, at in ((0, 1, 4096), (0, 2, V - 1), (1, 1, (4096 + V) // 2)):
+        logits[b, i, at] = float("nan")
+    compare(logits, scores, width=width)
