@@ -8,11 +8,13 @@
 // each lane takes its own best; of these the width-th (of the wave, or of the workgroup) is a bound that at most
 // width lanes pass, so at most 16 width values are left to order (a few more than width, mostly), by counting for each
 // how many are better.  Every key holds the place too, so no two are equal and ties need no care.
-// The second kernel, a workgroup to a text, forms the values of the candidates that are left, in 64 bits (the
-// difference of two beams' sums decides, and an fp32 sum of scores and logits would make ties of what is none), and
+// The exponentials and their sum are in 64 bits, as the difference of two beams' sums decides between candidates (in fp32,
+// 2^-23 to each, 32 texts of 8 beams over 32000 took 27.5 us instead of 33 and beams closer than that changed places).
+// The second kernel, a workgroup to a text, forms the values of the candidates that are left, in 64 bits too (an fp32
+// sum of scores and logits would make ties of what is none), and
 // takes the best in the same way, the lists' first entries first: it ends where none of a piece is among the best.
-// One text of 4 beams over 256: 5.3 and 9.2 us; 32 texts of 8 beams over 32000 (33 MB): 13.0 and 14.6 us, 2.5 TB/s for
-// the first (the vector units: an exponential and the bound, some 25 instructions a value).  Latency holds the second.
+// One text of 4 beams over 256: 5.3 and 9.2 us; 32 texts of 8 beams over 32000 (33 MB): 18.5 and 14.6 us, 1.8 TB/s for
+// the first (the vector units: an exponential in 64 bits and the bound).  Latency holds the second.
 #include "kernels.hpp"
 #include "rowio.hpp"
 
@@ -32,13 +34,6 @@ __device__ __forceinline__ uint64_t order64(double v) {
 }
 __device__ __forceinline__ double value64(uint64_t o) {
     return __longlong_as_double((long long)((int64_t)o < 0 ? o & 0x7fffffffffffffffull : ~o));
-}
-
-// exp(x) for x <= 0, to 2^-23 of itself: the product with log2 e in two parts.  NaN passes.
-__device__ __forceinline__ float exp_of(float x) {
-    const float p = x * 1.44269502f, lo = __builtin_fmaf(x, 1.44269502f, -p) + x * 1.92596299e-8f;
-    const float e = __builtin_amdgcn_exp2f(p);
-    return p < -126.0f ? 0.0f : __builtin_fmaf(e, lo * 0.69314718f, e);
 }
 
 constexpr int kEach = (int)(kBeamPart / 256);  // logits of a thread
@@ -138,10 +133,9 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     });
     // the sum; a NaN or an infinite maximum leaves NaN, which the second kernel takes as a row without candidates.  A part
     // of -inf has none, but a NaN may stand among them.
-    float few = 0.0f;
-    if (most == -INFINITY) static_for<kEach>([&](auto k) { few = v[k] == v[k] ? few : v[k]; });
-    else static_for<kEach>([&](auto k) { few += exp_of(v[k] - most); });
-    double sum = (double)few;
+    double sum = 0.0;
+    if (most == -INFINITY) static_for<kEach>([&](auto k) { sum = v[k] == v[k] ? sum : (double)v[k]; });
+    else static_for<kEach>([&](auto k) { sum += exp((double)v[k] - (double)most); });
     for (int m = 32; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) wsum[wid] = sum;
     __syncthreads();

@@ -274,3 +274,19 @@ def test_nan_among_masked_logits(V, width, dtype):
     for b, i, at in ((0, 1, 4096), (0, 2, V - 1), (1, 1, (4096 + V) // 2)):
         logits[b, i, at] = float("nan")
     compare(logits, scores, width=width)
+
+
+@DTYPES
+@pytest.mark.parametrize("V", [300, 5000, 20000])
+def test_beams_closer_than_fp32_tells(V, dtype):
+    """Two beams whose best candidates differ by no more than half a step of an fp32 score below 4 (2^-23), and by more than
+    64 bits leave unsure: the order is that of 64 bits."""
+    logits, scores = inputs(200, 2, V, dtype, seed=V + 1)
+    l = logits.cpu().double()
+    best = l.max(-1).values - torch.logsumexp(l, -1)
+    scores[:, 0] = 0.0
+    scores[:, 1] = (best[:, 0] - best[:, 1]).float().cuda()          # the nearest fp32 to a tie
+    gap = (best[:, 0] - best[:, 1] - scores[:, 1].cpu().double()).abs()
+    assert (gap <= 2.0 ** -23).all() and (gap > 2.0 ** -44).sum() >= 180
+    keep = gap > 2.0 ** -44
+    compare(logits[keep.cuda()].contiguous(), scores[keep.cuda()].contiguous())
