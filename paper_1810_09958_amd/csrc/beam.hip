@@ -152,10 +152,10 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     if (tid == 0) a.sums[row * a.parts + part] = make_double2((double)most, (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]));
 }
 
-// A candidate: its value's order (0: none) and its place, lowest first.
+// A candidate: its value's order (0: none) and its place, lowest first; the order of its logit (0: none of a beam that goes on).
 struct Cand {
     uint64_t order;
-    uint32_t place;
+    uint32_t place, logit;
 };
 __device__ __forceinline__ bool ahead(const Cand& x, const Cand& y) {
     return x.order > y.order || (x.order == y.order && x.order && x.place < y.place);
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
     __shared__ bool over[kBeamMax];           // finished
     __shared__ Cand list[4 * (kAtOnce + 1) * kBeamMax];
     __shared__ Cand best[kBeamMax];
-    __shared__ int count;
+    __shared__ int count, some[4];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, W = (int)a.width, parts = (int)a.parts, beams = (int)a.beams;
     const int64_t b = blockIdx.x;
     // candidate c: of list c % lists (a part of a beam) the c / lists-th
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
             over[i] = done;
         }
     }
-    for (int k = tid; k < W; k += 256) best[k] = Cand{0, 0};
+    for (int k = tid; k < W; k += 256) best[k] = Cand{0, 0, 0};
     __syncthreads();
     // of a beam that can go on the parts' best, else the first tokens
     const double none = -INFINITY;
@@ -215,30 +215,30 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
         const double o = offset[i];
         if (over[i] || o == none) {
             // (a finished beam: its end token, then the others)
-            if (l != i * (uint32_t)parts || k >= V) return Cand{0, 0};
+            if (l != i * (uint32_t)parts || k >= V) return Cand{0, 0, 0};
             if (over[i] && o != none) {
                 const uint32_t v = k == 0 ? end : k - 1 < end ? k - 1 : k;
-                return Cand{order64(k == 0 ? o : none), i * V + v};
+                return Cand{order64(k == 0 ? o : none), i * V + v, 0};
             }
-            return Cand{order64(none), i * V + k};
+            return Cand{order64(none), i * V + k, 0};
         }
         const uint64_t u = c < 256 ? early : from[l * W + k];
-        if (!u) return Cand{0, 0};
+        if (!u) return Cand{0, 0, 0};
         const double v = o + (double)value32((uint32_t)(u >> 32));
-        return Cand{order64(v == v ? v : none), i * V + ~(uint32_t)u};
+        return Cand{order64(v == v ? v : none), i * V + ~(uint32_t)u, (uint32_t)(u >> 32)};
     };
     for (uint32_t c0 = 0; c0 < all; c0 += 256 * kAtOnce) {
         Cand mine[kAtOnce + 1];
         const Cand last = best[W - 1];  // (nothing behind it can be among the best any more)
         static_for<kAtOnce>([&](auto k) {
             const uint32_t c = c0 + k * 256 + tid;
-            mine[k] = Cand{0, 0};
+            mine[k] = Cand{0, 0, 0};
             if (c0 + k * 256 < all && c < all) mine[k] = candidate(c);
             if (ahead(last, mine[k])) mine[k].order = 0;
         });
-        mine[kAtOnce] = tid < W ? best[tid] : Cand{0, 0};
+        mine[kAtOnce] = tid < W ? best[tid] : Cand{0, 0, 0};
         if (tid == 0) count = 0;
-        Cand first{0, 0};
+        Cand first{0, 0, 0};
         static_for<kAtOnce + 1>([&](auto k) { first = ahead(mine[k], first) ? mine[k] : first; });
         // the width-th of the wave's firsts, as above: its order in two halves, then (where that many are equal) its place
         const uint32_t hi = (uint32_t)(first.order >> 32), lo = (uint32_t)first.order;
@@ -273,6 +273,49 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
 #pragma unroll 4
             for (int j = 0; j < n; ++j) rank += ahead(list[j], u);
             if (rank < W) best[rank] = u;
+        }
+        __syncthreads();
+    }
+    // Unequal logits may have equal values (beside a score of the type's lowest value all have): of the last of the best's
+    // value the lists hold their parts' largest logits, not the lowest places.  A place left out of a list, or behind where
+    // the walk ended, is ahead of that last one only where the list has an entry of the same value that is not, behind it or
+    // the last itself, and so only in the part of the last: its places of that value are looked through.
+    const Cand low = best[W - 1];
+    const uint32_t beam = low.place / V;
+    auto order_of = [&](uint32_t logit) { return order64(offset[beam] + (double)value32(logit)); };
+    const bool merged = low.logit && (order_of(low.logit + 1) == low.order ||
+                                      order_of(low.logit - (low.logit == 0x80000000u ? 2 : 1)) == low.order);  // (past -0)
+    if (merged) {
+        const uint32_t v0 = (low.place - beam * V) / (uint32_t)kBeamPart * (uint32_t)kBeamPart, n = min(V - v0, (uint32_t)kBeamPart);
+        const uint32_t p0 = beam * V + v0;
+        const int64_t base = b * a.lg_b + beam * a.lg_n + v0;
+        for (int k = tid; k < W; k += 256) {
+            Cand u = best[k];
+            if (u.order == low.order && u.place - p0 < n) u.order = 0;
+            list[k] = u;
+        }
+        int found = 0;
+        for (uint32_t v = 0; v < n && found < W; v += 256) {
+            uint32_t logit = 0;
+            if (v + tid < n) logit = order32(a.type == kBF16 ? Row16<2>::get(a.logits, base + v + tid) : Row16<4>::get(a.logits, base + v + tid));
+            const bool same = logit && order_of(logit) == low.order;
+            const uint64_t with = __ballot(same);
+            if (lane == 0) some[wid] = __builtin_popcountll(with);
+            __syncthreads();
+            int at = found + __builtin_popcountll(with & ((1ull << lane) - 1));
+            for (int w = 0; w < 4; ++w) {
+                at += w < wid ? some[w] : 0;
+                found += some[w];
+            }
+            if (same && at < W) list[W + at] = Cand{low.order, p0 + v + tid, logit};
+            __syncthreads();
+        }
+        const int all = W + min(found, W);
+        for (int k = tid; k < all; k += 256) {
+            const Cand u = list[k];
+            int rank = 0;
+            for (int j = 0; j < all; ++j) rank += ahead(list[j], u);
+            if (u.order && rank < W) best[rank] = u;
         }
         __syncthreads();
     }

@@ -290,3 +290,39 @@ def test_beams_closer_than_fp32_tells(V, dtype):
     assert (gap <= 2.0 ** -23).all() and (gap > 2.0 ** -44).sum() >= 180
     keep = gap > 2.0 ** -44
     compare(logits[keep.cuda()].contiguous(), scores[keep.cuda()].contiguous())
+
+
+@DTYPES
+@pytest.mark.parametrize("width", [1, 2, 16, 17, 64])
+@pytest.mark.parametrize("V", [100, 5000, 9000])
+def test_unequal_logits_of_equal_values(V, width, dtype):
+    """Scores beside which 64 bits tell no logits apart: the lowest places, in texts whose other beam is finished too."""
+    logits, scores = inputs(3, 2, V, dtype, seed=V)
+    scores[:] = torch.finfo(torch.float32).min
+    compare(logits, scores, width=width)
+    scores[1, 0] = -1.0
+    scores[2, 1] = -2.0
+    fin = torch.zeros((3, 2), dtype=torch.bool, device="cuda")
+    fin[1, 0] = fin[2, 1] = True
+    compare(logits, scores, width=width, finished=fin, end=7)
+    logits, scores = inputs(3, 2, V, dtype, seed=V)
+    compare(logits * 2.0 ** -100, scores, width=width)               # (the same beside an ordinary score)
+    logits[:, :, ::5] = -math.inf
+    compare(logits * 2.0 ** -100, scores, width=width)
+
+
+@pytest.mark.parametrize("width", [1, 5, 16, 17, 40, 64])
+@pytest.mark.parametrize("V", [600, 9000, 30000])
+def test_classes_of_equal_values(V, width):
+    """Some candidates ahead, then many of one value with unequal logits in every part: steps of 2^31 of the values, the
+    logits' classes 2^36 and 2^37 with digits from 2^14 to 2^20 behind."""
+    g = torch.Generator().manual_seed(V + width)
+    logits = torch.full((2, 3, V), 2.0 ** 36) + torch.randint(0, 64, (2, 3, V), generator=g) * 2.0 ** 14
+    for b in range(2):
+        for i in range(3):
+            at = torch.randperm(V, generator=g)[:5]
+            logits[b, i, at] = 2.0 ** 37 + torch.randint(0, 32, (5,), generator=g) * 2.0 ** 15
+            logits[b, i, torch.rand(V, generator=g) < 0.3] = -(2.0 ** 36)
+    scores = torch.full((2, 3), -(2.0 ** 83))
+    scores[1, 1:] = -(2.0 ** 84)
+    compare(logits.cuda(), scores.cuda(), width=width)
