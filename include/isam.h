@@ -470,6 +470,7 @@ size_t isam_selective_scan_backward_workspace_size(int64_t T, int64_t batch, int
  *   state_T the same for the next call, or NULL: the last K - 1 inputs, zeros where a reset lies after
  *           them; may be state itself up to 8 tokens
  * Sums are fp32; y is rounded once.  T == 0: state_T = state (or zeros); batch or C == 0: no-op.
+ * A row of C values takes at most 2^32 bytes.
  */
 isam_status_t isam_causal_conv(int64_t T, int64_t batch, int64_t C, int64_t K, int type, int act, const void* x, int64_t x_stride_t,
                                int64_t x_stride_b, const float* w, const float* bias, const void* state, const uint8_t* reset,

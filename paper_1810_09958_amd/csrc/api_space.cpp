@@ -290,8 +290,9 @@ extern "C" size_t isam_selective_scan_backward_workspace_size(int64_t T, int64_t
 // ---------------------------------------------------------------------------
 namespace {
 
-bool conv_sizes(int64_t T, int64_t batch, int64_t C) {
-    return T < ((int64_t)1 << 40) && batch < ((int64_t)1 << 31) && C < ((int64_t)1 << 31) &&
+// (a lane's place in its row is kept in 32 bits)
+bool conv_sizes(int64_t T, int64_t batch, int64_t C, int type) {
+    return C <= ((int64_t)1 << 32) / (int64_t)dsize(type) && T < ((int64_t)1 << 40) && batch < ((int64_t)1 << 31) && C < ((int64_t)1 << 31) &&
            (__int128)std::max<int64_t>(T, 1) * std::max<int64_t>(batch, 1) * std::max<int64_t>(C, 1) < ((__int128)1 << 42);
 }
 
@@ -301,8 +302,8 @@ isam_status_t conv_check(int64_t T, int64_t batch, int64_t C, int64_t K, int typ
     if (!valid_dtype(type)) return fail(ISAM_ERR_INVALID_ARG, "%s: dtype must be ISAM_F32 (0) or ISAM_BF16 (1)", who);
     if (act != ISAM_ACT_NONE && act != ISAM_ACT_SILU)
         return fail(ISAM_ERR_INVALID_ARG, "%s: activation must be ISAM_ACT_NONE or ISAM_ACT_SILU", who);
-    if (K > kConvMaxK || !conv_sizes(T, batch, C))
-        return fail(ISAM_ERR_UNSUPPORTED, "%s: K=%lld above %lld, or sizes too large", who, (long long)K, (long long)kConvMaxK);
+    if (K > kConvMaxK || !conv_sizes(T, batch, C, type))
+        return fail(ISAM_ERR_UNSUPPORTED, "%s: K=%lld above %lld, or sizes too large (a row: 2^32 bytes)", who, (long long)K, (long long)kConvMaxK);
     return ISAM_OK;
 }
 
@@ -408,7 +409,7 @@ extern "C" isam_status_t isam_causal_conv_backward(int64_t T, int64_t batch, int
 }
 
 extern "C" size_t isam_causal_conv_backward_workspace_size(int64_t T, int64_t batch, int64_t C, int64_t K, int type) {
-    if (T <= 0 || batch <= 0 || C <= 0 || K <= 0 || K > kConvMaxK || !valid_dtype(type) || !conv_sizes(T, batch, C)) return 0;
+    if (T <= 0 || batch <= 0 || C <= 0 || K <= 0 || K > kConvMaxK || !valid_dtype(type) || !conv_sizes(T, batch, C, type)) return 0;
     // (the rows' strides decide whether a wave has several sequences, and that how long its runs are)
     return room(std::max(conv_part_bytes(conv_args(T, batch, C, K, type, ISAM_ACT_NONE, true)),
                          conv_part_bytes(conv_args(T, batch, C, K, type, ISAM_ACT_NONE, false))));

@@ -109,6 +109,16 @@ def test_causal_conv_backward_refusals(L, kw, code):
     refused(L, code, conv_bwd(L, **kw))
 
 
+@pytest.mark.parametrize("C,dt,fits", [((1 << 30) + 1, F32, False), (1 << 30, F32, True), ((1 << 31) - 1, F32, False), ((1 << 31) - 1, BF16, True)])
+def test_causal_conv_rows_of_32_bits(L, C, dt, fits):
+    # a lane's place in its row: rows of more than 2^32 bytes are refused, in the query too
+    assert (L.isam_causal_conv_backward_workspace_size(1, 1, C, 4, dt) > 0) == fits
+    kw = dict(T=1, B=1, C=C, dt=dt, x=(at(0), C, C), dx=(at(7), C, C), dy=(at(5), C, C), ws=None)
+    refused(L, WORKSPACE if fits else UNSUPPORTED, conv_bwd(L, **kw))
+    if not fits:
+        refused(L, UNSUPPORTED, conv(L, T=1, B=1, C=C, dt=dt, x=(at(0), C, C), y=(at(5), C, C)))
+
+
 def test_causal_conv_no_op_and_workspace(L):
     assert conv(L, B=0) == OK and conv(L, C=0) == OK
     q = L.isam_causal_conv_backward_workspace_size
