@@ -444,7 +444,7 @@ size_t isam_selective_scan_workspace_size(int64_t T, int64_t batch, int64_t D, i
  *   dA = sums of g_t a_t h_{t-1} d_t, dskip of dv_t x_t, ddt_bias of ddt_t, over t and b;  dh0 = a_0 g_0
  *   dx, ddt, dz  rows of D values (type), dB, dC  of N, at their own strides; dz NULL without z
  *   dA [D][N], dskip, ddt_bias [D], dh0 [batch][D][N] fp32; each of these, and dz, may be NULL
- * Sums are fp32, in a fixed order.  T or batch == 0: dA, dskip and ddt_bias are 0, dh0 = dh_T (or zeros).
+ * Sums are fp32, in a fixed order.  T or batch == 0: dA, dskip and ddt_bias are 0, dh0 = dh_T (or zeros).  D == 0: dB and dC are 0.
  */
 isam_status_t isam_selective_scan_backward(
     int64_t T, int64_t batch, int64_t D, int64_t N, int type, const void* x, int64_t x_stride_t, int64_t x_stride_b, const void* dt,

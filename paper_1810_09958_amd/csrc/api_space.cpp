@@ -210,7 +210,23 @@ extern "C" isam_status_t isam_selective_scan_backward(
     clear_error();
     const char* who = "isam_selective_scan_backward";
     isam_status_t st = scan_check(T, batch, D, N, type, who);
-    if (st != ISAM_OK || D == 0) return st;
+    if (st != ISAM_OK) return st;
+    if (D == 0) {  // (dB and dC are sums of nothing)
+        if (T == 0 || batch == 0) return ISAM_OK;
+        if (!dB || !dC) return fail(ISAM_ERR_INVALID_ARG, "%s: dB or dC is NULL", who);
+        RowsArg sums[] = {{"dB", dB, dB_stride_t, dB_stride_b, N, true}, {"dC", dC, dC_stride_t, dC_stride_b, N, true}};
+        const Tensor none[] = {{"workspace", nullptr, 0, true}};
+        if ((st = rows_check(sums, none, T, batch, dsize(type), who)) != ISAM_OK) return st;
+        ScanArgs a{};
+        a.T = T;
+        a.batch = batch;
+        a.N = N;
+        a.type = type;
+        a.dB = rows_of(sums[0]);
+        a.dC = rows_of(sums[1]);
+        const hipError_t e = launch_scan_backward(a, static_cast<hipStream_t>(stream));
+        return e == hipSuccess ? ISAM_OK : hip_fail(e, who);
+    }
     const bool work = T > 0 && batch > 0;
     if (work && (!x || !dt || !A || !B || !C || !states)) return fail(ISAM_ERR_INVALID_ARG, "%s: x, dt, A, B, C or states is NULL", who);
     if (work && (!dx || !ddt || !dB || !dC)) return fail(ISAM_ERR_INVALID_ARG, "%s: dx, ddt, dB or dC is NULL", who);

@@ -388,20 +388,22 @@ hipError_t launch_scan_backward(const ScanArgs& a, hipStream_t s) {
     hipError_t e;
     if (a.T > 0 && a.batch > 0) {
         const int64_t blocks = (a.D + scan_channels(a.N) - 1) / scan_channels(a.N), groups = a.batch * blocks;
-        if (groups * a.segs > INT32_MAX) return hipErrorInvalidValue;
-        const ScanShapeOf shape = scan_shape(a.N);
-        auto ok = [&](const ScanRows& r) { return scan_pieces(r, a.D, a.N, a.type); };
-        const bool vec = ok(a.x) && ok(a.dt) && ok(a.z) && ok(a.dy) && ok(a.dx) && ok(a.ddt) && ok(a.dz);
-        if (a.segs > 1) {
-            const ScanFn fn = a.type == kBF16 ? (vec ? scan_bwd_fn<2, true, true>(shape) : scan_bwd_fn<2, false, true>(shape))
-                                              : (vec ? scan_bwd_fn<4, true, true>(shape) : scan_bwd_fn<4, false, true>(shape));
-            hipLaunchKernelGGL(fn, dim3((unsigned)(groups * (a.segs - 1))), dim3(256), 0, s, a);
+        if (blocks > 0) {
+            if (groups * a.segs > INT32_MAX) return hipErrorInvalidValue;
+            const ScanShapeOf shape = scan_shape(a.N);
+            auto ok = [&](const ScanRows& r) { return scan_pieces(r, a.D, a.N, a.type); };
+            const bool vec = ok(a.x) && ok(a.dt) && ok(a.z) && ok(a.dy) && ok(a.dx) && ok(a.ddt) && ok(a.dz);
+            if (a.segs > 1) {
+                const ScanFn fn = a.type == kBF16 ? (vec ? scan_bwd_fn<2, true, true>(shape) : scan_bwd_fn<2, false, true>(shape))
+                                                  : (vec ? scan_bwd_fn<4, true, true>(shape) : scan_bwd_fn<4, false, true>(shape));
+                hipLaunchKernelGGL(fn, dim3((unsigned)(groups * (a.segs - 1))), dim3(256), 0, s, a);
+                if ((e = hipGetLastError()) != hipSuccess) return e;
+            }
+            const ScanFn fn = a.type == kBF16 ? (vec ? scan_bwd_fn<2, true, false>(shape) : scan_bwd_fn<2, false, false>(shape))
+                                              : (vec ? scan_bwd_fn<4, true, false>(shape) : scan_bwd_fn<4, false, false>(shape));
+            hipLaunchKernelGGL(fn, dim3((unsigned)(groups * a.segs)), dim3(256), 0, s, a);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        const ScanFn fn = a.type == kBF16 ? (vec ? scan_bwd_fn<2, true, false>(shape) : scan_bwd_fn<2, false, false>(shape))
-                                          : (vec ? scan_bwd_fn<4, true, false>(shape) : scan_bwd_fn<4, false, false>(shape));
-        hipLaunchKernelGGL(fn, dim3((unsigned)(groups * a.segs)), dim3(256), 0, s, a);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
         const int64_t n = (a.T * a.batch * 2 * a.N + 255) / 256;
         hipLaunchKernelGGL((a.type == kBF16 ? scan_bc_kernel<2> : scan_bc_kernel<4>), dim3((unsigned)(n < 8192 ? n : 8192)), dim3(256), 0,
                            s, a, blocks);

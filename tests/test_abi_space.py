@@ -78,6 +78,13 @@ def test_selective_scan_backward_refusals(L, kw, code):
     refused(L, code, scan_bwd(L, **kw))
 
 
+def test_selective_scan_backward_without_channels(L):
+    none = dict(D=0, x=(None, 0, 0), d=(None, 0, 0), A=None, z=(None, 0, 0), ws=None, wsb=0)
+    assert scan_bwd(L, T=0, **none) == OK and scan_bwd(L, B=0, **none) == OK
+    for kw in (dict(dB=(None, 0, 0)), dict(dC=(None, 0, 0)), dict(dB=(at(18), 6, 3)), dict(dC=(at(18), 5, 3)), dict(dB=(at(17), -6, 3))):
+        refused(L, INVALID, scan_bwd(L, **none, **kw))
+
+
 def conv(L, T=9, B=2, C=8, K=4, dt=BF16, act=1, x=(at(0), 16, 8), w=at(1), bias=at(2), state=at(3), reset=(at(4), 2, 1), y=(at(5), 16, 8),
          sT=at(6)):
     return L.isam_causal_conv(T, B, C, K, dt, act, *x, w, bias, state, *reset, *y, sT, None)

@@ -254,6 +254,21 @@ def test_empty():
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,B,N", [(1, 1, 1), (5, 3, 8), (100, 2, 64)])
+def test_gradient_without_channels(T, B, N, dtype):
+    # dB and dC are sums over no channels, as parts of wider rows whose other values stay
+    x = inputs(T, B, 0, N, dtype)
+    seq, opt = tuple(x[k] for k in ("x", "dt", "A", "B", "C")), {k: x[k] for k in ("skip", "z", "dt_bias")}
+    states = torch.empty(isam.selective_scan_states_shape(T, B, 0, N), device="cuda")
+    assert isam.selective_scan(*seq, states=states, **opt)[0].shape == (T, B, 0)
+    wide = torch.full((T, B, 2 * N + 3), 7.0, device="cuda", dtype=dtype)
+    out = dict(zip(NAMES, isam.selective_scan_backward(*seq, x["dy"], states=states, dB=wide[..., :N], dC=wide[..., N + 1:2 * N + 1], **opt)))
+    assert (out["dB"] == 0).all() and (out["dC"] == 0).all()
+    assert (wide[..., N] == 7).all() and (wide[..., 2 * N + 1:] == 7).all()
+    assert out["dA"].shape == (0, N) and out["dh0"].shape == (B, 0, N)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("T", [6, 60, 500])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_reset_cuts_off_bad_values(T, dtype, bad):
