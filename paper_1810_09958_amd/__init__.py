@@ -787,9 +787,9 @@ def beam_reorder(state: torch.Tensor, parent: torch.Tensor, *, dim=0, out=None):
     if not -len(shape) <= dim < len(shape):
         raise ValueError(f"state has no dimension {dim}")
     dim %= len(shape)
-    if not state.is_contiguous() or b == 0 or w == 0 or shape[dim] % b or shape[dim] == 0:
+    if not state.is_contiguous() or w == 0 or (shape[dim] % b or shape[dim] == 0 if b else shape[dim]):
         raise ValueError("state must be contiguous, with batch * beams rows along dim")
-    beams, outer, inner = shape[dim] // b, 1, state.element_size()
+    beams, outer, inner = shape[dim] // b if b else 1, 1, state.element_size()
     for i, n in enumerate(shape):
         if i < dim:
             outer *= n

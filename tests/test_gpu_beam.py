@@ -326,3 +326,15 @@ def test_classes_of_equal_values(V, width):
     scores = torch.full((2, 3), -(2.0 ** 83))
     scores[1, 1:] = -(2.0 ** 84)
     compare(logits.cuda(), scores.cuda(), width=width)
+
+
+@DTYPES
+def test_no_texts(dtype):
+    # a batch of none goes through the step and the reordering alike
+    got = isam.beam_step(torch.empty((0, 3, 50), device="cuda", dtype=dtype), torch.empty((0, 3), device="cuda"), width=4, end=2)
+    assert [tuple(t.shape) for t in got] == [(0, 4)] * 4
+    assert isam.beam_reorder(torch.empty((2, 0, 5), device="cuda", dtype=dtype), got[1], dim=1).shape == (2, 0, 5)
+    out = torch.empty((0, 7), device="cuda", dtype=dtype)
+    assert isam.beam_reorder(torch.empty((0, 7), device="cuda", dtype=dtype), got[1], out=out) is out
+    with pytest.raises(ValueError):
+        isam.beam_reorder(torch.empty((2, 6, 5), device="cuda", dtype=dtype), got[1], dim=1)
