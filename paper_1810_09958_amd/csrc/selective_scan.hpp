@@ -243,9 +243,13 @@ __device__ __forceinline__ bool meet(int N, bool wild) {
 
 // Segments: [segment][batch][D] sums of steps (sign bit set: a reset lies inside, nothing passes),
 // and [segment][batch][D][N] end states from zero.  What passes is at least 2^-126 of h, so that an infinity stays one
-// where the tokens' factors are above zero and their product is not.
+// where the tokens' factors are above zero and their product is not.  A product above 2^126 (states that grow) goes in
+// three equal factors: no infinity meets a state of zero, and a small state grows as far as token by token.
 __device__ __forceinline__ float pass_on(float sum, float a2, float h, float end) {
-    return (int)__float_as_uint(sum) < 0 ? end : __builtin_fmaf(fmaxf(__builtin_amdgcn_exp2f(sum * a2), 0x1p-126f), h, end);
+    const float e = sum * a2;
+    const bool far = e > 126.0f;
+    const float f = fmaxf(__builtin_amdgcn_exp2f(far ? fminf(e, 378.0f) * (1.0f / 3) : e), 0x1p-126f), again = far ? f : 1.0f;
+    return (int)__float_as_uint(sum) < 0 ? end : __builtin_fmaf(f, h * again * again, end);
 }
 
 // Instances by N and type: (lanes to a channel, values to a lane).

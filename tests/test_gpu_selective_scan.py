@@ -477,3 +477,59 @@ def test_refusals():
     state = long["h0"].clone()
     with pytest.raises(isam.IsamError):          # the state in place beyond a few tokens
         isam.selective_scan(*(long[k] for k in ("x", "dt", "A", "B", "C")), h0=state, h_T=state)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N", [4, 13, 16, 40])
+def test_growing_states_over_segments(N, dtype):
+    """A above 0: a segment's factors multiply to more than the type holds.  A state of zero stays zero through them, and a
+    small one grows as far as it does token by token.  Every term is positive, so errors are relative: of 20 tokens' factors
+    of up to e^2.6, 13 2^-24 each (the exponent's rounding and the exponential's), and the rows' own rounding."""
+    T, B, D, few = 2048, 1, 4, 20
+    g = torch.Generator().manual_seed(N)
+
+    def rows(w):
+        return (torch.rand((T, B, w), generator=g) + 0.5).to(dtype).cuda()
+
+    x, dt, Bs, Cs, dy = rows(D), rows(D), rows(N), rows(N), rows(D)
+    A = (torch.rand((D, N), generator=g) + 0.5).cuda()                # a factor of some e to a token
+    skip, states = torch.ones(D, device="cuda"), torch.empty(isam.selective_scan_states_shape(T, B, D, N), device="cuda")
+    tol = 2.0 ** -14 + torch.finfo(dtype).eps
+    # inputs in the last tokens only, as if they were the whole text
+    x[:T - few] = 0
+    y, h = isam.selective_scan(x, dt, A, Bs, Cs, skip=skip)
+    y2, h2 = isam.selective_scan(*(v[T - few:] for v in (x, dt)), A, *(v[T - few:] for v in (Bs, Cs)), skip=skip)
+    assert (y[:T - few] == 0).all() and h.isfinite().all()
+    assert ((h - h2).abs() <= tol * h2).all() and ((y[T - few:].float() - y2.float()).abs() <= tol * y2.float()).all()
+    # gradients of the first tokens only
+    x, dy = rows(D), dy.clone()
+    dy[few:] = 0
+    dt[few:] = -30.0                                                  # (the states of the forward pass stay finite)
+    dt[600:900] = 3.0                                                 # (states of zero from token 500 on)
+    x[500:900] = 0
+    Cs[few:] = 0
+    h0 = torch.zeros((B, D, N), device="cuda")
+    reset = torch.zeros((T, B), dtype=torch.bool, device="cuda")
+    reset[500] = True
+    isam.selective_scan(x, dt, A, Bs, Cs, skip=skip, h0=h0, reset=reset, states=states)
+    out = dict(zip(NAMES, isam.selective_scan_backward(x, dt, A, Bs, Cs, dy, states=states, skip=skip, reset=reset)))
+    part = torch.empty(isam.selective_scan_states_shape(few, B, D, N), device="cuda")
+    first = tuple(v[:few] for v in (x, dt))
+    weights = tuple(v[:few] for v in (Bs, Cs))
+    isam.selective_scan(*first, A, *weights, skip=skip, states=part)
+    want = dict(zip(NAMES, isam.selective_scan_backward(*first, A, *weights, dy[:few], states=part, skip=skip)))
+    for k in ("dx", "ddt", "dB"):
+        assert ((out[k][:few].float() - want[k].float()).abs() <= tol * want[k].float().abs()).all(), k
+        assert (out[k][few:] == 0).all(), k
+    for k in ("dA", "dh0", "dskip"):
+        assert ((out[k] - want[k]).abs() <= tol * want[k].abs()).all(), k
+    # a small state through one segment's growth: the sum of 64 steps up to 136 is off by 2^-12.4 at most, the rest by 2^-14
+    dt = torch.full((T, B, D), -30.0).to(dtype).cuda()
+    dt[:64] = 2.0
+    A = torch.full((D, N), 1.0, device="cuda")
+    step = torch.nn.functional.softplus(torch.tensor([2.0, -30.0], dtype=torch.float64))
+    growth = float(64 * step[0] + (T - 64) * step[1])                 # 136 in powers of e, 196 of 2
+    h0 = torch.full((B, D, N), 2.0 ** -100, device="cuda")
+    _, h = isam.selective_scan(torch.zeros_like(x), dt, A, Bs, Cs, h0=h0)
+    want = 2.0 ** -100 * math.exp(growth)
+    assert ((h.double() - want).abs() <= 2.0 ** -11 * want).all()
