@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a) {
         }
         const uint32_t reset = marks.bits();
         fetch(t0 + TT);  // (past the end: zeros)
-        wild = meet<NP>(N, wild);
+        wild = meet(N != NP, wild);
         // FAST: a whole tile without a reset (or an infinity that would reach the padding of N).  The next four tokens' values are on their way from LDS while
         // four are walked.
         auto walk = [&](auto fast) {

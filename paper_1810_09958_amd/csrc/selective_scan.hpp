@@ -152,6 +152,15 @@ struct ScanWeights {
             else h[i] = (uint16_t)buf_load2(rs, off);
         });
     }
+    // Whether one of them is an infinity or NaN.
+    __device__ __forceinline__ bool wild() const {
+        bool any = false;
+        static_for<BE>([&](auto i) {
+            if constexpr (ES == 4) any = any || (__float_as_uint(f[i]) & 0x7f800000u) == 0x7f800000u;
+            else any = any || (h[i] & 0x7f80u) == 0x7f80u;
+        });
+        return any;
+    }
     // To LDS: [token][lane group][B or C][R].
     template <int R>
     __device__ __forceinline__ void put(float* bc, int which, int tid) const {
@@ -233,10 +242,10 @@ struct ScanMarks {
 
 __device__ __forceinline__ bool not_finite(float v) { return !(__builtin_fabsf(v) < __builtin_inff()); }
 
-// A barrier; and whether a thread before it had an infinity or NaN that meets the zeros which pad N.
-template <int NP>
-__device__ __forceinline__ bool meet(int N, bool wild) {
-    if (N != NP) return __syncthreads_or(wild);
+// A barrier; and, where N or the channels are padded, whether a thread before it had an infinity or NaN that meets the
+// zeros there.
+__device__ __forceinline__ bool meet(bool padded, bool wild) {
+    if (padded) return __syncthreads_or(wild);
     __syncthreads();
     return false;
 }

@@ -66,6 +66,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
     const int64_t b = rest / blocks, blk = rest - b * blocks, c0 = blk * CH, ch = c0 + cl;
     const int64_t tbeg = seg * a.seg_len, tend = min(a.T, tbeg + a.seg_len);
     const bool in = ch < a.D;
+    const bool ragged = !SUM && c0 + CH > a.D;  // some lanes' channels are none: their zeros must stay out of dB and dC
     const int N = (int)a.N;
 
     float A2[R], G[R], dA[R];
@@ -174,12 +175,13 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
         {
             int id = tid;
             if constexpr (LEAN) asm volatile("" : "+v"(id));
+            if (ragged) wild = wild || wb.wild() || wc.wild();
             wc.template put<R>(bc, 1, id);
             if constexpr (!SUM) wb.template put<R>(bc, 0, id);
         }
         const uint32_t reset = marks.bits();
         fetch(t0 - TT);  // (before the segment: zeros)
-        wild = meet<NP>(N, wild);
+        wild = meet(N != NP || ragged, wild);
         auto walk = [&](auto fast) {
             constexpr bool FAST = decltype(fast)::value;
             if constexpr (SUM) {
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                         const bool drop = !FAST && (reset >> (tc + i) & 1), live = tc + i < left;
                         float acc = 0.0f;
                         static_for<R>([&](auto r) {
-                            const bool on = FAST || (live && g * R + r < N);
+                            const bool on = FAST || (live && in && g * R + r < N);
                             const float aw = on ? __builtin_amdgcn_exp2f(s.s.x * A2[r]) : 1.0f;
                             av[i][r] = aw;
                             const float hn = __builtin_fmaf(aw, drop ? 0.0f : h[i][r], s.s.y * s.B[r]);
@@ -258,7 +260,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a) {
                         float aq = 0.0f, gb = 0.0f, sums[2 * R];
                         static_for<R>([&](auto r) {
                             const float gn = __builtin_fmaf(s.C[r], dv, G[r]);
-                            G[r] = FAST || g * R + r < N ? gn : 0.0f;
+                            G[r] = FAST || (in && g * R + r < N) ? gn : 0.0f;
                             sums[r] = G[r] * s.s.y;
                             sums[R + r] = h[i + 1][r] * dv;
                             gb = r == 0 ? G[0] * s.B[0] : __builtin_fmaf(G[r], s.B[r], gb);

@@ -533,3 +533,27 @@ def test_growing_states_over_segments(N, dtype):
     _, h = isam.selective_scan(torch.zeros_like(x), dt, A, Bs, Cs, h0=h0)
     want = 2.0 ** -100 * math.exp(growth)
     assert ((h.double() - want).abs() <= 2.0 ** -11 * want).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [12, 100, 300])
+@pytest.mark.parametrize("N", [4, 7, 8, 16, 32, 40, 64])
+def test_infinite_weight_beside_no_channel(N, T, dtype):
+    """An infinite value of B (C) with positive inputs and gradients makes infinite sums over the channels in dC (dB) from
+    its token on (back), whatever the channels are padded to, and every other sum stays as it is."""
+    x = inputs(T, 2, 21, N, dtype, gate=False)
+    for k in ("x", "B", "C", "dy", "skip"):
+        x[k] = x[k].abs() + 0.5
+    x["A"] = x["A"] * (0.01 / N)                          # (no factor is lost to underflow)
+    x["dh_T"] = None
+    plain, at, inf = run(x), T // 2, float("inf")
+    for name, grad, other, when in (("B", "dC", "dB", slice(at, T)), ("C", "dB", "dC", slice(0, at + 1))):
+        old = x[name].clone()
+        x[name][at, 1, N - 1] = inf
+        got = run(x)
+        x[name] = old
+        hit = torch.zeros((T, 2, N), dtype=torch.bool, device="cuda")
+        hit[when, 1, N - 1] = True
+        assert (got[grad][hit] == inf).all() and torch.equal(got[grad][~hit], plain[grad][~hit]), grad
+        assert torch.equal(got[other], plain[other]), other
+        assert torch.equal(got["dx"][:, 0], plain["dx"][:, 0]) and (got["dx"][at, 1] == inf).all()
