@@ -10,7 +10,7 @@ using namespace isam::api;
 namespace {
 
 // A [T][batch] tensor of rows of `width` elements in a call.  Two of them that share their strides may
-// lie in one wider tensor (as halves of its rows): they overlap only where their rows do.
+// lie in one wider tensor (as halves of its rows, or turn by turn): they overlap only where their rows do.
 struct RowsArg {
     const char* name;
     const void* p;
@@ -18,14 +18,39 @@ struct RowsArg {
     bool out;
 };
 
+// Integers k with lo < k n < hi, n > 0, |k| <= most: the first and the last.
+struct Multiples {
+    int64_t first, last;
+};
+Multiples multiples(int64_t lo, int64_t hi, int64_t n, int64_t most) {
+    auto floor_div = [&](int64_t v) { return v >= 0 ? v / n : -((-v + n - 1) / n); };
+    return {std::max(floor_div(lo) + 1, -most), std::min(-(floor_div(-hi) + 1), most)};
+}
+
+// (extents stay within 2^46 bytes)
 bool rows_overlap(const RowsArg& a, size_t a_b, const RowsArg& b, size_t b_b, int64_t T, int64_t batch, size_t es) {
     if (!overlaps(a.p, a_b, b.p, b_b)) return false;
     if ((T > 1 && a.st != b.st) || (batch > 1 && a.sb != b.sb)) return true;
-    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p, lo = std::min(pa, pb);
-    const uint64_t gap = std::max(pa, pb) - lo, first = (uint64_t)(pa < pb ? a.width : b.width) * es;
-    if (gap < first || gap % es) return true;  // the rows themselves meet
-    const int64_t whole = (int64_t)(gap / es) + (pa < pb ? b.width : a.width);
-    return !rows_apart(T, a.st, batch, a.sb, whole);
+    const intptr_t bytes = (intptr_t)b.p - (intptr_t)a.p;
+    if (bytes % (intptr_t)es) return true;
+    // A row of b lies gap + k far + l near elements from one of a, |k| < fars, |l| < nears; the two meet where that is
+    // above -b.width and below a.width.
+    const int64_t gap = bytes / (intptr_t)es;
+    const bool time_far = a.st >= a.sb;
+    const int64_t far = time_far ? a.st : a.sb, fars = (time_far ? T : batch) - 1, near = time_far ? a.sb : a.st,
+                  nears = (time_far ? batch : T) - 1;
+    const int64_t reach = near * nears;
+    const Multiples k = far ? multiples(-b.width - reach - gap, a.width + reach - gap, far, fars) : Multiples{0, 0};
+    if (k.last - k.first > 8) return true;  // (rows far from nested: not looked into)
+    for (int64_t i = k.first; i <= k.last; ++i) {
+        const int64_t at = gap + i * far;
+        if (near == 0 ? at > -b.width && at < a.width : [&] {
+                const Multiples l = multiples(-b.width - at, a.width - at, near, nears);
+                return l.first <= l.last;
+            }())
+            return true;
+    }
+    return false;
 }
 
 // Checks the strides, extents and overlaps of the rows of a call, and of the rows with its dense tensors.

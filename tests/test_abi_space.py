@@ -1,6 +1,7 @@
 """C-ABI checks of the state-space block's and beam search's entry points that need no GPU: bad arguments are
 refused during host-side validation (before any HIP call)."""
 import ctypes
+import random
 
 import pytest
 
@@ -56,6 +57,33 @@ def test_selective_scan_no_op_and_workspace(L):
     assert qb(40, 2, 100, 16, F32) >= 40 * 2 * 32 * 4 + 2 * 100 * 18 * 4
     for bad in ((0, 1, 1, 1, F32), (5, 0, 1, 1, F32), (5, 1, 0, 1, F32), (5, 1, 1, 0, F32), (5, 1, 1, 65, F32), (5, 1, 1, 1, 9), (1 << 41, 1, 1, 1, F32)):
         assert q(*bad) == 0 and qb(*bad) == 0
+
+
+def test_rows_of_one_tensor(L):
+    # An output among the rows of an input with the same strides: refused where an element is shared, else not.  (The marks'
+    # stride is refused by a later check, so that no call is launched.)
+    far = (at(9), 1 << 27, 1)
+    T, B, D, g = 9, 3, 4, random.Random(1)
+    refused(L, UNSUPPORTED, scan(L, T=T, B=B, x=(at(0), 24, 4), y=(at(0, 48), 24, 4), reset=far))        # [T][2][B][D]
+    refused(L, UNSUPPORTED, scan(L, T=T, B=B, x=(at(0), 12, 4), y=(at(0, 9 * 48), 12, 4), reset=far))    # [2][T][B][D]
+    met = 0
+    for _ in range(600):
+        if g.random() < 0.5:
+            sb = g.randint(D, 14)
+            st = g.randint((B - 1) * sb + D, 70)
+        else:
+            st = g.randint(D, 14)
+            sb = g.randint((T - 1) * st + D, 200)
+        gap = g.randint(-80, 80) * g.choice((1, 1, 4))
+        rows = {t * st + b * sb + c for t in range(T) for b in range(B) for c in range(D)}
+        shared = any(gap + v in rows for v in rows)
+        met += shared
+        code = scan(L, T=T, B=B, x=(at(0, 1 << 20), st, sb), y=(at(0, (1 << 20) + 4 * gap), st, sb), reset=far)
+        refused(L, INVALID if shared else UNSUPPORTED, code)
+        shared = any(gap + v in rows for t in range(T) for b in range(B) for v in range(t * st + b * sb, t * st + b * sb + 3))
+        code = scan(L, T=T, B=B, y=(at(0, 1 << 20), st, sb), Bm=(at(0, (1 << 20) + 4 * gap), st, sb), reset=far)       # (rows of 3)
+        refused(L, INVALID if shared else UNSUPPORTED, code)
+    assert 200 < met < 500
 
 
 def scan_bwd(L, T=9, B=2, D=4, N=3, dt=F32, x=(at(0), 8, 4), d=(at(1), 8, 4), A=at(2), Bm=(at(3), 6, 3), Cm=(at(4), 6, 3), skip=at(5),

@@ -331,3 +331,21 @@ def test_refusals():
     with pytest.raises(isam.IsamError) as e:
         isam.causal_conv_backward(x["x"], x["w"], x["dy"], workspace=torch.empty(16, device="cuda", dtype=torch.uint8))
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_input_and_output_turn_by_turn(dtype):
+    # [T][2][batch][C]: the tokens' inputs and outputs one after the other in one tensor
+    T, B, C, K = 50, 3, 20, 4
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn((T, B, C), generator=g).to(dtype).cuda()
+    w = torch.randn((K, C), generator=g).cuda()
+    both = torch.full((T, 2, B, C), 7.0, dtype=dtype, device="cuda")
+    both[:, 0] = x
+    y, _ = isam.causal_conv(both[:, 0], w, y=both[:, 1])
+    want, _ = isam.causal_conv(x, w)
+    assert torch.equal(both[:, 1], want) and torch.equal(both[:, 0], x)
+    dx = isam.causal_conv_backward(x, w, both[:, 0], dx=both[:, 1])[0]
+    assert torch.equal(dx, isam.causal_conv_backward(x, w, x)[0]) and torch.equal(both[:, 0], x)
+    with pytest.raises(isam.IsamError):
+        isam.causal_conv(both[:, 0], w, y=both.view(T, -1)[:, C:C + B * C].view(T, B, C))
