@@ -608,6 +608,15 @@ bool linear_few(int64_t M, int64_t K, int64_t N, bool aligned) {
 // 24, 24, 26, 35 / 21, 24, 30, 38; 8192x2048 38, 38, 38, 40 / 23, 23, 32, 41; 16384x512 64, 64, 65, 64 / 24, 24, 27, 33.
 bool linear_deep(int64_t M, int64_t K, int64_t N) { return K >= 4096 && 2 * cdiv(M, 64) * cdiv(N, 64) <= (int64_t)device_cus(); }
 
+// fp32 grids of few tiles take linear_f32_kernel by the gated block's rule, up to 24 rounds of 64 values of K.  us of the
+// product and pass / the kernel, silu, forward (rounds): 128x512x2048 17.5 / 10.2 (8), 100x333x5001 23.4 / 14.9 (12),
+// 256x1024x1024 20.7 / 15.6 and 512x1024x1024 26.6 / 15.9 (16), 1000x768x1000 29.1 / 22.9 and 128x1536x2048 23.1 / 20.8 (24),
+// 512x512x4096 30.2 / 31.9, 512x1024x2048 31.0 / 28.5, 128x2048x2048 26.2 / 25.9 and 1000x1000x1000 32.9 / 25.2 (32),
+// 512x2048x2048 45 / 50 and 2048x512x2048 51 / 62 (64); whole gradients lie alike.  The bf16 tiles are chosen by that
+// block's rounds too: 64 / 128 / 256 rows, us:
+// 256x2048x2048 12.4 / 20.4 / 38.8, 576x256x4096 11.0 / 8.3 / 14.0, 1024x1024x8192 41 / 23.5 / 30.6, 1792x1024x8192 68 / 40 / 35.3,
+// 2048x1024x8192 75 / 42.7 / 37.7, 2304x1024x8192 84 / 51.6 / 59, 2944x1024x8192 106 / 60.3 / 63.2, 3328x1024x8192 120 / 69.3 / 65.0.
+//
 // Forward.  plain: no activation, and no residual but out itself: the library's product has that epilogue in every
 // one of its plans.
 LinearPlan linear_forward_plan(int64_t M, int64_t K, int64_t N, int type, bool plain, bool x_ok, bool w_ok) {

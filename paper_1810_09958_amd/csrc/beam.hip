@@ -13,8 +13,9 @@
 // The second kernel, a workgroup to a text, forms the values of the candidates that are left, in 64 bits too (an fp32
 // sum of scores and logits would make ties of what is none), and
 // takes the best in the same way, the lists' first entries first: it ends where none of a piece is among the best.
-// One text of 4 beams over 256: 5.3 and 9.2 us; 32 texts of 8 beams over 32000 (33 MB): 18.5 and 14.6 us, 1.8 TB/s for
-// the first (the vector units: an exponential in 64 bits and the bound).  Latency holds the second.
+// In a kernel trace: one text of 4 beams over 256 5.4 and 9.9 us; 32 texts of 8 beams over 32000 (33 MB) 19.8 and 15.9,
+// 1.7 TB/s for the first (52 vector instructions a value, most of them the exponential in 64 bits, and the loads and
+// exchanges of a workgroup's one piece before and after them).  Latency holds the second.
 #include "kernels.hpp"
 #include "rowio.hpp"
 
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(256) void beam_part_kernel(BeamArgs a) {
     most = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
     // the width-th of the firsts, by value and then (where that many are equal) by place; 0: fewer lanes have any.
     // ALL: of the workgroup's, four times the comparisons, which pays where many pass (32 texts of 8 beams over 32000
-    // 13.0 of a wave's against 15.6 us, 4 texts of 64 beams 671 against 445 with the second kernel).
+    // 13.0 of a wave's against 15.6 us, 4 texts of 64 beams 671 against 445 with the second kernel, with sums in fp32).
     uint64_t least = 0;
     if constexpr (ALL) {
         uint32_t hi[4], lo[4], low = 0, rest = 0;

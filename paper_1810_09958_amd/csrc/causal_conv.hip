@@ -11,9 +11,9 @@
 // The gradient goes forward in time too: the K sums dx of the last tokens are kept in registers until
 // they are complete, pre is formed again.  The gradients of w and bias are kept over a run, added over a
 // workgroup's four runs in LDS, and over workgroups by a second kernel.
-// 4096x8x2048 (tokens, sequences, channels), K = 4, silu, bf16, resets: forward 57 us, 4.7 TB/s (268 MB), backward 113
-// and 4.7 for the sums (403 MB, 3.6 TB/s: 68 registers of values on their way and a silu with its slope on the vector
-// units).  One token of 32x2048: 3.3 us.
+// 4096x8x2048 (tokens, sequences, channels), K = 4, silu, bf16, resets, in a kernel trace: forward 60 us, 4.5 TB/s (268 MB),
+// backward 127 and 4.9 for the sums (403 MB, 3.2 TB/s; the vector units are busy for 53 and 58 % of it, with the silu and,
+// backward, its slope; 150 registers leave the gradient three waves a SIMD).  One token of 32x2048: 4.5 us.
 #include "kernels.hpp"
 #include "rowio.hpp"
 

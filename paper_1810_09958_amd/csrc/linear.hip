@@ -13,10 +13,10 @@
 // needs it.  (Bytes and latency hide the second term up to some 128 rows, 12 and 12 us either way at 128x1024x4096,
 // but a tile's LDS has room for one term.)  The bias' gradient is summed before that rounding.
 // Up to 16 rows (64 over little work) the weights are streamed once, straight into the matrix instructions' operand
-// registers: 1x1024x4096 (M x K x N) 4.2 us, 2 TB/s between start and end of one launch.  bf16 tiles: 8192x8192x2048
+// registers: 1x1024x4096 (M x K x N) 4.0 us, 2.1 TB/s between start and end of one launch.  bf16 tiles: 8192x8192x2048
 // with a residual 212 us, 1.30 PFLOP/s, power, as the large product; 8192x2048x8192 280 us without an activation and 308
 // with gelu, whose epilogue (67 M values on the vector units) nothing covers.  Gradient of 2048x1024x4096 with gelu 100 us:
-// dP about 31, dx 31, dW 24 and the transposed copy of its operand 13.
+// dP 29, dx 32, dW 26 and the transposed copy of its operand 13.
 // fp32 grids of few tiles run on the fp32 matrix instructions, straight from memory; larger ones, and deep bf16 products
 // of few tiles, go through the library's product and an element-wise pass.
 #include "gated_ffn.hpp"
@@ -327,7 +327,9 @@ __global__ __launch_bounds__(512) void linear_token_kernel(LinearArgs a) {
 // fp32 grids of few tiles: 32 rows x 64 columns on the fp32 matrix instructions, straight from memory
 // (any alignment of 4 bytes) into their operand registers.  The eight waves take every eighth 16-deep K step (32
 // matrix instructions on 6 loads, two steps in flight) and meet in LDS, each wave then holding a 16 x 16 block.
-// 500x511x771 (M x K x N, 208 tiles) 13.3 us (four waves 15.5, four steps in flight 14.6; the matrix instructions 4).
+// 500x511x771 (M x K x N, 208 tiles) 13.5 us (four waves 15.5; the matrix instructions 4).  A call with two steps in
+// flight, and with four: 128x512x2048 10.0, 11.1; 100x333x5001 14.8, 21.1; 256x1024x1024 15.6, 18.5; 1000x768x1000 22.8, 32.3;
+// 1000x1000x1000 24.9, 33.1.
 template <bool BWD>
 __global__ __launch_bounds__(512) void linear_f32_kernel(LinearArgs a, TileMapArgs tmap) {
     constexpr int NW = 8, U = 2;  // waves, steps loaded together
